@@ -382,6 +382,101 @@ sphinx_status sphinx_scatter_masked(const sphinx_request* reqs, int32_t R, const
                                     sphinx_layout layout, void* stream);
 
 /* ------------------------------------------------------------------------
+ * 8-bit key/value cache: the latent cache in half the bytes of a bf16 one, and
+ * the attention that reads it.  A slice holds the keys and values of one
+ * denoiser block (or of any attention layer) for the tokens of `nseg`
+ * segments: segment i has tokens [cu_kv[i], cu_kv[i+1]) (host int32 [nseg+1],
+ * non-decreasing from 0, 1 <= nseg <= SPHINX_MAX_REQUESTS), each with kv_heads
+ * keys and values of head_dim dims (64 or 72).
+ *
+ * The tokens of a segment are grouped in blocks of SPHINX_KV8_BLOCK from its
+ * first one; the last block may be partial.  For each block and head the keys,
+ * and likewise the values, are kept as e4m3 numbers with one scale: with A the
+ * largest finite magnitude among them, e is the smallest integer with
+ * A <= 448 2^e, held in -100 .. 119 (-100 for A = 0), and x is kept as
+ * e4m3(x 2^-e) 2^e, rounded once to nearest even; finite values past 448 2^119
+ * saturate, infinities and NaN become NaN.  bf16 and f32 hold these values
+ * exactly.
+ *
+ * The caller owns a slice (sphinx_kv8_bytes bytes, 16-byte aligned) and clears
+ * it to zero bytes before its first use: a cleared slice holds zeros.  Its bytes
+ * are in an order of the library's own.  Slices of the same cu_kv, kv_heads and
+ * head_dim may follow each other in memory (the size is a multiple of 256).
+ * ------------------------------------------------------------------------ */
+#define SPHINX_KV8_BLOCK 64
+
+/* Bytes of one slice.  SPHINX_E_UNSUPPORTED for another head_dim. */
+sphinx_status sphinx_kv8_bytes(int32_t kv_heads, int32_t head_dim, const int32_t* cu_kv /*host[nseg+1]*/,
+                               int32_t nseg, size_t* bytes);
+
+/* Quantises rows as they are written.  Row j of k and v (dev, dtype f32 or
+ * bf16; row j at element j*ld, head h at its columns [h head_dim, (h+1)
+ * head_dim)) becomes the key and value of token idx[j] (dev int32 [n],
+ * ascending) or, with idx = NULL, of token j (then n <= the slice's tokens).
+ * Every block that a row falls into takes its new rows beside the values that
+ * its other rows held and is quantised anew by the rule above: rows not written
+ * keep their values exactly unless the block's scale grows (by 2^g: values
+ * below 2^(e+g-6) are rounded to multiples of 2^(e+g-9)).  A token outside the
+ * slice is skipped; one listed twice takes its last row.  Where idx does not
+ * ascend, which rows are stored is not defined (nothing outside the slice is
+ * touched).  ld >= kv_heads*head_dim and a multiple of 8; pointers 16-byte
+ * aligned; k and v may be columns of one matrix.  n = 0 is a no-op.
+ * Deterministic. */
+sphinx_status sphinx_kv8_store(sphinx_dtype dtype, int32_t kv_heads, int32_t head_dim, const void* k, const void* v,
+                               int64_t ld, const int32_t* idx, int32_t n, const int32_t* cu_kv, int32_t nseg,
+                               void* slice, void* stream);
+
+/* Reads rows back: row j of k and v (dev out, laid out as in
+ * sphinx_kv8_store) gets the values of token idx[j] (ascending; a token may be
+ * listed more than once) or of token j.  Rows whose token lies outside the
+ * slice are left unwritten; where idx does not ascend, which rows are written
+ * is not defined. */
+sphinx_status sphinx_kv8_load(sphinx_dtype dtype, int32_t kv_heads, int32_t head_dim, const void* slice,
+                              const int32_t* cu_kv, int32_t nseg, const int32_t* idx, int32_t n, void* k, void* v,
+                              int64_t ld, void* stream);
+
+/* Attention over the cache, as sphinx_varlen_attention with the keys and
+ * values that a slice holds:
+ *   o[j] = sum_t 2^(q[j].k[t]) v[t] / sum_t 2^(q[j].k[t])
+ * for query rows j in [cu_q[i], cu_q[i+1]) and the first kv_len[i] tokens t of
+ * segment i (host int32 [nseg], 0 <= kv_len[i] <= its tokens; NULL: all).  What
+ * the cache holds behind them is not looked at.  A query without keys gives
+ * zeros.  heads is a multiple of kv_heads; query head h uses key/value head
+ * h / (heads / kv_heads).  q (dev, row j at element j*ldq) must already be
+ * multiplied by log2(e)/sqrt(d).
+ *   dtype: SPHINX_BF16 (head_dim 64 or 72; probabilities rounded to bf16, sums
+ *          in fp32, o rounded to bf16) or SPHINX_F32 (head_dim 64).
+ * o: dev, row j at element j*heads*head_dim.  ldq >= heads*head_dim and a
+ * multiple of 8; heads*head_dim <= 65536; pointers 16-byte aligned.  ws: dev,
+ * 256-byte aligned, sphinx_kv8_attention_workspace_bytes bytes (which covers
+ * every kv_len), not shared with work that may run at the same time.  Enqueues
+ * at most two kernels, synchronizes nothing and may be captured in a graph. */
+sphinx_status sphinx_kv8_attention_workspace_bytes(sphinx_dtype dtype, int32_t heads, int32_t kv_heads,
+                                                   int32_t head_dim, const int32_t* cu_q, const int32_t* cu_kv,
+                                                   int32_t nseg, size_t* bytes);
+sphinx_status sphinx_kv8_attention(sphinx_dtype dtype, int32_t heads, int32_t kv_heads, int32_t head_dim,
+                                   const void* q, int64_t ldq, const void* slice, const int32_t* cu_q,
+                                   const int32_t* cu_kv, const int32_t* kv_len, int32_t nseg, void* o, void* ws,
+                                   size_t ws_bytes, void* stream);
+
+/* The latent cache in 8 bits: L slices, one per denoiser block, whose segments
+ * are the requests.  sphinx_refine_step_kv8 is sphinx_refine_step_cached with
+ * this cache: every block stores the forwarded rows' keys and values with
+ * sphinx_kv8_store (idx ascending), and its rows attend to the tokens of their
+ * request through sphinx_kv8_attention.  A factorised model reads the slice
+ * back into the workspace (sphinx_kv8_load) for its spatial and temporal
+ * attention.  Models with head_dim 64 or 72 (f32: 64); SPHINX_E_UNSUPPORTED
+ * otherwise.  The workspace is larger than sphinx_refine_step's. */
+sphinx_status sphinx_kv8_cache_bytes(const sphinx_model_desc* m, const sphinx_request* reqs, int32_t R,
+                                     size_t* bytes);
+sphinx_status sphinx_refine_kv8_workspace_bytes(const sphinx_model_desc* m, const sphinx_request* reqs, int32_t R,
+                                                int64_t max_sel, size_t* bytes);
+sphinx_status sphinx_refine_step_kv8(const sphinx_model_desc* m, const sphinx_request* reqs, int32_t R,
+                                     const int32_t* idx, int32_t n, const int32_t* cu_host, const int32_t* tau,
+                                     const float* c1, const float* c2, float* x, void* kv_cache, void* ws,
+                                     size_t ws_bytes, void* stream);
+
+/* ------------------------------------------------------------------------
  * Mask front-end (Sec. 5.3 spatially selective refinement; Alg. 1
  * laplacian_var, otsu(norm(.)), the opacity mask 1[O < tau_o] and their
  * union): the token mask of every request from the regression output frames

@@ -56,6 +56,8 @@ from typing import Dict, List, Optional, Sequence
 
 import numpy as np
 
+from . import kv8
+
 T_TRAIN = 1000
 BETA_START = 1e-4
 BETA_END = 2e-2
@@ -464,6 +466,8 @@ def denoise(model: Model, x: np.ndarray, f, y, xx, tau_tok: np.ndarray, seg: np.
         else:
             cache[l][0][rows] = k
             cache[l][1][rows] = v
+            if isinstance(cache, Kv8Cache):
+                cache.requantise(l, H)
             if kind == "joint":
                 o = rnd(attention(q, cache[l][0], cache[l][1], H, seg, kv_seg=kv_seg, scale=sscale))
             else:
@@ -576,16 +580,34 @@ def new_cache(model: Model, n_tokens: int) -> list:
     return [(np.zeros((n_tokens, model.D)), np.zeros((n_tokens, model.D))) for _ in range(model.L)]
 
 
+class Kv8Cache(list):
+    """A latent cache whose keys and values are the numbers that an 8-bit cache
+    holds: blocks of 64 tokens from each request's first one, quantised per
+    block and head (kv8.quantise) whenever rows have been written."""
+
+    def __init__(self, blocks: list, bounds):
+        super().__init__(blocks)
+        self.bounds = np.asarray(bounds, np.int64)
+
+    def requantise(self, l: int, heads: int):
+        for x in self[l]:
+            n, D = x.shape
+            x[:] = kv8.quantise(x.reshape(n, heads, D // heads), self.bounds).reshape(n, D)
+
+
 def refine(wl, precision: str = "model", denoiser=None, trace: bool = False, steps: Optional[int] = None,
-           period: int = 0, per_frame_grid: bool = False):
+           period: int = 0, per_frame_grid: bool = False, cache8: bool = False):
     """Run the whole partial-denoising loop; returns the final NCHW state (float64)
     and, with trace=True, the list of per-step results.  period > 0 turns on
-    the latent cache with a full step every ``period`` steps."""
+    the latent cache with a full step every ``period`` steps, cache8 keeps it in
+    8 bits."""
     model = model_from_workload(wl)
     plans = plan_steps([r.frames for r in wl.requests], wl.s_start, wl.nsteps, period, per_frame_grid)
     info = token_info(wl.requests)
     state = np.asarray(wl.z0, dtype=np.float64).copy()
     cache = new_cache(model, wl.N) if period > 0 else None
+    if cache8:
+        cache = Kv8Cache(cache, wl.tok_offset)
     out = []
     for i, p in enumerate(plans[: steps if steps is not None else len(plans)]):
         if cache is not None:

@@ -23,6 +23,7 @@ NCHW, TOKENS = 0, 1  # sphinx_layout
 ATTN_JOINT, ATTN_FACTORISED = 0, 1  # sphinx_attention
 GRID_SHARED, GRID_PER_FRAME = 0, 1  # sphinx_grid
 MAX_REQUESTS = 64
+KV8_BLOCK = 64  # tokens of a block of the 8-bit cache
 STATUS_NAMES = {0: "SPHINX_OK", 1: "SPHINX_E_INVALID", 2: "SPHINX_E_UNSUPPORTED", 3: "SPHINX_E_WORKSPACE",
                 4: "SPHINX_E_HIP"}
 PARAMS = ["PE_W", "PE_B", "T1_W", "T1_B", "T2_W", "T2_B", "COND_W", "COND_B", "QKV_W", "QKV_B", "O_W", "O_B",
@@ -34,7 +35,10 @@ EXPORTED = ["sphinx_status_string", "sphinx_model_blob_bytes", "sphinx_model_par
             "sphinx_refine_step", "sphinx_scatter_blend", "sphinx_timing_enable", "sphinx_timing_read",
             "sphinx_peak_mfma", "sphinx_plan_cache", "sphinx_kv_cache_bytes", "sphinx_gather_ctx",
             "sphinx_refine_step_cached", "sphinx_scatter_masked", "sphinx_mask_frontend_workspace_bytes",
-            "sphinx_mask_frontend", "sphinx_adaptive_start", "sphinx_select_mask_static", "sphinx_varlen_attention"]
+            "sphinx_mask_frontend", "sphinx_adaptive_start", "sphinx_select_mask_static", "sphinx_varlen_attention",
+            "sphinx_kv8_bytes", "sphinx_kv8_store", "sphinx_kv8_load", "sphinx_kv8_attention_workspace_bytes",
+            "sphinx_kv8_attention", "sphinx_kv8_cache_bytes", "sphinx_refine_kv8_workspace_bytes",
+            "sphinx_refine_step_kv8"]
 PEAK_BLOCKS = 2048
 PEAK_CONSTANT, PEAK_RANDOM = 0, 1
 KERNEL_CLASSES = ["select", "gather", "cond", "embed", "ln", "gemm_qkv", "attention", "gemm_out", "gemm_mlp1",
@@ -113,6 +117,18 @@ def lib() -> ctypes.CDLL:
                                         P, P, P, P, P]),
         "sphinx_refine_step_cached": (c_int32, [POINTER(ModelDesc), POINTER(Request), c_int32, P, c_int32, P, P, P,
                                                 P, P, P, P, c_size_t, P]),
+        "sphinx_kv8_bytes": (c_int32, [c_int32, c_int32, P, c_int32, POINTER(c_size_t)]),
+        "sphinx_kv8_store": (c_int32, [c_int32, c_int32, c_int32, P, P, c_int64, P, c_int32, P, c_int32, P, P]),
+        "sphinx_kv8_load": (c_int32, [c_int32, c_int32, c_int32, P, P, c_int32, P, c_int32, P, P, c_int64, P]),
+        "sphinx_kv8_attention_workspace_bytes": (c_int32, [c_int32, c_int32, c_int32, c_int32, P, P, c_int32,
+                                                           POINTER(c_size_t)]),
+        "sphinx_kv8_attention": (c_int32, [c_int32, c_int32, c_int32, c_int32, P, c_int64, P, P, P, P, c_int32, P, P,
+                                           c_size_t, P]),
+        "sphinx_kv8_cache_bytes": (c_int32, [POINTER(ModelDesc), POINTER(Request), c_int32, POINTER(c_size_t)]),
+        "sphinx_refine_kv8_workspace_bytes": (c_int32, [POINTER(ModelDesc), POINTER(Request), c_int32, c_int64,
+                                                        POINTER(c_size_t)]),
+        "sphinx_refine_step_kv8": (c_int32, [POINTER(ModelDesc), POINTER(Request), c_int32, P, c_int32, P, P, P, P, P,
+                                             P, P, c_size_t, P]),
         "sphinx_scatter_masked": (c_int32, [POINTER(Request), c_int32, P, P, c_int32, P, P, c_int32, c_int32, P]),
         "sphinx_mask_frontend_workspace_bytes": (c_int32, [POINTER(Request), c_int32, POINTER(c_size_t)]),
         "sphinx_adaptive_start": (c_int32, [POINTER(Request), c_int32, P, P, ctypes.c_float, POINTER(KLogic), c_int32,
@@ -344,6 +360,98 @@ def sphinx_refine_step_cached(desc: ModelDesc, reqs, idx, n: int, cu_host: np.nd
                               stream=None):
     cu = np.ascontiguousarray(cu_host, dtype=np.int32)
     _check("sphinx_refine_step_cached", lib().sphinx_refine_step_cached(
+        ctypes.byref(desc), reqs, len(reqs), _ptr(idx), n, _ptr(cu), _ptr(tau), _ptr(c1), _ptr(c2), _ptr(x),
+        _ptr(kv_cache), _ptr(ws), ws.numel() * ws.element_size(), _stream(stream)))
+
+
+def _host_cu(cu) -> np.ndarray:
+    return np.ascontiguousarray(cu, dtype=np.int32)
+
+
+def _on_current_device(*tensors):
+    """The 8-bit cache's calls run on the current device: tensors of another one are refused."""
+    import torch
+
+    here = torch.cuda.current_device()
+    for t in tensors:
+        if isinstance(t, torch.Tensor) and (not t.is_cuda or t.device.index != here):
+            raise ValueError(f"tensor on {t.device}, the current device is cuda:{here}")
+
+
+def sphinx_kv8_bytes(kv_heads: int, head_dim: int, cu_kv) -> int:
+    """Bytes of one slice of the 8-bit cache (cu_kv: host int sequence of token bounds, as in the calls below)."""
+    cu, out = _host_cu(cu_kv), c_size_t()
+    _check("sphinx_kv8_bytes", lib().sphinx_kv8_bytes(kv_heads, head_dim, _ptr(cu), cu.size - 1, ctypes.byref(out)))
+    return out.value
+
+
+def sphinx_kv8_store(dtype: int, kv_heads: int, head_dim: int, k, v, ld: int, idx, n: int, cu_kv, cache, stream=None):
+    """Quantises rows j < n of k and v into the slice `cache` (zeroed before its first use) at tokens idx[j]
+    (ascending; None: token j)."""
+    cu = _host_cu(cu_kv)
+    _on_current_device(k, v, idx, cache)
+    if cache.numel() * cache.element_size() < sphinx_kv8_bytes(kv_heads, head_dim, cu):
+        raise ValueError("the cache slice is smaller than sphinx_kv8_bytes")
+    _check("sphinx_kv8_store", lib().sphinx_kv8_store(
+        dtype, kv_heads, head_dim, _ptr(k), _ptr(v), ld, _ptr(idx), n, _ptr(cu), cu.size - 1, _ptr(cache),
+        _stream(stream)))
+
+
+def sphinx_kv8_load(dtype: int, kv_heads: int, head_dim: int, cache, cu_kv, idx, n: int, k, v, ld: int, stream=None):
+    """Rows j < n of k and v <- the values of tokens idx[j] (ascending; None: token j)."""
+    cu = _host_cu(cu_kv)
+    _on_current_device(k, v, idx, cache)
+    if cache.numel() * cache.element_size() < sphinx_kv8_bytes(kv_heads, head_dim, cu):
+        raise ValueError("the cache slice is smaller than sphinx_kv8_bytes")
+    _check("sphinx_kv8_load", lib().sphinx_kv8_load(
+        dtype, kv_heads, head_dim, _ptr(cache), _ptr(cu), cu.size - 1, _ptr(idx), n, _ptr(k), _ptr(v), ld,
+        _stream(stream)))
+
+
+def sphinx_kv8_attention_workspace_bytes(dtype: int, heads: int, kv_heads: int, head_dim: int, cu_q, cu_kv) -> int:
+    cq, ck, out = _host_cu(cu_q), _host_cu(cu_kv), c_size_t()
+    if cq.size != ck.size:
+        raise ValueError("cu_q and cu_kv differ in length")
+    _check("sphinx_kv8_attention_workspace_bytes", lib().sphinx_kv8_attention_workspace_bytes(
+        dtype, heads, kv_heads, head_dim, _ptr(cq), _ptr(ck), cq.size - 1, ctypes.byref(out)))
+    return out.value
+
+
+def sphinx_kv8_attention(dtype: int, heads: int, kv_heads: int, head_dim: int, q, ldq: int, cache, cu_kv, kv_len, o,
+                         cu_q, ws, stream=None):
+    """Attention over the 8-bit cache (base-2 softmax; q already scaled by log2(e)/sqrt(d)).  cu_q, cu_kv: host int
+    sequences of segment bounds; kv_len: host ints, the tokens of each segment that take part (None: all)."""
+    cq, ck = _host_cu(cu_q), _host_cu(cu_kv)
+    kl = None if kv_len is None else _host_cu(kv_len)
+    if cq.size != ck.size or (kl is not None and kl.size != ck.size - 1):
+        raise ValueError("cu_q, cu_kv and kv_len differ in length")
+    _on_current_device(q, cache, o, ws)
+    if cache.numel() * cache.element_size() < sphinx_kv8_bytes(kv_heads, head_dim, ck):
+        raise ValueError("the cache slice is smaller than sphinx_kv8_bytes")
+    _check("sphinx_kv8_attention", lib().sphinx_kv8_attention(
+        dtype, heads, kv_heads, head_dim, _ptr(q), ldq, _ptr(cache), _ptr(cq), _ptr(ck), _ptr(kl), cq.size - 1,
+        _ptr(o), _ptr(ws), ws.numel() * ws.element_size(), _stream(stream)))
+
+
+def sphinx_kv8_cache_bytes(desc: ModelDesc, reqs) -> int:
+    out = c_size_t()
+    _check("sphinx_kv8_cache_bytes", lib().sphinx_kv8_cache_bytes(ctypes.byref(desc), reqs, len(reqs),
+                                                                  ctypes.byref(out)))
+    return out.value
+
+
+def sphinx_refine_kv8_workspace_bytes(desc: ModelDesc, reqs, max_sel: int) -> int:
+    out = c_size_t()
+    _check("sphinx_refine_kv8_workspace_bytes", lib().sphinx_refine_kv8_workspace_bytes(
+        ctypes.byref(desc), reqs, len(reqs), max_sel, ctypes.byref(out)))
+    return out.value
+
+
+def sphinx_refine_step_kv8(desc: ModelDesc, reqs, idx, n: int, cu_host: np.ndarray, tau, c1, c2, x, kv_cache, ws,
+                           stream=None):
+    """sphinx_refine_step_cached with the 8-bit cache."""
+    cu = np.ascontiguousarray(cu_host, dtype=np.int32)
+    _check("sphinx_refine_step_kv8", lib().sphinx_refine_step_kv8(
         ctypes.byref(desc), reqs, len(reqs), _ptr(idx), n, _ptr(cu), _ptr(tau), _ptr(c1), _ptr(c2), _ptr(x),
         _ptr(kv_cache), _ptr(ws), ws.numel() * ws.element_size(), _stream(stream)))
 

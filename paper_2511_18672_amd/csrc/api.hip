@@ -8,6 +8,7 @@
 #include <vector>
 
 #include "kernels.hpp"
+#include "kv8.hpp"
 #include "sphinx_prof.h"
 
 using namespace sphinx;
@@ -580,13 +581,187 @@ sphinx_status sphinx_kv_cache_bytes(const sphinx_model_desc* m, const sphinx_req
 }
 
 namespace {
+// Segments of an 8-bit cache from their token bounds (checked before).
+Kv8Segs kv8_segs(const int32_t* cu_kv, int nseg) {
+  Kv8Segs S;
+  std::memset(&S, 0, sizeof(S));
+  S.nseg = nseg;
+  for (int i = 0; i < nseg; ++i) {
+    S.tok[i + 1] = cu_kv[i + 1];
+    S.blk[i + 1] = S.blk[i] + (int)(((int64_t)cu_kv[i + 1] - cu_kv[i] + kKv8Block - 1) / kKv8Block);
+  }
+  return S;
+}
+
+sphinx_status kv8_check(int32_t kv_heads, int32_t head_dim, const int32_t* cu_kv, int32_t nseg) {
+  if (kv_heads < 1 || head_dim < 1 || nseg < 1 || cu_kv == nullptr || cu_kv[0] != 0) return SPHINX_E_INVALID;
+  if (nseg > SPHINX_MAX_REQUESTS || (head_dim != 64 && head_dim != 72)) return SPHINX_E_UNSUPPORTED;
+  if ((int64_t)kv_heads * head_dim > 65536) return SPHINX_E_UNSUPPORTED;
+  for (int i = 0; i < nseg; ++i)
+    if (cu_kv[i + 1] < cu_kv[i]) return SPHINX_E_INVALID;
+  return SPHINX_OK;
+}
+
+Kv8Slice kv8_slice(void* base, int32_t kv_heads, int32_t head_dim, int64_t nblk) {
+  unsigned char* b = static_cast<unsigned char*>(base);
+  return Kv8Slice{b, b + kv8_scale_offset(kv_heads, head_dim, nblk), kv_heads, nblk};
+}
+
+// Arguments that storing and reading back share; *todo: there are rows.
+sphinx_status kv8_rows_check(sphinx_dtype dtype, int32_t kv_heads, int32_t head_dim, const void* k, const void* v,
+                             int64_t ld, const int32_t* idx, int32_t n, const int32_t* cu_kv, int32_t nseg,
+                             const void* slice, bool* todo) {
+  *todo = false;
+  if (!valid_dtype(dtype)) return SPHINX_E_UNSUPPORTED;
+  const sphinx_status st = kv8_check(kv_heads, head_dim, cu_kv, nseg);
+  if (st != SPHINX_OK) return st;
+  if (n < 0 || (idx == nullptr && n > cu_kv[nseg])) return SPHINX_E_INVALID;
+  if (ld < (int64_t)kv_heads * head_dim || ld % 8 != 0) return SPHINX_E_INVALID;
+  if (n == 0 || cu_kv[nseg] == 0) return SPHINX_OK;
+  if (!k || !v || !slice || !aligned(k, 16) || !aligned(v, 16) || !aligned(slice, 16) || !aligned(idx, 16))
+    return SPHINX_E_INVALID;
+  *todo = true;
+  return SPHINX_OK;
+}
+}  // namespace
+
+sphinx_status sphinx_kv8_bytes(int32_t kv_heads, int32_t head_dim, const int32_t* cu_kv, int32_t nseg,
+                               size_t* bytes) {
+  const sphinx_status st = kv8_check(kv_heads, head_dim, cu_kv, nseg);
+  if (st != SPHINX_OK) return st;
+  if (bytes == nullptr) return SPHINX_E_INVALID;
+  *bytes = kv8_slice_bytes(kv_heads, head_dim, kv8_segs(cu_kv, nseg).blk[nseg]);
+  return SPHINX_OK;
+}
+
+sphinx_status sphinx_kv8_store(sphinx_dtype dtype, int32_t kv_heads, int32_t head_dim, const void* k, const void* v,
+                               int64_t ld, const int32_t* idx, int32_t n, const int32_t* cu_kv, int32_t nseg,
+                               void* slice, void* stream) {
+  bool todo;
+  const sphinx_status st = kv8_rows_check(dtype, kv_heads, head_dim, k, v, ld, idx, n, cu_kv, nseg, slice, &todo);
+  if (st != SPHINX_OK || !todo) return st;
+  const Kv8Segs S = kv8_segs(cu_kv, nseg);
+  hipStream_t s = (hipStream_t)stream;
+  Bracket br(SPHINX_K_KV_STORE, s);
+  return hip_status(launch_kv8_store(dtype, head_dim, S, kv8_slice(slice, kv_heads, head_dim, S.blk[nseg]),
+                                     Kv8Rows{idx, n, ld}, k, v, s));
+}
+
+sphinx_status sphinx_kv8_load(sphinx_dtype dtype, int32_t kv_heads, int32_t head_dim, const void* slice,
+                              const int32_t* cu_kv, int32_t nseg, const int32_t* idx, int32_t n, void* k, void* v,
+                              int64_t ld, void* stream) {
+  bool todo;
+  const sphinx_status st = kv8_rows_check(dtype, kv_heads, head_dim, k, v, ld, idx, n, cu_kv, nseg, slice, &todo);
+  if (st != SPHINX_OK || !todo) return st;
+  const Kv8Segs S = kv8_segs(cu_kv, nseg);
+  hipStream_t s = (hipStream_t)stream;
+  Bracket br(SPHINX_K_KV_STORE, s);
+  return hip_status(launch_kv8_load(dtype, head_dim, S,
+                                    kv8_slice(const_cast<void*>(slice), kv_heads, head_dim, S.blk[nseg]),
+                                    Kv8Rows{idx, n, ld}, k, v, s));
+}
+
+namespace {
+sphinx_status kv8_attention_check(sphinx_dtype dtype, int32_t heads, int32_t kv_heads, int32_t head_dim,
+                                  const int32_t* cu_q, const int32_t* cu_kv, int32_t nseg) {
+  if (!valid_dtype(dtype)) return SPHINX_E_UNSUPPORTED;
+  const sphinx_status st = kv8_check(kv_heads, head_dim, cu_kv, nseg);
+  if (st != SPHINX_OK) return st;
+  if (heads < 1 || heads % kv_heads != 0 || cu_q == nullptr || cu_q[0] != 0) return SPHINX_E_INVALID;
+  if ((dtype == SPHINX_F32 && head_dim != 64) || (int64_t)heads * head_dim > 65536) return SPHINX_E_UNSUPPORTED;
+  for (int i = 0; i < nseg; ++i)
+    if (cu_q[i + 1] < cu_q[i]) return SPHINX_E_INVALID;
+  // rows (queries x heads) are counted in 32 bits
+  if ((int64_t)cu_q[nseg] * heads >= ((int64_t)1 << 31)) return SPHINX_E_UNSUPPORTED;
+  return SPHINX_OK;
+}
+}  // namespace
+
+sphinx_status sphinx_kv8_attention_workspace_bytes(sphinx_dtype dtype, int32_t heads, int32_t kv_heads,
+                                                   int32_t head_dim, const int32_t* cu_q, const int32_t* cu_kv,
+                                                   int32_t nseg, size_t* bytes) {
+  const sphinx_status st = kv8_attention_check(dtype, heads, kv_heads, head_dim, cu_q, cu_kv, nseg);
+  if (st != SPHINX_OK) return st;
+  if (bytes == nullptr) return SPHINX_E_INVALID;
+  *bytes = 256;
+  return SPHINX_OK;
+}
+
+sphinx_status sphinx_kv8_attention(sphinx_dtype dtype, int32_t heads, int32_t kv_heads, int32_t head_dim,
+                                   const void* q, int64_t ldq, const void* slice, const int32_t* cu_q,
+                                   const int32_t* cu_kv, const int32_t* kv_len, int32_t nseg, void* o, void* ws,
+                                   size_t ws_bytes, void* stream) {
+  sphinx_status st = kv8_attention_check(dtype, heads, kv_heads, head_dim, cu_q, cu_kv, nseg);
+  if (st != SPHINX_OK) return st;
+  const int64_t D = (int64_t)heads * head_dim;
+  if (ldq < D || ldq % 8 != 0) return SPHINX_E_INVALID;
+  for (int i = 0; kv_len != nullptr && i < nseg; ++i)
+    if (kv_len[i] < 0 || kv_len[i] > cu_kv[i + 1] - cu_kv[i]) return SPHINX_E_INVALID;
+  if (cu_q[nseg] == 0) return SPHINX_OK;
+  if (!q || !o || !slice || !ws || !aligned(q, 16) || !aligned(o, 16) || !aligned(slice, 16) || !aligned(ws, 256))
+    return SPHINX_E_INVALID;
+  size_t need;
+  st = sphinx_kv8_attention_workspace_bytes(dtype, heads, kv_heads, head_dim, cu_q, cu_kv, nseg, &need);
+  if (st != SPHINX_OK) return st;
+  if (ws_bytes < need) return SPHINX_E_WORKSPACE;
+  const Kv8Segs S = kv8_segs(cu_kv, nseg);
+  Kv8Attn A;
+  std::memset(&A, 0, sizeof(A));
+  A.q = q;
+  A.o = o;
+  A.ldq = ldq;
+  A.ldo = D;
+  A.group = heads / kv_heads;
+  auto keys = [&](int i) { return kv_len ? kv_len[i] : cu_kv[i + 1] - cu_kv[i]; };
+  int order[SPHINX_MAX_REQUESTS];  // segments with queries, most keys first
+  for (int i = 0; i < nseg; ++i) {
+    if (cu_q[i + 1] == cu_q[i]) continue;
+    int at = A.nseg++;
+    for (; at > 0 && keys(order[at - 1]) < keys(i); --at) order[at] = order[at - 1];
+    order[at] = i;
+  }
+  for (int j = 0; j < A.nseg; ++j) {
+    const int i = order[j];
+    A.q0[j] = cu_q[i];
+    A.nq[j] = cu_q[i + 1] - cu_q[i];
+    A.klen[j] = keys(i);
+    A.blk[j] = S.blk[i];
+  }
+  hipStream_t s = (hipStream_t)stream;
+  Bracket br(SPHINX_K_ATTENTION, s);
+  return hip_status(launch_kv8_attention(
+      dtype, head_dim, A, kv8_slice(const_cast<void*>(slice), kv_heads, head_dim, S.blk[nseg]), s));
+}
+
+namespace {
+// The requests as the segments of an 8-bit cache.
+Kv8Segs kv8_request_segs(const ReqTable& T) {
+  int32_t cu[SPHINX_MAX_REQUESTS + 1];
+  for (int r = 0; r <= T.R; ++r) cu[r] = (int32_t)T.tok_off[r];
+  return kv8_segs(cu, T.R);
+}
+
+sphinx_status kv8_model_check(const sphinx_model_desc* m) {
+  return m->head_dim == 64 || (m->head_dim == 72 && m->dtype == SPHINX_BF16) ? SPHINX_OK : SPHINX_E_UNSUPPORTED;
+}
+
+// Workspace of a refine step with the 8-bit cache, behind the ordinary one:
+// the attention's, or a factorised model's read-back slice.
+size_t kv8_refine_extra(const sphinx_model_desc& m, const ReqTable& T) {
+  if (m.attention == SPHINX_ATTN_FACTORISED) return align256((size_t)T.tok_off[T.R] * 2 * m.D * esize(m.dtype));
+  return 256;
+}
+
 // One denoiser pass plus the DDIM update over the n forwarded rows; with a
 // cache (kv_cache != NULL) every block stores the rows' keys and values and
-// attends over all tokens of each request through the cache.
+// attends over all tokens of each request through the cache, which holds the
+// model's dtype or (kv8) 8 bits.
 sphinx_status refine_impl(const sphinx_model_desc* m, const sphinx_request* reqs, int32_t R, const int32_t* idx,
                           int32_t n_sel, const int32_t* cu_sel_host, const int32_t* tau, const float* c1,
-                          const float* c2, float* x_sel, void* kv_cache, void* ws, size_t ws_bytes, void* stream) {
+                          const float* c2, float* x_sel, void* kv_cache, bool kv8, void* ws, size_t ws_bytes,
+                          void* stream) {
   sphinx_status st = check_model(m);
+  if (st == SPHINX_OK && kv8) st = kv8_model_check(m);
   if (st != SPHINX_OK) return st;
   ReqTable T;
   int64_t N;
@@ -616,7 +791,7 @@ sphinx_status refine_impl(const sphinx_model_desc* m, const sphinx_request* reqs
       if (T.frames[r] > 64) return SPHINX_E_UNSUPPORTED;
   }
   const RefineWs W = refine_layout(*m, T, G, n_sel);
-  if (ws_bytes < W.total) return SPHINX_E_WORKSPACE;
+  if (ws_bytes < W.total + (kv8 ? kv8_refine_extra(*m, T) : 0)) return SPHINX_E_WORKSPACE;
   const bool cached = kv_cache != nullptr;
 
   // segments: requests with forwarded tokens, most keys first for the attention schedule
@@ -638,6 +813,23 @@ sphinx_status refine_impl(const sphinx_model_desc* m, const sphinx_request* reqs
     S.kv_start[i] = cached ? (int)T.tok_off[r] : S.start[i];
     S.kv_len[i] = (int)keys(r);
     S.tile_prefix[i + 1] = S.tile_prefix[i] + (S.len[i] + kAttnQueryTile - 1) / kAttnQueryTile;
+  }
+
+  // the same segments as attention over the 8-bit cache
+  Kv8Segs S8;
+  Kv8Attn A8;
+  std::memset(&S8, 0, sizeof(S8));
+  std::memset(&A8, 0, sizeof(A8));
+  if (kv8) {
+    S8 = kv8_request_segs(T);
+    A8.group = 1;
+    A8.nseg = S.nseg;
+    for (int i = 0; i < S.nseg; ++i) {
+      A8.q0[i] = S.start[i];
+      A8.nq[i] = S.len[i];
+      A8.klen[i] = S.kv_len[i];
+      A8.blk[i] = S8.blk[order[i]];
+    }
   }
 
   hipStream_t s = (hipStream_t)stream;
@@ -733,7 +925,22 @@ sphinx_status refine_impl(const sphinx_model_desc* m, const sphinx_request* reqs
     }
     AttnIO io{qkv, static_cast<const unsigned char*>(qkv) + (size_t)D * esize(dt),
               static_cast<const unsigned char*>(qkv) + 2 * (size_t)D * esize(dt), obuf, 3 * D, 3 * D};
-    if (cached) {
+    Kv8Slice slice = {};
+    if (kv8) {
+      const int64_t nblk = S8.blk[R];
+      slice = kv8_slice(static_cast<unsigned char*>(kv_cache) +
+                            (size_t)l * kv8_slice_bytes(m->heads, m->head_dim, nblk), m->heads, m->head_dim, nblk);
+      Bracket br(SPHINX_K_KV_STORE, s);
+      SPHINX_TRY(launch_kv8_store(dt, m->head_dim, S8, slice, Kv8Rows{idx, n, io.ldkv}, io.k, io.v, s));
+      if (factorised) {  // its attention reads rows: the whole slice, key beside value
+        unsigned char* rows = base + W.total;
+        io.k = rows;
+        io.v = rows + (size_t)D * esize(dt);
+        io.ldkv = 2 * D;
+        SPHINX_TRY(launch_kv8_load(dt, m->head_dim, S8, slice, Kv8Rows{nullptr, (int)N, io.ldkv}, rows,
+                                   rows + (size_t)D * esize(dt), s));
+      }
+    } else if (cached) {
       unsigned char* cl = static_cast<unsigned char*>(kv_cache) + (size_t)l * (size_t)N * 2 * D * esize(dt);
       Bracket br(SPHINX_K_KV_STORE, s);
       SPHINX_TRY(launch_kv_store(dt, qkv, n, D, idx, N, cl, s));
@@ -743,7 +950,13 @@ sphinx_status refine_impl(const sphinx_model_desc* m, const sphinx_request* reqs
     }
     {
       Bracket br(SPHINX_K_ATTENTION, s);
-      if (!factorised)
+      if (kv8 && !factorised) {
+        A8.q = io.q;
+        A8.o = io.o;
+        A8.ldq = io.ldq;
+        A8.ldo = D;
+        SPHINX_TRY(launch_kv8_attention(dt, m->head_dim, A8, slice, s));
+      } else if (!factorised)
         SPHINX_TRY(launch_attention(dt, io, D, m->heads, m->head_dim, S, s));
       else if (l % 2 == 0)  // spatial: within the frame
         SPHINX_TRY(launch_attention(dt, io, D, m->heads, m->head_dim, Sf, s));
@@ -783,7 +996,7 @@ sphinx_status sphinx_refine_step(const sphinx_model_desc* m, const sphinx_reques
                                  const int32_t* idx, int32_t n_sel, const int32_t* cu_sel_host,
                                  const int32_t* tau, const float* c1, const float* c2, float* x_sel, void* ws,
                                  size_t ws_bytes, void* stream) {
-  return refine_impl(m, reqs, R, idx, n_sel, cu_sel_host, tau, c1, c2, x_sel, nullptr, ws, ws_bytes, stream);
+  return refine_impl(m, reqs, R, idx, n_sel, cu_sel_host, tau, c1, c2, x_sel, nullptr, false, ws, ws_bytes, stream);
 }
 
 sphinx_status sphinx_refine_step_cached(const sphinx_model_desc* m, const sphinx_request* reqs, int32_t R,
@@ -791,7 +1004,46 @@ sphinx_status sphinx_refine_step_cached(const sphinx_model_desc* m, const sphinx
                                         const float* c1, const float* c2, float* x, void* kv_cache, void* ws,
                                         size_t ws_bytes, void* stream) {
   if (kv_cache == nullptr) return SPHINX_E_INVALID;
-  return refine_impl(m, reqs, R, idx, n, cu_host, tau, c1, c2, x, kv_cache, ws, ws_bytes, stream);
+  return refine_impl(m, reqs, R, idx, n, cu_host, tau, c1, c2, x, kv_cache, false, ws, ws_bytes, stream);
+}
+
+sphinx_status sphinx_refine_step_kv8(const sphinx_model_desc* m, const sphinx_request* reqs, int32_t R,
+                                     const int32_t* idx, int32_t n, const int32_t* cu_host, const int32_t* tau,
+                                     const float* c1, const float* c2, float* x, void* kv_cache, void* ws,
+                                     size_t ws_bytes, void* stream) {
+  if (kv_cache == nullptr) return SPHINX_E_INVALID;
+  return refine_impl(m, reqs, R, idx, n, cu_host, tau, c1, c2, x, kv_cache, true, ws, ws_bytes, stream);
+}
+
+sphinx_status sphinx_kv8_cache_bytes(const sphinx_model_desc* m, const sphinx_request* reqs, int32_t R,
+                                     size_t* bytes) {
+  sphinx_status st = check_model(m);
+  if (st != SPHINX_OK) return st;
+  st = kv8_model_check(m);
+  if (st != SPHINX_OK) return st;
+  ReqTable T;
+  int64_t N;
+  int32_t G;
+  st = build_table(reqs, R, &T, &N, &G);
+  if (st != SPHINX_OK) return st;
+  if (bytes == nullptr) return SPHINX_E_INVALID;
+  *bytes = (size_t)m->L * kv8_slice_bytes(m->heads, m->head_dim, kv8_request_segs(T).blk[R]);
+  return SPHINX_OK;
+}
+
+sphinx_status sphinx_refine_kv8_workspace_bytes(const sphinx_model_desc* m, const sphinx_request* reqs, int32_t R,
+                                                int64_t max_sel, size_t* bytes) {
+  sphinx_status st = sphinx_refine_workspace_bytes(m, reqs, R, max_sel, bytes);
+  if (st != SPHINX_OK) return st;
+  st = kv8_model_check(m);
+  if (st != SPHINX_OK) return st;
+  ReqTable T;
+  int64_t N;
+  int32_t G;
+  st = build_table(reqs, R, &T, &N, &G);
+  if (st != SPHINX_OK) return st;
+  *bytes += kv8_refine_extra(*m, T);
+  return SPHINX_OK;
 }
 
 sphinx_status sphinx_varlen_attention(sphinx_dtype dtype, int32_t heads, int32_t head_dim, const void* q,

@@ -13,6 +13,8 @@ step is a full step that forwards every token of the live requests (a second
 ``sphinx_select_mask`` with threshold -inf over the frames of full requests),
 and every step runs ``sphinx_gather_ctx``, ``sphinx_refine_step_cached`` and
 ``sphinx_scatter_masked`` so that only the write set (the mask) is updated.
+``cache_dtype="fp8"`` keeps the cache in 8 bits with a scale per block of 64
+tokens and head (``sphinx_refine_step_kv8``): half the bytes of a bf16 cache.
 
 The fp32 state of record and the noise live token-major by default (token t's
 16 values contiguous at 16*t), so each gathered or scattered token is one
@@ -70,7 +72,11 @@ class Refiner:
     def __init__(self, requests: Sequence, cfg, blob: torch.Tensor, s_start: np.ndarray, nsteps: np.ndarray,
                  u: np.ndarray, thr: np.ndarray, z0: np.ndarray, eps: np.ndarray, device="cuda",
                  max_sel: Optional[int] = None, layout: int = B.TOKENS, cache_period: int = 0,
-                 per_frame_grid: bool = False):
+                 per_frame_grid: bool = False, cache_dtype: str = "model"):
+        if cache_dtype not in ("model", "fp8"):
+            raise ValueError(f"cache_dtype {cache_dtype!r}: 'model' or 'fp8'")
+        if cache_dtype != "model" and cache_period <= 0:
+            raise ValueError("cache_dtype needs a cache: set cache_period")
         if not torch.cuda.is_available():
             raise RuntimeError("Refiner needs a GPU: the selective-refinement step has no CPU path")
         B.lib()
@@ -109,8 +115,9 @@ class Refiner:
         self.max_sel = self.N if max_sel is None else int(max_sel)
         self.x_sel = torch.empty(16 * self.max_sel, dtype=torch.float32, device=dev)
         self.ws_sel = torch.empty(B.sphinx_select_workspace_bytes(self.N), dtype=torch.uint8, device=dev)
-        self.ws = torch.empty(B.sphinx_refine_workspace_bytes(self.desc, self.reqs, self.max_sel),
-                              dtype=torch.uint8, device=dev)
+        self.kv8 = cache_dtype == "fp8"
+        ws_bytes = B.sphinx_refine_kv8_workspace_bytes if self.kv8 else B.sphinx_refine_workspace_bytes
+        self.ws = torch.empty(ws_bytes(self.desc, self.reqs, self.max_sel), dtype=torch.uint8, device=dev)
         self.total_steps = int(np.max(nsteps))
         self.grid = B.GRID_PER_FRAME if per_frame_grid else B.GRID_SHARED
         plans = [B.sphinx_plan_step(self.reqs, s_start, nsteps, i, self.grid) for i in range(self.total_steps)]
@@ -126,7 +133,8 @@ class Refiner:
         if self.cache_period > 0:
             if self.max_sel != self.N:
                 raise ValueError("the latent cache forwards every token on full steps: max_sel must be N")
-            self.kv_cache = torch.zeros(B.sphinx_kv_cache_bytes(self.desc, self.reqs), dtype=torch.uint8, device=dev)
+            cache_bytes = B.sphinx_kv8_cache_bytes if self.kv8 else B.sphinx_kv_cache_bytes
+            self.kv_cache = torch.zeros(cache_bytes(self.desc, self.reqs), dtype=torch.uint8, device=dev)
             cplans = [B.sphinx_plan_cache(self.reqs, s_start, nsteps, i, self.cache_period, self.grid)
                       for i in range(self.total_steps)]
             self.cache_host = {k: np.stack([p[k] for p in cplans]) for k in cplans[0]}
@@ -232,8 +240,9 @@ class Refiner:
             return 0
         B.sphinx_gather_ctx(self.reqs, self.layout, self.z, B.F32, self.eps, self.dt, idx_f, n_f, self.mask,
                             P["a"][k], P["b"][k], C["a_ctx"][k], C["b_ctx"][k], self.x_sel, stream)
-        B.sphinx_refine_step_cached(self.desc, self.reqs, idx_f, n_f, cu_f, P["tau"][k], P["c1"][k], P["c2"][k],
-                                    self.x_sel, self.kv_cache, self.ws, stream)
+        refine = B.sphinx_refine_step_kv8 if self.kv8 else B.sphinx_refine_step_cached
+        refine(self.desc, self.reqs, idx_f, n_f, cu_f, P["tau"][k], P["c1"][k], P["c2"][k], self.x_sel, self.kv_cache,
+               self.ws, stream)
         B.sphinx_scatter_masked(self.reqs, self.x_sel, idx_f, n_f, self.mask, self.z, B.F32, self.layout, stream)
         return n
 
