@@ -683,7 +683,12 @@ sphinx_status sphinx_kv8_attention_workspace_bytes(sphinx_dtype dtype, int32_t h
   const sphinx_status st = kv8_attention_check(dtype, heads, kv_heads, head_dim, cu_q, cu_kv, nseg);
   if (st != SPHINX_OK) return st;
   if (bytes == nullptr) return SPHINX_E_INVALID;
-  *bytes = 256;
+  int nq[SPHINX_MAX_REQUESTS], klen[SPHINX_MAX_REQUESTS];
+  for (int i = 0; i < nseg; ++i) {
+    nq[i] = cu_q[i + 1] - cu_q[i];
+    klen[i] = cu_kv[i + 1] - cu_kv[i];
+  }
+  *bytes = kv8_attention_ws_bytes(kv_heads, head_dim, heads / kv_heads, nseg, nq, klen);
   return SPHINX_OK;
 }
 
@@ -730,7 +735,7 @@ sphinx_status sphinx_kv8_attention(sphinx_dtype dtype, int32_t heads, int32_t kv
   hipStream_t s = (hipStream_t)stream;
   Bracket br(SPHINX_K_ATTENTION, s);
   return hip_status(launch_kv8_attention(
-      dtype, head_dim, A, kv8_slice(const_cast<void*>(slice), kv_heads, head_dim, S.blk[nseg]), s));
+      dtype, head_dim, A, kv8_slice(const_cast<void*>(slice), kv_heads, head_dim, S.blk[nseg]), ws, s));
 }
 
 namespace {
@@ -747,9 +752,15 @@ sphinx_status kv8_model_check(const sphinx_model_desc* m) {
 
 // Workspace of a refine step with the 8-bit cache, behind the ordinary one:
 // the attention's, or a factorised model's read-back slice.
-size_t kv8_refine_extra(const sphinx_model_desc& m, const ReqTable& T) {
+// `sel`: forwarded tokens at most, of whichever requests.
+size_t kv8_refine_extra(const sphinx_model_desc& m, const ReqTable& T, int64_t sel) {
   if (m.attention == SPHINX_ATTN_FACTORISED) return align256((size_t)T.tok_off[T.R] * 2 * m.D * esize(m.dtype));
-  return 256;
+  int nq[SPHINX_MAX_REQUESTS], klen[SPHINX_MAX_REQUESTS];
+  for (int r = 0; r < T.R; ++r) {
+    klen[r] = (int)(T.tok_off[r + 1] - T.tok_off[r]);
+    nq[r] = (int)std::min<int64_t>(sel, klen[r]);
+  }
+  return align256(kv8_attention_ws_bytes(m.heads, m.head_dim, 1, T.R, nq, klen));
 }
 
 // One denoiser pass plus the DDIM update over the n forwarded rows; with a
@@ -791,7 +802,7 @@ sphinx_status refine_impl(const sphinx_model_desc* m, const sphinx_request* reqs
       if (T.frames[r] > 64) return SPHINX_E_UNSUPPORTED;
   }
   const RefineWs W = refine_layout(*m, T, G, n_sel);
-  if (ws_bytes < W.total + (kv8 ? kv8_refine_extra(*m, T) : 0)) return SPHINX_E_WORKSPACE;
+  if (ws_bytes < W.total + (kv8 ? kv8_refine_extra(*m, T, n_sel) : 0)) return SPHINX_E_WORKSPACE;
   const bool cached = kv_cache != nullptr;
 
   // segments: requests with forwarded tokens, most keys first for the attention schedule
@@ -955,7 +966,7 @@ sphinx_status refine_impl(const sphinx_model_desc* m, const sphinx_request* reqs
         A8.o = io.o;
         A8.ldq = io.ldq;
         A8.ldo = D;
-        SPHINX_TRY(launch_kv8_attention(dt, m->head_dim, A8, slice, s));
+        SPHINX_TRY(launch_kv8_attention(dt, m->head_dim, A8, slice, base + W.total, s));
       } else if (!factorised)
         SPHINX_TRY(launch_attention(dt, io, D, m->heads, m->head_dim, S, s));
       else if (l % 2 == 0)  // spatial: within the frame
@@ -1042,7 +1053,7 @@ sphinx_status sphinx_refine_kv8_workspace_bytes(const sphinx_model_desc* m, cons
   int32_t G;
   st = build_table(reqs, R, &T, &N, &G);
   if (st != SPHINX_OK) return st;
-  *bytes += kv8_refine_extra(*m, T);
+  *bytes += kv8_refine_extra(*m, T, std::max<int64_t>(max_sel, 1));
   return SPHINX_OK;
 }
 

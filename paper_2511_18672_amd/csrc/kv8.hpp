@@ -61,9 +61,10 @@ hipError_t launch_kv8_store(sphinx_dtype dt, int head_dim, const Kv8Segs& S, con
 hipError_t launch_kv8_load(sphinx_dtype dt, int head_dim, const Kv8Segs& S, const Kv8Slice& c, const Kv8Rows& rows,
                            void* k, void* v, hipStream_t s);
 
-// One attention launch: segment i has queries [q0[i], q0[i] + nq[i]), which
-// attend to the first klen[i] tokens of slice segment i.  A row is a query of
-// one of the `group` query heads that share a key/value head.
+// One attention call: segment i (of those with queries, most keys first) has
+// queries [q0[i], q0[i] + nq[i]), which attend to the first klen[i] tokens of
+// the slice's segment that starts at block blk[i].  A row is a query of one of
+// the `group` query heads that share a key/value head.
 struct Kv8Attn {
   const void* q;
   void* o;
@@ -73,11 +74,14 @@ struct Kv8Attn {
   int q0[SPHINX_MAX_REQUESTS];
   int nq[SPHINX_MAX_REQUESTS];
   int klen[SPHINX_MAX_REQUESTS];
-  int blk[SPHINX_MAX_REQUESTS];           // first block
-  int tile_prefix[SPHINX_MAX_REQUESTS + 1];  // row tiles of the segments before
+  int blk[SPHINX_MAX_REQUESTS];
 };
 
 // kv8_attention.hip
-hipError_t launch_kv8_attention(sphinx_dtype dt, int head_dim, const Kv8Attn& A, const Kv8Slice& c, hipStream_t s);
+// Workspace of a call with these segments, whatever part of their tokens counts
+// (klen up to the given ones).
+size_t kv8_attention_ws_bytes(int kv_heads, int head_dim, int group, int nseg, const int* nq, const int* klen);
+hipError_t launch_kv8_attention(sphinx_dtype dt, int head_dim, const Kv8Attn& A, const Kv8Slice& c, void* ws,
+                                hipStream_t s);
 
 }  // namespace sphinx
