@@ -14,7 +14,7 @@ namespace {
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 constexpr int kTPB = 256;
-constexpr int kRows = kKv8RowTile;  // rows (queries of the heads that share a key/value head) per workgroup
+constexpr int kRows = 32;  // rows (queries of the heads that share a key/value head) per workgroup
 
 __device__ __forceinline__ float fast_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
 
@@ -270,6 +270,493 @@ __global__ __launch_bounds__(kTPB, 2) void k_kv8_attn_rows(Kv8Attn A, Kv8Slice c
   }
 }
 
+// ---------------------------------------------------------------------------
+// Many rows: one workgroup = 128 rows of one segment and key/value head against
+// one chunk of its keys, four waves of 32 rows.  The matrix cores set the floor
+// (bf16 products: 256 cycles a wave for K Q^T of 64 keys at head_dim 64 and as
+// many for V^T P^T), next to the exponentials; so bytes become bf16 once per
+// workgroup, not once per wave:
+//  * thread t holds chunk t of a block's key tile and of its value tile (one
+//    16-byte load each, issued an iteration ahead), turns them into two
+//    fragments each and writes these to LDS in the order in which a wave reads
+//    them (fragment f at 1024 f, 16 bytes a lane), so that writes and reads
+//    are consecutive and free of bank conflicts, with constant offsets;
+//  * iteration t does K Q^T of block t + 1 and V^T P^T of block t - 1 next to the
+//    softmax of block t, none of which waits on another, as one straight run of
+//    steps: a product, two exponentials, the rounding and the sum of a pair of
+//    probabilities, and a conversion of the staged bytes;
+//  * LDS holds two blocks of keys and two of values: in iteration t the keys
+//    t + 1 and the values t - 1 are read, the keys t + 2 and the values t
+//    written, and one barrier ends it;
+//  * no maximum is taken per block: probabilities are 2^(score - m) with m fixed
+//    at 0 (or at the first block's maximum, if that is not in [-24, 24]) until
+//    a block's probabilities sum past 2^32; then m moves to that block's
+//    maximum, O and l are rescaled and the block's probabilities are made again
+//    from its bytes.
+template <int HD>
+struct TileGeo {
+  static constexpr int DB = (HD + 31) / 32;   // 32-row blocks of O^T (head_dim 72: of the third, 8 rows count)
+  static constexpr int NPV = 4 * DB, NQK = HD == 72 ? 10 : 8;
+  static constexpr int SLOT = 8192 + (HD == 72 ? 1024 : 0);  // one block's keys, or its values, as bf16
+  static constexpr int TILE = kKv8Block * HD;                // the same as bytes
+};
+template <int HD>
+struct TileSmem {
+  unsigned char k[2][TileGeo<HD>::SLOT];
+  unsigned char v[2][TileGeo<HD>::SLOT];
+};
+constexpr float kPsumMax = 4294967296.0f;  // 2^32
+
+// acc + p.x + p.y; volatile, so that it stays in its step
+__device__ __forceinline__ float add_pair(float acc, bf16x2 p) {
+  asm volatile("v_dot2c_f32_bf16_e32 %0, 0x3f803f80, %1" : "+v"(acc) : "v"(__builtin_bit_cast(unsigned, p)));
+  return acc;
+}
+__device__ __forceinline__ bf16x2 cvt2(uint32_t w, float scale, bool hi) {
+  return hi ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, scale, true)
+            : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, scale, false);
+}
+__device__ __forceinline__ uint32_t keep_keys(uint32_t w, int left) {  // the first `left` of four bytes
+  const int n = min(max(left, 0), 4);
+  return w & (n == 4 ? ~0u : (1u << (8 * n)) - 1u);
+}
+
+template <int HD>
+__global__ __launch_bounds__(kTPB, HD == 64 ? 3 : 2) void k_kv8_attn_tiles(Kv8Attn A, Kv8Slice c, Kv8Plan P,
+                                                                            Parts part, int first, int total) {
+  typedef TileGeo<HD> G;
+  constexpr int DB = G::DB, NPV = G::NPV, NSTEP = G::NPV + G::NQK;
+  __shared__ __attribute__((aligned(16))) TileSmem<HD> sm;
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int g = lane >> 5, r32 = lane & 31;
+  // whole heads per XCD, and within a head the row tiles of a chunk side by side:
+  // they read the same bytes
+  const int unit = xcd_tile(first + (int)blockIdx.x, total), items = P.item[A.nseg];
+  const int h = unit / items, item = unit - h * items;
+  int s = 0;
+  while (s + 1 < A.nseg && P.item[s + 1] <= item) ++s;
+  const int chunks = P.chunks[s], tiles = (P.item[s + 1] - P.item[s]) / chunks;
+  const int chunk = (item - P.item[s]) / tiles, tile = item - P.item[s] - chunk * tiles;
+  const int nrows = A.nq[s] * A.group;
+  const int L = A.klen[s], b0 = chunk * P.chunk, nkt = min((L + kKv8Block - 1) / kKv8Block - b0, P.chunk);
+  const int row = tile * 128 + wave * 32 + r32;
+  auto row_of = [&](int64_t ld) -> int64_t {
+    const int q = row / A.group;
+    return (A.q0[s] + (int64_t)q) * ld + (int64_t)(h * A.group + row - q * A.group) * HD;
+  };
+  const bf16x8 zero8 = {};
+  bf16x8 qf[4];
+  s16x4 q4 = {};
+#pragma unroll
+  for (int ks = 0; ks < 4; ++ks) qf[ks] = zero8;
+  if (row < nrows) {
+    const bf16* Q = static_cast<const bf16*>(A.q) + row_of(A.ldq);
+#pragma unroll
+    for (int ks = 0; ks < 4; ++ks) qf[ks] = *reinterpret_cast<const bf16x8*>(Q + 32 * g + 8 * ks);
+    if constexpr (HD == 72) q4 = *reinterpret_cast<const s16x4*>(Q + 64 + 4 * g);
+  }
+  const unsigned char* base = c.tiles + ((int64_t)h * c.nblk + A.blk[s] + b0) * 2 * G::TILE;
+  const unsigned char* scales = c.scales + ((int64_t)h * c.nblk + A.blk[s] + b0) * 2;
+  const int last = L - (b0 + nkt - 1) * kKv8Block;  // keys of the chunk's last block (64 and more: whole)
+
+  // Staged bytes: chunk `tid` of a key tile and of a value tile; head_dim 72:
+  // also the eight bytes behind the key chunks of row `lane` (wave 0) and the
+  // chunk behind the value chunks (wave 1, 32 lanes).
+  uint4 sk, sv;
+  uint4 st = make_uint4(0u, 0u, 0u, 0u);
+  float ksc, vsc;
+  auto fetch_k = [&](int t) {
+    const unsigned char* p = base + (int64_t)t * 2 * G::TILE;
+    sk = *reinterpret_cast<const uint4*>(p + tid * 16);
+    ksc = byte_scale(scales[2 * (int64_t)t]);
+    if constexpr (HD == 72) {
+      if (wave == 0) {
+        const uint2 x = *reinterpret_cast<const uint2*>(p + 4096 + lane * 8);
+        st.x = x.x;
+        st.y = x.y;
+      }
+    }
+  };
+  auto fetch_v = [&](int t) {
+    const unsigned char* p = base + (int64_t)t * 2 * G::TILE + G::TILE;
+    sv = *reinterpret_cast<const uint4*>(p + tid * 16);
+    vsc = byte_scale(scales[2 * (int64_t)t + 1]);
+    if constexpr (HD == 72) {
+      if (wave == 1) st = *reinterpret_cast<const uint4*>(p + 4096 + (lane & 31) * 16);
+    }
+  };
+  // what lies behind the segment's last key may hold anything: its values become zero
+  auto trim_v = [&]() {
+    const int kb = wave & 1;
+    uint32_t* w = reinterpret_cast<uint32_t*>(&sv);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = keep_keys(w[i], last - (32 * kb + 8 * i + 4 * g));
+    if constexpr (HD == 72) {
+      if (wave == 1) {
+        uint32_t* x = reinterpret_cast<uint32_t*>(&st);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] = keep_keys(x[i], last - (32 * ((lane >> 4) & 1) + 8 * i + 4 * ((lane >> 3) & 1)));
+      }
+    }
+  };
+  auto put = [&](unsigned char* slot, int e, const uint4& b, float scale) {  // half e of a chunk: fragment 2 wave + e
+    const uint32_t w0 = e ? b.z : b.x, w1 = e ? b.w : b.y;
+    bf16x8 f;
+    const bf16x2 a0 = cvt2(w0, scale, false), a1 = cvt2(w0, scale, true);
+    const bf16x2 a2 = cvt2(w1, scale, false), a3 = cvt2(w1, scale, true);
+    f[0] = a0[0]; f[1] = a0[1]; f[2] = a1[0]; f[3] = a1[1];
+    f[4] = a2[0]; f[5] = a2[1]; f[6] = a3[0]; f[7] = a3[1];
+    *reinterpret_cast<bf16x8*>(slot + (2 * wave + e) * 1024 + lane * 16) = f;
+  };
+  auto put_k8 = [&](unsigned char* slot) {  // dims 64 .. 71: [32-row block][g][row] eight bytes
+    if (wave != 0) return;
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      const uint32_t w = e ? st.y : st.x;
+      bf16x4 f;
+      const bf16x2 a0 = cvt2(w, ksc, false), a1 = cvt2(w, ksc, true);
+      f[0] = a0[0]; f[1] = a0[1]; f[2] = a1[0]; f[3] = a1[1];
+      *reinterpret_cast<bf16x4*>(slot + 8192 + (lane >> 5) * 512 + e * 256 + (lane & 31) * 8) = f;
+    }
+  };
+  auto put_v8 = [&](unsigned char* slot) {  // [32-key block][half][g][dim] sixteen bytes
+    if (wave != 1 || lane >= 32) return;
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      const uint32_t w0 = e ? st.z : st.x, w1 = e ? st.w : st.y;
+      bf16x8 f;
+      const bf16x2 a0 = cvt2(w0, vsc, false), a1 = cvt2(w0, vsc, true);
+      const bf16x2 a2 = cvt2(w1, vsc, false), a3 = cvt2(w1, vsc, true);
+      f[0] = a0[0]; f[1] = a0[1]; f[2] = a1[0]; f[3] = a1[1];
+      f[4] = a2[0]; f[5] = a2[1]; f[6] = a3[0]; f[7] = a3[1];
+      *reinterpret_cast<bf16x8*>(slot + 8192 + ((lane >> 4) * 2 + e) * 256 + (lane & 15) * 16) = f;
+    }
+  };
+  // Fragment reads.  keys: 32-row block rb, k-step ks; values: key block kb, half hf, dim block db
+  auto key_frag = [&](const unsigned char* slot, int rb, int ks) -> bf16x8 {
+    return *reinterpret_cast<const bf16x8*>(slot + (rb * 4 + ks) * 1024 + lane * 16);
+  };
+  auto key_tail = [&](const unsigned char* slot, int rb) -> s16x4 {
+    return *reinterpret_cast<const s16x4*>(slot + 8192 + rb * 512 + lane * 8);
+  };
+  auto val_frag = [&](const unsigned char* slot, int kb, int hf, int db) -> bf16x8 {
+    if (db < 2) return *reinterpret_cast<const bf16x8*>(slot + ((db * 2 + kb) * 2 + hf) * 1024 + lane * 16);
+    return *reinterpret_cast<const bf16x8*>(slot + 8192 + (kb * 2 + hf) * 256 + g * 128 + (r32 & 7) * 16);
+  };
+  auto qk = [&](const unsigned char* slot, f32x16& s0, f32x16& s1) {
+    s0 = f32x16{};
+    s1 = f32x16{};
+#pragma unroll
+    for (int ks = 0; ks < 4; ++ks) {
+      s0 = __builtin_amdgcn_mfma_f32_32x32x16_bf16(key_frag(slot, 0, ks), qf[ks], s0, 0, 0, 0);
+      s1 = __builtin_amdgcn_mfma_f32_32x32x16_bf16(key_frag(slot, 1, ks), qf[ks], s1, 0, 0, 0);
+    }
+    if constexpr (HD == 72) {
+      s0 = __builtin_amdgcn_mfma_f32_32x32x8bf16_1k(key_tail(slot, 0), q4, s0, 0, 0, 0);
+      s1 = __builtin_amdgcn_mfma_f32_32x32x8bf16_1k(key_tail(slot, 1), q4, s1, 0, 0, 0);
+    }
+  };
+  auto mask_tail = [&](f32x16& s0, f32x16& s1) {  // of the chunk's last block
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      const int key = (r >> 2) * 8 + g * 4 + (r & 3);
+      if (key >= last) s0[r] = -INFINITY;
+      if (key + 32 >= last) s1[r] = -INFINITY;
+    }
+  };
+
+  f32x16 oacc[DB];
+#pragma unroll
+  for (int db = 0; db < DB; ++db) oacc[db] = f32x16{};
+  float m_run = 0.0f, l_run = 0.0f;
+  bool shifted = false;  // wave-uniform: m_run is subtracted from the scores
+
+  // Scores of 32 keys of a block once more, from its bytes (rare).
+  auto rescore = [&](int t, int rb) -> f32x16 {
+    const unsigned char* p = base + (int64_t)t * 2 * G::TILE;
+    const float scale = byte_scale(scales[2 * (int64_t)t]);
+    f32x16 a = f32x16{};
+#pragma unroll
+    for (int hf = 0; hf < 2; ++hf) {
+      bf16x8 f[2];
+      operand(*reinterpret_cast<const uint4*>(p + ((rb * 2 + hf) * 64 + lane) * 16), scale, f);
+#pragma unroll
+      for (int e = 0; e < 2; ++e) a = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[e], qf[2 * hf + e], a, 0, 0, 0);
+    }
+    if constexpr (HD == 72) {
+      const uint32_t w = *reinterpret_cast<const uint32_t*>(p + 4096 + (32 * rb + r32) * 8 + 4 * g);
+      const bf16x2 a0 = cvt2(w, scale, false), a1 = cvt2(w, scale, true);
+      bf16x4 f;
+      f[0] = a0[0]; f[1] = a0[1]; f[2] = a1[0]; f[3] = a1[1];
+      a = __builtin_amdgcn_mfma_f32_32x32x8bf16_1k(__builtin_bit_cast(s16x4, f), q4, a, 0, 0, 0);
+    }
+#pragma unroll
+    for (int r = 0; r < 16; ++r)
+      a[r] = t == nkt - 1 && 32 * rb + (r >> 2) * 8 + g * 4 + (r & 3) >= last ? -INFINITY : a[r] - m_run;
+    return a;
+  };
+  // Moves the maximum to block t's where that is larger; O holds the blocks up to t - 1.
+  auto rebase = [&](int t, bf16x8 (&pf)[2][2]) -> float {
+    float mx = -INFINITY;
+#pragma unroll 1
+    for (int rb = 0; rb < 2; ++rb) {
+      const f32x16 a = rescore(t, rb);
+#pragma unroll
+      for (int r = 0; r < 16; ++r) mx = fmaxf(mx, a[r]);
+    }
+    mx = fmaxf(mx, __shfl_xor(mx, 32, kWave));
+    const float delta = mx > 0.0f ? mx : 0.0f, alpha = fast_exp2(-delta);
+#pragma unroll
+    for (int db = 0; db < DB; ++db) oacc[db] *= alpha;
+    l_run *= alpha;
+    m_run += delta;
+    shifted = true;
+    float psum = 0.0f;
+    bf16x8 q0[2], q1[2];
+#pragma unroll 1
+    for (int rb = 0; rb < 2; ++rb) {
+      const f32x16 a = rescore(t, rb);
+      bf16x8 x[2];
+#pragma unroll
+      for (int r = 0; r < 16; r += 2) {
+        bf16x2 pr;
+        pr[0] = (bf16)fast_exp2(a[r]);
+        pr[1] = (bf16)fast_exp2(a[r + 1]);
+        psum = add_pair(psum, pr);
+        x[r >> 3][r & 7] = pr[0];
+        x[r >> 3][(r & 7) + 1] = pr[1];
+      }
+      if (rb == 0) {
+        q0[0] = x[0];
+        q0[1] = x[1];
+      } else {
+        q1[0] = x[0];
+        q1[1] = x[1];
+      }
+    }
+    pf[0][0] = q0[0];
+    pf[0][1] = q0[1];
+    pf[1][0] = q1[0];
+    pf[1][1] = q1[1];
+    return psum;
+  };
+  auto settle = [&](f32x16& a, f32x16& b) {
+    if (shifted)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        a[r] -= m_run;
+        b[r] -= m_run;
+      }
+  };
+  auto barrier = [&]() {
+    __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0): this wave's LDS writes; loads stay in flight
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+  };
+  // Product step st: V^T P^T first (its probabilities die while new ones are made), then K Q^T
+  auto frag = [&](const unsigned char* ks_, const unsigned char* vs_, int st_) -> bf16x8 {
+    if (st_ < NPV) return val_frag(vs_, st_ / (2 * DB), (st_ / DB) & 1, st_ % DB);
+    const int ks = (st_ - NPV) >> 1, rb = (st_ - NPV) & 1;
+    if (HD == 72 && ks == 4) {
+      const s16x4 x = key_tail(ks_, rb);
+      const s16x4 r[2] = {x, x};
+      return *reinterpret_cast<const bf16x8*>(r);
+    }
+    return key_frag(ks_, rb, ks);
+  };
+  // Iteration t; PAR = t % 2.  c: scores of block t, n: of block t + 1; pp: probabilities of block t - 1, pn: of t.
+  auto iter = [&](int t, auto PAR, f32x16& c0, f32x16& c1, f32x16& n0, f32x16& n1, bf16x8 (&pp)[2][2],
+                  bf16x8 (&pn)[2][2]) {
+    constexpr int par = decltype(PAR)::value;
+    const unsigned char* kr = sm.k[par ^ 1];
+    const unsigned char* vr = sm.v[par ^ 1];
+    unsigned char* kw = sm.k[par];
+    unsigned char* vw = sm.v[par];
+    settle(c0, c1);
+    bf16x8 fr[3];
+    fr[0] = frag(kr, vr, 0);
+    fr[1] = frag(kr, vr, 1);
+    auto score = [&](int i, int e) -> float {  // pair i of the block's 16 pairs a lane
+      const int r = (i >> 3) * 8 + 2 * ((i >> 1) & 3) + e;
+      return (i & 1) ? c1[r] : c0[r];
+    };
+    float ex[16][2];
+#pragma unroll
+    for (int e = 0; e < 2; ++e) ex[0][e] = fast_exp2(score(0, e));
+    __builtin_amdgcn_sched_barrier(0);
+    float psum = 0.0f;
+    const f32x16 zero16 = {};
+#pragma unroll
+    for (int i = 0; i < NSTEP; ++i) {
+      if (i + 2 < NSTEP) fr[(i + 2) % 3] = frag(kr, vr, i + 2);
+      if (i < NPV) {
+        oacc[i % DB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fr[i % 3], pp[i / (2 * DB)][(i / DB) & 1], oacc[i % DB],
+                                                                0, 0, 0);
+      } else {
+        const int ks = (i - NPV) >> 1;
+        f32x16& n = ((i - NPV) & 1) ? n1 : n0;
+        if (HD == 72 && ks == 4)
+          n = __builtin_amdgcn_mfma_f32_32x32x8bf16_1k(*reinterpret_cast<const s16x4*>(&fr[i % 3]), q4, n, 0, 0, 0);
+        else
+          n = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fr[i % 3], qf[ks], ks == 0 ? zero16 : n, 0, 0, 0);
+      }
+      if (i + 1 < 16)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) ex[i + 1][e] = fast_exp2(score(i + 1, e));
+      if (i < 16) {
+        const int hf = i >> 3, j = (i >> 1) & 3, w = i & 1;
+        bf16x2 pr;
+        pr[0] = (bf16)ex[i][0];
+        pr[1] = (bf16)ex[i][1];
+        psum = add_pair(psum, pr);
+        pn[w][hf][2 * j] = pr[0];
+        pn[w][hf][2 * j + 1] = pr[1];
+      }
+      // the staged bytes: keys t + 2, values t; then the next loads
+      if (i == 2) put(kw, 0, sk, ksc);
+      if (i == 4) {
+        put(kw, 1, sk, ksc);
+        if constexpr (HD == 72) put_k8(kw);
+      }
+      if (i == 8) put(vw, 0, sv, vsc);
+      if (i == 10) {
+        put(vw, 1, sv, vsc);
+        if constexpr (HD == 72) put_v8(vw);
+      }
+      if (i == 12) {
+        fetch_k(min(t + 3, nkt - 1));
+        fetch_v(t + 1);
+        if (t + 2 == nkt && last < kKv8Block) trim_v();
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    // the probabilities are made here, not after the next branch
+#pragma unroll
+    for (int w = 0; w < 2; ++w)
+#pragma unroll
+      for (int hf = 0; hf < 2; ++hf) asm volatile("" : "+v"(pn[w][hf]));
+    asm volatile("" : "+v"(psum));
+    if (__ballot(!(psum <= kPsumMax)) != 0) psum = rebase(t, pn);
+    l_run += psum;
+    barrier();
+  };
+
+  if (nkt > 0) {
+    // values of "block -1": zeros, times zero probabilities
+    for (int i = tid; i < G::SLOT / 16; i += kTPB) reinterpret_cast<bf16x8*>(sm.v[1])[i] = zero8;
+    fetch_k(0);
+    put(sm.k[0], 0, sk, ksc);
+    put(sm.k[0], 1, sk, ksc);
+    if constexpr (HD == 72) put_k8(sm.k[0]);
+    fetch_k(min(1, nkt - 1));
+    put(sm.k[1], 0, sk, ksc);
+    put(sm.k[1], 1, sk, ksc);
+    if constexpr (HD == 72) put_k8(sm.k[1]);
+    fetch_k(min(2, nkt - 1));
+    fetch_v(0);
+    if (nkt == 1 && last < kKv8Block) trim_v();
+    barrier();
+    f32x16 a0, a1, d0, d1;
+    qk(sm.k[0], a0, a1);
+    if (nkt == 1 && last < kKv8Block) mask_tail(a0, a1);
+    {
+      float mx = -INFINITY;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) mx = fmaxf(mx, fmaxf(a0[r], a1[r]));
+      mx = fmaxf(mx, __shfl_xor(mx, 32, kWave));
+      shifted = __ballot(!(mx >= -24.0f && mx <= 24.0f)) != 0;
+      m_run = shifted && mx > -INFINITY ? mx : 0.0f;
+    }
+    barrier();  // every wave is done with keys 0, whose slot takes keys 2
+    bf16x8 pa[2][2] = {{zero8, zero8}, {zero8, zero8}}, pb[2][2];
+    using Even = std::integral_constant<int, 0>;
+    using Odd = std::integral_constant<int, 1>;
+    int t = 0;
+    for (; t + 2 < nkt; t += 2) {
+      iter(t, Even{}, a0, a1, d0, d1, pa, pb);
+      iter(t + 1, Odd{}, d0, d1, a0, a1, pb, pa);
+    }
+    if (t + 1 < nkt) {
+      iter(t, Even{}, a0, a1, d0, d1, pa, pb);
+      a0 = d0;
+      a1 = d1;
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+        for (int hf = 0; hf < 2; ++hf) pa[kb][hf] = pb[kb][hf];
+      ++t;
+    }
+    // the last block
+    unsigned char* vw = sm.v[t & 1];
+    const unsigned char* vr = sm.v[(t & 1) ^ 1];
+    put(vw, 0, sv, vsc);
+    put(vw, 1, sv, vsc);
+    if constexpr (HD == 72) put_v8(vw);
+    settle(a0, a1);
+    if (last < kKv8Block) mask_tail(a0, a1);
+    float psum = 0.0f;
+#pragma unroll
+    for (int r = 0; r < 16; r += 2) {
+      bf16x2 x, y;
+      x[0] = (bf16)fast_exp2(a0[r]);
+      x[1] = (bf16)fast_exp2(a0[r + 1]);
+      y[0] = (bf16)fast_exp2(a1[r]);
+      y[1] = (bf16)fast_exp2(a1[r + 1]);
+      psum = add_pair(add_pair(psum, x), y);
+      pb[0][r >> 3][r & 7] = x[0];
+      pb[0][r >> 3][(r & 7) + 1] = x[1];
+      pb[1][r >> 3][r & 7] = y[0];
+      pb[1][r >> 3][(r & 7) + 1] = y[1];
+    }
+    auto pv = [&](const unsigned char* slot, const bf16x8 (&p)[2][2]) {
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+        for (int hf = 0; hf < 2; ++hf)
+#pragma unroll
+          for (int db = 0; db < DB; ++db)
+            oacc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(val_frag(slot, kb, hf, db), p[kb][hf], oacc[db], 0, 0, 0);
+    };
+    pv(vr, pa);
+    if (__ballot(!(psum <= kPsumMax)) != 0) psum = rebase(t, pb);
+    l_run += psum;
+    barrier();
+    pv(vw, pb);
+    l_run += __shfl_xor(l_run, 32, kWave);
+  }
+  if (row >= nrows) return;
+  if (chunks == 1) {
+    const float inv = L > 0 ? 1.0f / l_run : 0.0f;
+    bf16* o = static_cast<bf16*>(A.o) + row_of(A.ldo);
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+      for (int rr = 0; rr < 4; ++rr)
+        if (db * 32 + rr * 8 < HD) {
+          bf16x4 v;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) v[e] = (bf16)(oacc[db][rr * 4 + e] * inv);
+          *reinterpret_cast<bf16x4*>(o + db * 32 + rr * 8 + g * 4) = v;
+        }
+  } else {
+    const int64_t at = P.part[s] + ((int64_t)h * nrows + row) * chunks + chunk;
+    float* o = part.o + at * HD;
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+      for (int rr = 0; rr < 4; ++rr)
+        if (db * 32 + rr * 8 < HD) {
+          f32x4 v;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) v[e] = oacc[db][rr * 4 + e];
+          *reinterpret_cast<f32x4*>(o + db * 32 + rr * 8 + g * 4) = v;
+        }
+    if (g == 0) part.ml[at] = make_float2(m_run, l_run);
+  }
+}
+
 // Joins the chunks of a row: one workgroup of eight waves per row and head, wave
 // w taking chunks w (mod 8), or (few chunks) one wave per row.  A lane has one
 // dim; at head_dim 72 eight lanes have a second one.
@@ -343,7 +830,7 @@ hipError_t launch_kv8_attention(sphinx_dtype dt, int head_dim, const Kv8Attn& A,
                                 hipStream_t s) {
   int64_t rows[SPHINX_MAX_REQUESTS];
   for (int i = 0; i < A.nseg; ++i) rows[i] = (int64_t)A.nq[i] * A.group;
-  const Kv8Plan P = plan_kv8(c.kv_heads, A.nseg, rows, A.klen);
+  const Kv8Plan P = plan_kv8(dt == SPHINX_BF16, c.kv_heads, head_dim, A.nseg, rows, A.klen);
   const size_t parts = (size_t)P.part[A.nseg];
   const Parts part{static_cast<float2*>(ws),
                    reinterpret_cast<float*>(static_cast<unsigned char*>(ws) + ((parts * 8 + 255) & ~(size_t)255))};
@@ -352,8 +839,15 @@ hipError_t launch_kv8_attention(sphinx_dtype dt, int head_dim, const Kv8Attn& A,
   auto go = [&](auto t, auto hd) {
     using T = decltype(t);
     constexpr int HD = decltype(hd)::value;
-    for (int first = 0; first < total; first += most_wg)
+    for (int first = 0; first < total; first += most_wg) {
+      if constexpr (sizeof(T) == 2) {
+        if (P.tile == 128) {
+          k_kv8_attn_tiles<HD><<<std::min(most_wg, total - first), kTPB, 0, s>>>(A, c, P, part, first, total);
+          continue;
+        }
+      }
       k_kv8_attn_rows<T, HD><<<std::min(most_wg, total - first), kTPB, 0, s>>>(A, c, P, part, first);
+    }
     if (parts == 0) return;
     const int join = P.row[A.nseg];
     int most = 0;

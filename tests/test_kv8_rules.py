@@ -15,10 +15,11 @@ ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 SOURCE = r"""
 #include <string.h>
 #include "kv8_rules.hpp"
-extern "C" void plan(int heads, int nseg, const int64_t* rows, const int* klen, int* chunk, int* chunks, int* item,
-                     int* row, int64_t* part) {
-  const sphinx::Kv8Plan p = sphinx::plan_kv8(heads, nseg, rows, klen);
-  *chunk = p.chunk;
+extern "C" void plan(int bf16, int heads, int head_dim, int nseg, const int64_t* rows, const int* klen, int* chunk,
+                     int* chunks, int* item, int* row, int64_t* part) {
+  const sphinx::Kv8Plan p = sphinx::plan_kv8(bf16 != 0, heads, head_dim, nseg, rows, klen);
+  chunk[0] = p.chunk;
+  chunk[1] = p.tile;
   memcpy(chunks, p.chunks, 4 * nseg);
   memcpy(item, p.item, 4 * (nseg + 1));
   memcpy(row, p.row, 4 * (nseg + 1));
@@ -27,7 +28,6 @@ extern "C" void plan(int heads, int nseg, const int64_t* rows, const int* klen, 
 extern "C" int64_t most(int heads, int nseg, const int64_t* rows, const int* klen) {
   return sphinx::kv8_most_parts(heads, nseg, rows, klen);
 }
-extern "C" int tile(int64_t rows) { return sphinx::kv8_tiles(rows); }
 """
 
 
@@ -49,13 +49,13 @@ def ptr(a):
     return a.ctypes.data_as(ctypes.c_void_p)
 
 
-def plan(heads, rows, klen):
+def plan(heads, rows, klen, bf16=True, head_dim=64):
     n = len(rows)
     rows, klen = np.ascontiguousarray(rows, np.int64), np.ascontiguousarray(klen, np.int32)
-    chunk = np.zeros(1, np.int32)
+    chunk = np.zeros(2, np.int32)
     out = [np.zeros(n, np.int32), np.zeros(n + 1, np.int32), np.zeros(n + 1, np.int32), np.zeros(n + 1, np.int64)]
-    lib().plan(heads, n, ptr(rows), ptr(klen), ptr(chunk), *(ptr(a) for a in out))
-    return (int(chunk[0]), *out)
+    lib().plan(int(bf16), heads, head_dim, n, ptr(rows), ptr(klen), ptr(chunk), *(ptr(a) for a in out))
+    return (int(chunk[0]), int(chunk[1]), *out)
 
 
 def most(heads, rows, klen):
@@ -63,8 +63,9 @@ def most(heads, rows, klen):
                       ptr(np.ascontiguousarray(klen, np.int32)))
 
 
+@pytest.mark.parametrize("bf16,head_dim", [(True, 64), (True, 72), (False, 64)])
 @pytest.mark.parametrize("seed", range(40))
-def test_plan_covers_every_key_once_and_fits_its_workspace(seed):
+def test_plan_covers_every_key_once_and_fits_its_workspace(seed, bf16, head_dim):
     rng = np.random.default_rng(seed)
     n = int(rng.integers(1, 65))
     heads = int(rng.choice([1, 2, 5, 16, 64]))
@@ -72,24 +73,31 @@ def test_plan_covers_every_key_once_and_fits_its_workspace(seed):
     cap = np.exp(rng.uniform(0, np.log(rng.choice([100, 30000, 4000000])), n)).astype(np.int64)
     bound = most(heads, rows, cap)
     for klen in (cap, (cap * rng.random(n)).astype(np.int64), cap * (rng.random(n) < 0.2)):
-        chunk, chunks, item, row, part = plan(heads, rows, klen)
+        chunk, tile, chunks, item, row, part = plan(heads, rows, klen, bf16, head_dim)
         blocks = (klen + 63) // 64
-        assert chunk >= 4 and (chunks >= 1).all()
+        assert chunk >= 4 and (chunks >= 1).all() and tile in ((32, 128) if bf16 else (32,))
         # the last chunk of a segment holds a block, and the chunks together hold all of them
         assert (chunks * chunk >= blocks).all() and (((chunks - 1) * chunk < blocks) | (chunks == 1)).all()
         split = chunks > 1
         assert np.array_equal(np.diff(row), np.where(split, rows, 0)) and row[0] == 0
         assert np.array_equal(np.diff(part), np.where(split, rows * heads * chunks, 0)) and part[0] == 0
-        tiles = np.diff(item) // chunks
-        assert np.array_equal(np.diff(item), tiles * chunks)
+        assert np.array_equal(np.diff(item), (rows + tile - 1) // tile * chunks) and item[0] == 0
         assert part[-1] <= bound
         # a call is not cut finer than its purpose asks
-        assert (tiles * chunks * heads)[split].sum() <= 2048
+        assert (np.diff(item) * heads)[split].sum() <= 2048
+
+
+def test_rows_choose_the_tile():
+    assert plan(4, [1], [9000])[1] == 32 and plan(4, [64], [9000])[1] == 32
+    assert plan(4, [65], [9000])[1] == 128 and plan(4, [5000], [9000])[1] == 128
+    assert plan(4, [5000], [9000], bf16=False)[1] == 32
+    assert plan(4, [1] * 40 + [100], [9000] * 41)[1] == 32  # mostly single queries
+    assert plan(4, [1] + [3000], [64, 9000])[1] == 128
 
 
 def test_largest_calls_stay_in_range():
     rows = [(1 << 31) - 1]
-    chunk, chunks, item, row, part = plan(1, rows, [(1 << 31) - 1])
-    assert chunks[0] == 1 and item[1] == lib().tile(ctypes.c_int64(rows[0])) and part[1] == 0
-    chunk, chunks, item, row, part = plan(1, [1], [(1 << 31) - 1])
+    chunk, tile, chunks, item, row, part = plan(1, rows, [(1 << 31) - 1])
+    assert chunks[0] == 1 and item[1] == 1 << 24 and part[1] == 0
+    chunk, tile, chunks, item, row, part = plan(1, [1], [(1 << 31) - 1])
     assert chunks[0] * chunk >= 1 << 25 and part[1] == chunks[0] <= most(1, [1], [(1 << 31) - 1])
