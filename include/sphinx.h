@@ -401,7 +401,9 @@ sphinx_status sphinx_scatter_masked(const sphinx_request* reqs, int32_t R, const
  * The caller owns a slice (sphinx_kv8_bytes bytes, 16-byte aligned) and clears
  * it to zero bytes before its first use: a cleared slice holds zeros.  Its bytes
  * are in an order of the library's own.  Slices of the same cu_kv, kv_heads and
- * head_dim may follow each other in memory (the size is a multiple of 256).
+ * head_dim may follow each other in memory (the size is a multiple of 256).  The
+ * calls below take the bytes at hand (slice_bytes) and return
+ * SPHINX_E_WORKSPACE where a slice needs more.
  * ------------------------------------------------------------------------ */
 #define SPHINX_KV8_BLOCK 64
 
@@ -424,7 +426,7 @@ sphinx_status sphinx_kv8_bytes(int32_t kv_heads, int32_t head_dim, const int32_t
  * Deterministic. */
 sphinx_status sphinx_kv8_store(sphinx_dtype dtype, int32_t kv_heads, int32_t head_dim, const void* k, const void* v,
                                int64_t ld, const int32_t* idx, int32_t n, const int32_t* cu_kv, int32_t nseg,
-                               void* slice, void* stream);
+                               void* slice, size_t slice_bytes, void* stream);
 
 /* Reads rows back: row j of k and v (dev out, laid out as in
  * sphinx_kv8_store) gets the values of token idx[j] (ascending; a token may be
@@ -432,8 +434,8 @@ sphinx_status sphinx_kv8_store(sphinx_dtype dtype, int32_t kv_heads, int32_t hea
  * slice are left unwritten; where idx does not ascend, which rows are written
  * is not defined. */
 sphinx_status sphinx_kv8_load(sphinx_dtype dtype, int32_t kv_heads, int32_t head_dim, const void* slice,
-                              const int32_t* cu_kv, int32_t nseg, const int32_t* idx, int32_t n, void* k, void* v,
-                              int64_t ld, void* stream);
+                              size_t slice_bytes, const int32_t* cu_kv, int32_t nseg, const int32_t* idx, int32_t n,
+                              void* k, void* v, int64_t ld, void* stream);
 
 /* Attention over the cache, as sphinx_varlen_attention with the keys and
  * values that a slice holds:
@@ -455,9 +457,9 @@ sphinx_status sphinx_kv8_attention_workspace_bytes(sphinx_dtype dtype, int32_t h
                                                    int32_t head_dim, const int32_t* cu_q, const int32_t* cu_kv,
                                                    int32_t nseg, size_t* bytes);
 sphinx_status sphinx_kv8_attention(sphinx_dtype dtype, int32_t heads, int32_t kv_heads, int32_t head_dim,
-                                   const void* q, int64_t ldq, const void* slice, const int32_t* cu_q,
-                                   const int32_t* cu_kv, const int32_t* kv_len, int32_t nseg, void* o, void* ws,
-                                   size_t ws_bytes, void* stream);
+                                   const void* q, int64_t ldq, const void* slice, size_t slice_bytes,
+                                   const int32_t* cu_q, const int32_t* cu_kv, const int32_t* kv_len, int32_t nseg,
+                                   void* o, void* ws, size_t ws_bytes, void* stream);
 
 /* The latent cache in 8 bits: L slices, one per denoiser block, whose segments
  * are the requests.  sphinx_refine_step_kv8 is sphinx_refine_step_cached with

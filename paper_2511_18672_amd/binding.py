@@ -118,12 +118,14 @@ def lib() -> ctypes.CDLL:
         "sphinx_refine_step_cached": (c_int32, [POINTER(ModelDesc), POINTER(Request), c_int32, P, c_int32, P, P, P,
                                                 P, P, P, P, c_size_t, P]),
         "sphinx_kv8_bytes": (c_int32, [c_int32, c_int32, P, c_int32, POINTER(c_size_t)]),
-        "sphinx_kv8_store": (c_int32, [c_int32, c_int32, c_int32, P, P, c_int64, P, c_int32, P, c_int32, P, P]),
-        "sphinx_kv8_load": (c_int32, [c_int32, c_int32, c_int32, P, P, c_int32, P, c_int32, P, P, c_int64, P]),
+        "sphinx_kv8_store": (c_int32, [c_int32, c_int32, c_int32, P, P, c_int64, P, c_int32, P, c_int32, P,
+                                       c_size_t, P]),
+        "sphinx_kv8_load": (c_int32, [c_int32, c_int32, c_int32, P, c_size_t, P, c_int32, P, c_int32, P, P, c_int64,
+                                      P]),
         "sphinx_kv8_attention_workspace_bytes": (c_int32, [c_int32, c_int32, c_int32, c_int32, P, P, c_int32,
                                                            POINTER(c_size_t)]),
-        "sphinx_kv8_attention": (c_int32, [c_int32, c_int32, c_int32, c_int32, P, c_int64, P, P, P, P, c_int32, P, P,
-                                           c_size_t, P]),
+        "sphinx_kv8_attention": (c_int32, [c_int32, c_int32, c_int32, c_int32, P, c_int64, P, c_size_t, P, P, P,
+                                           c_int32, P, P, c_size_t, P]),
         "sphinx_kv8_cache_bytes": (c_int32, [POINTER(ModelDesc), POINTER(Request), c_int32, POINTER(c_size_t)]),
         "sphinx_refine_kv8_workspace_bytes": (c_int32, [POINTER(ModelDesc), POINTER(Request), c_int32, c_int64,
                                                         POINTER(c_size_t)]),
@@ -368,44 +370,42 @@ def _host_cu(cu) -> np.ndarray:
     return np.ascontiguousarray(cu, dtype=np.int32)
 
 
-def _on_current_device(*tensors):
-    """The 8-bit cache's calls run on the current device: tensors of another one are refused."""
+def _here(stream, *tensors) -> Optional[int]:
+    """The stream of a call on the current device; tensors that are not on it are refused."""
     import torch
 
-    here = torch.cuda.current_device()
+    dev = torch.cuda.current_device()
     for t in tensors:
-        if isinstance(t, torch.Tensor) and (not t.is_cuda or t.device.index != here):
-            raise ValueError(f"tensor on {t.device}, the current device is cuda:{here}")
+        if t is not None and not isinstance(t, int) and t.get_device() != dev:
+            raise ValueError(f"tensor on {t.device}, the current device is cuda:{dev}")
+    if stream is None:
+        return torch.cuda.current_stream(dev).cuda_stream
+    return stream if isinstance(stream, int) else stream.cuda_stream
 
 
 def sphinx_kv8_bytes(kv_heads: int, head_dim: int, cu_kv) -> int:
     """Bytes of one slice of the 8-bit cache (cu_kv: host int sequence of token bounds, as in the calls below)."""
     cu, out = _host_cu(cu_kv), c_size_t()
-    _check("sphinx_kv8_bytes", lib().sphinx_kv8_bytes(kv_heads, head_dim, _ptr(cu), cu.size - 1, ctypes.byref(out)))
+    _check("sphinx_kv8_bytes", lib().sphinx_kv8_bytes(kv_heads, head_dim, cu.ctypes.data, cu.size - 1,
+                                                      ctypes.byref(out)))
     return out.value
 
 
 def sphinx_kv8_store(dtype: int, kv_heads: int, head_dim: int, k, v, ld: int, idx, n: int, cu_kv, cache, stream=None):
     """Quantises rows j < n of k and v into the slice `cache` (zeroed before its first use) at tokens idx[j]
     (ascending; None: token j)."""
-    cu = _host_cu(cu_kv)
-    _on_current_device(k, v, idx, cache)
-    if cache.numel() * cache.element_size() < sphinx_kv8_bytes(kv_heads, head_dim, cu):
-        raise ValueError("the cache slice is smaller than sphinx_kv8_bytes")
+    cu, s = _host_cu(cu_kv), _here(stream, k, v, idx, cache)
     _check("sphinx_kv8_store", lib().sphinx_kv8_store(
-        dtype, kv_heads, head_dim, _ptr(k), _ptr(v), ld, _ptr(idx), n, _ptr(cu), cu.size - 1, _ptr(cache),
-        _stream(stream)))
+        dtype, kv_heads, head_dim, k.data_ptr(), v.data_ptr(), ld, _ptr(idx), n, cu.ctypes.data, cu.size - 1,
+        cache.data_ptr(), cache.nbytes, s))
 
 
 def sphinx_kv8_load(dtype: int, kv_heads: int, head_dim: int, cache, cu_kv, idx, n: int, k, v, ld: int, stream=None):
     """Rows j < n of k and v <- the values of tokens idx[j] (ascending; None: token j)."""
-    cu = _host_cu(cu_kv)
-    _on_current_device(k, v, idx, cache)
-    if cache.numel() * cache.element_size() < sphinx_kv8_bytes(kv_heads, head_dim, cu):
-        raise ValueError("the cache slice is smaller than sphinx_kv8_bytes")
+    cu, s = _host_cu(cu_kv), _here(stream, k, v, idx, cache)
     _check("sphinx_kv8_load", lib().sphinx_kv8_load(
-        dtype, kv_heads, head_dim, _ptr(cache), _ptr(cu), cu.size - 1, _ptr(idx), n, _ptr(k), _ptr(v), ld,
-        _stream(stream)))
+        dtype, kv_heads, head_dim, cache.data_ptr(), cache.nbytes, cu.ctypes.data, cu.size - 1, _ptr(idx), n,
+        k.data_ptr(), v.data_ptr(), ld, s))
 
 
 def sphinx_kv8_attention_workspace_bytes(dtype: int, heads: int, kv_heads: int, head_dim: int, cu_q, cu_kv) -> int:
@@ -413,7 +413,7 @@ def sphinx_kv8_attention_workspace_bytes(dtype: int, heads: int, kv_heads: int, 
     if cq.size != ck.size:
         raise ValueError("cu_q and cu_kv differ in length")
     _check("sphinx_kv8_attention_workspace_bytes", lib().sphinx_kv8_attention_workspace_bytes(
-        dtype, heads, kv_heads, head_dim, _ptr(cq), _ptr(ck), cq.size - 1, ctypes.byref(out)))
+        dtype, heads, kv_heads, head_dim, cq.ctypes.data, ck.ctypes.data, cq.size - 1, ctypes.byref(out)))
     return out.value
 
 
@@ -425,12 +425,11 @@ def sphinx_kv8_attention(dtype: int, heads: int, kv_heads: int, head_dim: int, q
     kl = None if kv_len is None else _host_cu(kv_len)
     if cq.size != ck.size or (kl is not None and kl.size != ck.size - 1):
         raise ValueError("cu_q, cu_kv and kv_len differ in length")
-    _on_current_device(q, cache, o, ws)
-    if cache.numel() * cache.element_size() < sphinx_kv8_bytes(kv_heads, head_dim, ck):
-        raise ValueError("the cache slice is smaller than sphinx_kv8_bytes")
+    s = _here(stream, q, cache, o, ws)
     _check("sphinx_kv8_attention", lib().sphinx_kv8_attention(
-        dtype, heads, kv_heads, head_dim, _ptr(q), ldq, _ptr(cache), _ptr(cq), _ptr(ck), _ptr(kl), cq.size - 1,
-        _ptr(o), _ptr(ws), ws.numel() * ws.element_size(), _stream(stream)))
+        dtype, heads, kv_heads, head_dim, q.data_ptr(), ldq, cache.data_ptr(), cache.nbytes, cq.ctypes.data,
+        ck.ctypes.data, None if kl is None else kl.ctypes.data, cq.size - 1, o.data_ptr(), ws.data_ptr(), ws.nbytes,
+        s))
 
 
 def sphinx_kv8_cache_bytes(desc: ModelDesc, reqs) -> int:

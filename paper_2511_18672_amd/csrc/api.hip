@@ -597,9 +597,13 @@ sphinx_status kv8_check(int32_t kv_heads, int32_t head_dim, const int32_t* cu_kv
   if (kv_heads < 1 || head_dim < 1 || nseg < 1 || cu_kv == nullptr || cu_kv[0] != 0) return SPHINX_E_INVALID;
   if (nseg > SPHINX_MAX_REQUESTS || (head_dim != 64 && head_dim != 72)) return SPHINX_E_UNSUPPORTED;
   if ((int64_t)kv_heads * head_dim > 65536) return SPHINX_E_UNSUPPORTED;
-  for (int i = 0; i < nseg; ++i)
+  int64_t nblk = 0;
+  for (int i = 0; i < nseg; ++i) {
     if (cu_kv[i + 1] < cu_kv[i]) return SPHINX_E_INVALID;
-  return SPHINX_OK;
+    nblk += ((int64_t)cu_kv[i + 1] - cu_kv[i] + kKv8Block - 1) / kKv8Block;
+  }
+  // blocks of all heads are counted in 32 bits (2^31 of them hold 16 TB)
+  return nblk * kv_heads < ((int64_t)1 << 31) ? SPHINX_OK : SPHINX_E_UNSUPPORTED;
 }
 
 Kv8Slice kv8_slice(void* base, int32_t kv_heads, int32_t head_dim, int64_t nblk) {
@@ -610,16 +614,18 @@ Kv8Slice kv8_slice(void* base, int32_t kv_heads, int32_t head_dim, int64_t nblk)
 // Arguments that storing and reading back share; *todo: there are rows.
 sphinx_status kv8_rows_check(sphinx_dtype dtype, int32_t kv_heads, int32_t head_dim, const void* k, const void* v,
                              int64_t ld, const int32_t* idx, int32_t n, const int32_t* cu_kv, int32_t nseg,
-                             const void* slice, bool* todo) {
+                             const void* slice, size_t slice_bytes, bool* todo) {
   *todo = false;
   if (!valid_dtype(dtype)) return SPHINX_E_UNSUPPORTED;
   const sphinx_status st = kv8_check(kv_heads, head_dim, cu_kv, nseg);
   if (st != SPHINX_OK) return st;
   if (n < 0 || (idx == nullptr && n > cu_kv[nseg])) return SPHINX_E_INVALID;
   if (ld < (int64_t)kv_heads * head_dim || ld % 8 != 0) return SPHINX_E_INVALID;
+  if ((int64_t)n * kv_heads >= ((int64_t)1 << 31)) return SPHINX_E_UNSUPPORTED;  // rows of all heads, in 32 bits
   if (n == 0 || cu_kv[nseg] == 0) return SPHINX_OK;
   if (!k || !v || !slice || !aligned(k, 16) || !aligned(v, 16) || !aligned(slice, 16) || !aligned(idx, 16))
     return SPHINX_E_INVALID;
+  if (slice_bytes < kv8_slice_bytes(kv_heads, head_dim, kv8_segs(cu_kv, nseg).blk[nseg])) return SPHINX_E_WORKSPACE;
   *todo = true;
   return SPHINX_OK;
 }
@@ -636,9 +642,10 @@ sphinx_status sphinx_kv8_bytes(int32_t kv_heads, int32_t head_dim, const int32_t
 
 sphinx_status sphinx_kv8_store(sphinx_dtype dtype, int32_t kv_heads, int32_t head_dim, const void* k, const void* v,
                                int64_t ld, const int32_t* idx, int32_t n, const int32_t* cu_kv, int32_t nseg,
-                               void* slice, void* stream) {
+                               void* slice, size_t slice_bytes, void* stream) {
   bool todo;
-  const sphinx_status st = kv8_rows_check(dtype, kv_heads, head_dim, k, v, ld, idx, n, cu_kv, nseg, slice, &todo);
+  const sphinx_status st = kv8_rows_check(dtype, kv_heads, head_dim, k, v, ld, idx, n, cu_kv, nseg, slice, slice_bytes,
+                                         &todo);
   if (st != SPHINX_OK || !todo) return st;
   const Kv8Segs S = kv8_segs(cu_kv, nseg);
   hipStream_t s = (hipStream_t)stream;
@@ -648,10 +655,11 @@ sphinx_status sphinx_kv8_store(sphinx_dtype dtype, int32_t kv_heads, int32_t hea
 }
 
 sphinx_status sphinx_kv8_load(sphinx_dtype dtype, int32_t kv_heads, int32_t head_dim, const void* slice,
-                              const int32_t* cu_kv, int32_t nseg, const int32_t* idx, int32_t n, void* k, void* v,
-                              int64_t ld, void* stream) {
+                              size_t slice_bytes, const int32_t* cu_kv, int32_t nseg, const int32_t* idx, int32_t n,
+                              void* k, void* v, int64_t ld, void* stream) {
   bool todo;
-  const sphinx_status st = kv8_rows_check(dtype, kv_heads, head_dim, k, v, ld, idx, n, cu_kv, nseg, slice, &todo);
+  const sphinx_status st = kv8_rows_check(dtype, kv_heads, head_dim, k, v, ld, idx, n, cu_kv, nseg, slice, slice_bytes,
+                                         &todo);
   if (st != SPHINX_OK || !todo) return st;
   const Kv8Segs S = kv8_segs(cu_kv, nseg);
   hipStream_t s = (hipStream_t)stream;
@@ -693,9 +701,9 @@ sphinx_status sphinx_kv8_attention_workspace_bytes(sphinx_dtype dtype, int32_t h
 }
 
 sphinx_status sphinx_kv8_attention(sphinx_dtype dtype, int32_t heads, int32_t kv_heads, int32_t head_dim,
-                                   const void* q, int64_t ldq, const void* slice, const int32_t* cu_q,
-                                   const int32_t* cu_kv, const int32_t* kv_len, int32_t nseg, void* o, void* ws,
-                                   size_t ws_bytes, void* stream) {
+                                   const void* q, int64_t ldq, const void* slice, size_t slice_bytes,
+                                   const int32_t* cu_q, const int32_t* cu_kv, const int32_t* kv_len, int32_t nseg,
+                                   void* o, void* ws, size_t ws_bytes, void* stream) {
   sphinx_status st = kv8_attention_check(dtype, heads, kv_heads, head_dim, cu_q, cu_kv, nseg);
   if (st != SPHINX_OK) return st;
   const int64_t D = (int64_t)heads * head_dim;
@@ -708,8 +716,8 @@ sphinx_status sphinx_kv8_attention(sphinx_dtype dtype, int32_t heads, int32_t kv
   size_t need;
   st = sphinx_kv8_attention_workspace_bytes(dtype, heads, kv_heads, head_dim, cu_q, cu_kv, nseg, &need);
   if (st != SPHINX_OK) return st;
-  if (ws_bytes < need) return SPHINX_E_WORKSPACE;
   const Kv8Segs S = kv8_segs(cu_kv, nseg);
+  if (ws_bytes < need || slice_bytes < kv8_slice_bytes(kv_heads, head_dim, S.blk[nseg])) return SPHINX_E_WORKSPACE;
   Kv8Attn A;
   std::memset(&A, 0, sizeof(A));
   A.q = q;

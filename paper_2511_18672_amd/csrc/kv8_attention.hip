@@ -757,13 +757,16 @@ __global__ __launch_bounds__(kTPB, HD == 64 ? 3 : 2) void k_kv8_attn_tiles(Kv8At
   }
 }
 
-// Joins the chunks of a row: one workgroup of eight waves per row and head, wave
-// w taking chunks w (mod 8), or (few chunks) one wave per row.  A lane has one
-// dim; at head_dim 72 eight lanes have a second one.
+// Joins the chunks of a row and head: one wave per row and head, or (few rows of
+// many chunks) a workgroup of eight waves, wave w taking chunks w (mod 8).  A
+// lane has one dim; at head_dim 72 eight lanes have a second one.  Bound by the
+// latency of the loads: a wave asks for the maxima, sums and values of eight
+// chunks at once and joins them as it goes.
 template <typename T, int HD, int WAVES>
 __global__ __launch_bounds__(512) void k_kv8_attn_join(Kv8Attn A, int kv_heads, Kv8Plan P, Parts part, int rows) {
   __shared__ float sO[WAVES][HD], sL[WAVES], sM[WAVES];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const int unit = WAVES == 1 ? (int)blockIdx.x * 8 + wave : (int)blockIdx.x;  // row * kv_heads + head
   if (unit >= rows * kv_heads) return;  // only with one wave per row, which has no barrier
   const int h = unit % kv_heads, at = unit / kv_heads;
@@ -771,14 +774,9 @@ __global__ __launch_bounds__(512) void k_kv8_attn_join(Kv8Attn A, int kv_heads, 
   while (s + 1 < A.nseg && P.row[s + 1] <= at) ++s;
   const int row = at - P.row[s], chunks = P.chunks[s], nrows = A.nq[s] * A.group;
   const int64_t first = P.part[s] + ((int64_t)h * nrows + row) * chunks;
-  const int w0 = WAVES == 1 ? 0 : wave;
-  float m = -INFINITY;
-  for (int j = lane; j < chunks; j += kWave) m = fmaxf(m, part.ml[first + j].x);
-  m = wave_max(m);
-  const float base = m == -INFINITY ? 0.0f : m;
-  float num = 0.0f, num2 = 0.0f, den = 0.0f;
+  float m = -INFINITY, num = 0.0f, num2 = 0.0f, den = 0.0f;
   constexpr int U = 8;
-  for (int j0 = w0; j0 < chunks; j0 += WAVES * U) {
+  for (int j0 = WAVES == 1 ? 0 : wave; j0 < chunks; j0 += WAVES * U) {
     float2 ml[U];
     float o[U], o2[U];
 #pragma unroll
@@ -788,6 +786,17 @@ __global__ __launch_bounds__(512) void k_kv8_attn_join(Kv8Attn A, int kv_heads, 
       o[u] = part.o[j * HD + lane];
       o2[u] = HD == 72 ? part.o[j * HD + 64 + (lane & 7)] : 0.0f;
     }
+    float mn = m;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (j0 + u * WAVES >= chunks) ml[u] = make_float2(-INFINITY, 0.0f);
+      mn = fmaxf(mn, ml[u].x);
+    }
+    const float base = mn == -INFINITY ? 0.0f : mn, f0 = fast_exp2(m - base);
+    num *= f0;
+    num2 *= f0;
+    den *= f0;
+    m = mn;
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       if (j0 + u * WAVES >= chunks) break;
@@ -800,15 +809,23 @@ __global__ __launch_bounds__(512) void k_kv8_attn_join(Kv8Attn A, int kv_heads, 
   if constexpr (WAVES > 1) {
     sO[wave][lane] = num;
     if (HD == 72 && lane < 8) sO[wave][64 + lane] = num2;
-    if (lane == 0) sL[wave] = den;
+    if (lane == 0) {
+      sL[wave] = den;
+      sM[wave] = m;
+    }
     __syncthreads();
     if (wave != 0) return;
+    m = sM[0];
+#pragma unroll
+    for (int w = 1; w < WAVES; ++w) m = fmaxf(m, sM[w]);
+    const float base = m == -INFINITY ? 0.0f : m;
     num = num2 = den = 0.0f;
 #pragma unroll
-    for (int w = 0; w < WAVES; ++w) {
-      num += sO[w][lane];
-      if (HD == 72) num2 += sO[w][64 + (lane & 7)];
-      den += sL[w];
+    for (int w = 0; w < WAVES; ++w) {  // a wave without a chunk has m = -inf and weighs 0
+      const float f = fast_exp2(sM[w] - base);
+      num = fmaf(sO[w][lane], f, num);
+      if (HD == 72) num2 = fmaf(sO[w][64 + (lane & 7)], f, num2);
+      den = fmaf(sL[w], f, den);
     }
   }
   const int q = row / A.group;
@@ -852,7 +869,8 @@ hipError_t launch_kv8_attention(sphinx_dtype dt, int head_dim, const Kv8Attn& A,
     const int join = P.row[A.nseg];
     int most = 0;
     for (int i = 0; i < A.nseg; ++i) most = std::max(most, P.chunks[i]);
-    if (most <= 8)
+    // a wave per row where they fill the chip or have few chunks to walk
+    if (most <= 16 || (int64_t)join * c.kv_heads >= 2048)
       k_kv8_attn_join<T, HD, 1><<<(unsigned)(((int64_t)join * c.kv_heads + 7) / 8), 512, 0, s>>>(A, c.kv_heads, P,
                                                                                               part, join);
     else

@@ -61,12 +61,13 @@ __device__ __forceinline__ void unpack4(uint32_t w, float scale, float* x) {
 // n (a multiple of 4) consecutive elements as floats, and back.
 template <int N>
 __device__ __forceinline__ void load_row(const bf16* p, float* x) {
-  static_assert(N % 4 == 0, "whole 8-byte pieces");
+  constexpr int W = N % 8 == 0 ? 8 : 4;
+  typedef __bf16 vec __attribute__((ext_vector_type(W)));
 #pragma unroll
-  for (int i = 0; i < N; i += 4) {
-    const bf16x4 v = *reinterpret_cast<const bf16x4*>(p + i);
+  for (int i = 0; i < N; i += W) {
+    const vec v = *reinterpret_cast<const vec*>(p + i);
 #pragma unroll
-    for (int e = 0; e < 4; ++e) x[i + e] = (float)v[e];
+    for (int e = 0; e < W; ++e) x[i + e] = (float)v[e];
   }
 }
 template <int N>
@@ -81,11 +82,11 @@ __device__ __forceinline__ void load_row(const float* p, float* x) {
 template <int N>
 __device__ __forceinline__ void store_row(bf16* p, const float* x) {
 #pragma unroll
-  for (int i = 0; i < N; i += 4) {
-    bf16x4 v;
+  for (int i = 0; i < N; i += 8) {
+    bf16x8 v;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] = (bf16)x[i + e];  // exact: e4m3 times a power of two
-    *reinterpret_cast<bf16x4*>(p + i) = v;
+    for (int e = 0; e < 8; ++e) v[e] = (bf16)x[i + e];  // exact: e4m3 times a power of two
+    *reinterpret_cast<bf16x8*>(p + i) = v;
   }
 }
 template <int N>
@@ -126,121 +127,129 @@ __device__ __forceinline__ int block_of(const Kv8Segs& S, int t, int* row) {
   return S.blk[s] + (at >> 6);
 }
 
-// The rows of a call that fall into one block: rows [first, first + count) of
-// the call.  Work unit w of a call with listed tokens is row w, and only the
-// first row of a run of rows in one block has work; without listed tokens unit w
-// is block w.
-struct Run {
-  int block, first, count;
-};
-__device__ __forceinline__ bool find_run(const Kv8Segs& S, const Kv8Rows& rows, int w, Run* run) {
-  int at;
+// The rows of a call fall into runs, one per block, since listed tokens ascend.
+// A workgroup looks at `group` rows (of one head) and does the runs that start
+// among them; without listed tokens it does block `unit`.  body(block, first row).
+template <typename F>
+__device__ __forceinline__ void for_each_run(const Kv8Segs& S, const Kv8Rows& rows, int group, int unit, const F& body) {
   if (rows.idx == nullptr) {
     int lo = 0, hi = S.nseg - 1;
     while (lo < hi) {
       const int mid = (lo + hi + 1) >> 1;
-      if (S.blk[mid] <= w) lo = mid; else hi = mid - 1;
+      if (S.blk[mid] <= unit) lo = mid; else hi = mid - 1;
     }
-    run->block = w;
-    run->first = S.tok[lo] + (w - S.blk[lo]) * kKv8Block;
-    run->count = min(min(kKv8Block, S.tok[lo + 1] - run->first), rows.n - run->first);
-    return run->count > 0;
+    const int first = S.tok[lo] + (unit - S.blk[lo]) * kKv8Block;
+    if (first < rows.n) body(unit, first);
+    return;
   }
-  run->block = block_of(S, rows.idx[w], &at);
-  if (run->block < 0 || (w > 0 && block_of(S, rows.idx[w - 1], &at) == run->block)) return false;
-  run->first = w;
   const int lane = lane_id();
-  int n = 0;
-  for (;;) {  // lanes look 64 rows ahead
-    const int j = w + n + lane;
-    const bool in = j < rows.n && block_of(S, rows.idx[j], &at) == run->block;
-    const uint64_t out = ~__ballot(in);
-    if (out != 0) {
-      n += __builtin_ctzll(out);
-      break;
-    }
-    n += kWave;
+  const int64_t j = (int64_t)unit * group + lane;
+  const bool in = lane < group && j < rows.n;
+  int at, block = in ? block_of(S, rows.idx[j], &at) : -1;
+  const int before = in && j > 0 ? block_of(S, rows.idx[j - 1], &at) : -1;
+  uint64_t starts = __ballot(block >= 0 && block != before);  // the same in every wave
+  while (starts != 0) {
+    const int l = __builtin_ctzll(starts);
+    starts &= starts - 1;
+    body(__builtin_amdgcn_readlane(block, l), unit * group + l);
   }
-  run->count = n;
-  return true;
 }
 
-// Largest value over the workgroup, in every thread (two at once).
-__device__ __forceinline__ void block_max(float& a, float& b, float (*sh)[2]) {
-  a = wave_max(a);
-  b = wave_max(b);
-  __syncthreads();
-  if (lane_id() == 0) {
-    sh[threadIdx.x >> 6][0] = a;
-    sh[threadIdx.x >> 6][1] = b;
+// The units of all heads over the workgroups: neighbouring heads of a unit on
+// one XCD, one after the other, since a head's piece of a row (144 bytes at
+// head_dim 72) shares cache lines with the next head's.
+template <typename F>
+__device__ __forceinline__ void for_each_unit(const Kv8Segs& S, const Kv8Rows& rows, int kv_heads, int group, int units,
+                                              const F& body) {
+  const int total = units * kv_heads;
+  for (int64_t b = blockIdx.x; b < total; b += gridDim.x) {
+    const int u = xcd_tile((int)b, total), unit = u / kv_heads, h = u - unit * kv_heads;
+    for_each_run(S, rows, group, unit, [&](int block, int first) { body(h, block, first); });
   }
-  __syncthreads();
-  a = fmaxf(fmaxf(sh[0][0], sh[1][0]), fmaxf(sh[2][0], sh[3][0]));
-  b = fmaxf(fmaxf(sh[0][1], sh[1][1]), fmaxf(sh[2][1], sh[3][1]));
 }
 
-// One workgroup writes one block of one head: the rows of the call and the kept
-// rows of the block come together in registers as floats, give the new scales,
-// and are rounded once.  A thread has 16 dims of one key row and four dims of
-// four value rows (then four keys of a dim are one 4-byte store); head_dim 72:
-// one wave more key dims, half a wave more value dims.
+// Row of the call for each row of a block, -1 where none names it; by one wave.
+// A token listed more than once takes its last row.
+__device__ __forceinline__ void map_rows(const Kv8Segs& S, const Kv8Rows& rows, int block, int first, int* row_at) {
+  const int lane = lane_id();
+  if (rows.idx == nullptr) {
+    const int s = segment_of(S, first), j = first + lane;
+    row_at[lane] = j < min(S.tok[s + 1], rows.n) ? j : -1;
+    return;
+  }
+  row_at[lane] = -1;
+  for (int64_t j = first + lane;; j += kWave) {
+    int at = 0;
+    const bool in = j < rows.n && block_of(S, rows.idx[j], &at) == block;
+    if (in) atomicMax(&row_at[at], (int)j);
+    if (~__ballot(in) != 0) break;  // the run ends here
+  }
+}
+
+// One workgroup writes one block of one head at a time: the rows of the call and
+// the kept rows come together in registers as floats, give the new scales, and
+// are rounded once.  A thread has 16 dims of one key row (neighbouring threads
+// the same row's next dims, so that a row of a head is read in one piece) and
+// four dims of four value rows; head_dim 72: 64 threads more key dims, 32 threads
+// more value dims.  Four keys of a dim are four neighbouring bytes of the value
+// tile, which is put together in LDS, so that its old bytes come in and its new
+// ones go out as consecutive 16-byte pieces.
+// Bound by bytes: a full step's rows in and tiles out, in a partial step also
+// the old tiles in.
 template <typename T, int HD>
 __global__ __launch_bounds__(kTPB) void k_kv8_store(Kv8Segs S, Kv8Slice c, Kv8Rows rows, const T* __restrict__ k,
-                                                    const T* __restrict__ v, int64_t units) {
-  __shared__ int row_at[kKv8Block];  // row of the call for each row of the block, -1: kept
+                                                    const T* __restrict__ v, int group, int units) {
+  constexpr int NV = kKv8Block * HD / 16;  // 16-byte pieces of a tile
+  __shared__ __attribute__((aligned(16))) uint4 image[NV];  // the value tile
+  __shared__ int row_at[kKv8Block];
   __shared__ float sh[4][2];
   const int tid = threadIdx.x;
-  for (int64_t u = blockIdx.x; u < units; u += gridDim.x) {
-    const int h = (int)(u % c.kv_heads), w = (int)(u / c.kv_heads);
-    Run run;
-    if (!find_run(S, rows, w, &run)) continue;  // the same for all threads
-    __syncthreads();
-    if (tid < kKv8Block) row_at[tid] = -1;
-    __syncthreads();
-    for (int i = tid; i < run.count; i += kTPB) {
-      int at = i;
-      if (rows.idx != nullptr) block_of(S, rows.idx[run.first + i], &at);
-      atomicMax(&row_at[at], run.first + i);  // a token listed twice takes its last row
-    }
-    __syncthreads();
-    unsigned char* kt = c.tiles + ((int64_t)h * c.nblk + run.block) * 2 * kKv8Block * HD;
+  const int kr = tid >> 2, kp = tid & 3, va = tid >> 4, vd = (tid & 15) * 4;
+  unsigned char* img = reinterpret_cast<unsigned char*>(image);
+  auto body = [&](int h, int block, int first) {
+    unsigned char* kt = c.tiles + ((int64_t)h * c.nblk + block) * 2 * kKv8Block * HD;
     unsigned char* vt = kt + kKv8Block * HD;
-    unsigned char* sc = c.scales + ((int64_t)h * c.nblk + run.block) * 2;
+    unsigned char* sc = c.scales + ((int64_t)h * c.nblk + block) * 2;
+    __syncthreads();  // the block before is done with LDS
     const float ks = __uint_as_float((uint32_t)sc[0] << 23), vs = __uint_as_float((uint32_t)sc[1] << 23);
-    const int kr = tid >> 2, kp = tid & 3, va = tid >> 4, vd = (tid & 15) * 4;
+    const bool whole = rows.idx == nullptr && first + kKv8Block <= rows.n;  // no row is kept, or only padding
+    uint4 old = make_uint4(0u, 0u, 0u, 0u);
+    uint2 old2 = make_uint2(0u, 0u);
+    if (!whole) {
+      old = *reinterpret_cast<const uint4*>(kt + key_off(kr, kp));
+      if (HD == 72 && tid < 64) old2 = *reinterpret_cast<const uint2*>(kt + key_off(tid, 4));
+      for (int i = tid; i < NV; i += kTPB) image[i] = reinterpret_cast<const uint4*>(vt)[i];
+    }
+    if (tid < kWave) map_rows(S, rows, block, first, row_at);
+    __syncthreads();
     float kx[16], vx[4][4], kx2[8], vx2[4][4];
     float ka = 0.0f, vm = 0.0f;
-    {
-      const int j = row_at[kr];
-      if (j >= 0) {
-        load_row<16>(k + j * rows.ld + h * HD + kp * 16, kx);
-      } else {
-        const uint4 b = *reinterpret_cast<const uint4*>(kt + key_off(kr, kp));
-        unpack4(b.x, ks, kx);
-        unpack4(b.y, ks, kx + 4);
-        unpack4(b.z, ks, kx + 8);
-        unpack4(b.w, ks, kx + 12);
-      }
-#pragma unroll
-      for (int i = 0; i < 16; ++i) ka = fmaxf(ka, finite_abs(kx[i]));
+    const int j = row_at[kr];
+    if (j >= 0) {
+      load_row<16>(k + j * rows.ld + h * HD + kp * 16, kx);
+    } else {
+      unpack4(old.x, ks, kx);
+      unpack4(old.y, ks, kx + 4);
+      unpack4(old.z, ks, kx + 8);
+      unpack4(old.w, ks, kx + 12);
     }
     // values [dim][key]
     auto gather_v = [&](int a, int d0, float (&x)[4][4]) {
-      bool kept = false;
+      const int4 at = *reinterpret_cast<const int4*>(row_at + 4 * a);
+      const int js[4] = {at.x, at.y, at.z, at.w};
+      if (min(min(js[0], js[1]), min(js[2], js[3])) < 0)
 #pragma unroll
-      for (int r = 0; r < 4; ++r) kept |= row_at[4 * a + r] < 0;
-      if (kept)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) unpack4(*reinterpret_cast<const uint32_t*>(vt + val_off(a, d0 + e)), vs, x[e]);
+        for (int e = 0; e < 4; ++e) unpack4(*reinterpret_cast<const uint32_t*>(img + val_off(a, d0 + e)), vs, x[e]);
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
-        const int j = row_at[4 * a + r];
-        if (j < 0) continue;
+        if (js[r] < 0) continue;
         float t[4];
-        load_row<4>(v + j * rows.ld + h * HD + d0, t);
+        load_row<4>(v + js[r] * rows.ld + h * HD + d0, t);
 #pragma unroll
         for (int e = 0; e < 4; ++e) x[e][r] = t[e];
       }
+    };
+    auto top_v = [&](const float (&x)[4][4]) {
 #pragma unroll
       for (int e = 0; e < 4; ++e)
 #pragma unroll
@@ -249,65 +258,78 @@ __global__ __launch_bounds__(kTPB) void k_kv8_store(Kv8Segs S, Kv8Slice c, Kv8Ro
     gather_v(va, vd, vx);
     if constexpr (HD == 72) {
       if (tid < 64) {
-        const int j = row_at[tid];
-        if (j >= 0) {
-          load_row<8>(k + j * rows.ld + h * HD + 64, kx2);
+        const int j2 = row_at[tid];
+        if (j2 >= 0) {
+          load_row<8>(k + j2 * rows.ld + h * HD + 64, kx2);
         } else {
-          const uint2 b = *reinterpret_cast<const uint2*>(kt + key_off(tid, 4));
-          unpack4(b.x, ks, kx2);
-          unpack4(b.y, ks, kx2 + 4);
+          unpack4(old2.x, ks, kx2);
+          unpack4(old2.y, ks, kx2 + 4);
         }
 #pragma unroll
         for (int i = 0; i < 8; ++i) ka = fmaxf(ka, finite_abs(kx2[i]));
       } else if (tid < 96) {
         gather_v((tid - 64) >> 1, 64 + 4 * (tid & 1), vx2);
+        top_v(vx2);
       }
     }
-    block_max(ka, vm, sh);
-    const int kb = scale_byte(ka), vb = scale_byte(vm);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) ka = fmaxf(ka, finite_abs(kx[i]));
+    top_v(vx);
+    ka = wave_max(ka);
+    vm = wave_max(vm);
+    if (lane_id() == 0) {
+      sh[tid >> 6][0] = ka;
+      sh[tid >> 6][1] = vm;
+    }
+    __syncthreads();
+    const int kb = scale_byte(fmaxf(fmaxf(sh[0][0], sh[1][0]), fmaxf(sh[2][0], sh[3][0])));
+    const int vb = scale_byte(fmaxf(fmaxf(sh[0][1], sh[1][1]), fmaxf(sh[2][1], sh[3][1])));
     const float ki = two_to(127 - kb), vi = two_to(127 - vb);
     *reinterpret_cast<uint4*>(kt + key_off(kr, kp)) =
         make_uint4(pack4(kx, ki), pack4(kx + 4, ki), pack4(kx + 8, ki), pack4(kx + 12, ki));
 #pragma unroll
-    for (int e = 0; e < 4; ++e) *reinterpret_cast<uint32_t*>(vt + val_off(va, vd + e)) = pack4(vx[e], vi);
+    for (int e = 0; e < 4; ++e) *reinterpret_cast<uint32_t*>(img + val_off(va, vd + e)) = pack4(vx[e], vi);
     if constexpr (HD == 72) {
       if (tid < 64)
         *reinterpret_cast<uint2*>(kt + key_off(tid, 4)) = make_uint2(pack4(kx2, ki), pack4(kx2 + 4, ki));
       else if (tid < 96)
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-          *reinterpret_cast<uint32_t*>(vt + val_off((tid - 64) >> 1, 64 + 4 * (tid & 1) + e)) = pack4(vx2[e], vi);
+          *reinterpret_cast<uint32_t*>(img + val_off((tid - 64) >> 1, 64 + 4 * (tid & 1) + e)) = pack4(vx2[e], vi);
     }
     if (tid == 0) {
       sc[0] = (unsigned char)kb;
       sc[1] = (unsigned char)vb;
     }
-  }
+    __syncthreads();
+    for (int i = tid; i < NV; i += kTPB) reinterpret_cast<uint4*>(vt)[i] = image[i];
+  };
+  for_each_unit(S, rows, c.kv_heads, group, units, body);
 }
 
-// One workgroup reads the listed rows of one block of one head.
+// One workgroup reads the listed rows of one block of one head at a time.
 template <typename T, int HD>
 __global__ __launch_bounds__(kTPB) void k_kv8_load(Kv8Segs S, Kv8Slice c, Kv8Rows rows, T* __restrict__ k,
-                                                   T* __restrict__ v, int64_t units) {
+                                                   T* __restrict__ v, int group, int units) {
   __shared__ __attribute__((aligned(16))) unsigned char sv[kKv8Block * HD];
+  constexpr int NP = HD / 8;  // pieces of eight dims
   const int tid = threadIdx.x;
-  for (int64_t u = blockIdx.x; u < units; u += gridDim.x) {
-    const int h = (int)(u % c.kv_heads), w = (int)(u / c.kv_heads);
-    Run run;
-    if (!find_run(S, rows, w, &run)) continue;  // the same for all threads
-    const unsigned char* kt = c.tiles + ((int64_t)h * c.nblk + run.block) * 2 * kKv8Block * HD;
+  auto body = [&](int h, int block, int first) {
+    const unsigned char* kt = c.tiles + ((int64_t)h * c.nblk + block) * 2 * kKv8Block * HD;
     const unsigned char* vt = kt + kKv8Block * HD;
-    const unsigned char* sc = c.scales + ((int64_t)h * c.nblk + run.block) * 2;
-    const float ks = __uint_as_float((uint32_t)sc[0] << 23), vs = __uint_as_float((uint32_t)sc[1] << 23);
-    __syncthreads();
+    const unsigned char* sc = c.scales + ((int64_t)h * c.nblk + block) * 2;
+    __syncthreads();  // the block before is done with LDS
     for (int i = tid; i < kKv8Block * HD / 16; i += kTPB)
       reinterpret_cast<uint4*>(sv)[i] = reinterpret_cast<const uint4*>(vt)[i];
+    const float ks = __uint_as_float((uint32_t)sc[0] << 23), vs = __uint_as_float((uint32_t)sc[1] << 23);
     __syncthreads();
-    constexpr int NP = HD / 8;  // pieces of eight dims
-    for (int i = tid; i < run.count * NP; i += kTPB) {
-      const int j = run.first + i / NP, p = i % NP;
-      int at = j - run.first;
-      if (rows.idx != nullptr) block_of(S, rows.idx[j], &at);
+    const int end = rows.idx == nullptr ? min(rows.n, S.tok[segment_of(S, first) + 1]) : rows.n;
+    for (int i = tid;; i += kTPB) {
+      const int64_t j = (int64_t)first + i / NP;
+      const int p = i % NP;
+      if (j >= end) break;
+      int at = (int)(j - first);
+      if (rows.idx == nullptr ? at >= kKv8Block : block_of(S, rows.idx[j], &at) != block) break;
       float x[8];
       const int off = p < 8 ? key_off(at, p >> 1) + 8 * (p & 1) : key_off(at, 4);
       const uint2 b = *reinterpret_cast<const uint2*>(kt + off);
@@ -319,7 +341,8 @@ __global__ __launch_bounds__(kTPB) void k_kv8_load(Kv8Segs S, Kv8Slice c, Kv8Row
         x[e] = __builtin_amdgcn_cvt_pk_f32_fp8((int)sv[val_off(at >> 2, p * 8 + e) + (at & 3)], false)[0] * vs;
       store_row<8>(v + j * rows.ld + h * HD + p * 8, x);
     }
-  }
+  };
+  for_each_unit(S, rows, c.kv_heads, group, units, body);
 }
 
 template <typename F>
@@ -330,27 +353,40 @@ hipError_t by_type(sphinx_dtype dt, int head_dim, const F& go) {
   else go(float{}, std::integral_constant<int, 72>{});
   return hipGetLastError();
 }
-// workgroups of a launch: one per unit, at most 2^20 (each then takes several)
-unsigned unit_grid(int64_t units) { return (unsigned)std::min<int64_t>(units, 1 << 20); }
+
+// Rows that a workgroup looks at: one workgroup per row and head where that makes
+// no more than about 8192 (four rounds of a full chip); with many rows several of
+// them share a block anyway.
+struct Split {
+  int group, units;
+  unsigned grid;
+};
+Split split(const Kv8Slice& c, const Kv8Rows& rows) {
+  Split p;
+  p.group = (int)std::clamp<int64_t>((int64_t)rows.n * c.kv_heads / 8192, 1, 16);
+  p.units = rows.idx ? (int)(((int64_t)rows.n + p.group - 1) / p.group) : (int)c.nblk;
+  p.grid = (unsigned)std::min<int64_t>((int64_t)p.units * c.kv_heads, 1 << 20);  // each then takes several
+  return p;
+}
 }  // namespace
 
 hipError_t launch_kv8_store(sphinx_dtype dt, int head_dim, const Kv8Segs& S, const Kv8Slice& c, const Kv8Rows& rows,
                             const void* k, const void* v, hipStream_t s) {
-  const int64_t units = (rows.idx ? (int64_t)rows.n : c.nblk) * c.kv_heads;
+  const Split p = split(c, rows);
   return by_type(dt, head_dim, [&](auto t, auto hd) {
     using T = decltype(t);
-    k_kv8_store<T, decltype(hd)::value><<<unit_grid(units), kTPB, 0, s>>>(
-        S, c, rows, static_cast<const T*>(k), static_cast<const T*>(v), units);
+    k_kv8_store<T, decltype(hd)::value><<<p.grid, kTPB, 0, s>>>(S, c, rows, static_cast<const T*>(k),
+                                                                static_cast<const T*>(v), p.group, p.units);
   });
 }
 
 hipError_t launch_kv8_load(sphinx_dtype dt, int head_dim, const Kv8Segs& S, const Kv8Slice& c, const Kv8Rows& rows,
                            void* k, void* v, hipStream_t s) {
-  const int64_t units = (rows.idx ? (int64_t)rows.n : c.nblk) * c.kv_heads;
+  const Split p = split(c, rows);
   return by_type(dt, head_dim, [&](auto t, auto hd) {
     using T = decltype(t);
     k_kv8_load<T, decltype(hd)::value>
-        <<<unit_grid(units), kTPB, 0, s>>>(S, c, rows, static_cast<T*>(k), static_cast<T*>(v), units);
+        <<<p.grid, kTPB, 0, s>>>(S, c, rows, static_cast<T*>(k), static_cast<T*>(v), p.group, p.units);
   });
 }
 

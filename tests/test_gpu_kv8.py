@@ -375,12 +375,12 @@ def test_cache_past_32_bit_offsets():
         assert (err <= mag * 2.0 ** -6 + 2.0 ** -8 * np.abs(ref)).all()
 
 
-def test_tensors_of_another_device_are_refused():
+def test_tensors_of_another_device_and_short_slices_are_refused():
     c = Cache(1, 64, [0, 64])
     cpu = torch.zeros(64, 64)
     with pytest.raises(ValueError):
         B.sphinx_kv8_store(B.F32, 1, 64, cpu, cpu, 64, None, 64, c.bounds, c.slice)
-    with pytest.raises(ValueError):
+    with pytest.raises(S.SphinxError):  # a slice of too few bytes
         B.sphinx_kv8_load(B.F32, 1, 64, c.slice[:64], c.bounds, None, 64, cpu.cuda(), cpu.cuda(), 64)
 
 

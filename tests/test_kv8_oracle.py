@@ -99,6 +99,7 @@ def test_bytes_and_their_refusals(L):
     assert f(1, 64, _cu(0, 64), 0) == INVALID
     assert f(1, 64, _cu(*range(66)), 65) == UNSUPPORTED
     assert f(2048, 64, _cu(0, 64), 1) == UNSUPPORTED
+    assert f(64, 64, _cu(0, (1 << 31) - 1), 1) == UNSUPPORTED  # 2^31 blocks of all heads
     assert L.sphinx_kv8_bytes(1, 64, _cu(0, 64), 1, None) == INVALID
     # long caches: sizes past 32 bits
     assert f(16, 64, _cu(0, 1 << 30), 1) == OK and out.value == (1 << 30) * 2048 + (1 << 24) * 16 * 2
@@ -108,19 +109,21 @@ def test_bytes_and_their_refusals(L):
 def test_store_and_load_refusals(L, load):
     P = ctypes.c_void_p
 
-    def call(dt=1, hk=1, d=64, k=256, v=256, ld=64, idx=256, n=3, cu=_cu(0, 8), nseg=1, c=256):
+    def call(dt=1, hk=1, d=64, k=256, v=256, ld=64, idx=256, n=3, cu=_cu(0, 8), nseg=1, c=256, have=1 << 40):
         if load:
-            return L.sphinx_kv8_load(dt, hk, d, P(c), cu, nseg, P(idx), n, P(k), P(v), ld, None)
-        return L.sphinx_kv8_store(dt, hk, d, P(k), P(v), ld, P(idx), n, cu, nseg, P(c), None)
+            return L.sphinx_kv8_load(dt, hk, d, P(c), have, cu, nseg, P(idx), n, P(k), P(v), ld, None)
+        return L.sphinx_kv8_store(dt, hk, d, P(k), P(v), ld, P(idx), n, cu, nseg, P(c), have, None)
 
     assert call(dt=2) == UNSUPPORTED
     assert call(d=80, ld=80) == UNSUPPORTED
     assert call(ld=56) == INVALID and call(ld=68) == INVALID and call(hk=2) == INVALID
     assert call(n=-1) == INVALID
+    assert call(hk=2, ld=128, n=1 << 30) == UNSUPPORTED  # 2^31 rows of all heads
     assert call(idx=None, n=9) == INVALID  # more rows than tokens
     for kw in (dict(k=None), dict(v=None), dict(c=None), dict(k=264), dict(v=8), dict(c=260), dict(idx=4)):
         assert call(**kw) == INVALID, kw
     assert call(cu=_cu(0, 8, 4), nseg=2) == INVALID
+    assert call(have=2 * 64 * 64 + 255) == WORKSPACE  # a block of one head needs 256 more than its tiles
     assert call(n=0, k=None, v=None, c=None, idx=None) == OK  # nothing to do
     assert call(cu=_cu(0, 0), n=5, k=None, v=None, c=None) == OK  # no tokens: every row is skipped
 
@@ -133,8 +136,9 @@ def test_attention_refusals(L):
         return L.sphinx_kv8_attention_workspace_bytes(dt, h, hk, d, cq, ck, nseg, None if out is None else ctypes.byref(out))
 
     def call(dt=1, h=2, hk=1, d=64, q=256, ldq=128, c=256, cq=_cu(0, 4), ck=_cu(0, 8), kl=None, nseg=1, o=256, ws=256,
-             nbytes=1 << 40):
-        return L.sphinx_kv8_attention(dt, h, hk, d, P(q), ldq, P(c), cq, ck, kl, nseg, P(o), P(ws), nbytes, None)
+             nbytes=1 << 40, have=1 << 40):
+        return L.sphinx_kv8_attention(dt, h, hk, d, P(q), ldq, P(c), have, cq, ck, kl, nseg, P(o), P(ws), nbytes,
+                                      None)
 
     assert size() == OK and need.value > 0
     for f in (size, call):
@@ -155,6 +159,7 @@ def test_attention_refusals(L):
                dict(ws=128)):
         assert call(**kw) == INVALID, kw
     assert call(nbytes=need.value - 1) == WORKSPACE
+    assert call(have=2 * 64 * 64 + 255) == WORKSPACE
     assert call(cq=_cu(0, 0), q=None, o=None, c=None, ws=None, nbytes=0) == OK  # no queries
 
 
