@@ -602,8 +602,8 @@ sphinx_status kv8_check(int32_t kv_heads, int32_t head_dim, const int32_t* cu_kv
     if (cu_kv[i + 1] < cu_kv[i]) return SPHINX_E_INVALID;
     nblk += ((int64_t)cu_kv[i + 1] - cu_kv[i] + kKv8Block - 1) / kKv8Block;
   }
-  // blocks of all heads are counted in 32 bits (2^31 of them hold 16 TB)
-  return nblk * kv_heads < ((int64_t)1 << 31) ? SPHINX_OK : SPHINX_E_UNSUPPORTED;
+  // tiles are counted in 32 bits (2^31 of them hold 8 TB)
+  return 2 * nblk * kv_heads < ((int64_t)1 << 31) ? SPHINX_OK : SPHINX_E_UNSUPPORTED;
 }
 
 Kv8Slice kv8_slice(void* base, int32_t kv_heads, int32_t head_dim, int64_t nblk) {
@@ -621,7 +621,7 @@ sphinx_status kv8_rows_check(sphinx_dtype dtype, int32_t kv_heads, int32_t head_
   if (st != SPHINX_OK) return st;
   if (n < 0 || (idx == nullptr && n > cu_kv[nseg])) return SPHINX_E_INVALID;
   if (ld < (int64_t)kv_heads * head_dim || ld % 8 != 0) return SPHINX_E_INVALID;
-  if ((int64_t)n * kv_heads >= ((int64_t)1 << 31)) return SPHINX_E_UNSUPPORTED;  // rows of all heads, in 32 bits
+  if (2 * (int64_t)n * kv_heads >= ((int64_t)1 << 31)) return SPHINX_E_UNSUPPORTED;  // rows of all tiles, in 32 bits
   if (n == 0 || cu_kv[nseg] == 0) return SPHINX_OK;
   if (!k || !v || !slice || !aligned(k, 16) || !aligned(v, 16) || !aligned(slice, 16) || !aligned(idx, 16))
     return SPHINX_E_INVALID;

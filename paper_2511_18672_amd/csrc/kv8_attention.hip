@@ -18,6 +18,17 @@ constexpr int kRows = 32;  // rows (queries of the heads that share a key/value 
 
 __device__ __forceinline__ float fast_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
 
+// Segment of a work item or of a row to join: the last whose first one (of the
+// prefix sums `first`) is not behind it.
+__device__ __forceinline__ int find_segment(const int* first, int nseg, int at) {
+  int lo = 0, hi = nseg - 1;
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) >> 1;
+    if (first[mid] <= at) lo = mid; else hi = mid - 1;
+  }
+  return lo;
+}
+
 // Partial results: row r of head h, chunk j of segment i is number
 // part[i] + (h rows_i + r) chunks_i + j: its running maximum and sum, and O.
 struct Parts {
@@ -66,7 +77,7 @@ __device__ __forceinline__ void operand(const uint4& b, float scale, float (&f)[
 // bf16: 32x32x16 products, P rounded to bf16 for the product, the row sum adding
 // the same rounded values; f32: 32x32x2 products, nothing rounded.
 template <typename T, int HD>
-__global__ __launch_bounds__(kTPB, 2) void k_kv8_attn_rows(Kv8Attn A, Kv8Slice c, Kv8Plan P, Parts part, int first) {
+__global__ __launch_bounds__(kTPB, sizeof(T) == 2 && HD == 64 ? 3 : 2) void k_kv8_attn_rows(Kv8Attn A, Kv8Slice c, Kv8Plan P, Parts part, int first) {
   constexpr bool F32 = sizeof(T) == 4;
   constexpr int DB = (HD + 31) / 32;
   __shared__ float sO[4][kRows][DB * 32 + 1];
@@ -75,11 +86,10 @@ __global__ __launch_bounds__(kTPB, 2) void k_kv8_attn_rows(Kv8Attn A, Kv8Slice c
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int g = lane >> 5, r32 = lane & 31;
   const int unit = first + (int)blockIdx.x, h = unit % c.kv_heads, item = unit / c.kv_heads;
-  int s = 0;
-  while (s + 1 < A.nseg && P.item[s + 1] <= item) ++s;
+  const int s = find_segment(P.item, A.nseg, item);
   const int chunks = P.chunks[s], tile = (item - P.item[s]) / chunks, chunk = item - P.item[s] - tile * chunks;
   const int row0 = tile * kRows, nrows = A.nq[s] * A.group;
-  const int L = A.klen[s], b0 = chunk * P.chunk, nb = min((L + kKv8Block - 1) / kKv8Block, b0 + P.chunk);
+  const int L = A.klen[s], b0 = chunk * P.size[s], nb = min((L + kKv8Block - 1) / kKv8Block, b0 + P.size[s]);
   auto row_of = [&](int row, int64_t ld) -> int64_t {  // element of a row in q or o
     const int q = row / A.group;
     return (A.q0[s] + (int64_t)q) * ld + (int64_t)(h * A.group + row - q * A.group) * HD;
@@ -334,13 +344,13 @@ __global__ __launch_bounds__(kTPB, HD == 64 ? 3 : 2) void k_kv8_attn_tiles(Kv8At
   // they read the same bytes
   const int unit = xcd_tile(first + (int)blockIdx.x, total), items = P.item[A.nseg];
   const int h = unit / items, item = unit - h * items;
-  int s = 0;
-  while (s + 1 < A.nseg && P.item[s + 1] <= item) ++s;
+  const int s = find_segment(P.item, A.nseg, item);
   const int chunks = P.chunks[s], tiles = (P.item[s + 1] - P.item[s]) / chunks;
   const int chunk = (item - P.item[s]) / tiles, tile = item - P.item[s] - chunk * tiles;
   const int nrows = A.nq[s] * A.group;
-  const int L = A.klen[s], b0 = chunk * P.chunk, nkt = min((L + kKv8Block - 1) / kKv8Block - b0, P.chunk);
+  const int L = A.klen[s], b0 = chunk * P.size[s], nkt = min((L + kKv8Block - 1) / kKv8Block - b0, P.size[s]);
   const int row = tile * 128 + wave * 32 + r32;
+  const bool active = tile * 128 + wave * 32 < nrows;  // a wave without rows only stages bytes
   auto row_of = [&](int64_t ld) -> int64_t {
     const int q = row / A.group;
     return (A.q0[s] + (int64_t)q) * ld + (int64_t)(h * A.group + row - q * A.group) * HD;
@@ -566,6 +576,12 @@ __global__ __launch_bounds__(kTPB, HD == 64 ? 3 : 2) void k_kv8_attn_tiles(Kv8At
     }
     return key_frag(ks_, rb, ks);
   };
+  // loads of iteration t: keys t + 3, values t + 1
+  auto fetch = [&](int t) {
+    fetch_k(min(t + 3, nkt - 1));
+    fetch_v(t + 1);
+    if (t + 2 == nkt && last < kKv8Block) trim_v();
+  };
   // Iteration t; PAR = t % 2.  c: scores of block t, n: of block t + 1; pp: probabilities of block t - 1, pn: of t.
   auto iter = [&](int t, auto PAR, f32x16& c0, f32x16& c1, f32x16& n0, f32x16& n1, bf16x8 (&pp)[2][2],
                   bf16x8 (&pn)[2][2]) {
@@ -625,11 +641,7 @@ __global__ __launch_bounds__(kTPB, HD == 64 ? 3 : 2) void k_kv8_attn_tiles(Kv8At
         put(vw, 1, sv, vsc);
         if constexpr (HD == 72) put_v8(vw);
       }
-      if (i == 12) {
-        fetch_k(min(t + 3, nkt - 1));
-        fetch_v(t + 1);
-        if (t + 2 == nkt && last < kKv8Block) trim_v();
-      }
+      if (i == 12) fetch(t);
       __builtin_amdgcn_sched_barrier(0);
     }
     // the probabilities are made here, not after the next branch
@@ -658,6 +670,25 @@ __global__ __launch_bounds__(kTPB, HD == 64 ? 3 : 2) void k_kv8_attn_tiles(Kv8At
     fetch_v(0);
     if (nkt == 1 && last < kKv8Block) trim_v();
     barrier();
+    if (!active) {
+      barrier();
+      int t = 0;
+      for (; t < nkt; ++t) {  // at the last block only its values are left to stage
+        unsigned char* vw = sm.v[t & 1];
+        put(vw, 0, sv, vsc);
+        put(vw, 1, sv, vsc);
+        if constexpr (HD == 72) put_v8(vw);
+        if (t + 1 < nkt) {
+          unsigned char* kw = sm.k[t & 1];
+          put(kw, 0, sk, ksc);
+          put(kw, 1, sk, ksc);
+          if constexpr (HD == 72) put_k8(kw);
+          fetch(t);
+        }
+        barrier();
+      }
+      return;
+    }
     f32x16 a0, a1, d0, d1;
     qk(sm.k[0], a0, a1);
     if (nkt == 1 && last < kKv8Block) mask_tail(a0, a1);
@@ -694,6 +725,15 @@ __global__ __launch_bounds__(kTPB, HD == 64 ? 3 : 2) void k_kv8_attn_tiles(Kv8At
     put(vw, 0, sv, vsc);
     put(vw, 1, sv, vsc);
     if constexpr (HD == 72) put_v8(vw);
+    auto pv = [&](const unsigned char* slot, const bf16x8 (&p)[2][2]) {
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+        for (int hf = 0; hf < 2; ++hf)
+#pragma unroll
+          for (int db = 0; db < DB; ++db)
+            oacc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(val_frag(slot, kb, hf, db), p[kb][hf], oacc[db], 0, 0, 0);
+    };
     settle(a0, a1);
     if (last < kKv8Block) mask_tail(a0, a1);
     float psum = 0.0f;
@@ -710,15 +750,6 @@ __global__ __launch_bounds__(kTPB, HD == 64 ? 3 : 2) void k_kv8_attn_tiles(Kv8At
       pb[1][r >> 3][r & 7] = y[0];
       pb[1][r >> 3][(r & 7) + 1] = y[1];
     }
-    auto pv = [&](const unsigned char* slot, const bf16x8 (&p)[2][2]) {
-#pragma unroll
-      for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-        for (int hf = 0; hf < 2; ++hf)
-#pragma unroll
-          for (int db = 0; db < DB; ++db)
-            oacc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(val_frag(slot, kb, hf, db), p[kb][hf], oacc[db], 0, 0, 0);
-    };
     pv(vr, pa);
     if (__ballot(!(psum <= kPsumMax)) != 0) psum = rebase(t, pb);
     l_run += psum;
@@ -758,20 +789,19 @@ __global__ __launch_bounds__(kTPB, HD == 64 ? 3 : 2) void k_kv8_attn_tiles(Kv8At
 }
 
 // Joins the chunks of a row and head: one wave per row and head, or (few rows of
-// many chunks) a workgroup of eight waves, wave w taking chunks w (mod 8).  A
+// many chunks) a workgroup of 16 waves, wave w taking chunks w (mod 16).  A
 // lane has one dim; at head_dim 72 eight lanes have a second one.  Bound by the
 // latency of the loads: a wave asks for the maxima, sums and values of eight
 // chunks at once and joins them as it goes.
 template <typename T, int HD, int WAVES>
-__global__ __launch_bounds__(512) void k_kv8_attn_join(Kv8Attn A, int kv_heads, Kv8Plan P, Parts part, int rows) {
+__global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void k_kv8_attn_join(Kv8Attn A, int kv_heads, Kv8Plan P, Parts part, int rows) {
   __shared__ float sO[WAVES][HD], sL[WAVES], sM[WAVES];
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-  const int unit = WAVES == 1 ? (int)blockIdx.x * 8 + wave : (int)blockIdx.x;  // row * kv_heads + head
+  const int unit = WAVES == 1 ? (int)blockIdx.x * 4 + wave : (int)blockIdx.x;  // row * kv_heads + head
   if (unit >= rows * kv_heads) return;  // only with one wave per row, which has no barrier
   const int h = unit % kv_heads, at = unit / kv_heads;
-  int s = 0;
-  while (s + 1 < A.nseg && P.row[s + 1] <= at) ++s;
+  const int s = find_segment(P.row, A.nseg, at);
   const int row = at - P.row[s], chunks = P.chunks[s], nrows = A.nq[s] * A.group;
   const int64_t first = P.part[s] + ((int64_t)h * nrows + row) * chunks;
   float m = -INFINITY, num = 0.0f, num2 = 0.0f, den = 0.0f;
@@ -869,12 +899,12 @@ hipError_t launch_kv8_attention(sphinx_dtype dt, int head_dim, const Kv8Attn& A,
     const int join = P.row[A.nseg];
     int most = 0;
     for (int i = 0; i < A.nseg; ++i) most = std::max(most, P.chunks[i]);
-    // a wave per row where they fill the chip or have few chunks to walk
-    if (most <= 16 || (int64_t)join * c.kv_heads >= 2048)
-      k_kv8_attn_join<T, HD, 1><<<(unsigned)(((int64_t)join * c.kv_heads + 7) / 8), 512, 0, s>>>(A, c.kv_heads, P,
-                                                                                              part, join);
+    // a wave per row where a wave's first eight loads see all chunks, or rows fill the chip
+    const int units = join * c.kv_heads;
+    if (most <= 8 || units >= 1024)
+      k_kv8_attn_join<T, HD, 1><<<(units + 3) / 4, 256, 0, s>>>(A, c.kv_heads, P, part, join);
     else
-      k_kv8_attn_join<T, HD, 8><<<(unsigned)join * (unsigned)c.kv_heads, 512, 0, s>>>(A, c.kv_heads, P, part, join);
+      k_kv8_attn_join<T, HD, 16><<<units, 1024, 0, s>>>(A, c.kv_heads, P, part, join);
   };
   if (dt == SPHINX_F32)
     go(float{}, std::integral_constant<int, 64>{});

@@ -30,23 +30,19 @@ __device__ __forceinline__ int scale_byte(float top) {
   return min(max(e, kExpMin), kExpMax) + 127;
 }
 
-__device__ __forceinline__ float finite_abs(float x) {
-  const float a = fabsf(x);
-  return a < INFINITY ? a : 0.0f;  // NaN compares false
-}
-
-// Two values scaled and rounded into half `hi` of `old`.  The hardware rounds to
+// Two values scaled and rounded into half HI of `old`.  The hardware rounds to
 // nearest even and turns what is past 464, infinities and NaN into NaN; finite
-// values past 448, which the largest scale leaves, saturate.
-template <bool HI>
+// values past 448, which only the largest scale leaves, saturate (FULL).
+template <bool HI, bool FULL>
 __device__ __forceinline__ uint32_t pack2(float a, float b, float inv, uint32_t old) {
   float x = a * inv, y = b * inv;
-  if (fabsf(a) < INFINITY) x = fminf(fmaxf(x, -448.0f), 448.0f);
-  if (fabsf(b) < INFINITY) y = fminf(fmaxf(y, -448.0f), 448.0f);
+  if (FULL && fabsf(a) < INFINITY) x = fminf(fmaxf(x, -448.0f), 448.0f);
+  if (FULL && fabsf(b) < INFINITY) y = fminf(fmaxf(y, -448.0f), 448.0f);
   return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(x, y, (int)old, HI);
 }
+template <bool FULL>
 __device__ __forceinline__ uint32_t pack4(const float* x, float inv) {
-  return pack2<true>(x[2], x[3], inv, pack2<false>(x[0], x[1], inv, 0u));
+  return pack2<true, FULL>(x[2], x[3], inv, pack2<false, FULL>(x[0], x[1], inv, 0u));
 }
 
 // The values of four stored bytes.
@@ -58,27 +54,7 @@ __device__ __forceinline__ void unpack4(uint32_t w, float scale, float* x) {
   x[3] = b[1] * scale;
 }
 
-// n (a multiple of 4) consecutive elements as floats, and back.
-template <int N>
-__device__ __forceinline__ void load_row(const bf16* p, float* x) {
-  constexpr int W = N % 8 == 0 ? 8 : 4;
-  typedef __bf16 vec __attribute__((ext_vector_type(W)));
-#pragma unroll
-  for (int i = 0; i < N; i += W) {
-    const vec v = *reinterpret_cast<const vec*>(p + i);
-#pragma unroll
-    for (int e = 0; e < W; ++e) x[i + e] = (float)v[e];
-  }
-}
-template <int N>
-__device__ __forceinline__ void load_row(const float* p, float* x) {
-#pragma unroll
-  for (int i = 0; i < N; i += 4) {
-    const f32x4 v = *reinterpret_cast<const f32x4*>(p + i);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) x[i + e] = v[e];
-  }
-}
+// n consecutive floats as elements.
 template <int N>
 __device__ __forceinline__ void store_row(bf16* p, const float* x) {
 #pragma unroll
@@ -111,25 +87,51 @@ __device__ __forceinline__ int val_off(int a, int dim) {
   return chunk * 16 + hf * 8 + j4 * 4;
 }
 
-__device__ __forceinline__ int segment_of(const Kv8Segs& S, int t) {
-  int lo = 0, hi = S.nseg - 1;
-  while (lo < hi) {
-    const int mid = (lo + hi + 1) >> 1;
-    if (S.tok[mid] <= t) lo = mid; else hi = mid - 1;
-  }
-  return lo;
-}
-// Block of token t, and its row there; -1 for a token outside the slice.
+// Block of token t, and its row there; -1 for a token outside the slice.  Every
+// lane looks at every segment, whose bounds come through scalar loads; a search
+// by lanes would be a chain of vector loads from the kernel's arguments.
 __device__ __forceinline__ int block_of(const Kv8Segs& S, int t, int* row) {
-  if (t < 0 || t >= S.tok[S.nseg]) return -1;
-  const int s = segment_of(S, t), at = t - S.tok[s];
+  int tok = 0, blk = 0;
+  for (int s = 1; s < S.nseg; ++s) {
+    const bool behind = t >= S.tok[s];
+    tok = behind ? S.tok[s] : tok;
+    blk = behind ? S.blk[s] : blk;
+  }
+  const int at = t - tok;
   *row = at & (kKv8Block - 1);
-  return S.blk[s] + (at >> 6);
+  return t < 0 || t >= S.tok[S.nseg] ? -1 : blk + (at >> 6);
+}
+
+// Largest number over a wave.
+__device__ __forceinline__ uint32_t wave_top(uint32_t v) {
+  auto other = [&](auto ctrl) {
+    return (uint32_t)__builtin_amdgcn_mov_dpp((int)v, decltype(ctrl)::value, 0xf, 0xf, false);
+  };
+  v = max(v, other(std::integral_constant<int, 0xB1>{}));   // lane ^ 1
+  v = max(v, other(std::integral_constant<int, 0x4E>{}));   // lane ^ 2
+  v = max(v, other(std::integral_constant<int, 0x141>{}));  // the other quad of the 8-lane half
+  v = max(v, other(std::integral_constant<int, 0x140>{}));  // the other half of the row
+  const auto r16 = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+  v = max((uint32_t)r16[0], (uint32_t)r16[1]);
+  const auto r32 = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+  return max((uint32_t)r32[0], (uint32_t)r32[1]);
+}
+
+// LDS operations of a wave are done in order; this keeps the compiler from moving
+// them across.
+__device__ __forceinline__ void lds_order() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_wave_barrier();
 }
 
 // The rows of a call fall into runs, one per block, since listed tokens ascend.
-// A workgroup looks at `group` rows (of one head) and does the runs that start
-// among them; without listed tokens it does block `unit`.  body(block, first row).
+// A wave (or every wave of a workgroup alike) looks at `group` rows and does the
+// runs that start among them; without listed tokens it does block `unit`.
+struct Run {
+  int block, first;  // the run's block and its first row of the call
+  int count;         // rows of the block, from its first, that rows `first` and on fill; -1: listed tokens
+  int from, at, lane_block;  // listed tokens: row of the call, row and block of this lane's token (rows from .. + 63)
+};
 template <typename F>
 __device__ __forceinline__ void for_each_run(const Kv8Segs& S, const Kv8Rows& rows, int group, int unit, const F& body) {
   if (rows.idx == nullptr) {
@@ -139,172 +141,260 @@ __device__ __forceinline__ void for_each_run(const Kv8Segs& S, const Kv8Rows& ro
       if (S.blk[mid] <= unit) lo = mid; else hi = mid - 1;
     }
     const int first = S.tok[lo] + (unit - S.blk[lo]) * kKv8Block;
-    if (first < rows.n) body(unit, first);
+    const int count = min(min(kKv8Block, S.tok[lo + 1] - first), rows.n - first);
+    if (count > 0) body(Run{unit, first, count, 0, 0, 0});
     return;
   }
-  const int lane = lane_id();
-  const int64_t j = (int64_t)unit * group + lane;
-  const bool in = lane < group && j < rows.n;
-  int at, block = in ? block_of(S, rows.idx[j], &at) : -1;
-  const int before = in && j > 0 ? block_of(S, rows.idx[j - 1], &at) : -1;
-  uint64_t starts = __ballot(block >= 0 && block != before);  // the same in every wave
+  const int lane = lane_id(), from = unit * group;
+  const int64_t j = (int64_t)from + lane;
+  const int prev = from > 0 ? rows.idx[from - 1] : -1;
+  int at, before_at;
+  const int block = block_of(S, j < rows.n ? rows.idx[j] : -1, &at);
+  int before = __shfl_up(block, 1, kWave);
+  if (lane == 0) before = block_of(S, prev, &before_at);
+  uint64_t starts = __ballot(lane < group && block >= 0 && block != before);  // the same in every wave
   while (starts != 0) {
     const int l = __builtin_ctzll(starts);
     starts &= starts - 1;
-    body(__builtin_amdgcn_readlane(block, l), unit * group + l);
+    body(Run{__builtin_amdgcn_readlane(block, l), from + l, -1, from, at, block});
   }
 }
 
 // The units of all heads over the workgroups: neighbouring heads of a unit on
 // one XCD, one after the other, since a head's piece of a row (144 bytes at
-// head_dim 72) shares cache lines with the next head's.
+// head_dim 72) shares cache lines with the next head's.  `per`: units that a
+// workgroup does at a time, this is its `mine`-th.
 template <typename F>
-__device__ __forceinline__ void for_each_unit(const Kv8Segs& S, const Kv8Rows& rows, int kv_heads, int group, int units,
-                                              const F& body) {
-  const int total = units * kv_heads;
-  for (int64_t b = blockIdx.x; b < total; b += gridDim.x) {
-    const int u = xcd_tile((int)b, total), unit = u / kv_heads, h = u - unit * kv_heads;
-    for_each_run(S, rows, group, unit, [&](int block, int first) { body(h, block, first); });
+__device__ __forceinline__ void for_each_unit(const Kv8Segs& S, const Kv8Rows& rows, int heads, int group, int units,
+                                              int per, int mine, const F& body) {
+  const int total = units * heads, groups = (total + per - 1) / per;
+  for (int64_t b = blockIdx.x; b < groups; b += gridDim.x) {
+    const int u = xcd_tile((int)b, groups) * per + mine;
+    if (u >= total) continue;
+    const int unit = u / heads, h = u - unit * heads;
+    for_each_run(S, rows, group, unit, [&](const Run& run) { body(h, run); });
   }
 }
 
-// Row of the call for each row of a block, -1 where none names it; by one wave.
-// A token listed more than once takes its last row.
-__device__ __forceinline__ void map_rows(const Kv8Segs& S, const Kv8Rows& rows, int block, int first, int* row_at) {
+// Row of the call for each row of a run's block, -1 where none names it, in LDS;
+// by one wave.  A token listed more than once takes its last row.
+__device__ __forceinline__ void map_rows(const Kv8Segs& S, const Kv8Rows& rows, const Run& run, int* row_at) {
   const int lane = lane_id();
-  if (rows.idx == nullptr) {
-    const int s = segment_of(S, first), j = first + lane;
-    row_at[lane] = j < min(S.tok[s + 1], rows.n) ? j : -1;
+  if (run.count >= 0) {
+    row_at[lane] = lane < run.count ? run.first + lane : -1;
     return;
   }
   row_at[lane] = -1;
-  for (int64_t j = first + lane;; j += kWave) {
+  lds_order();
+  const bool here = run.from + lane >= run.first && run.lane_block == run.block;
+  if (here) atomicMax(&row_at[run.at], run.from + lane);
+  if ((__ballot(here) >> 63) == 0) return;  // the run ends among the lanes' tokens
+  for (int64_t j = (int64_t)run.from + kWave + lane;; j += kWave) {
     int at = 0;
-    const bool in = j < rows.n && block_of(S, rows.idx[j], &at) == block;
+    const bool in = block_of(S, j < rows.n ? rows.idx[j] : -1, &at) == run.block;
     if (in) atomicMax(&row_at[at], (int)j);
-    if (~__ballot(in) != 0) break;  // the run ends here
+    if (~__ballot(in) != 0) return;
   }
 }
 
-// One workgroup writes one block of one head at a time: the rows of the call and
-// the kept rows come together in registers as floats, give the new scales, and
-// are rounded once.  A thread has 16 dims of one key row (neighbouring threads
-// the same row's next dims, so that a row of a head is read in one piece) and
-// four dims of four value rows; head_dim 72: 64 threads more key dims, 32 threads
-// more value dims.  Four keys of a dim are four neighbouring bytes of the value
-// tile, which is put together in LDS, so that its old bytes come in and its new
-// ones go out as consecutive 16-byte pieces.
-// Bound by bytes: a full step's rows in and tiles out, in a partial step also
-// the old tiles in.
+// Eight elements of a row as they came.  peak: the largest magnitude, as the bits
+// of a float.  set: values of stored bytes, which both types hold exactly.
+template <typename T>
+struct Piece;
+template <>
+struct Piece<bf16> {
+  uint32_t w[4];
+  __device__ __forceinline__ void load(const bf16* p) {
+    const uint4 x = *reinterpret_cast<const uint4*>(p);
+    w[0] = x.x; w[1] = x.y; w[2] = x.z; w[3] = x.w;
+  }
+  __device__ __forceinline__ float get(int i) const {
+    return __uint_as_float((i & 1) ? (w[i >> 1] & 0xffff0000u) : (w[i >> 1] << 16));
+  }
+  __device__ __forceinline__ void set2(int i, float a, float b) {
+    bf16x2 v;
+    v[0] = (bf16)a;
+    v[1] = (bf16)b;
+    w[i >> 1] = __builtin_bit_cast(uint32_t, v);
+  }
+  __device__ __forceinline__ uint32_t peak() const {
+    typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+    u16x2 m = __builtin_bit_cast(u16x2, w[0] & 0x7fff7fffu);
+#pragma unroll
+    for (int i = 1; i < 4; ++i) m = __builtin_elementwise_max(m, __builtin_bit_cast(u16x2, w[i] & 0x7fff7fffu));
+    return (uint32_t)max(m[0], m[1]) << 16;
+  }
+};
+template <>
+struct Piece<float> {
+  float x[8];
+  __device__ __forceinline__ void load(const float* p) {
+    const f32x4 a = *reinterpret_cast<const f32x4*>(p), b = *reinterpret_cast<const f32x4*>(p + 4);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      x[i] = a[i];
+      x[4 + i] = b[i];
+    }
+  }
+  __device__ __forceinline__ float get(int i) const { return x[i]; }
+  __device__ __forceinline__ void set2(int i, float a, float b) {
+    x[i] = a;
+    x[i + 1] = b;
+  }
+  __device__ __forceinline__ uint32_t peak() const {
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(x[i]) & 0x7fffffffu);
+    return m;
+  }
+};
+template <typename T>
+__device__ __forceinline__ uint32_t finite_peak(const Piece<T>& p) {  // the same of the finite ones
+  uint32_t m = 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const uint32_t b = __float_as_uint(p.get(i)) & 0x7fffffffu;
+    m = b < 0x7f800000u ? max(m, b) : m;
+  }
+  return m;
+}
+
+// One wave writes the keys or the values of one block of one head at a time:
+// lane (a, c) = (l / 8, l % 8) has dims 8 c .. + 7 of rows 8 a .. + 7, so that
+// eight loads bring the 64 rows, eight whole rows each; head_dim 72: lane l also
+// has the last eight dims of row l.  Rows that are kept are made from the old
+// tile, which comes into LDS in consecutive 16-byte pieces, and are then treated
+// like new ones.  The largest magnitude is one reduction over the wave; the
+// rounded bytes are put in the tile's order in LDS and leave in 16-byte pieces.
+// Bound by bytes: a full step's rows in and tiles out, in a partial step also the
+// old tiles in.  A wave and not a workgroup per tile: a workgroup spends the way
+// of a row to its bytes on barriers.
 template <typename T, int HD>
-__global__ __launch_bounds__(kTPB) void k_kv8_store(Kv8Segs S, Kv8Slice c, Kv8Rows rows, const T* __restrict__ k,
-                                                    const T* __restrict__ v, int group, int units) {
+__global__ __launch_bounds__(kTPB, sizeof(T) == 2 ? 3 : 2) void k_kv8_store(Kv8Segs S, Kv8Slice c, Kv8Rows rows, const T* __restrict__ k,
+                                                       const T* __restrict__ v, int group, int units) {
   constexpr int NV = kKv8Block * HD / 16;  // 16-byte pieces of a tile
-  __shared__ __attribute__((aligned(16))) uint4 image[NV];  // the value tile
-  __shared__ int row_at[kKv8Block];
-  __shared__ float sh[4][2];
-  const int tid = threadIdx.x;
-  const int kr = tid >> 2, kp = tid & 3, va = tid >> 4, vd = (tid & 15) * 4;
-  unsigned char* img = reinterpret_cast<unsigned char*>(image);
-  auto body = [&](int h, int block, int first) {
-    unsigned char* kt = c.tiles + ((int64_t)h * c.nblk + block) * 2 * kKv8Block * HD;
-    unsigned char* vt = kt + kKv8Block * HD;
-    unsigned char* sc = c.scales + ((int64_t)h * c.nblk + block) * 2;
-    __syncthreads();  // the block before is done with LDS
-    const float ks = __uint_as_float((uint32_t)sc[0] << 23), vs = __uint_as_float((uint32_t)sc[1] << 23);
-    const bool whole = rows.idx == nullptr && first + kKv8Block <= rows.n;  // no row is kept, or only padding
-    uint4 old = make_uint4(0u, 0u, 0u, 0u);
-    uint2 old2 = make_uint2(0u, 0u);
-    if (!whole) {
-      old = *reinterpret_cast<const uint4*>(kt + key_off(kr, kp));
-      if (HD == 72 && tid < 64) old2 = *reinterpret_cast<const uint2*>(kt + key_off(tid, 4));
-      for (int i = tid; i < NV; i += kTPB) image[i] = reinterpret_cast<const uint4*>(vt)[i];
-    }
-    if (tid < kWave) map_rows(S, rows, block, first, row_at);
-    __syncthreads();
-    float kx[16], vx[4][4], kx2[8], vx2[4][4];
-    float ka = 0.0f, vm = 0.0f;
-    const int j = row_at[kr];
-    if (j >= 0) {
-      load_row<16>(k + j * rows.ld + h * HD + kp * 16, kx);
+  __shared__ __attribute__((aligned(16))) uint4 images[4][NV];
+  __shared__ __attribute__((aligned(16))) int maps[4][kKv8Block];
+  const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+  unsigned char* img = reinterpret_cast<unsigned char*>(images[wave]);
+  int* row_at = maps[wave];
+  const int a = lane >> 3, cc = lane & 7;
+  auto body = [&](int hh, const Run& run) {
+    const int h = hh >> 1;
+    const bool values = (hh & 1) != 0;  // the same for the whole wave
+    unsigned char* tile = c.tiles + (((int64_t)h * c.nblk + run.block) * 2 + (values ? 1 : 0)) * kKv8Block * HD;
+    unsigned char* sc = c.scales + ((int64_t)h * c.nblk + run.block) * 2 + (values ? 1 : 0);
+    const T* src = (values ? v : k) + h * HD;
+    Piece<T> p[8], pt;
+    lds_order();  // the tile before has left LDS
+    if (run.count == kKv8Block) {  // no row is kept
+      const T* row = src + (run.first + 8 * a) * rows.ld + 8 * cc;
+#pragma unroll
+      for (int r = 0; r < 8; ++r) p[r].load(row + r * rows.ld);
+      if constexpr (HD == 72) pt.load(src + (run.first + lane) * rows.ld + 64);
     } else {
-      unpack4(old.x, ks, kx);
-      unpack4(old.y, ks, kx + 4);
-      unpack4(old.z, ks, kx + 8);
-      unpack4(old.w, ks, kx + 12);
-    }
-    // values [dim][key]
-    auto gather_v = [&](int a, int d0, float (&x)[4][4]) {
-      const int4 at = *reinterpret_cast<const int4*>(row_at + 4 * a);
-      const int js[4] = {at.x, at.y, at.z, at.w};
-      if (min(min(js[0], js[1]), min(js[2], js[3])) < 0)
+      for (int i = lane; i < NV; i += kWave) images[wave][i] = reinterpret_cast<const uint4*>(tile)[i];
+      const float old = __uint_as_float((uint32_t)*sc << 23);
+      map_rows(S, rows, run, row_at);
+      lds_order();
+      const int4 x = *reinterpret_cast<const int4*>(row_at + 8 * a), y = *reinterpret_cast<const int4*>(row_at + 8 * a + 4);
+      const int js[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
+      // the kept rows' loads are of row 0 of the call and are replaced
 #pragma unroll
-        for (int e = 0; e < 4; ++e) unpack4(*reinterpret_cast<const uint32_t*>(img + val_off(a, d0 + e)), vs, x[e]);
+      for (int r = 0; r < 8; ++r) p[r].load(src + max(js[r], 0) * rows.ld + 8 * cc);
+      const int jt = row_at[lane];
+      if constexpr (HD == 72) pt.load(src + max(jt, 0) * rows.ld + 64);
+      if (__ballot(jt < 0) != 0) {
+        if (!values) {
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        if (js[r] < 0) continue;
-        float t[4];
-        load_row<4>(v + js[r] * rows.ld + h * HD + d0, t);
+          for (int r = 0; r < 8; ++r) {
+            const uint2 w = *reinterpret_cast<const uint2*>(img + key_off(8 * a + r, cc >> 1) + 8 * (cc & 1));
+            float t[8];
+            unpack4(w.x, old, t);
+            unpack4(w.y, old, t + 4);
+            if (js[r] < 0)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) x[e][r] = t[e];
-      }
-    };
-    auto top_v = [&](const float (&x)[4][4]) {
+              for (int e = 0; e < 8; e += 2) p[r].set2(e, t[e], t[e + 1]);
+          }
+          if constexpr (HD == 72) {
+            const uint2 w = *reinterpret_cast<const uint2*>(img + key_off(lane, 4));
+            float t[8];
+            unpack4(w.x, old, t);
+            unpack4(w.y, old, t + 4);
+            if (jt < 0)
 #pragma unroll
-      for (int e = 0; e < 4; ++e)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) vm = fmaxf(vm, finite_abs(x[e][r]));
-    };
-    gather_v(va, vd, vx);
-    if constexpr (HD == 72) {
-      if (tid < 64) {
-        const int j2 = row_at[tid];
-        if (j2 >= 0) {
-          load_row<8>(k + j2 * rows.ld + h * HD + 64, kx2);
+              for (int e = 0; e < 8; e += 2) pt.set2(e, t[e], t[e + 1]);
+          }
         } else {
-          unpack4(old2.x, ks, kx2);
-          unpack4(old2.y, ks, kx2 + 4);
-        }
 #pragma unroll
-        for (int i = 0; i < 8; ++i) ka = fmaxf(ka, finite_abs(kx2[i]));
-      } else if (tid < 96) {
-        gather_v((tid - 64) >> 1, 64 + 4 * (tid & 1), vx2);
-        top_v(vx2);
+          for (int e = 0; e < 8; e += 2)
+#pragma unroll
+            for (int g = 0; g < 2; ++g) {  // keys 8 a + 4 g .. + 3 of dims 8 c + e and the next
+              float t[4], u[4];
+              unpack4(*reinterpret_cast<const uint32_t*>(img + val_off(2 * a + g, 8 * cc + e)), old, t);
+              unpack4(*reinterpret_cast<const uint32_t*>(img + val_off(2 * a + g, 8 * cc + e + 1)), old, u);
+#pragma unroll
+              for (int r = 0; r < 4; ++r)
+                if (js[4 * g + r] < 0) p[4 * g + r].set2(e, t[r], u[r]);
+            }
+          if constexpr (HD == 72) {
+            if (jt < 0) {
+              float t[8];
+#pragma unroll
+              for (int e = 0; e < 8; ++e)
+                t[e] = __builtin_amdgcn_cvt_pk_f32_fp8((int)img[val_off(lane >> 2, 64 + e) + (lane & 3)], false)[0] * old;
+#pragma unroll
+              for (int e = 0; e < 8; e += 2) pt.set2(e, t[e], t[e + 1]);
+            }
+          }
+        }
       }
     }
+    uint32_t top = p[0].peak();
 #pragma unroll
-    for (int i = 0; i < 16; ++i) ka = fmaxf(ka, finite_abs(kx[i]));
-    top_v(vx);
-    ka = wave_max(ka);
-    vm = wave_max(vm);
-    if (lane_id() == 0) {
-      sh[tid >> 6][0] = ka;
-      sh[tid >> 6][1] = vm;
-    }
-    __syncthreads();
-    const int kb = scale_byte(fmaxf(fmaxf(sh[0][0], sh[1][0]), fmaxf(sh[2][0], sh[3][0])));
-    const int vb = scale_byte(fmaxf(fmaxf(sh[0][1], sh[1][1]), fmaxf(sh[2][1], sh[3][1])));
-    const float ki = two_to(127 - kb), vi = two_to(127 - vb);
-    *reinterpret_cast<uint4*>(kt + key_off(kr, kp)) =
-        make_uint4(pack4(kx, ki), pack4(kx + 4, ki), pack4(kx + 8, ki), pack4(kx + 12, ki));
+    for (int r = 1; r < 8; ++r) top = max(top, p[r].peak());
+    if constexpr (HD == 72) top = max(top, pt.peak());
+    top = wave_top(top);
+    if (top >= 0x7f800000u) {  // infinities or NaN among them (rare)
+      top = 0;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) *reinterpret_cast<uint32_t*>(img + val_off(va, vd + e)) = pack4(vx[e], vi);
-    if constexpr (HD == 72) {
-      if (tid < 64)
-        *reinterpret_cast<uint2*>(kt + key_off(tid, 4)) = make_uint2(pack4(kx2, ki), pack4(kx2 + 4, ki));
-      else if (tid < 96)
+      for (int r = 0; r < 8; ++r) top = max(top, finite_peak(p[r]));
+      if constexpr (HD == 72) top = max(top, finite_peak(pt));
+      top = wave_top(top);
+    }
+    const int b = scale_byte(__uint_as_float(top));
+    const float inv = two_to(127 - b);
+    if (lane == 0) *sc = (unsigned char)b;
+    const bool full = b == kExpMax + 127;  // only this scale leaves finite values past 448
+    auto pack = [&](float x0, float x1, float x2, float x3) -> uint32_t {
+      const float x[4] = {x0, x1, x2, x3};
+      return full ? pack4<true>(x, inv) : pack4<false>(x, inv);
+    };
+    auto put_key = [&](int off, const Piece<T>& q) {
+      *reinterpret_cast<uint2*>(img + off) = make_uint2(pack(q.get(0), q.get(1), q.get(2), q.get(3)),
+                                                        pack(q.get(4), q.get(5), q.get(6), q.get(7)));
+    };
+    lds_order();
+    if (!values) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-          *reinterpret_cast<uint32_t*>(img + val_off((tid - 64) >> 1, 64 + 4 * (tid & 1) + e)) = pack4(vx2[e], vi);
+      for (int r = 0; r < 8; ++r) put_key(key_off(8 * a + r, cc >> 1) + 8 * (cc & 1), p[r]);
+      if constexpr (HD == 72) put_key(key_off(lane, 4), pt);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+#pragma unroll
+        for (int g = 0; g < 2; ++g)
+          *reinterpret_cast<uint32_t*>(img + val_off(2 * a + g, 8 * cc + e)) =
+              pack(p[4 * g].get(e), p[4 * g + 1].get(e), p[4 * g + 2].get(e), p[4 * g + 3].get(e));
+      if constexpr (HD == 72)
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          img[val_off(lane >> 2, 64 + e) + (lane & 3)] = (unsigned char)pack(pt.get(e), 0.0f, 0.0f, 0.0f);
     }
-    if (tid == 0) {
-      sc[0] = (unsigned char)kb;
-      sc[1] = (unsigned char)vb;
-    }
-    __syncthreads();
-    for (int i = tid; i < NV; i += kTPB) reinterpret_cast<uint4*>(vt)[i] = image[i];
+    lds_order();
+    for (int i = lane; i < NV; i += kWave) reinterpret_cast<uint4*>(tile)[i] = images[wave][i];
   };
-  for_each_unit(S, rows, c.kv_heads, group, units, body);
+  for_each_unit(S, rows, 2 * c.kv_heads, group, units, 4, wave, body);
 }
 
 // One workgroup reads the listed rows of one block of one head at a time.
@@ -314,22 +404,20 @@ __global__ __launch_bounds__(kTPB) void k_kv8_load(Kv8Segs S, Kv8Slice c, Kv8Row
   __shared__ __attribute__((aligned(16))) unsigned char sv[kKv8Block * HD];
   constexpr int NP = HD / 8;  // pieces of eight dims
   const int tid = threadIdx.x;
-  auto body = [&](int h, int block, int first) {
-    const unsigned char* kt = c.tiles + ((int64_t)h * c.nblk + block) * 2 * kKv8Block * HD;
+  auto body = [&](int h, const Run& run) {
+    const unsigned char* kt = c.tiles + ((int64_t)h * c.nblk + run.block) * 2 * kKv8Block * HD;
     const unsigned char* vt = kt + kKv8Block * HD;
-    const unsigned char* sc = c.scales + ((int64_t)h * c.nblk + block) * 2;
+    const unsigned char* sc = c.scales + ((int64_t)h * c.nblk + run.block) * 2;
     __syncthreads();  // the block before is done with LDS
     for (int i = tid; i < kKv8Block * HD / 16; i += kTPB)
       reinterpret_cast<uint4*>(sv)[i] = reinterpret_cast<const uint4*>(vt)[i];
     const float ks = __uint_as_float((uint32_t)sc[0] << 23), vs = __uint_as_float((uint32_t)sc[1] << 23);
     __syncthreads();
-    const int end = rows.idx == nullptr ? min(rows.n, S.tok[segment_of(S, first) + 1]) : rows.n;
     for (int i = tid;; i += kTPB) {
-      const int64_t j = (int64_t)first + i / NP;
+      const int64_t j = (int64_t)run.first + i / NP;
       const int p = i % NP;
-      if (j >= end) break;
-      int at = (int)(j - first);
-      if (rows.idx == nullptr ? at >= kKv8Block : block_of(S, rows.idx[j], &at) != block) break;
+      int at = i / NP;
+      if (run.count >= 0 ? at >= run.count : block_of(S, j < rows.n ? rows.idx[j] : -1, &at) != run.block) break;
       float x[8];
       const int off = p < 8 ? key_off(at, p >> 1) + 8 * (p & 1) : key_off(at, 4);
       const uint2 b = *reinterpret_cast<const uint2*>(kt + off);
@@ -342,7 +430,7 @@ __global__ __launch_bounds__(kTPB) void k_kv8_load(Kv8Segs S, Kv8Slice c, Kv8Row
       store_row<8>(v + j * rows.ld + h * HD + p * 8, x);
     }
   };
-  for_each_unit(S, rows, c.kv_heads, group, units, body);
+  for_each_unit(S, rows, c.kv_heads, group, units, 1, 0, body);
 }
 
 template <typename F>
@@ -354,25 +442,25 @@ hipError_t by_type(sphinx_dtype dt, int head_dim, const F& go) {
   return hipGetLastError();
 }
 
-// Rows that a workgroup looks at: one workgroup per row and head where that makes
-// no more than about 8192 (four rounds of a full chip); with many rows several of
-// them share a block anyway.
+// Rows that a worker looks at (a wave when storing, a workgroup when reading
+// back): as many as leave `workers` of them, at most 16.  Listed rows mostly come
+// in runs, and a worker without a run's first row has nothing to do.
 struct Split {
   int group, units;
   unsigned grid;
 };
-Split split(const Kv8Slice& c, const Kv8Rows& rows) {
+Split split(int parts, int64_t nblk, const Kv8Rows& rows, int workers, int per) {  // parts: tiles or heads of a block
   Split p;
-  p.group = (int)std::clamp<int64_t>((int64_t)rows.n * c.kv_heads / 8192, 1, 16);
-  p.units = rows.idx ? (int)(((int64_t)rows.n + p.group - 1) / p.group) : (int)c.nblk;
-  p.grid = (unsigned)std::min<int64_t>((int64_t)p.units * c.kv_heads, 1 << 20);  // each then takes several
+  p.group = (int)std::clamp<int64_t>((int64_t)rows.n * parts / workers, 1, 16);
+  p.units = rows.idx ? (int)(((int64_t)rows.n + p.group - 1) / p.group) : (int)nblk;
+  p.grid = (unsigned)std::min<int64_t>(((int64_t)p.units * parts + per - 1) / per, 1 << 20);  // each then takes several
   return p;
 }
 }  // namespace
 
 hipError_t launch_kv8_store(sphinx_dtype dt, int head_dim, const Kv8Segs& S, const Kv8Slice& c, const Kv8Rows& rows,
                             const void* k, const void* v, hipStream_t s) {
-  const Split p = split(c, rows);
+  const Split p = split(2 * c.kv_heads, c.nblk, rows, 16384, 4);
   return by_type(dt, head_dim, [&](auto t, auto hd) {
     using T = decltype(t);
     k_kv8_store<T, decltype(hd)::value><<<p.grid, kTPB, 0, s>>>(S, c, rows, static_cast<const T*>(k),
@@ -382,7 +470,7 @@ hipError_t launch_kv8_store(sphinx_dtype dt, int head_dim, const Kv8Segs& S, con
 
 hipError_t launch_kv8_load(sphinx_dtype dt, int head_dim, const Kv8Segs& S, const Kv8Slice& c, const Kv8Rows& rows,
                            void* k, void* v, hipStream_t s) {
-  const Split p = split(c, rows);
+  const Split p = split(c.kv_heads, c.nblk, rows, 2048, 1);
   return by_type(dt, head_dim, [&](auto t, auto hd) {
     using T = decltype(t);
     k_kv8_load<T, decltype(hd)::value>

@@ -10,62 +10,103 @@
 
 namespace sphinx {
 
-// The keys of a segment are cut into chunks of `chunk` blocks; a workgroup takes
-// one chunk of one row tile and key/value head.  Segments of more than one chunk
-// leave partial results, which a second kernel joins.
+// The keys of segment i are cut into chunks[i] chunks of size[i] blocks (the last
+// may hold fewer); a workgroup takes one chunk of one row tile and key/value
+// head.  Segments of more than one chunk leave partial results, which a second
+// kernel joins.
 struct Kv8Plan {
   int tile;                                  // rows per workgroup, 32 or 128
-  int chunk;                                 // blocks per chunk
-  int chunks[SPHINX_MAX_REQUESTS];           // of a segment, at least 1
+  int chunks[SPHINX_MAX_REQUESTS];           // at least 1
+  int size[SPHINX_MAX_REQUESTS];             // blocks, at least 1
   int item[SPHINX_MAX_REQUESTS + 1];         // work items of the segments before (one head)
   int row[SPHINX_MAX_REQUESTS + 1];          // rows to join of the segments before (one head)
   int64_t part[SPHINX_MAX_REQUESTS + 1];     // partial rows of the segments before (all heads)
 };
 
-// Workgroups that a call is cut into where its keys allow, and the blocks that a
-// chunk holds at least.  32-row tiles: four workgroups per CU, a block for each of
-// their waves.  128-row tiles: as many workgroups as run at once, three per CU (two
-// at head_dim 72), and eight blocks for the work around a chunk.
-constexpr int kKv8ItemsRows = 1024, kKv8MinChunkRows = 4;
-constexpr int kKv8ItemsTiles = 768, kKv8ItemsTiles72 = 512, kKv8MinChunkTiles = 8;
+constexpr int kKv8Cus = 256;
+// 32-row tiles: as many workgroups as run at once (three per CU, two in the kernels
+// with more registers), with a block for each of their waves at least.
+constexpr int kKv8ItemsRows = 3 * kKv8Cus, kKv8ItemsRows2 = 2 * kKv8Cus, kKv8MinChunkRows = 4;
+// 128-row tiles: cut into this many workgroups at most, of eight blocks at least.
+constexpr int kKv8ItemsTiles = 6 * kKv8Cus, kKv8MinChunkTiles = 8;
 
 inline int kv8_tiles(int64_t rows, int tile) { return (int)((rows + tile - 1) / tile); }
 inline int kv8_blocks(int tokens) { return (int)(((int64_t)tokens + 63) / 64); }
 
-// rows[i]: queries times group of segment i; klen[i]: its tokens that count.
-inline Kv8Plan plan_kv8(bool bf16, int kv_heads, int head_dim, int nseg, const int64_t* rows, const int* klen) {
-  Kv8Plan p = {};
-  int64_t small = 0, tall = 0;  // blocks times tiles of 32 and of 128 rows
+// Cuts every segment into chunks of at most `most` blocks.
+inline void cut_kv8(Kv8Plan& p, int kv_heads, int nseg, const int64_t* rows, const int* klen, int64_t most) {
   for (int i = 0; i < nseg; ++i) {
-    small += (int64_t)kv8_tiles(rows[i], 32) * kv8_blocks(klen[i]);
-    tall += (int64_t)kv8_tiles(rows[i], 128) * kv8_blocks(klen[i]);
-  }
-  // a 128-row tile takes about 2.4 times a 32-row tile's time
-  p.tile = bf16 && 5 * small > 12 * tall ? 128 : 32;
-  const int64_t work = (p.tile == 128 ? tall : small) * kv_heads;
-  const int items = p.tile == 32 ? kKv8ItemsRows : head_dim == 64 ? kKv8ItemsTiles : kKv8ItemsTiles72;
-  const int least = p.tile == 32 ? kKv8MinChunkRows : kKv8MinChunkTiles;
-  // no segment has 2^26 blocks
-  p.chunk = (int)std::clamp<int64_t>((work + items - 1) / items, least, 1 << 26);
-  for (int i = 0; i < nseg; ++i) {
-    p.chunks[i] = std::max(1, (kv8_blocks(klen[i]) + p.chunk - 1) / p.chunk);
+    const int nb = std::max(1, kv8_blocks(klen[i]));
+    p.chunks[i] = (int)((nb + most - 1) / most);
+    p.size[i] = (nb + p.chunks[i] - 1) / p.chunks[i];
+    p.chunks[i] = (nb + p.size[i] - 1) / p.size[i];  // no empty chunk
     const bool split = p.chunks[i] > 1;
     p.item[i + 1] = p.item[i] + kv8_tiles(rows[i], p.tile) * p.chunks[i];
     p.row[i + 1] = p.row[i] + (split ? (int)rows[i] : 0);
     p.part[i + 1] = p.part[i] + (split ? rows[i] * kv_heads * p.chunks[i] : 0);
   }
-  return p;
+}
+
+// rows[i]: queries times group of segment i; klen[i]: its tokens that count.
+inline Kv8Plan plan_kv8(bool bf16, int kv_heads, int head_dim, int nseg, const int64_t* rows, const int* klen) {
+  Kv8Plan p = {};
+  int64_t small = 0, tall = 0;  // blocks times tiles of 32 and of 128 rows
+  int longest = 1;
+  for (int i = 0; i < nseg; ++i) {
+    small += (int64_t)kv8_tiles(rows[i], 32) * kv8_blocks(klen[i]);
+    tall += (int64_t)kv8_tiles(rows[i], 128) * kv8_blocks(klen[i]);
+    longest = std::max(longest, kv8_blocks(klen[i]));
+  }
+  // a 128-row tile takes about 2.4 times a 32-row tile's time
+  p.tile = bf16 && 5 * small > 12 * tall ? 128 : 32;
+  if (p.tile == 32) {
+    // chunks of equal work for all workgroups that run at once
+    const int items = bf16 && head_dim == 64 ? kKv8ItemsRows : kKv8ItemsRows2;
+    cut_kv8(p, kv_heads, nseg, rows, klen, std::max<int64_t>((small * kv_heads + items - 1) / items, kKv8MinChunkRows));
+    return p;
+  }
+  // The number of chunks of the longest segment with the least estimated time, in
+  // blocks of one workgroup: a CU gets through its workgroups' blocks one after
+  // the other, those of equal chunks come in whole numbers per CU, and the last
+  // one alone does not fill it (16 heads against 504 blocks: 324, 550, 760, 988 us
+  // for 1, 2, 3, 4 workgroups per CU); three blocks' time goes by around a chunk.
+  // Joining moves each partial row twice, at about 4 TB/s, after a launch of 3 us.
+  const double block_us = head_dim == 64 ? 0.47 : 0.63;
+  Kv8Plan best = p;
+  double least = 0.0;
+  for (int k = 1; k <= longest; k += k < 16 ? 1 : k / 8) {
+    const int most = std::max(kKv8MinChunkTiles, (longest + k - 1) / k);
+    Kv8Plan q = p;
+    cut_kv8(q, kv_heads, nseg, rows, klen, most);
+    double total = 0.0;
+    int64_t cut = 0;
+    for (int i = 0; i < nseg; ++i) {
+      const int64_t n = (int64_t)(q.item[i + 1] - q.item[i]) * kv_heads;
+      total += (double)n * (q.size[i] + 3);
+      if (q.chunks[i] > 1) cut += n;
+    }
+    if (cut > kKv8ItemsTiles) break;
+    const int64_t rounds = (int64_t)(total / ((double)kKv8Cus * (most + 3)) + 0.999);
+    const double join = q.part[nseg] == 0 ? 0.0 : 3.0 + (double)q.part[nseg] * (head_dim * 4 + 8) * 2.0 / 4e6;
+    const double us = ((double)rounds + 0.36) * (most + 3) * block_us + join;
+    if (k == 1 || us < least) {
+      least = us;
+      best = q;
+    }
+    if (most == kKv8MinChunkTiles) break;
+  }
+  return best;
 }
 
 // Partial rows that no plan for these segments passes, with any klen up to the
-// given one.  A chunk holds four blocks at least; and only segments of more than
-// `chunk` blocks are cut, into fewer than 2 blocks / chunk pieces, so that at
-// most twice the items above leave partial rows, one tile each.
+// given one.  A chunk of several holds more than half of four blocks; 32-row
+// tiles: a segment is cut into pieces of more than half of work / items blocks,
+// so at most twice the items leave partial rows; each item leaves one tile's.
 inline int64_t kv8_most_parts(int kv_heads, int nseg, const int64_t* rows, const int* klen) {
   int64_t by_chunk = 0, by_item = 0;
   for (int i = 0; i < nseg; ++i) {
     by_item = std::max(by_item, std::max(2 * kKv8ItemsRows * std::min<int64_t>(rows[i], 32),
-                                         2 * kKv8ItemsTiles * std::min<int64_t>(rows[i], 128)));
+                                         kKv8ItemsTiles * std::min<int64_t>(rows[i], 128)));
     const int64_t chunks = (kv8_blocks(klen[i]) + kKv8MinChunkRows - 1) / kKv8MinChunkRows;
     if (chunks > 1) by_chunk += rows[i] * kv_heads * chunks;
   }

@@ -99,7 +99,7 @@ def test_bytes_and_their_refusals(L):
     assert f(1, 64, _cu(0, 64), 0) == INVALID
     assert f(1, 64, _cu(*range(66)), 65) == UNSUPPORTED
     assert f(2048, 64, _cu(0, 64), 1) == UNSUPPORTED
-    assert f(64, 64, _cu(0, (1 << 31) - 1), 1) == UNSUPPORTED  # 2^31 blocks of all heads
+    assert f(32, 64, _cu(0, (1 << 31) - 1), 1) == UNSUPPORTED  # 2^31 tiles
     assert L.sphinx_kv8_bytes(1, 64, _cu(0, 64), 1, None) == INVALID
     # long caches: sizes past 32 bits
     assert f(16, 64, _cu(0, 1 << 30), 1) == OK and out.value == (1 << 30) * 2048 + (1 << 24) * 16 * 2
@@ -118,7 +118,7 @@ def test_store_and_load_refusals(L, load):
     assert call(d=80, ld=80) == UNSUPPORTED
     assert call(ld=56) == INVALID and call(ld=68) == INVALID and call(hk=2) == INVALID
     assert call(n=-1) == INVALID
-    assert call(hk=2, ld=128, n=1 << 30) == UNSUPPORTED  # 2^31 rows of all heads
+    assert call(hk=2, ld=128, n=1 << 29) == UNSUPPORTED  # 2^31 rows of all tiles
     assert call(idx=None, n=9) == INVALID  # more rows than tokens
     for kw in (dict(k=None), dict(v=None), dict(c=None), dict(k=264), dict(v=8), dict(c=260), dict(idx=4)):
         assert call(**kw) == INVALID, kw

@@ -15,11 +15,11 @@ ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 SOURCE = r"""
 #include <string.h>
 #include "kv8_rules.hpp"
-extern "C" void plan(int bf16, int heads, int head_dim, int nseg, const int64_t* rows, const int* klen, int* chunk,
-                     int* chunks, int* item, int* row, int64_t* part) {
+extern "C" void plan(int bf16, int heads, int head_dim, int nseg, const int64_t* rows, const int* klen, int* tile,
+                     int* size, int* chunks, int* item, int* row, int64_t* part) {
   const sphinx::Kv8Plan p = sphinx::plan_kv8(bf16 != 0, heads, head_dim, nseg, rows, klen);
-  chunk[0] = p.chunk;
-  chunk[1] = p.tile;
+  memcpy(size, p.size, 4 * nseg);
+  *tile = p.tile;
   memcpy(chunks, p.chunks, 4 * nseg);
   memcpy(item, p.item, 4 * (nseg + 1));
   memcpy(row, p.row, 4 * (nseg + 1));
@@ -52,10 +52,10 @@ def ptr(a):
 def plan(heads, rows, klen, bf16=True, head_dim=64):
     n = len(rows)
     rows, klen = np.ascontiguousarray(rows, np.int64), np.ascontiguousarray(klen, np.int32)
-    chunk = np.zeros(2, np.int32)
-    out = [np.zeros(n, np.int32), np.zeros(n + 1, np.int32), np.zeros(n + 1, np.int32), np.zeros(n + 1, np.int64)]
-    lib().plan(int(bf16), heads, head_dim, n, ptr(rows), ptr(klen), ptr(chunk), *(ptr(a) for a in out))
-    return (int(chunk[0]), int(chunk[1]), *out)
+    tile = np.zeros(1, np.int32)
+    out = [np.zeros(n, np.int32), np.zeros(n, np.int32), np.zeros(n + 1, np.int32), np.zeros(n + 1, np.int32), np.zeros(n + 1, np.int64)]
+    lib().plan(int(bf16), heads, head_dim, n, ptr(rows), ptr(klen), ptr(tile), *(ptr(a) for a in out))
+    return (int(tile[0]), *out)  # tile, size, chunks, item, row, part
 
 
 def most(heads, rows, klen):
@@ -73,31 +73,31 @@ def test_plan_covers_every_key_once_and_fits_its_workspace(seed, bf16, head_dim)
     cap = np.exp(rng.uniform(0, np.log(rng.choice([100, 30000, 4000000])), n)).astype(np.int64)
     bound = most(heads, rows, cap)
     for klen in (cap, (cap * rng.random(n)).astype(np.int64), cap * (rng.random(n) < 0.2)):
-        chunk, tile, chunks, item, row, part = plan(heads, rows, klen, bf16, head_dim)
+        tile, size, chunks, item, row, part = plan(heads, rows, klen, bf16, head_dim)
         blocks = (klen + 63) // 64
-        assert chunk >= 4 and (chunks >= 1).all() and tile in ((32, 128) if bf16 else (32,))
+        assert (size >= 1).all() and (chunks >= 1).all() and tile in ((32, 128) if bf16 else (32,))
         # the last chunk of a segment holds a block, and the chunks together hold all of them
-        assert (chunks * chunk >= blocks).all() and (((chunks - 1) * chunk < blocks) | (chunks == 1)).all()
+        assert (chunks * size >= blocks).all() and (((chunks - 1) * size < blocks) | (chunks == 1)).all()
         split = chunks > 1
         assert np.array_equal(np.diff(row), np.where(split, rows, 0)) and row[0] == 0
         assert np.array_equal(np.diff(part), np.where(split, rows * heads * chunks, 0)) and part[0] == 0
         assert np.array_equal(np.diff(item), (rows + tile - 1) // tile * chunks) and item[0] == 0
         assert part[-1] <= bound
         # a call is not cut finer than its purpose asks
-        assert (np.diff(item) * heads)[split].sum() <= 2048
+        assert (np.diff(item) * heads)[split].sum() <= 1536
 
 
 def test_rows_choose_the_tile():
-    assert plan(4, [1], [9000])[1] == 32 and plan(4, [64], [9000])[1] == 32
-    assert plan(4, [65], [9000])[1] == 128 and plan(4, [5000], [9000])[1] == 128
-    assert plan(4, [5000], [9000], bf16=False)[1] == 32
-    assert plan(4, [1] * 40 + [100], [9000] * 41)[1] == 32  # mostly single queries
-    assert plan(4, [1] + [3000], [64, 9000])[1] == 128
+    assert plan(4, [1], [9000])[0] == 32 and plan(4, [64], [9000])[0] == 32
+    assert plan(4, [65], [9000])[0] == 128 and plan(4, [5000], [9000])[0] == 128
+    assert plan(4, [5000], [9000], bf16=False)[0] == 32
+    assert plan(4, [1] * 40 + [100], [9000] * 41)[0] == 32  # mostly single queries
+    assert plan(4, [1] + [3000], [64, 9000])[0] == 128
 
 
 def test_largest_calls_stay_in_range():
     rows = [(1 << 31) - 1]
-    chunk, tile, chunks, item, row, part = plan(1, rows, [(1 << 31) - 1])
-    assert chunks[0] == 1 and item[1] == 1 << 24 and part[1] == 0
-    chunk, tile, chunks, item, row, part = plan(1, [1], [(1 << 31) - 1])
-    assert chunks[0] * chunk >= 1 << 25 and part[1] == chunks[0] <= most(1, [1], [(1 << 31) - 1])
+    tile, size, chunks, item, row, part = plan(1, rows, [(1 << 31) - 1])
+    assert chunks[0] == 1 and size[0] == 1 << 25 and item[1] == 1 << 24 and part[1] == 0
+    tile, size, chunks, item, row, part = plan(1, [1], [(1 << 31) - 1])
+    assert chunks[0] * int(size[0]) >= 1 << 25 and part[1] == chunks[0] <= most(1, [1], [(1 << 31) - 1])
