@@ -397,12 +397,17 @@ __global__ __launch_bounds__(kTPB, sizeof(T) == 2 ? 3 : 2) void k_kv8_store(Kv8S
   for_each_unit(S, rows, 2 * c.kv_heads, group, units, 4, wave, body);
 }
 
-// One workgroup reads the listed rows of one block of one head at a time.
+// One workgroup reads the listed rows of one block of one head at a time: the
+// value tile comes into LDS in consecutive 16-byte pieces, a thread takes eight
+// dims of a row.  Bound by bytes.  (A wave per tile, as in the store, was no
+// faster: all of 32256 tokens of 16 heads 45 us against 42, 1905 rows 22 us
+// against 17.)
 template <typename T, int HD>
 __global__ __launch_bounds__(kTPB) void k_kv8_load(Kv8Segs S, Kv8Slice c, Kv8Rows rows, T* __restrict__ k,
                                                    T* __restrict__ v, int group, int units) {
   __shared__ __attribute__((aligned(16))) unsigned char sv[kKv8Block * HD];
-  constexpr int NP = HD / 8;  // pieces of eight dims
+  __shared__ int listed[kWave];  // listed tokens: rows of the block of the run's first rows, -1 behind them
+  constexpr int NP = HD / 8;     // pieces of eight dims
   const int tid = threadIdx.x;
   auto body = [&](int h, const Run& run) {
     const unsigned char* kt = c.tiles + ((int64_t)h * c.nblk + run.block) * 2 * kKv8Block * HD;
@@ -412,12 +417,22 @@ __global__ __launch_bounds__(kTPB) void k_kv8_load(Kv8Segs S, Kv8Slice c, Kv8Row
     for (int i = tid; i < kKv8Block * HD / 16; i += kTPB)
       reinterpret_cast<uint4*>(sv)[i] = reinterpret_cast<const uint4*>(vt)[i];
     const float ks = __uint_as_float((uint32_t)sc[0] << 23), vs = __uint_as_float((uint32_t)sc[1] << 23);
+    const int known = run.count >= 0 ? 0 : kWave - (run.first - run.from);  // rows of the run that lanes look at
+    if (run.count < 0 && tid < kWave && tid >= kWave - known)
+      listed[tid - (kWave - known)] = run.lane_block == run.block ? run.at : -1;
     __syncthreads();
     for (int i = tid;; i += kTPB) {
-      const int64_t j = (int64_t)run.first + i / NP;
-      const int p = i % NP;
-      int at = i / NP;
-      if (run.count >= 0 ? at >= run.count : block_of(S, j < rows.n ? rows.idx[j] : -1, &at) != run.block) break;
+      const int r = i / NP, p = i % NP;
+      const int64_t j = (int64_t)run.first + r;
+      int at = r;
+      if (run.count >= 0) {
+        if (r >= run.count) break;
+      } else if (r < known) {
+        at = listed[r];
+        if (at < 0) break;
+      } else if (block_of(S, j < rows.n ? rows.idx[j] : -1, &at) != run.block) {
+        break;
+      }
       float x[8];
       const int off = p < 8 ? key_off(at, p >> 1) + 8 * (p & 1) : key_off(at, 4);
       const uint2 b = *reinterpret_cast<const uint2*>(kt + off);
