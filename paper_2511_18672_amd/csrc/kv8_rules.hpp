@@ -24,9 +24,9 @@ struct Kv8Plan {
 };
 
 constexpr int kKv8Cus = 256;
-// 32-row tiles: as many workgroups as run at once (three per CU, two in the kernels
-// with more registers), with a block for each of their waves at least.
-constexpr int kKv8ItemsRows = 3 * kKv8Cus, kKv8ItemsRows2 = 2 * kKv8Cus, kKv8MinChunkRows = 4;
+// 32-row tiles: as many workgroups as run at once (three per CU at bf16 and
+// head_dim 64, two else), with a block for each of their waves at least.
+constexpr int kKv8ItemsRows = 3 * kKv8Cus, kKv8MinChunkRows = 4;
 // 128-row tiles: cut into this many workgroups at most, of eight blocks at least.
 constexpr int kKv8ItemsTiles = 6 * kKv8Cus, kKv8MinChunkTiles = 8;
 
@@ -60,9 +60,17 @@ inline Kv8Plan plan_kv8(bool bf16, int kv_heads, int head_dim, int nseg, const i
   // a 128-row tile takes about 2.4 times a 32-row tile's time
   p.tile = bf16 && 5 * small > 12 * tall ? 128 : 32;
   if (p.tile == 32) {
-    // chunks of equal work for all workgroups that run at once
-    const int items = bf16 && head_dim == 64 ? kKv8ItemsRows : kKv8ItemsRows2;
-    cut_kv8(p, kv_heads, nseg, rows, klen, std::max<int64_t>((small * kv_heads + items - 1) / items, kKv8MinChunkRows));
+    // Chunks of equal work for all workgroups that run at once, counting that cutting
+    // leaves half a chunk per tile on average.  fp32 is bound by the matrix cores,
+    // which one workgroup keeps nearly as busy as two: tiles that fill the chip
+    // are not cut for a second (1024 queries against 2048 keys of 8 heads, 256
+    // tiles: 50 us in two chunks, KF32 us whole).
+    int64_t units = 0;
+    for (int i = 0; i < nseg; ++i) units += (int64_t)kv8_tiles(rows[i], 32) * kv_heads;
+    const int64_t slots = bf16 && head_dim == 64 ? kKv8ItemsRows : !bf16 && units >= kKv8Cus ? kKv8Cus : 2 * kKv8Cus;
+    const int64_t pieces = bf16 ? std::max(slots - units / 2, slots / 2) : slots;
+    cut_kv8(p, kv_heads, nseg, rows, klen,
+            std::max<int64_t>((small * kv_heads + pieces - 1) / pieces, kKv8MinChunkRows));
     return p;
   }
   // The number of chunks of the longest segment with the least estimated time, in
