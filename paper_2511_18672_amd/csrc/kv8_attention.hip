@@ -144,39 +144,39 @@ __global__ __launch_bounds__(kTPB, sizeof(T) == 2 && HD == 64 ? 3 : 2) void k_kv
     ks = ksn;
     vs = vsn;
     if (b + 4 < nb) fetch(b + 4);
-    f32x16 sc[2];
+    // The products of the two key blocks alternate, so that none waits for the one before.
+    f32x16 sc[2] = {f32x16{}, f32x16{}};
 #pragma unroll
-    for (int rb = 0; rb < 2; ++rb) {
-      sc[rb] = f32x16{};
+    for (int hf = 0; hf < 2; ++hf) {
+      if constexpr (F32) {
+        float k0[16], k1[16];
+        operand(kc[0][hf], ks, k0);
+        operand(kc[1][hf], ks, k1);
 #pragma unroll
-      for (int hf = 0; hf < 2; ++hf) {
-        if constexpr (F32) {
-          float kf[16];
-          operand(kc[rb][hf], ks, kf);
+        for (int i = 0; i < 16; ++i) {
+          sc[0] = __builtin_amdgcn_mfma_f32_32x32x2f32(k0[i], qf[16 * hf + i], sc[0], 0, 0, 0);
+          sc[1] = __builtin_amdgcn_mfma_f32_32x32x2f32(k1[i], qf[16 * hf + i], sc[1], 0, 0, 0);
+        }
+      } else {
+        bf16x8 k0[2], k1[2];
+        operand(kc[0][hf], ks, k0);
+        operand(kc[1][hf], ks, k1);
 #pragma unroll
-          for (int i = 0; i < 16; ++i)
-            sc[rb] = __builtin_amdgcn_mfma_f32_32x32x2f32(kf[i], qf[16 * hf + i], sc[rb], 0, 0, 0);
-        } else {
-          bf16x8 kf[2];
-          operand(kc[rb][hf], ks, kf);
+        for (int e = 0; e < 2; ++e) {
+          bf16x8 qv;
 #pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            bf16x8 qv;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) qv[i] = qf[16 * hf + 8 * e + i];
-            sc[rb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[e], qv, sc[rb], 0, 0, 0);
-          }
+          for (int i = 0; i < 8; ++i) qv[i] = qf[16 * hf + 8 * e + i];
+          sc[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k0[e], qv, sc[0], 0, 0, 0);
+          sc[1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k1[e], qv, sc[1], 0, 0, 0);
         }
       }
-      if constexpr (HD == 72) {
-        const uint32_t w = kt8[rb];
-        bf16x4 kv;
-        const bf16x2 lo = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, ks, false);
-        const bf16x2 hi = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, ks, true);
-        kv[0] = lo[0];
-        kv[1] = lo[1];
-        kv[2] = hi[0];
-        kv[3] = hi[1];
+    }
+    if constexpr (HD == 72) {
+#pragma unroll
+      for (int rb = 0; rb < 2; ++rb) {
+        const bf16x2 lo = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(kt8[rb], ks, false);
+        const bf16x2 hi = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(kt8[rb], ks, true);
+        const bf16x4 kv = {lo[0], lo[1], hi[0], hi[1]};
         sc[rb] = __builtin_amdgcn_mfma_f32_32x32x8bf16_1k(__builtin_bit_cast(s16x4, kv), q4, sc[rb], 0, 0, 0);
       }
     }
@@ -220,20 +220,23 @@ __global__ __launch_bounds__(kTPB, sizeof(T) == 2 && HD == 64 ? 3 : 2) void k_kv
           sc[kb][r] = fast_exp2(sc[kb][r] - at);
           ps += sc[kb][r];
         }
-#pragma unroll
-        for (int db = 0; db < DB; ++db) {
-          float vf[16];
-          operand(vc[db][kb], vs, vf);
-#pragma unroll
-          for (int r = 0; r < 16; ++r)
-            oacc[db] = __builtin_amdgcn_mfma_f32_32x32x2f32(vf[r], sc[kb][r], oacc[db], 0, 0, 0);
-        }
-      } else {
-        bf16x8 pf[2];
+        float v0[16], v1[16];
+        operand(vc[0][kb], vs, v0);
+        operand(vc[1][kb], vs, v1);
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
-          pf[r >> 3][r & 7] = (bf16)fast_exp2(sc[kb][r] - at);
-          ps += (float)pf[r >> 3][r & 7];
+          oacc[0] = __builtin_amdgcn_mfma_f32_32x32x2f32(v0[r], sc[kb][r], oacc[0], 0, 0, 0);
+          oacc[1] = __builtin_amdgcn_mfma_f32_32x32x2f32(v1[r], sc[kb][r], oacc[1], 0, 0, 0);
+        }
+      } else {
+        const bf16x2 ones = {(bf16)1.0f, (bf16)1.0f};
+        bf16x8 pf[2];
+#pragma unroll
+        for (int r = 0; r < 16; r += 2) {
+          const bf16x2 pr = {(bf16)fast_exp2(sc[kb][r] - at), (bf16)fast_exp2(sc[kb][r + 1] - at)};
+          ps = __builtin_amdgcn_fdot2_f32_bf16(pr, ones, ps, false);
+          pf[r >> 3][r & 7] = pr[0];
+          pf[r >> 3][(r & 7) + 1] = pr[1];
         }
 #pragma unroll
         for (int db = 0; db < DB; ++db) {
