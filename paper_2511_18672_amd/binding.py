@@ -376,7 +376,7 @@ def _here(stream, *tensors) -> Optional[int]:
 
     dev = torch.cuda.current_device()
     for t in tensors:
-        if t is not None and not isinstance(t, int) and t.get_device() != dev:
+        if t is not None and t.get_device() != dev:
             raise ValueError(f"tensor on {t.device}, the current device is cuda:{dev}")
     if stream is None:
         return torch.cuda.current_stream(dev).cuda_stream

@@ -683,6 +683,17 @@ sphinx_status kv8_attention_check(sphinx_dtype dtype, int32_t heads, int32_t kv_
   if ((int64_t)cu_q[nseg] * heads >= ((int64_t)1 << 31)) return SPHINX_E_UNSUPPORTED;
   return SPHINX_OK;
 }
+
+// Workspace bytes of a checked call, whatever part of the tokens counts.
+size_t kv8_attention_need(int32_t heads, int32_t kv_heads, int32_t head_dim, const int32_t* cu_q,
+                          const int32_t* cu_kv, int32_t nseg) {
+  int nq[SPHINX_MAX_REQUESTS], klen[SPHINX_MAX_REQUESTS];
+  for (int i = 0; i < nseg; ++i) {
+    nq[i] = cu_q[i + 1] - cu_q[i];
+    klen[i] = cu_kv[i + 1] - cu_kv[i];
+  }
+  return kv8_attention_ws_bytes(kv_heads, head_dim, heads / kv_heads, nseg, nq, klen);
+}
 }  // namespace
 
 sphinx_status sphinx_kv8_attention_workspace_bytes(sphinx_dtype dtype, int32_t heads, int32_t kv_heads,
@@ -691,12 +702,7 @@ sphinx_status sphinx_kv8_attention_workspace_bytes(sphinx_dtype dtype, int32_t h
   const sphinx_status st = kv8_attention_check(dtype, heads, kv_heads, head_dim, cu_q, cu_kv, nseg);
   if (st != SPHINX_OK) return st;
   if (bytes == nullptr) return SPHINX_E_INVALID;
-  int nq[SPHINX_MAX_REQUESTS], klen[SPHINX_MAX_REQUESTS];
-  for (int i = 0; i < nseg; ++i) {
-    nq[i] = cu_q[i + 1] - cu_q[i];
-    klen[i] = cu_kv[i + 1] - cu_kv[i];
-  }
-  *bytes = kv8_attention_ws_bytes(kv_heads, head_dim, heads / kv_heads, nseg, nq, klen);
+  *bytes = kv8_attention_need(heads, kv_heads, head_dim, cu_q, cu_kv, nseg);
   return SPHINX_OK;
 }
 
@@ -713,9 +719,7 @@ sphinx_status sphinx_kv8_attention(sphinx_dtype dtype, int32_t heads, int32_t kv
   if (cu_q[nseg] == 0) return SPHINX_OK;
   if (!q || !o || !slice || !ws || !aligned(q, 16) || !aligned(o, 16) || !aligned(slice, 16) || !aligned(ws, 256))
     return SPHINX_E_INVALID;
-  size_t need;
-  st = sphinx_kv8_attention_workspace_bytes(dtype, heads, kv_heads, head_dim, cu_q, cu_kv, nseg, &need);
-  if (st != SPHINX_OK) return st;
+  const size_t need = kv8_attention_need(heads, kv_heads, head_dim, cu_q, cu_kv, nseg);
   const Kv8Segs S = kv8_segs(cu_kv, nseg);
   if (ws_bytes < need || slice_bytes < kv8_slice_bytes(kv_heads, head_dim, S.blk[nseg])) return SPHINX_E_WORKSPACE;
   Kv8Attn A;

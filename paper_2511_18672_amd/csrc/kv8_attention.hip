@@ -36,10 +36,11 @@ struct Parts {
   float* o;  // [number][head_dim]
 };
 
-__device__ __forceinline__ float byte_scale(int b) { return __uint_as_float((uint32_t)b << 23); }
+// A cleared block has byte 0 and holds zeros, at any scale.
+__device__ __forceinline__ float byte_scale(int b) { return __uint_as_float((uint32_t)max(b, 1) << 23); }
 
-// Sixteen stored bytes as operands: two bf16 fragments of eight, or 16 floats.
-// The scale is a power of two, so both forms hold the values exactly.
+// Sixteen stored bytes as operands: two bf16 fragments of eight, which hold the
+// scaled values exactly (the scale is a power of two), or 16 floats.
 __device__ __forceinline__ void operand(const uint4& b, float scale, bf16x8 (&f)[2]) {
   const uint32_t w[4] = {b.x, b.y, b.z, b.w};
 #pragma unroll
@@ -52,21 +53,21 @@ __device__ __forceinline__ void operand(const uint4& b, float scale, bf16x8 (&f)
     f[i >> 1][4 * (i & 1) + 3] = hi[1];
   }
 }
-__device__ __forceinline__ void operand(const uint4& b, float scale, float (&f)[16]) {
+__device__ __forceinline__ void operand(const uint4& b, float (&f)[16]) {  // without the scale
   const uint32_t w[4] = {b.x, b.y, b.z, b.w};
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)w[i], false);
     const f32x2 hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)w[i], true);
-    f[4 * i] = lo[0] * scale;
-    f[4 * i + 1] = lo[1] * scale;
-    f[4 * i + 2] = hi[0] * scale;
-    f[4 * i + 3] = hi[1] * scale;
+    f[4 * i] = lo[0];
+    f[4 * i + 1] = lo[1];
+    f[4 * i + 2] = hi[0];
+    f[4 * i + 3] = hi[1];
   }
 }
 
 // One workgroup = 32 rows of one segment and key/value head against one chunk of
-// the segment's keys; its four waves take the chunk's blocks in turn and merge
+// the segment's keys; its four or eight waves take the chunk's blocks in turn and merge
 // (m, l, O) through LDS.  A wave reads a block's bytes straight into the operand
 // layouts, the next block's while it works on this one's:
 //  * S^T = K Q^T in two 32-key tiles: lane l = 32 g + r has key r and dims
@@ -75,13 +76,16 @@ __device__ __forceinline__ void operand(const uint4& b, float scale, float (&f)[
 //    that byte 8 hf + j of the values' chunk (db, kb) holds;
 //  * O^T = V^T P^T leaves the row on the lane.
 // bf16: 32x32x16 products, P rounded to bf16 for the product, the row sum adding
-// the same rounded values; f32: 32x32x2 products, nothing rounded.
-template <typename T, int HD>
-__global__ __launch_bounds__(kTPB, sizeof(T) == 2 && HD == 64 ? 3 : 2) void k_kv8_attn_rows(Kv8Attn A, Kv8Slice c, Kv8Plan P, Parts part, int first) {
+// the same rounded values; f32: 32x32x2 products of the unscaled bytes, nothing
+// rounded (the keys' scale goes into the exponent, the values' into P: a
+// product per byte between its conversion and its matrix instruction kept the
+// two from overlapping).
+template <typename T, int HD, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, sizeof(T) == 2 && HD == 64 && WAVES == 4 ? 3 : 2) void k_kv8_attn_rows(Kv8Attn A, Kv8Slice c, Kv8Plan P, Parts part, int first) {
   constexpr bool F32 = sizeof(T) == 4;
   constexpr int DB = (HD + 31) / 32;
-  __shared__ float sO[4][kRows][DB * 32 + 1];
-  __shared__ float sM[4][kRows], sL[4][kRows];
+  __shared__ float sO[WAVES][kRows][DB * 32 + 1];
+  __shared__ float sM[WAVES][kRows], sL[WAVES][kRows];
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int g = lane >> 5, r32 = lane & 31;
@@ -129,7 +133,7 @@ __global__ __launch_bounds__(kTPB, sizeof(T) == 2 && HD == 64 ? 3 : 2) void k_kv
             vt + (db < 2 ? ((db * 2 + kb) * 64 + lane) * 16 : 4096 + ((kb * 2 + g) * 8 + (r32 & 7)) * 16));
   };
   if (b0 + wave < nb) fetch(b0 + wave);
-  for (int b = b0 + wave; b < nb; b += 4) {
+  for (int b = b0 + wave; b < nb; b += WAVES) {
     const int left = L - b * kKv8Block;  // keys from this block on
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
@@ -143,15 +147,15 @@ __global__ __launch_bounds__(kTPB, sizeof(T) == 2 && HD == 64 ? 3 : 2) void k_kv
       for (int j = 0; j < 2; ++j) vc[i][j] = vn[i][j];
     ks = ksn;
     vs = vsn;
-    if (b + 4 < nb) fetch(b + 4);
+    if (b + WAVES < nb) fetch(b + WAVES);
     // The products of the two key blocks alternate, so that none waits for the one before.
     f32x16 sc[2] = {f32x16{}, f32x16{}};
 #pragma unroll
     for (int hf = 0; hf < 2; ++hf) {
       if constexpr (F32) {
         float k0[16], k1[16];
-        operand(kc[0][hf], ks, k0);
-        operand(kc[1][hf], ks, k1);
+        operand(kc[0][hf], k0);
+        operand(kc[1][hf], k1);
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
           sc[0] = __builtin_amdgcn_mfma_f32_32x32x2f32(k0[i], qf[16 * hf + i], sc[0], 0, 0, 0);
@@ -198,10 +202,11 @@ __global__ __launch_bounds__(kTPB, sizeof(T) == 2 && HD == 64 ? 3 : 2) void k_kv
           }
         }
     }
+    const float kscale = F32 ? ks : 1.0f;  // f32: the scores are of unscaled keys so far
     float mx = -INFINITY;
 #pragma unroll
     for (int r = 0; r < 16; ++r) mx = fmaxf(mx, fmaxf(sc[0][r], sc[1][r]));
-    mx = fmaxf(mx, __shfl_xor(mx, 32, kWave));
+    mx = fmaxf(mx, __shfl_xor(mx, 32, kWave)) * kscale;
     // while every score is -inf the base is 0: such keys weigh nothing
     const float mn = fmaxf(m, mx), at = mn == -INFINITY ? 0.0f : mn;
     if (__ballot(mn > m) != 0) {
@@ -217,12 +222,13 @@ __global__ __launch_bounds__(kTPB, sizeof(T) == 2 && HD == 64 ? 3 : 2) void k_kv
       if constexpr (F32) {
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
-          sc[kb][r] = fast_exp2(sc[kb][r] - at);
+          sc[kb][r] = fast_exp2(fmaf(sc[kb][r], kscale, -at));
           ps += sc[kb][r];
+          sc[kb][r] *= vs;
         }
         float v0[16], v1[16];
-        operand(vc[0][kb], vs, v0);
-        operand(vc[1][kb], vs, v1);
+        operand(vc[0][kb], v0);
+        operand(vc[1][kb], v1);
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
           oacc[0] = __builtin_amdgcn_mfma_f32_32x32x2f32(v0[r], sc[kb][r], oacc[0], 0, 0, 0);
@@ -261,14 +267,16 @@ __global__ __launch_bounds__(kTPB, sizeof(T) == 2 && HD == 64 ? 3 : 2) void k_kv
     for (int r = 0; r < 16; ++r) sO[wave][r32][32 * db + 8 * (r >> 2) + 4 * g + (r & 3)] = oacc[db][r];
   __syncthreads();
   const int64_t part0 = P.part[s] + ((int64_t)h * nrows + row0) * chunks + chunk;
-  for (int i = tid; i < kRows * HD; i += kTPB) {
+  for (int i = tid; i < kRows * HD; i += 64 * WAVES) {
     const int row = i / HD, d = i - row * HD;
     if (row0 + row >= nrows) break;
-    const float mm = fmaxf(fmaxf(sM[0][row], sM[1][row]), fmaxf(sM[2][row], sM[3][row]));
+    float mm = sM[0][row];
+#pragma unroll
+    for (int w = 1; w < WAVES; ++w) mm = fmaxf(mm, sM[w][row]);
     const float at = mm == -INFINITY ? 0.0f : mm;
     float num = 0.0f, den = 0.0f;
 #pragma unroll
-    for (int w = 0; w < 4; ++w) {  // a wave without a block has m = -inf and weighs 0
+    for (int w = 0; w < WAVES; ++w) {  // a wave without a block has m = -inf and weighs 0
       const float f = fast_exp2(sM[w][row] - at);
       num = fmaf(sO[w][row][d], f, num);
       den = fmaf(sL[w][row], f, den);
@@ -310,7 +318,7 @@ template <int HD>
 struct TileGeo {
   static constexpr int DB = (HD + 31) / 32;   // 32-row blocks of O^T (head_dim 72: of the third, 8 rows count)
   static constexpr int NPV = 4 * DB, NQK = HD == 72 ? 10 : 8;
-  static constexpr int SLOT = 8192 + (HD == 72 ? 1024 : 0);  // one block's keys, or its values, as bf16
+  static constexpr int SLOT = 8192 + (HD == 72 ? 1088 : 0);  // one block's keys, or its values, as bf16
   static constexpr int TILE = kKv8Block * HD;                // the same as bytes
 };
 template <int HD>
@@ -433,7 +441,10 @@ __global__ __launch_bounds__(kTPB, HD == 64 ? 3 : 2) void k_kv8_attn_tiles(Kv8At
       *reinterpret_cast<bf16x4*>(slot + 8192 + (lane >> 5) * 512 + e * 256 + (lane & 31) * 8) = f;
     }
   };
-  auto put_v8 = [&](unsigned char* slot) {  // [32-key block][half][g][dim] sixteen bytes
+  // [32-key block][half]: [g][dim] sixteen bytes, then sixteen zeros, which stand for
+  // the dims 72 .. 95 of the third block (zeros cost the matrix cores less power,
+  // and so the chip less clock, than any other bytes)
+  auto put_v8 = [&](unsigned char* slot) {
     if (wave != 1 || lane >= 32) return;
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
@@ -443,7 +454,7 @@ __global__ __launch_bounds__(kTPB, HD == 64 ? 3 : 2) void k_kv8_attn_tiles(Kv8At
       const bf16x2 a2 = cvt2(w1, vsc, false), a3 = cvt2(w1, vsc, true);
       f[0] = a0[0]; f[1] = a0[1]; f[2] = a1[0]; f[3] = a1[1];
       f[4] = a2[0]; f[5] = a2[1]; f[6] = a3[0]; f[7] = a3[1];
-      *reinterpret_cast<bf16x8*>(slot + 8192 + ((lane >> 4) * 2 + e) * 256 + (lane & 15) * 16) = f;
+      *reinterpret_cast<bf16x8*>(slot + 8192 + ((lane >> 4) * 2 + e) * 272 + (lane & 15) * 16) = f;
     }
   };
   // Fragment reads.  keys: 32-row block rb, k-step ks; values: key block kb, half hf, dim block db
@@ -453,9 +464,10 @@ __global__ __launch_bounds__(kTPB, HD == 64 ? 3 : 2) void k_kv8_attn_tiles(Kv8At
   auto key_tail = [&](const unsigned char* slot, int rb) -> s16x4 {
     return *reinterpret_cast<const s16x4*>(slot + 8192 + rb * 512 + lane * 8);
   };
+  const int third = r32 < 8 ? g * 128 + r32 * 16 : 256;
   auto val_frag = [&](const unsigned char* slot, int kb, int hf, int db) -> bf16x8 {
     if (db < 2) return *reinterpret_cast<const bf16x8*>(slot + ((db * 2 + kb) * 2 + hf) * 1024 + lane * 16);
-    return *reinterpret_cast<const bf16x8*>(slot + 8192 + (kb * 2 + hf) * 256 + g * 128 + (r32 & 7) * 16);
+    return *reinterpret_cast<const bf16x8*>(slot + 8192 + (kb * 2 + hf) * 272 + third);
   };
   auto qk = [&](const unsigned char* slot, f32x16& s0, f32x16& s1) {
     s0 = f32x16{};
@@ -659,8 +671,9 @@ __global__ __launch_bounds__(kTPB, HD == 64 ? 3 : 2) void k_kv8_attn_tiles(Kv8At
   };
 
   if (nkt > 0) {
-    // values of "block -1": zeros, times zero probabilities
+    // values of "block -1": zeros, times zero probabilities (and the zeros that stay)
     for (int i = tid; i < G::SLOT / 16; i += kTPB) reinterpret_cast<bf16x8*>(sm.v[1])[i] = zero8;
+    if (HD == 72 && tid < 4) *reinterpret_cast<bf16x8*>(sm.v[0] + 8192 + tid * 272 + 256) = zero8;
     fetch_k(0);
     put(sm.k[0], 0, sk, ksc);
     put(sm.k[0], 1, sk, ksc);
@@ -895,8 +908,12 @@ hipError_t launch_kv8_attention(sphinx_dtype dt, int head_dim, const Kv8Attn& A,
           k_kv8_attn_tiles<HD><<<std::min(most_wg, total - first), kTPB, 0, s>>>(A, c, P, part, first, total);
           continue;
         }
+        if (P.waves == 8) {
+          k_kv8_attn_rows<T, HD, 8><<<std::min(most_wg, total - first), 512, 0, s>>>(A, c, P, part, first);
+          continue;
+        }
       }
-      k_kv8_attn_rows<T, HD><<<std::min(most_wg, total - first), kTPB, 0, s>>>(A, c, P, part, first);
+      k_kv8_attn_rows<T, HD, 4><<<std::min(most_wg, total - first), kTPB, 0, s>>>(A, c, P, part, first);
     }
     if (parts == 0) return;
     const int join = P.row[A.nseg];

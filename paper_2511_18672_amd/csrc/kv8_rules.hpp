@@ -16,6 +16,7 @@ namespace sphinx {
 // kernel joins.
 struct Kv8Plan {
   int tile;                                  // rows per workgroup, 32 or 128
+  int waves;                                 // of a workgroup of a 32-row tile, 4 or 8
   int chunks[SPHINX_MAX_REQUESTS];           // at least 1
   int size[SPHINX_MAX_REQUESTS];             // blocks, at least 1
   int item[SPHINX_MAX_REQUESTS + 1];         // work items of the segments before (one head)
@@ -59,14 +60,23 @@ inline Kv8Plan plan_kv8(bool bf16, int kv_heads, int head_dim, int nseg, const i
   }
   // a 128-row tile takes about 2.4 times a 32-row tile's time
   p.tile = bf16 && 5 * small > 12 * tall ? 128 : 32;
+  p.waves = 4;
   if (p.tile == 32) {
+    int64_t units = 0;
+    for (int i = 0; i < nseg; ++i) units += (int64_t)kv8_tiles(rows[i], 32) * kv_heads;
+    // Small calls: eight waves take up to four blocks each, at about 1.5 us a block,
+    // which is less than a second kernel costs (one query against 4096 keys of 8
+    // heads, eight blocks a wave: 16.0 us whole, 12.6 us cut and joined).
+    if (bf16 && units <= kKv8Cus && longest <= 32) {
+      p.waves = 8;
+      cut_kv8(p, kv_heads, nseg, rows, klen, longest);
+      return p;
+    }
     // Chunks of equal work for all workgroups that run at once, counting that cutting
     // leaves half a chunk per tile on average.  fp32 is bound by the matrix cores,
     // which one workgroup keeps nearly as busy as two: tiles that fill the chip
     // are not cut for a second (1024 queries against 2048 keys of 8 heads, 256
-    // tiles: 50 us in two chunks, KF32 us whole).
-    int64_t units = 0;
-    for (int i = 0; i < nseg; ++i) units += (int64_t)kv8_tiles(rows[i], 32) * kv_heads;
+    // tiles: 50 us in two chunks, 48 us whole).
     const int64_t slots = bf16 && head_dim == 64 ? kKv8ItemsRows : !bf16 && units >= kKv8Cus ? kKv8Cus : 2 * kKv8Cus;
     const int64_t pieces = bf16 ? std::max(slots - units / 2, slots / 2) : slots;
     cut_kv8(p, kv_heads, nseg, rows, klen,
