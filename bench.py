@@ -57,6 +57,8 @@ def parse():
                     help="every frame on its own timestep grid from its own start (other reading of per-frame starts)")
     ap.add_argument("--cache-period", type=int, default=0,
                     help="latent cache with a full step every T steps (0: off, the default workload)")
+    ap.add_argument("--cache-dtype", default="model", choices=["model", "fp8"],
+                    help="latent cache in the model's type or in 8 bits (needs --cache-period)")
     ap.add_argument("--select-every-step", type=int, default=1,
                     help="1: run mask+compaction in every step (default); 0: only when the active set changes")
     return ap.parse_args()
@@ -411,7 +413,8 @@ def main():
         wl = W.CONFIGS[args.config](**kw)
     t_setup = time.perf_counter()
     R = S.from_workload(wl, layout=S.TOKENS if args.layout == "tokens" else S.NCHW,
-                        cache_period=args.cache_period, per_frame_grid=args.per_frame_grid)
+                        cache_period=args.cache_period, per_frame_grid=args.per_frame_grid,
+                        cache_dtype=args.cache_dtype)
     R.reset()
     stream = torch.cuda.current_stream()
     D, L, mlp, hd = wl.model.D, wl.model.L, wl.model.mlp, wl.model.head_dim
@@ -502,6 +505,8 @@ def main():
                 "kernel": (f"k_attn_bf16_dma{'' if hd == 64 else hd} (varlen flash attention, head_dim {hd})"
                            if wl.model.dtype == "bf16" else "k_attn_f32") if args.attention == "joint"
                 else "attention class: k_attn_bf16_dma per frame and k_attn_temporal per position, alternating",
+                **({"kernel": f"k_kv8_attn_tiles (attention over the 8-bit cache, head_dim {hd})"}
+                   if args.cache_dtype == "fp8" and args.attention == "joint" else {}),
                 "algorithmic_flop_per_launch": attn_flop}
     step_flop = L * (attn_flop + sum(gemm_flop.values()))
     mfma_util = step_flop / (ms_per_step * 1e-3) / (PEAK_BF16_TFLOPS * 1e12)
@@ -515,7 +520,8 @@ def main():
                                   f"{int(wl.max_steps)}-step DDIM schedule",
                       "selected_tokens": int(n), "tokens": int(wl.N), "select_every_step": force,
                       "state_layout": args.layout, "cache_period": args.cache_period,
-                      "attention": args.attention, "per_frame_grid": args.per_frame_grid},
+                      "attention": args.attention, "per_frame_grid": args.per_frame_grid,
+                      **({"cache_dtype": args.cache_dtype} if args.cache_dtype != "model" else {})},
            "mfma_util_step": round(mfma_util, 4),
            "roofline": roofline, "kernels": kernels,
            "kernels_note": f"per-class HIP-event averages from {n_breakdown} further untimed steps; "

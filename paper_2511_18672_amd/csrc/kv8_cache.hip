@@ -129,10 +129,10 @@ __device__ __forceinline__ void lds_order() {
 // runs that start among them; without listed tokens it does block `unit`.
 struct Run {
   int block, first;  // the run's block and its first row of the call
-  int count;         // rows of the block, from its first, that rows `first` and on fill; -1: listed tokens
+  int count;         // rows of the block, from its first, that rows `first` and on fill; -1: some listed tokens
   int from, at, lane_block;  // listed tokens: row of the call, row and block of this lane's token (rows from .. + 63)
 };
-template <typename F>
+template <bool WHOLE, typename F>
 __device__ __forceinline__ void for_each_run(const Kv8Segs& S, const Kv8Rows& rows, int group, int unit, const F& body) {
   if (rows.idx == nullptr) {
     int lo = 0, hi = S.nseg - 1;
@@ -148,15 +148,24 @@ __device__ __forceinline__ void for_each_run(const Kv8Segs& S, const Kv8Rows& ro
   const int lane = lane_id(), from = unit * group;
   const int64_t j = (int64_t)from + lane;
   const int prev = from > 0 ? rows.idx[from - 1] : -1;
+  const int token = j < rows.n ? rows.idx[j] : -1, further = WHOLE && j + kWave < rows.n ? rows.idx[j + kWave] : -1;
   int at, before_at;
-  const int block = block_of(S, j < rows.n ? rows.idx[j] : -1, &at);
+  const int block = block_of(S, token, &at);
   int before = __shfl_up(block, 1, kWave);
   if (lane == 0) before = block_of(S, prev, &before_at);
   uint64_t starts = __ballot(lane < group && block >= 0 && block != before);  // the same in every wave
   while (starts != 0) {
     const int l = __builtin_ctzll(starts);
     starts &= starts - 1;
-    body(Run{__builtin_amdgcn_readlane(block, l), from + l, -1, from, at, block});
+    // WHOLE: looks for runs of all 64 tokens of a block, one row each (the row behind
+    // them is another block's), which keep no row.
+    const int run_block = __builtin_amdgcn_readlane(block, l);
+    const int t0 = __builtin_amdgcn_readlane(token, l), row0 = __builtin_amdgcn_readlane(at, l);
+    const bool next = lane >= l ? token == t0 + lane - l : further == t0 + kWave + lane - l;
+    const bool whole = WHOLE && row0 == 0 && __ballot(next) == ~0ull &&
+                       block_of(S, t0 + kKv8Block - 1, &before_at) == run_block &&
+                       block_of(S, __builtin_amdgcn_readlane(further, l), &before_at) != run_block;
+    body(Run{run_block, from + l, whole ? kKv8Block : -1, from, at, block});
   }
 }
 
@@ -164,7 +173,7 @@ __device__ __forceinline__ void for_each_run(const Kv8Segs& S, const Kv8Rows& ro
 // one XCD, one after the other, since a head's piece of a row (144 bytes at
 // head_dim 72) shares cache lines with the next head's.  `per`: units that a
 // workgroup does at a time, this is its `mine`-th.
-template <typename F>
+template <bool WHOLE, typename F>
 __device__ __forceinline__ void for_each_unit(const Kv8Segs& S, const Kv8Rows& rows, int heads, int group, int units,
                                               int per, int mine, const F& body) {
   const int total = units * heads, groups = (total + per - 1) / per;
@@ -172,7 +181,7 @@ __device__ __forceinline__ void for_each_unit(const Kv8Segs& S, const Kv8Rows& r
     const int u = xcd_tile((int)b, groups) * per + mine;
     if (u >= total) continue;
     const int unit = u / heads, h = u - unit * heads;
-    for_each_run(S, rows, group, unit, [&](const Run& run) { body(h, run); });
+    for_each_run<WHOLE>(S, rows, group, unit, [&](const Run& run) { body(h, run); });
   }
 }
 
@@ -394,7 +403,7 @@ __global__ __launch_bounds__(kTPB, sizeof(T) == 2 ? 3 : 2) void k_kv8_store(Kv8S
     lds_order();
     for (int i = lane; i < NV; i += kWave) reinterpret_cast<uint4*>(tile)[i] = images[wave][i];
   };
-  for_each_unit(S, rows, 2 * c.kv_heads, group, units, 4, wave, body);
+  for_each_unit<true>(S, rows, 2 * c.kv_heads, group, units, 4, wave, body);
 }
 
 // One workgroup reads the listed rows of one block of one head at a time: the
@@ -445,7 +454,7 @@ __global__ __launch_bounds__(kTPB) void k_kv8_load(Kv8Segs S, Kv8Slice c, Kv8Row
       store_row<8>(v + j * rows.ld + h * HD + p * 8, x);
     }
   };
-  for_each_unit(S, rows, c.kv_heads, group, units, 1, 0, body);
+  for_each_unit<false>(S, rows, c.kv_heads, group, units, 1, 0, body);
 }
 
 template <typename F>

@@ -92,7 +92,7 @@ inline Kv8Plan plan_kv8(bool bf16, int kv_heads, int head_dim, int nseg, const i
   const double block_us = head_dim == 64 ? 0.47 : 0.63;
   Kv8Plan best = p;
   double least = 0.0;
-  for (int k = 1; k <= longest; k += k < 16 ? 1 : k / 8) {
+  for (int k = 1; k <= longest; k += k < 6 ? 1 : k / 3) {
     const int most = std::max(kKv8MinChunkTiles, (longest + k - 1) / k);
     Kv8Plan q = p;
     cut_kv8(q, kv_heads, nseg, rows, klen, most);

@@ -148,6 +148,23 @@ def test_a_slice_of_any_bytes_written_whole():
         c.check()
 
 
+@pytest.mark.parametrize("idx", [np.arange(300), np.arange(7, 290), np.r_[0:64, 63, 64:128], np.r_[-3, 0:128, 128, 128],
+                                 np.r_[0:32, 32:64, 128:192, 200:300], np.r_[0, 0, 2:64, 64:300]],
+                         ids=["all", "inner", "one_twice", "last_twice", "blocks", "gap_and_twice"])
+@pytest.mark.parametrize("bounds", [[0, 300], [0, 64, 130, 300], [0, 63, 300]])
+def test_listed_whole_blocks(idx, bounds):
+    """Runs that fill a block, that fill it and list a token again, that only seem to."""
+    rng = np.random.default_rng(11)
+    c = Cache(3, 72, bounds)
+    c.store(rows_of(rng, 300, 3, 72, "bf16"), rows_of(rng, 300, 3, 72, "bf16"))
+    c.store(rows_of(rng, idx.size, 3, 72, "bf16"), rows_of(rng, idx.size, 3, 72, "bf16"), idx)
+    c.check("bf16")
+    k, v = c.load("f32", idx)
+    inside = idx >= 0
+    assert np.array_equal(f64(k).reshape(-1, 3, 72)[inside], c.k[idx[inside]])
+    assert np.array_equal(f64(v).reshape(-1, 3, 72)[inside], c.v[idx[inside]])
+
+
 def test_load_some_rows():
     rng = np.random.default_rng(9)
     for heads, d, dtype in ((3, 64, "f32"), (2, 72, "bf16")):
