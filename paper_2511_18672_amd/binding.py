@@ -379,7 +379,9 @@ def _here(stream, *tensors) -> Optional[int]:
         if t is not None and t.get_device() != dev:
             raise ValueError(f"tensor on {t.device}, the current device is cuda:{dev}")
     if stream is None:
-        return torch.cuda.current_stream(dev).cuda_stream
+        # the handle alone, where torch offers it: a Stream object takes 1 us of a 7 us call
+        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+        return raw(dev) if raw is not None else torch.cuda.current_stream(dev).cuda_stream
     return stream if isinstance(stream, int) else stream.cuda_stream
 
 
