@@ -18,6 +18,15 @@ constexpr int kRows = 32;  // rows (queries of the heads that share a key/value 
 
 __device__ __forceinline__ float fast_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
 
+// Largest of 32 scores of a lane and of the lane 32 further (its row's other keys).
+__device__ __forceinline__ float row_max(const f32x16& a, const f32x16& b) {
+  float x = fmaxf(a[0], b[0]);
+#pragma unroll
+  for (int i = 1; i < 16; ++i) x = fmaxf(x, fmaxf(a[i], b[i]));
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+
 // Segment of a work item or of a row to join: the last whose first one (of the
 // prefix sums `first`) is not behind it.
 __device__ __forceinline__ int find_segment(const int* first, int nseg, int at) {
@@ -203,10 +212,7 @@ __global__ __launch_bounds__(64 * WAVES, sizeof(T) == 2 && HD == 64 && WAVES == 
         }
     }
     const float kscale = F32 ? ks : 1.0f;  // f32: the scores are of unscaled keys so far
-    float mx = -INFINITY;
-#pragma unroll
-    for (int r = 0; r < 16; ++r) mx = fmaxf(mx, fmaxf(sc[0][r], sc[1][r]));
-    mx = fmaxf(mx, __shfl_xor(mx, 32, kWave)) * kscale;
+    const float mx = row_max(sc[0], sc[1]) * kscale;
     // while every score is -inf the base is 0: such keys weigh nothing
     const float mn = fmaxf(m, mx), at = mn == -INFINITY ? 0.0f : mn;
     if (__ballot(mn > m) != 0) {
@@ -709,10 +715,7 @@ __global__ __launch_bounds__(kTPB, HD == 64 ? 3 : 2) void k_kv8_attn_tiles(Kv8At
     qk(sm.k[0], a0, a1);
     if (nkt == 1 && last < kKv8Block) mask_tail(a0, a1);
     {
-      float mx = -INFINITY;
-#pragma unroll
-      for (int r = 0; r < 16; ++r) mx = fmaxf(mx, fmaxf(a0[r], a1[r]));
-      mx = fmaxf(mx, __shfl_xor(mx, 32, kWave));
+      const float mx = row_max(a0, a1);
       shifted = __ballot(!(mx >= -24.0f && mx <= 24.0f)) != 0;
       m_run = shifted && mx > -INFINITY ? mx : 0.0f;
     }
