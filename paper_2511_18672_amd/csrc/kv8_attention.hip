@@ -159,18 +159,26 @@ __global__ __launch_bounds__(64 * WAVES, sizeof(T) == 2 && HD == 64 && WAVES == 
     if (b + WAVES < nb) fetch(b + WAVES);
     // The products of the two key blocks alternate, so that none waits for the one before.
     f32x16 sc[2] = {f32x16{}, f32x16{}};
+    if constexpr (F32) {
+      // two sums of 32 dims: a score's roundings are what an f32 result is off by
+      f32x16 more[2] = {f32x16{}, f32x16{}};
+      float k0[16], k1[16], k2[16], k3[16];
+      operand(kc[0][0], k0);
+      operand(kc[1][0], k1);
+      operand(kc[0][1], k2);
+      operand(kc[1][1], k3);
 #pragma unroll
-    for (int hf = 0; hf < 2; ++hf) {
-      if constexpr (F32) {
-        float k0[16], k1[16];
-        operand(kc[0][hf], k0);
-        operand(kc[1][hf], k1);
+      for (int i = 0; i < 16; ++i) {
+        sc[0] = __builtin_amdgcn_mfma_f32_32x32x2f32(k0[i], qf[i], sc[0], 0, 0, 0);
+        sc[1] = __builtin_amdgcn_mfma_f32_32x32x2f32(k1[i], qf[i], sc[1], 0, 0, 0);
+        more[0] = __builtin_amdgcn_mfma_f32_32x32x2f32(k2[i], qf[16 + i], more[0], 0, 0, 0);
+        more[1] = __builtin_amdgcn_mfma_f32_32x32x2f32(k3[i], qf[16 + i], more[1], 0, 0, 0);
+      }
+      sc[0] += more[0];
+      sc[1] += more[1];
+    } else {
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          sc[0] = __builtin_amdgcn_mfma_f32_32x32x2f32(k0[i], qf[16 * hf + i], sc[0], 0, 0, 0);
-          sc[1] = __builtin_amdgcn_mfma_f32_32x32x2f32(k1[i], qf[16 * hf + i], sc[1], 0, 0, 0);
-        }
-      } else {
+      for (int hf = 0; hf < 2; ++hf) {
         bf16x8 k0[2], k1[2];
         operand(kc[0][hf], ks, k0);
         operand(kc[1][hf], ks, k1);
