@@ -452,7 +452,8 @@ sphinx_status sphinx_kv8_load(sphinx_dtype dtype, int32_t kv_heads, int32_t head
  * multiple of 8; heads*head_dim <= 65536; pointers 16-byte aligned.  ws: dev,
  * 256-byte aligned, sphinx_kv8_attention_workspace_bytes bytes (which covers
  * every kv_len), not shared with work that may run at the same time.  Enqueues
- * at most two kernels, synchronizes nothing and may be captured in a graph. */
+ * a kernel or two, synchronizes nothing and may be captured in a graph.  Sums
+ * stay finite for values up to 2^90 in magnitude. */
 sphinx_status sphinx_kv8_attention_workspace_bytes(sphinx_dtype dtype, int32_t heads, int32_t kv_heads,
                                                    int32_t head_dim, const int32_t* cu_q, const int32_t* cu_kv,
                                                    int32_t nseg, size_t* bytes);

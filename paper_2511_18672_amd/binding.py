@@ -385,6 +385,11 @@ def _here(stream, *tensors) -> Optional[int]:
     return stream if isinstance(stream, int) else stream.cuda_stream
 
 
+def _check_idx(idx, n: int):
+    if idx is not None and (idx.element_size() != 4 or idx.is_floating_point() or idx.numel() < n):
+        raise ValueError(f"idx holds {idx.numel()} values of {idx.dtype}, {n} int32 are needed")
+
+
 def sphinx_kv8_bytes(kv_heads: int, head_dim: int, cu_kv) -> int:
     """Bytes of one slice of the 8-bit cache (cu_kv: host int sequence of token bounds, as in the calls below)."""
     cu, out = _host_cu(cu_kv), c_size_t()
@@ -396,6 +401,7 @@ def sphinx_kv8_bytes(kv_heads: int, head_dim: int, cu_kv) -> int:
 def sphinx_kv8_store(dtype: int, kv_heads: int, head_dim: int, k, v, ld: int, idx, n: int, cu_kv, cache, stream=None):
     """Quantises rows j < n of k and v into the slice `cache` (zeroed before its first use) at tokens idx[j]
     (ascending; None: token j)."""
+    _check_idx(idx, n)
     cu, s = _host_cu(cu_kv), _here(stream, k, v, idx, cache)
     _check("sphinx_kv8_store", lib().sphinx_kv8_store(
         dtype, kv_heads, head_dim, k.data_ptr(), v.data_ptr(), ld, _ptr(idx), n, cu.ctypes.data, cu.size - 1,
@@ -404,6 +410,7 @@ def sphinx_kv8_store(dtype: int, kv_heads: int, head_dim: int, k, v, ld: int, id
 
 def sphinx_kv8_load(dtype: int, kv_heads: int, head_dim: int, cache, cu_kv, idx, n: int, k, v, ld: int, stream=None):
     """Rows j < n of k and v <- the values of tokens idx[j] (ascending; None: token j)."""
+    _check_idx(idx, n)
     cu, s = _host_cu(cu_kv), _here(stream, k, v, idx, cache)
     _check("sphinx_kv8_load", lib().sphinx_kv8_load(
         dtype, kv_heads, head_dim, cache.data_ptr(), cache.nbytes, cu.ctypes.data, cu.size - 1, _ptr(idx), n,

@@ -312,6 +312,64 @@ def test_attention_nan_key_reaches_its_queries_only():
         assert torch.isnan(o[:nq, 1]).all() and torch.isfinite(o[:nq, 0]).all() and torch.isfinite(o[nq:]).all()
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("kv_heads,group,nq,nk", [(1, 96, 3, 500), (1, 512, 1, 100), (40, 1, 2, 70), (3, 7, 33, 129)])
+def test_attention_head_layouts(dtype, kv_heads, group, nq, nk):
+    rng = np.random.default_rng(28)
+    c = filled(rng, kv_heads, 64, [0, nk], dtype)
+    check_attention(c, queries(rng, nq, kv_heads * group, 64, dtype), kv_heads * group, [0, nq])
+
+
+def test_attention_of_64_segments():
+    """The most segments of a call, some without queries, some without keys, in blocks of every fill."""
+    rng = np.random.default_rng(29)
+    for scale in (1, 5):
+        nk = rng.integers(0, 300 * scale, 64)
+        nq = rng.integers(0, 3 * scale * scale, 64)
+        nk[[3, 40]], nq[[4, 41]], nk[63], nq[63] = 0, 0, 64, 2
+        c = filled(rng, 2, 72, np.concatenate([[0], np.cumsum(nk)]))
+        cu_q = np.concatenate([[0], np.cumsum(nq)])
+        check_attention(c, queries(rng, cu_q[-1], 6, 72, "bf16"), 6, cu_q)
+
+
+@pytest.mark.parametrize("nq", [1, 40, 300])
+def test_attention_over_a_cleared_slice_is_zero(nq):
+    c = Cache(2, 72, [0, 1000])
+    q = queries(np.random.default_rng(30), nq, 2, 72, "bf16")
+    assert (attend(c, q, 2, [0, nq]) == 0).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("nq", [5, 140])
+def test_attention_of_a_nan_or_infinite_query_leaves_the_others(dtype, nq):
+    rng = np.random.default_rng(31)
+    c = filled(rng, 2, 64, [0, 400], dtype)
+    q = queries(rng, nq, 2, 64, dtype)
+    q[1, 5] = float("nan")
+    q[3, 70] = float("inf")
+    o = f64(attend(c, q, 2, [0, nq])).reshape(nq, 2, 64)
+    assert np.isnan(o[1, 0]).all() and np.isnan(o[3, 1]).all()
+    qq = f64(q).reshape(nq, 2, 64)
+    qq[1, 0], qq[3, 1] = 0.0, 0.0
+    ref, mag, big = O.kv8.attention(qq, c.k, c.v, [0, nq], c.bounds)
+    err = np.abs(o - ref) - tolerance(dtype, ref, mag, big, 400, 64)
+    err[1, 0], err[3, 1] = -1.0, -1.0
+    assert err.max() <= 0.0
+
+
+def test_slice_at_any_16_bytes():
+    """A slice needs no more than 16-byte alignment."""
+    rng = np.random.default_rng(32)
+    c = Cache(3, 72, [0, 200])
+    whole = torch.zeros(c.slice.numel() + 64, dtype=torch.uint8, device="cuda")
+    c.slice = whole[48:48 + c.slice.numel()]
+    c.store(rows_of(rng, 200, 3, 72, "bf16"), rows_of(rng, 200, 3, 72, "bf16"))
+    c.check("bf16")
+    for nq in (2, 200):
+        check_attention(c, queries(rng, nq, 3, 72, "bf16"), 3, [0, nq])
+    assert (whole[:48] == 0).all() and (whole[48 + c.slice.numel():] == 0).all()
+
+
 @pytest.mark.parametrize("nq,nk", [(1, 8000), (400, 4000)])
 def test_attention_repeats_bit_for_bit_on_streams_and_in_graphs(nq, nk):
     rng = np.random.default_rng(25)
@@ -397,6 +455,12 @@ def test_tensors_of_another_device_and_short_slices_are_refused():
     cpu = torch.zeros(64, 64)
     with pytest.raises(ValueError):
         B.sphinx_kv8_store(B.F32, 1, 64, cpu, cpu, 64, None, 64, c.bounds, c.slice)
+    rows = torch.zeros(64, 64, device="cuda")
+    for idx in (torch.arange(64, device="cuda"), torch.arange(63, dtype=torch.int32, device="cuda")):  # int64; too few
+        with pytest.raises(ValueError):
+            B.sphinx_kv8_store(B.F32, 1, 64, rows, rows, 64, idx, 64, c.bounds, c.slice)
+        with pytest.raises(ValueError):
+            B.sphinx_kv8_load(B.F32, 1, 64, c.slice, c.bounds, idx, 64, rows, rows, 64)
     with pytest.raises(S.SphinxError):  # a slice of too few bytes
         B.sphinx_kv8_load(B.F32, 1, 64, c.slice[:64], c.bounds, None, 64, cpu.cuda(), cpu.cuda(), 64)
 
