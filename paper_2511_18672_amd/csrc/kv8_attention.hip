@@ -311,8 +311,8 @@ __global__ __launch_bounds__(64 * WAVES, sizeof(T) == 2 && HD == 64 && WAVES == 
 // (bf16 products: 256 cycles a wave for K Q^T of 64 keys at head_dim 64 and as
 // many for V^T P^T), next to the exponentials; so bytes become bf16 once per
 // workgroup, not once per wave:
-//  * thread t holds chunk t of a block's key tile and of its value tile (one
-//    16-byte load each, issued an iteration ahead), turns them into two
+//  * thread t takes chunk t of a block's key tile and of its value tile (copied
+//    straight to LDS, issued half an iteration ahead), turns them into two
 //    fragments each and writes these to LDS in the order in which a wave reads
 //    them (fragment f at 1024 f, 16 bytes a lane), so that writes and reads
 //    are consecutive and free of bank conflicts, with constant offsets;
@@ -339,6 +339,8 @@ template <int HD>
 struct TileSmem {
   unsigned char k[2][TileGeo<HD>::SLOT];
   unsigned char v[2][TileGeo<HD>::SLOT];
+  unsigned char rk[TileGeo<HD>::TILE];  // one block's bytes, as they came
+  unsigned char rv[TileGeo<HD>::TILE];
 };
 constexpr float kPsumMax = 4294967296.0f;  // 2^32
 
@@ -357,7 +359,7 @@ __device__ __forceinline__ uint32_t keep_keys(uint32_t w, int left) {  // the fi
 }
 
 template <int HD>
-__global__ __launch_bounds__(kTPB, HD == 64 ? 3 : 2) void k_kv8_attn_tiles(Kv8Attn A, Kv8Slice c, Kv8Plan P,
+__global__ __launch_bounds__(kTPB, 3) void k_kv8_attn_tiles(Kv8Attn A, Kv8Slice c, Kv8Plan P,
                                                                             Parts part, int first, int total) {
   typedef TileGeo<HD> G;
   constexpr int DB = G::DB, NPV = G::NPV, NSTEP = G::NPV + G::NQK;
@@ -395,31 +397,46 @@ __global__ __launch_bounds__(kTPB, HD == 64 ? 3 : 2) void k_kv8_attn_tiles(Kv8At
   const unsigned char* scales = c.scales + ((int64_t)h * c.nblk + A.blk[s] + b0) * 2;
   const int last = L - (b0 + nkt - 1) * kKv8Block;  // keys of the chunk's last block (64 and more: whole)
 
-  // Staged bytes: chunk `tid` of a key tile and of a value tile; head_dim 72:
-  // also the eight bytes behind the key chunks of row `lane` (wave 0) and the
-  // chunk behind the value chunks (wave 1, 32 lanes).
+  // Bytes of a block on their way: chunk `tid` of its key tile and of its value
+  // tile, copied straight into LDS by the wave that will convert them, which
+  // holds no registers meanwhile; head_dim 72: also the bytes behind the chunks,
+  // the keys' by wave 0 and the values' by wave 1.
   uint4 sk, sv;
   uint4 st = make_uint4(0u, 0u, 0u, 0u);
   float ksc, vsc;
   auto fetch_k = [&](int t) {
     const unsigned char* p = base + (int64_t)t * 2 * G::TILE;
-    sk = *reinterpret_cast<const uint4*>(p + tid * 16);
+    lds_dma16_at(p, tid * 16, sm.rk + wave * 1024);
+    if (HD == 72 && wave == 0 && lane < 32) lds_dma16_at(p + 4096, lane * 16, sm.rk + 4096);
     ksc = byte_scale(scales[2 * (int64_t)t]);
-    if constexpr (HD == 72) {
-      if (wave == 0) {
-        const uint2 x = *reinterpret_cast<const uint2*>(p + 4096 + lane * 8);
-        st.x = x.x;
-        st.y = x.y;
-      }
-    }
   };
   auto fetch_v = [&](int t) {
     const unsigned char* p = base + (int64_t)t * 2 * G::TILE + G::TILE;
-    sv = *reinterpret_cast<const uint4*>(p + tid * 16);
+    lds_dma16_at(p, tid * 16, sm.rv + wave * 1024);
+    if (HD == 72 && wave == 1 && lane < 32) lds_dma16_at(p + 4096, lane * 16, sm.rv + 4096);
     vsc = byte_scale(scales[2 * (int64_t)t + 1]);
-    if constexpr (HD == 72) {
-      if (wave == 1) st = *reinterpret_cast<const uint4*>(p + 4096 + (lane & 31) * 16);
+  };
+  // This wave's copies have landed (only it reads them).
+  auto landed = [&]() {
+    __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0)
+    asm volatile("" ::: "memory");
+  };
+  auto take_k = [&]() {
+    sk = *reinterpret_cast<const uint4*>(sm.rk + tid * 16);
+    if (HD == 72 && wave == 0) {
+      const uint2 x = *reinterpret_cast<const uint2*>(sm.rk + 4096 + lane * 8);
+      st.x = x.x;
+      st.y = x.y;
     }
+  };
+  auto take_v = [&]() {
+    sv = *reinterpret_cast<const uint4*>(sm.rv + tid * 16);
+    if (HD == 72 && wave == 1) st = *reinterpret_cast<const uint4*>(sm.rv + 4096 + (lane & 31) * 16);
+  };
+  // What was taken is in registers, so that its place may be filled again.
+  auto taken = [&]() {
+    __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0)
+    asm volatile("" ::: "memory");
   };
   // what lies behind the segment's last key may hold anything: its values become zero
   auto trim_v = [&]() {
@@ -609,7 +626,6 @@ __global__ __launch_bounds__(kTPB, HD == 64 ? 3 : 2) void k_kv8_attn_tiles(Kv8At
   auto fetch = [&](int t) {
     fetch_k(min(t + 3, nkt - 1));
     fetch_v(t + 1);
-    if (t + 2 == nkt && last < kKv8Block) trim_v();
   };
   // Iteration t; PAR = t % 2.  c: scores of block t, n: of block t + 1; pp: probabilities of block t - 1, pn: of t.
   auto iter = [&](int t, auto PAR, f32x16& c0, f32x16& c1, f32x16& n0, f32x16& n1, bf16x8 (&pp)[2][2],
@@ -659,7 +675,13 @@ __global__ __launch_bounds__(kTPB, HD == 64 ? 3 : 2) void k_kv8_attn_tiles(Kv8At
         pn[w][hf][2 * j] = pr[0];
         pn[w][hf][2 * j + 1] = pr[1];
       }
-      // the staged bytes: keys t + 2, values t; then the next loads
+      // the staged bytes: keys t + 2, values t; then the next copies (every step ends
+      // in a fence, so that what was taken has been converted by then)
+      if (i == 0) {
+        landed();
+        take_k();
+      }
+      if (i == 6) take_v();
       if (i == 2) put(kw, 0, sk, ksc);
       if (i == 4) {
         put(kw, 1, sk, ksc);
@@ -688,31 +710,37 @@ __global__ __launch_bounds__(kTPB, HD == 64 ? 3 : 2) void k_kv8_attn_tiles(Kv8At
     // values of "block -1": zeros, times zero probabilities (and the zeros that stay)
     for (int i = tid; i < G::SLOT / 16; i += kTPB) reinterpret_cast<bf16x8*>(sm.v[1])[i] = zero8;
     if (HD == 72 && tid < 4) *reinterpret_cast<bf16x8*>(sm.v[0] + 8192 + tid * 272 + 256) = zero8;
-    fetch_k(0);
-    put(sm.k[0], 0, sk, ksc);
-    put(sm.k[0], 1, sk, ksc);
-    if constexpr (HD == 72) put_k8(sm.k[0]);
-    fetch_k(min(1, nkt - 1));
-    put(sm.k[1], 0, sk, ksc);
-    put(sm.k[1], 1, sk, ksc);
-    if constexpr (HD == 72) put_k8(sm.k[1]);
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      fetch_k(min(t, nkt - 1));
+      landed();
+      take_k();
+      taken();
+      put(sm.k[t], 0, sk, ksc);
+      put(sm.k[t], 1, sk, ksc);
+      if constexpr (HD == 72) put_k8(sm.k[t]);
+    }
     fetch_k(min(2, nkt - 1));
     fetch_v(0);
-    if (nkt == 1 && last < kKv8Block) trim_v();
     barrier();
     if (!active) {
       barrier();
       int t = 0;
       for (; t < nkt; ++t) {  // at the last block only its values are left to stage
         unsigned char* vw = sm.v[t & 1];
+        landed();
+        take_v();
+        if (t + 1 == nkt && last < kKv8Block) trim_v();
         put(vw, 0, sv, vsc);
         put(vw, 1, sv, vsc);
         if constexpr (HD == 72) put_v8(vw);
         if (t + 1 < nkt) {
           unsigned char* kw = sm.k[t & 1];
+          take_k();
           put(kw, 0, sk, ksc);
           put(kw, 1, sk, ksc);
           if constexpr (HD == 72) put_k8(kw);
+          taken();
           fetch(t);
         }
         barrier();
@@ -749,6 +777,9 @@ __global__ __launch_bounds__(kTPB, HD == 64 ? 3 : 2) void k_kv8_attn_tiles(Kv8At
     // the last block
     unsigned char* vw = sm.v[t & 1];
     const unsigned char* vr = sm.v[(t & 1) ^ 1];
+    landed();
+    take_v();
+    if (last < kKv8Block) trim_v();
     put(vw, 0, sv, vsc);
     put(vw, 1, sv, vsc);
     if constexpr (HD == 72) put_v8(vw);
