@@ -339,8 +339,8 @@ template <int HD>
 struct TileSmem {
   unsigned char k[2][TileGeo<HD>::SLOT];
   unsigned char v[2][TileGeo<HD>::SLOT];
-  unsigned char rk[TileGeo<HD>::TILE];  // one block's bytes, as they came
-  unsigned char rv[TileGeo<HD>::TILE];
+  unsigned char rk[4096];  // one block's bytes, as they came
+  unsigned char rv[4096];
 };
 constexpr float kPsumMax = 4294967296.0f;  // 2^32
 
@@ -399,22 +399,26 @@ __global__ __launch_bounds__(kTPB, 3) void k_kv8_attn_tiles(Kv8Attn A, Kv8Slice 
 
   // Bytes of a block on their way: chunk `tid` of its key tile and of its value
   // tile, copied straight into LDS by the wave that will convert them, which
-  // holds no registers meanwhile; head_dim 72: also the bytes behind the chunks,
-  // the keys' by wave 0 and the values' by wave 1.
+  // holds no registers meanwhile; head_dim 72: also four of the bytes behind the
+  // chunks, the keys' in waves 0 and 1, the values' in waves 2 and 3 (so that no
+  // wave branches in the run of steps).
   uint4 sk, sv;
-  uint4 st = make_uint4(0u, 0u, 0u, 0u);
+  uint32_t st = 0;
   float ksc, vsc;
   auto fetch_k = [&](int t) {
     const unsigned char* p = base + (int64_t)t * 2 * G::TILE;
     lds_dma16_at(p, tid * 16, sm.rk + wave * 1024);
-    if (HD == 72 && wave == 0 && lane < 32) lds_dma16_at(p + 4096, lane * 16, sm.rk + 4096);
     ksc = byte_scale(scales[2 * (int64_t)t]);
   };
   auto fetch_v = [&](int t) {
     const unsigned char* p = base + (int64_t)t * 2 * G::TILE + G::TILE;
     lds_dma16_at(p, tid * 16, sm.rv + wave * 1024);
-    if (HD == 72 && wave == 1 && lane < 32) lds_dma16_at(p + 4096, lane * 16, sm.rv + 4096);
     vsc = byte_scale(scales[2 * (int64_t)t + 1]);
+  };
+  const bool vtail = wave >= 2;
+  auto fetch_tail = [&](int tk, int tv) {
+    const unsigned char* p = base + (int64_t)(vtail ? tv : tk) * 2 * G::TILE + (vtail ? G::TILE : 0) + 4096;
+    st = *reinterpret_cast<const uint32_t*>(p + (tid & 127) * 4);
   };
   // This wave's copies have landed (only it reads them).
   auto landed = [&]() {
@@ -423,15 +427,9 @@ __global__ __launch_bounds__(kTPB, 3) void k_kv8_attn_tiles(Kv8Attn A, Kv8Slice 
   };
   auto take_k = [&]() {
     sk = *reinterpret_cast<const uint4*>(sm.rk + tid * 16);
-    if (HD == 72 && wave == 0) {
-      const uint2 x = *reinterpret_cast<const uint2*>(sm.rk + 4096 + lane * 8);
-      st.x = x.x;
-      st.y = x.y;
-    }
   };
   auto take_v = [&]() {
     sv = *reinterpret_cast<const uint4*>(sm.rv + tid * 16);
-    if (HD == 72 && wave == 1) st = *reinterpret_cast<const uint4*>(sm.rv + 4096 + (lane & 31) * 16);
   };
   // What was taken is in registers, so that its place may be filled again.
   auto taken = [&]() {
@@ -444,13 +442,8 @@ __global__ __launch_bounds__(kTPB, 3) void k_kv8_attn_tiles(Kv8Attn A, Kv8Slice 
     uint32_t* w = reinterpret_cast<uint32_t*>(&sv);
 #pragma unroll
     for (int i = 0; i < 4; ++i) w[i] = keep_keys(w[i], last - (32 * kb + 8 * i + 4 * g));
-    if constexpr (HD == 72) {
-      if (wave == 1) {
-        uint32_t* x = reinterpret_cast<uint32_t*>(&st);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) x[i] = keep_keys(x[i], last - (32 * ((lane >> 4) & 1) + 8 * i + 4 * ((lane >> 3) & 1)));
-      }
-    }
+    // word w = tid - 128 behind the value chunks: keys 32 (w / 64) + 8 (w % 4) + 4 (w / 32 % 2) .. + 3
+    if (HD == 72 && vtail) st = keep_keys(st, last - (32 * ((tid >> 6) & 1) + 8 * (tid & 3) + 4 * ((tid >> 5) & 1)));
   };
   auto put = [&](unsigned char* slot, int e, const uint4& b, float scale) {  // half e of a chunk: fragment 2 wave + e
     const uint32_t w0 = e ? b.z : b.x, w1 = e ? b.w : b.y;
@@ -461,32 +454,19 @@ __global__ __launch_bounds__(kTPB, 3) void k_kv8_attn_tiles(Kv8Attn A, Kv8Slice 
     f[4] = a2[0]; f[5] = a2[1]; f[6] = a3[0]; f[7] = a3[1];
     *reinterpret_cast<bf16x8*>(slot + (2 * wave + e) * 1024 + lane * 16) = f;
   };
-  auto put_k8 = [&](unsigned char* slot) {  // dims 64 .. 71: [32-row block][g][row] eight bytes
-    if (wave != 0) return;
-#pragma unroll
-    for (int e = 0; e < 2; ++e) {
-      const uint32_t w = e ? st.y : st.x;
-      bf16x4 f;
-      const bf16x2 a0 = cvt2(w, ksc, false), a1 = cvt2(w, ksc, true);
-      f[0] = a0[0]; f[1] = a0[1]; f[2] = a1[0]; f[3] = a1[1];
-      *reinterpret_cast<bf16x4*>(slot + 8192 + (lane >> 5) * 512 + e * 256 + (lane & 31) * 8) = f;
-    }
-  };
-  // [32-key block][half]: [g][dim] sixteen bytes, then sixteen zeros, which stand for
-  // the dims 72 .. 95 of the third block (zeros cost the matrix cores less power,
-  // and so the chip less clock, than any other bytes)
-  auto put_v8 = [&](unsigned char* slot) {
-    if (wave != 1 || lane >= 32) return;
-#pragma unroll
-    for (int e = 0; e < 2; ++e) {
-      const uint32_t w0 = e ? st.z : st.x, w1 = e ? st.w : st.y;
-      bf16x8 f;
-      const bf16x2 a0 = cvt2(w0, vsc, false), a1 = cvt2(w0, vsc, true);
-      const bf16x2 a2 = cvt2(w1, vsc, false), a3 = cvt2(w1, vsc, true);
-      f[0] = a0[0]; f[1] = a0[1]; f[2] = a1[0]; f[3] = a1[1];
-      f[4] = a2[0]; f[5] = a2[1]; f[6] = a3[0]; f[7] = a3[1];
-      *reinterpret_cast<bf16x8*>(slot + 8192 + ((lane >> 4) * 2 + e) * 272 + (lane & 15) * 16) = f;
-    }
+  // The four bytes behind the chunks, in the slots of parity par.
+  // keys: dims 64 .. 71 as [32-row block][half of the dims][row] eight bytes
+  // values: [32-key block][half]: [g][dim] sixteen bytes, then sixteen zeros, which
+  // stand for the dims 72 .. 95 of the third block (zeros cost the matrix cores less
+  // power, and so the chip less clock, than any other bytes)
+  const int tail_at = vtail ? (int)(sm.v[0] - sm.k[0]) + 8192 + (((tid >> 6) & 1) * 2 + ((tid >> 1) & 1)) * 272 +
+                                  ((tid >> 2) & 15) * 16 + (tid & 1) * 8
+                            : 8192 + (tid >> 6) * 512 + (tid & 1) * 256 + ((tid >> 1) & 31) * 8;
+  auto put_tail = [&](int par) {
+    const float scale = vtail ? vsc : ksc;
+    const bf16x2 a0 = cvt2(st, scale, false), a1 = cvt2(st, scale, true);
+    const bf16x4 f = {a0[0], a0[1], a1[0], a1[1]};
+    *reinterpret_cast<bf16x4*>(sm.k[0] + tail_at + par * G::SLOT) = f;
   };
   // Fragment reads.  keys: 32-row block rb, k-step ks; values: key block kb, half hf, dim block db
   auto key_frag = [&](const unsigned char* slot, int rb, int ks) -> bf16x8 {
@@ -626,6 +606,7 @@ __global__ __launch_bounds__(kTPB, 3) void k_kv8_attn_tiles(Kv8Attn A, Kv8Slice 
   auto fetch = [&](int t) {
     fetch_k(min(t + 3, nkt - 1));
     fetch_v(t + 1);
+    if constexpr (HD == 72) fetch_tail(min(t + 3, nkt - 1), t + 1);
   };
   // Iteration t; PAR = t % 2.  c: scores of block t, n: of block t + 1; pp: probabilities of block t - 1, pn: of t.
   auto iter = [&](int t, auto PAR, f32x16& c0, f32x16& c1, f32x16& n0, f32x16& n1, bf16x8 (&pp)[2][2],
@@ -683,15 +664,10 @@ __global__ __launch_bounds__(kTPB, 3) void k_kv8_attn_tiles(Kv8Attn A, Kv8Slice 
       }
       if (i == 6) take_v();
       if (i == 2) put(kw, 0, sk, ksc);
-      if (i == 4) {
-        put(kw, 1, sk, ksc);
-        if constexpr (HD == 72) put_k8(kw);
-      }
+      if (i == 4) put(kw, 1, sk, ksc);
       if (i == 8) put(vw, 0, sv, vsc);
-      if (i == 10) {
-        put(vw, 1, sv, vsc);
-        if constexpr (HD == 72) put_v8(vw);
-      }
+      if (i == 10) put(vw, 1, sv, vsc);
+      if (HD == 72 && i == 11) put_tail(par);
       if (i == 12) fetch(t);
       __builtin_amdgcn_sched_barrier(0);
     }
@@ -713,15 +689,17 @@ __global__ __launch_bounds__(kTPB, 3) void k_kv8_attn_tiles(Kv8Attn A, Kv8Slice 
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
       fetch_k(min(t, nkt - 1));
+      if constexpr (HD == 72) fetch_tail(min(t, nkt - 1), 0);
       landed();
       take_k();
       taken();
       put(sm.k[t], 0, sk, ksc);
       put(sm.k[t], 1, sk, ksc);
-      if constexpr (HD == 72) put_k8(sm.k[t]);
+      if (HD == 72 && !vtail) put_tail(t);
     }
     fetch_k(min(2, nkt - 1));
     fetch_v(0);
+    if constexpr (HD == 72) fetch_tail(min(2, nkt - 1), 0);
     barrier();
     if (!active) {
       barrier();
@@ -733,13 +711,12 @@ __global__ __launch_bounds__(kTPB, 3) void k_kv8_attn_tiles(Kv8Attn A, Kv8Slice 
         if (t + 1 == nkt && last < kKv8Block) trim_v();
         put(vw, 0, sv, vsc);
         put(vw, 1, sv, vsc);
-        if constexpr (HD == 72) put_v8(vw);
+        if (HD == 72 && (vtail || t + 1 < nkt)) put_tail(t & 1);
         if (t + 1 < nkt) {
           unsigned char* kw = sm.k[t & 1];
           take_k();
           put(kw, 0, sk, ksc);
           put(kw, 1, sk, ksc);
-          if constexpr (HD == 72) put_k8(kw);
           taken();
           fetch(t);
         }
@@ -782,7 +759,7 @@ __global__ __launch_bounds__(kTPB, 3) void k_kv8_attn_tiles(Kv8Attn A, Kv8Slice 
     if (last < kKv8Block) trim_v();
     put(vw, 0, sv, vsc);
     put(vw, 1, sv, vsc);
-    if constexpr (HD == 72) put_v8(vw);
+    if (HD == 72 && vtail) put_tail(t & 1);
     auto pv = [&](const unsigned char* slot, const bf16x8 (&p)[2][2]) {
 #pragma unroll
       for (int kb = 0; kb < 2; ++kb)
