@@ -30,19 +30,11 @@ __device__ __forceinline__ int scale_byte(float top) {
   return min(max(e, kExpMin), kExpMax) + 127;
 }
 
-// Two values scaled and rounded into half HI of `old`.  The hardware rounds to
-// nearest even and turns what is past 464, infinities and NaN into NaN; finite
-// values past 448, which only the largest scale leaves, saturate (FULL).
-template <bool HI, bool FULL>
-__device__ __forceinline__ uint32_t pack2(float a, float b, float inv, uint32_t old) {
-  float x = a * inv, y = b * inv;
-  if (FULL && fabsf(a) < INFINITY) x = fminf(fmaxf(x, -448.0f), 448.0f);
-  if (FULL && fabsf(b) < INFINITY) y = fminf(fmaxf(y, -448.0f), 448.0f);
-  return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(x, y, (int)old, HI);
-}
-template <bool FULL>
-__device__ __forceinline__ uint32_t pack4(const float* x, float inv) {
-  return pack2<true, FULL>(x[2], x[3], inv, pack2<false, FULL>(x[0], x[1], inv, 0u));
+// Four values scaled and rounded.  The hardware rounds to nearest even and turns
+// what is past 464, infinities and NaN into NaN.
+__device__ __forceinline__ uint32_t pack4(float x0, float x1, float x2, float x3, float inv) {
+  const int lo = __builtin_amdgcn_cvt_pk_fp8_f32(x0 * inv, x1 * inv, 0, false);
+  return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(x2 * inv, x3 * inv, lo, true);
 }
 
 // The values of four stored bytes.
@@ -268,6 +260,21 @@ __device__ __forceinline__ uint32_t finite_peak(const Piece<T>& p) {  // the sam
   return m;
 }
 
+// Keeps what follows from being computed before here, where it would be held in
+// twice the registers.
+__device__ __forceinline__ void hold(Piece<bf16>& p) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) asm volatile("" : "+v"(p.w[i]));
+}
+__device__ __forceinline__ void hold(Piece<float>&) {}
+template <typename T>
+__device__ __forceinline__ void saturate(Piece<T>& p) {  // finite ones to 448 times the largest scale
+  const float lim = 448.0f * two_to(kExpMax);
+  auto of = [&](float x) { return fabsf(x) < INFINITY ? fminf(fmaxf(x, -lim), lim) : x; };
+#pragma unroll
+  for (int i = 0; i < 8; i += 2) p.set2(i, of(p.get(i)), of(p.get(i + 1)));
+}
+
 // One wave writes the keys or the values of one block of one head at a time:
 // lane (a, c) = (l / 8, l % 8) has dims 8 c .. + 7 of rows 8 a .. + 7, so that
 // eight loads bring the 64 rows, eight whole rows each; head_dim 72: lane l also
@@ -277,10 +284,13 @@ __device__ __forceinline__ uint32_t finite_peak(const Piece<T>& p) {  // the sam
 // rounded bytes are put in the tile's order in LDS and leave in 16-byte pieces.
 // Bound by bytes: a full step's rows in and tiles out, in a partial step also the
 // old tiles in.  A wave and not a workgroup per tile: a workgroup spends the way
-// of a row to its bytes on barriers.
+// of a row to its bytes on barriers.  bf16 has to fit 128 registers, so that four
+// waves per SIMD wait for memory at once: 9677 listed of 32256 tokens, 16 heads
+// of 64, caches not at hand: 56 -> 50 us; all of them: 55 -> 48.
 template <typename T, int HD>
-__global__ __launch_bounds__(kTPB, sizeof(T) == 2 ? 3 : 2) void k_kv8_store(Kv8Segs S, Kv8Slice c, Kv8Rows rows, const T* __restrict__ k,
-                                                       const T* __restrict__ v, int group, int units) {
+__global__ __launch_bounds__(kTPB, sizeof(T) == 2 ? 4 : 2)
+void k_kv8_store(Kv8Segs S, Kv8Slice c, Kv8Rows rows, const T* __restrict__ k, const T* __restrict__ v, int group,
+                 int units) {
   constexpr int NV = kKv8Block * HD / 16;  // 16-byte pieces of a tile
   __shared__ __attribute__((aligned(16))) uint4 images[4][NV];
   __shared__ __attribute__((aligned(16))) int maps[4][kKv8Block];
@@ -288,6 +298,10 @@ __global__ __launch_bounds__(kTPB, sizeof(T) == 2 ? 3 : 2) void k_kv8_store(Kv8S
   unsigned char* img = reinterpret_cast<unsigned char*>(images[wave]);
   int* row_at = maps[wave];
   const int a = lane >> 3, cc = lane & 7;
+  // Offsets in the tile, from which the others are constants further: 16 r of row
+  // 8 a + r, 512 g + 16 e of keys 8 a + 4 g .. + 3 of dim 8 c + e.
+  const int key0 = key_off(8 * a, cc >> 1) + 8 * (cc & 1), val0 = val_off(2 * a, 8 * cc);
+  const int key_tail = key_off(lane, 4), val_tail = val_off(lane >> 2, 64) + (lane & 3);
   auto body = [&](int hh, const Run& run) {
     const int h = hh >> 1;
     const bool values = (hh & 1) != 0;  // the same for the whole wave
@@ -319,7 +333,7 @@ __global__ __launch_bounds__(kTPB, sizeof(T) == 2 ? 3 : 2) void k_kv8_store(Kv8S
         if (!values) {
 #pragma unroll
           for (int r = 0; r < 8; ++r) {
-            const uint2 w = *reinterpret_cast<const uint2*>(img + key_off(8 * a + r, cc >> 1) + 8 * (cc & 1));
+            const uint2 w = *reinterpret_cast<const uint2*>(img + key0 + 16 * r);
             float t[8];
             unpack4(w.x, old, t);
             unpack4(w.y, old, t + 4);
@@ -328,7 +342,7 @@ __global__ __launch_bounds__(kTPB, sizeof(T) == 2 ? 3 : 2) void k_kv8_store(Kv8S
               for (int e = 0; e < 8; e += 2) p[r].set2(e, t[e], t[e + 1]);
           }
           if constexpr (HD == 72) {
-            const uint2 w = *reinterpret_cast<const uint2*>(img + key_off(lane, 4));
+            const uint2 w = *reinterpret_cast<const uint2*>(img + key_tail);
             float t[8];
             unpack4(w.x, old, t);
             unpack4(w.y, old, t + 4);
@@ -342,8 +356,8 @@ __global__ __launch_bounds__(kTPB, sizeof(T) == 2 ? 3 : 2) void k_kv8_store(Kv8S
 #pragma unroll
             for (int g = 0; g < 2; ++g) {  // keys 8 a + 4 g .. + 3 of dims 8 c + e and the next
               float t[4], u[4];
-              unpack4(*reinterpret_cast<const uint32_t*>(img + val_off(2 * a + g, 8 * cc + e)), old, t);
-              unpack4(*reinterpret_cast<const uint32_t*>(img + val_off(2 * a + g, 8 * cc + e + 1)), old, u);
+              unpack4(*reinterpret_cast<const uint32_t*>(img + val0 + 512 * g + 16 * e), old, t);
+              unpack4(*reinterpret_cast<const uint32_t*>(img + val0 + 512 * g + 16 * e + 16), old, u);
 #pragma unroll
               for (int r = 0; r < 4; ++r)
                 if (js[4 * g + r] < 0) p[4 * g + r].set2(e, t[r], u[r]);
@@ -353,7 +367,7 @@ __global__ __launch_bounds__(kTPB, sizeof(T) == 2 ? 3 : 2) void k_kv8_store(Kv8S
               float t[8];
 #pragma unroll
               for (int e = 0; e < 8; ++e)
-                t[e] = __builtin_amdgcn_cvt_pk_f32_fp8((int)img[val_off(lane >> 2, 64 + e) + (lane & 3)], false)[0] * old;
+                t[e] = __builtin_amdgcn_cvt_pk_f32_fp8((int)img[val_tail + 16 * e], false)[0] * old;
 #pragma unroll
               for (int e = 0; e < 8; e += 2) pt.set2(e, t[e], t[e + 1]);
             }
@@ -376,11 +390,12 @@ __global__ __launch_bounds__(kTPB, sizeof(T) == 2 ? 3 : 2) void k_kv8_store(Kv8S
     const int b = scale_byte(__uint_as_float(top));
     const float inv = two_to(127 - b);
     if (lane == 0) *sc = (unsigned char)b;
-    const bool full = b == kExpMax + 127;  // only this scale leaves finite values past 448
-    auto pack = [&](float x0, float x1, float x2, float x3) -> uint32_t {
-      const float x[4] = {x0, x1, x2, x3};
-      return full ? pack4<true>(x, inv) : pack4<false>(x, inv);
-    };
+    if (b == kExpMax + 127) {  // only this scale leaves finite values past 448 (rare)
+#pragma unroll
+      for (int r = 0; r < 8; ++r) saturate(p[r]);
+      if constexpr (HD == 72) saturate(pt);
+    }
+    auto pack = [&](float x0, float x1, float x2, float x3) { return pack4(x0, x1, x2, x3, inv); };
     auto put_key = [&](int off, const Piece<T>& q) {
       *reinterpret_cast<uint2*>(img + off) = make_uint2(pack(q.get(0), q.get(1), q.get(2), q.get(3)),
                                                         pack(q.get(4), q.get(5), q.get(6), q.get(7)));
@@ -388,19 +403,23 @@ __global__ __launch_bounds__(kTPB, sizeof(T) == 2 ? 3 : 2) void k_kv8_store(Kv8S
     lds_order();
     if (!values) {
 #pragma unroll
-      for (int r = 0; r < 8; ++r) put_key(key_off(8 * a + r, cc >> 1) + 8 * (cc & 1), p[r]);
-      if constexpr (HD == 72) put_key(key_off(lane, 4), pt);
+      for (int r = 0; r < 8; ++r) hold(p[r]);
+#pragma unroll
+      for (int r = 0; r < 8; ++r) put_key(key0 + 16 * r, p[r]);
+      if constexpr (HD == 72) put_key(key_tail, pt);
     } else {
+#pragma unroll
+      for (int r = 0; r < 8; ++r) hold(p[r]);
 #pragma unroll
       for (int e = 0; e < 8; ++e)
 #pragma unroll
         for (int g = 0; g < 2; ++g)
-          *reinterpret_cast<uint32_t*>(img + val_off(2 * a + g, 8 * cc + e)) =
+          *reinterpret_cast<uint32_t*>(img + val0 + 512 * g + 16 * e) =
               pack(p[4 * g].get(e), p[4 * g + 1].get(e), p[4 * g + 2].get(e), p[4 * g + 3].get(e));
       if constexpr (HD == 72)
 #pragma unroll
         for (int e = 0; e < 8; ++e)
-          img[val_off(lane >> 2, 64 + e) + (lane & 3)] = (unsigned char)pack(pt.get(e), 0.0f, 0.0f, 0.0f);
+          img[val_tail + 16 * e] = (unsigned char)pack(pt.get(e), 0.0f, 0.0f, 0.0f);
     }
     lds_order();
     for (int i = lane; i < NV; i += kWave) reinterpret_cast<uint4*>(tile)[i] = images[wave][i];
