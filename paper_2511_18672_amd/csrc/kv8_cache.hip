@@ -286,7 +286,7 @@ __device__ __forceinline__ void saturate(Piece<T>& p) {  // finite ones to 448 t
 // old tiles in.  A wave and not a workgroup per tile: a workgroup spends the way
 // of a row to its bytes on barriers.  bf16 has to fit 128 registers, so that four
 // waves per SIMD wait for memory at once: 9677 listed of 32256 tokens, 16 heads
-// of 64, caches not at hand: 56 -> 50 us; all of them: 55 -> 48.
+// of 64, caches not at hand: 56 -> 44, with the old tile past the registers us; all of them: 55 -> 48.
 template <typename T, int HD>
 __global__ __launch_bounds__(kTPB, sizeof(T) == 2 ? 4 : 2)
 void k_kv8_store(Kv8Segs S, Kv8Slice c, Kv8Rows rows, const T* __restrict__ k, const T* __restrict__ v, int group,
@@ -316,9 +316,11 @@ void k_kv8_store(Kv8Segs S, Kv8Slice c, Kv8Rows rows, const T* __restrict__ k, c
       for (int r = 0; r < 8; ++r) p[r].load(row + r * rows.ld);
       if constexpr (HD == 72) pt.load(src + (run.first + lane) * rows.ld + 64);
     } else {
-      // (held in registers until the rows are asked for, the old tile costs more than
-      // the wait for it: 30 % of 32256 tokens, 16 heads, with read-back 88 -> 98 us)
-      for (int i = lane; i < NV; i += kWave) images[wave][i] = reinterpret_cast<const uint4*>(tile)[i];
+      // the old tile goes straight to LDS while the rows are looked for
+#pragma unroll
+      for (int i = 0; i < NV; i += kWave)
+        if (i + kWave <= NV || lane < NV - i)
+          lds_dma16_at(tile, (uint32_t)(i + lane) * 16, &images[wave][i]);
       const float old = __uint_as_float((uint32_t)*sc << 23);
       map_rows(S, rows, run, row_at);
       lds_order();
@@ -329,6 +331,7 @@ void k_kv8_store(Kv8Segs S, Kv8Slice c, Kv8Rows rows, const T* __restrict__ k, c
       for (int r = 0; r < 8; ++r) p[r].load(src + max(js[r], 0) * rows.ld + 8 * cc);
       const int jt = row_at[lane];
       if constexpr (HD == 72) pt.load(src + max(jt, 0) * rows.ld + 64);
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // the old tile is in LDS
       if (__ballot(jt < 0) != 0) {
         if (!values) {
 #pragma unroll
