@@ -453,7 +453,9 @@ sphinx_status sphinx_kv8_load(sphinx_dtype dtype, int32_t kv_heads, int32_t head
  * 256-byte aligned, sphinx_kv8_attention_workspace_bytes bytes (which covers
  * every kv_len), not shared with work that may run at the same time.  Enqueues
  * a kernel or two, synchronizes nothing and may be captured in a graph.  Sums
- * stay finite for values up to 2^90 in magnitude. */
+ * stay finite for values up to 2^64 in magnitude.  Scores q.k past the range of
+ * f32: -inf weighs nothing, +inf and NaN make their query's o NaN, and so does a
+ * query whose scores are all -inf. */
 sphinx_status sphinx_kv8_attention_workspace_bytes(sphinx_dtype dtype, int32_t heads, int32_t kv_heads,
                                                    int32_t head_dim, const int32_t* cu_q, const int32_t* cu_kv,
                                                    int32_t nseg, size_t* bytes);

@@ -2,6 +2,8 @@
 // query head o = sum_t 2^(q.k_t) v_t / sum_t 2^(q.k_t) over the segment's cached
 // tokens, keys and values being the numbers that the cache's bytes stand for.
 
+#include <cfloat>
+
 #include <algorithm>
 #include <type_traits>
 
@@ -529,7 +531,7 @@ __global__ __launch_bounds__(kTPB, 3) void k_kv8_attn_tiles(Kv8Attn A, Kv8Slice 
     }
 #pragma unroll
     for (int r = 0; r < 16; ++r)
-      a[r] = t == nkt - 1 && 32 * rb + (r >> 2) * 8 + g * 4 + (r & 3) >= last ? -INFINITY : a[r] - m_run;
+      a[r] = t == nkt - 1 && 32 * rb + (r >> 2) * 8 + g * 4 + (r & 3) >= last ? -INFINITY : a[r];
     return a;
   };
   // Moves the maximum to block t's where that is larger; O holds the blocks up to t - 1.
@@ -542,11 +544,11 @@ __global__ __launch_bounds__(kTPB, 3) void k_kv8_attn_tiles(Kv8Attn A, Kv8Slice 
       for (int r = 0; r < 16; ++r) mx = fmaxf(mx, a[r]);
     }
     mx = fmaxf(mx, __shfl_xor(mx, 32, kWave));
-    const float delta = mx > 0.0f ? mx : 0.0f, alpha = fast_exp2(-delta);
+    const float to = fmaxf(m_run, mx), alpha = fast_exp2(m_run - to);
 #pragma unroll
     for (int db = 0; db < DB; ++db) oacc[db] *= alpha;
     l_run *= alpha;
-    m_run += delta;
+    m_run = to;
     shifted = true;
     float psum = 0.0f;
     bf16x8 q0[2], q1[2];
@@ -557,8 +559,8 @@ __global__ __launch_bounds__(kTPB, 3) void k_kv8_attn_tiles(Kv8Attn A, Kv8Slice 
 #pragma unroll
       for (int r = 0; r < 16; r += 2) {
         bf16x2 pr;
-        pr[0] = (bf16)fast_exp2(a[r]);
-        pr[1] = (bf16)fast_exp2(a[r + 1]);
+        pr[0] = (bf16)fast_exp2(a[r] - to);
+        pr[1] = (bf16)fast_exp2(a[r + 1] - to);
         psum = add_pair(psum, pr);
         x[r >> 3][r & 7] = pr[0];
         x[r >> 3][(r & 7) + 1] = pr[1];
@@ -730,7 +732,7 @@ __global__ __launch_bounds__(kTPB, 3) void k_kv8_attn_tiles(Kv8Attn A, Kv8Slice 
     {
       const float mx = row_max(a0, a1);
       shifted = __ballot(!(mx >= -24.0f && mx <= 24.0f)) != 0;
-      m_run = shifted && mx > -INFINITY ? mx : 0.0f;
+      m_run = !shifted ? 0.0f : mx > -INFINITY ? mx : -FLT_MAX;  // any score above it moves it
     }
     barrier();  // every wave is done with keys 0, whose slot takes keys 2
     bf16x8 pa[2][2] = {{zero8, zero8}, {zero8, zero8}}, pb[2][2];

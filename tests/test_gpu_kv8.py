@@ -290,6 +290,31 @@ def test_attention_of_large_and_small_scores(dtype, d, nq, size, shift):
     check_attention(c, q, 1, [0, nq])
 
 
+@pytest.mark.parametrize("dtype,d", [("bf16", 64), ("bf16", 72), ("f32", 64)])
+@pytest.mark.parametrize("nq", [1, 300])
+@pytest.mark.parametrize("low", [-(2.0 ** 100), -(2.0 ** 127)])
+@pytest.mark.parametrize("at", [0, 64, 320])
+def test_attention_of_a_block_whose_scores_are_far_below(dtype, d, nq, low, at):
+    """One block's scores are about -2^101 or past f32's range (-inf), all others of a row -192, -208 or -224: what a
+    score is taken relative to moves between them exactly, wherever that block stands."""
+    rng = np.random.default_rng(33)
+    nk = 400
+    c = Cache(1, d, [0, nk])
+    k = torch.zeros(nk, 1, d)
+    k[:, 0, 0] = torch.tensor([-192.0, -208.0, -224.0])[torch.arange(nk) % 3] / 2  # exact in 8 bits
+    k[at:at + 64, 0, 0] = low
+    v = rows_of(rng, nk, 1, d, dtype)
+    c.store(k.to(TDT[dtype]).cuda(), v)
+    q = torch.zeros(nq, d, dtype=TDT[dtype], device="cuda")
+    q[:, 0] = 2.0
+    assert (c.k[at:at + 64, 0, 0] == low).all() and c.k[(at + 64) % nk, 0, 0] > -113.0
+    ref, mag, _ = O.kv8.attention(f64(q).reshape(nq, 1, d), c.k, c.v, [0, nq], c.bounds)
+    o = f64(attend(c, q, 1, [0, nq])).reshape(nq, 1, d)
+    # the scores that weigh are exact
+    err = np.abs(o - ref) - tolerance(dtype, ref, mag, np.zeros_like(mag), nk, d)
+    assert np.isfinite(o).all() and err.max() <= 0.0
+
+
 def test_attention_strided_queries():
     rng = np.random.default_rng(23)
     c = filled(rng, 2, 64, [0, 300])
