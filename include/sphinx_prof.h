@@ -39,7 +39,7 @@ typedef SPHINX_ENUM {
   SPHINX_K_GEMM_MLP2,
   SPHINX_K_FINAL,      /* final LayerNorm + projection + DDIM update */
   SPHINX_K_SCATTER,
-  SPHINX_K_KV_STORE,   /* latent cache store of the forwarded rows' keys and values */
+  SPHINX_K_KV_STORE,   /* latent cache store of the forwarded rows' keys and values; the 8-bit cache: its read-back too */
   SPHINX_K_FRONTEND,   /* mask front-end (four or five kernels, one bracket) */
   SPHINX_K_COUNT
 } sphinx_kernel_class;

@@ -386,8 +386,10 @@ def _here(stream, *tensors) -> Optional[int]:
 
 
 def _check_idx(idx, n: int):
-    if idx is not None and (idx.element_size() != 4 or idx.is_floating_point() or idx.numel() < n):
-        raise ValueError(f"idx holds {idx.numel()} values of {idx.dtype}, {n} int32 are needed")
+    if idx is not None and (idx.element_size() != 4 or idx.is_floating_point() or idx.numel() < n
+                            or not idx.is_contiguous()):
+        raise ValueError(f"idx holds {idx.numel()} values of {idx.dtype}, strides {idx.stride()}; "
+                         f"{n} int32 in a row are needed")
 
 
 def sphinx_kv8_bytes(kv_heads: int, head_dim: int, cu_kv) -> int:

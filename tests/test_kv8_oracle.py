@@ -128,6 +128,20 @@ def test_store_and_load_refusals(L, load):
     assert call(cu=_cu(0, 0), n=5, k=None, v=None, c=None) == OK  # no tokens: every row is skipped
 
 
+@pytest.mark.parametrize("call", ["store", "load"])
+def test_index_tensors_that_are_not_int32_in_a_row_are_refused(call):
+    torch = pytest.importorskip("torch")
+    from paper_2511_18672_amd import binding as B
+    rows, cache = torch.zeros(8, 64), torch.zeros(8192, dtype=torch.uint8)
+    good = torch.arange(8, dtype=torch.int32)
+    for idx in (good.long(), good.float(), good[:7], torch.arange(16, dtype=torch.int32)[::2]):
+        with pytest.raises(ValueError, match="int32"):
+            if call == "store":
+                B.sphinx_kv8_store(B.F32, 1, 64, rows, rows, 64, idx, 8, [0, 64], cache)
+            else:
+                B.sphinx_kv8_load(B.F32, 1, 64, cache, [0, 64], idx, 8, rows, rows, 64)
+
+
 def test_attention_refusals(L):
     P = ctypes.c_void_p
     need = ctypes.c_size_t()
