@@ -491,15 +491,23 @@ hipError_t by_type(sphinx_dtype dt, int head_dim, const F& go) {
 }
 
 // Rows that a worker looks at (a wave when storing, a workgroup when reading
-// back): as many as leave `workers` of them, at most 16.  Listed rows mostly come
-// in runs, and a worker without a run's first row has nothing to do.
+// back): as many as leave `workers` of them, at most `most`.  Listed rows mostly
+// come in runs, and a worker without a run's first row has nothing to do; one
+// with several does them one after the other.  16 heads of 64, bf16, 32256 tokens:
+// storing 3 % in runs of 16 takes 14.3 us with 16384 workers, 8.7 with 4096 and
+// 8.3 with 2048, which take 39.8 instead of 31.5 where the 3 % are scattered; 90 %
+// in runs of 64 take 34.1 us with 16 rows each, 29.2 with 32, 30 % in runs of 8
+// 32.9, 33.7, and 36.9 with 64.  Reading back those 90 % takes 49.4 us with 16 rows
+// each, 39.4 with 32, 35.4 with 64, scattered 3 % 12.0 us with 2048 workers and
+// 17.1 with 8192.
 struct Split {
   int group, units;
   unsigned grid;
 };
-Split split(int parts, int64_t nblk, const Kv8Rows& rows, int workers, int per) {  // parts: tiles or heads of a block
+Split split(int parts, int64_t nblk, const Kv8Rows& rows, int workers, int most,
+            int per) {  // parts: tiles or heads of a block
   Split p;
-  p.group = (int)std::clamp<int64_t>((int64_t)rows.n * parts / workers, 1, 16);
+  p.group = (int)std::clamp<int64_t>((int64_t)rows.n * parts / workers, 1, most);
   p.units = rows.idx ? (int)(((int64_t)rows.n + p.group - 1) / p.group) : (int)nblk;
   p.grid = (unsigned)std::min<int64_t>(((int64_t)p.units * parts + per - 1) / per, 1 << 20);  // each then takes several
   return p;
@@ -508,7 +516,7 @@ Split split(int parts, int64_t nblk, const Kv8Rows& rows, int workers, int per) 
 
 hipError_t launch_kv8_store(sphinx_dtype dt, int head_dim, const Kv8Segs& S, const Kv8Slice& c, const Kv8Rows& rows,
                             const void* k, const void* v, hipStream_t s) {
-  const Split p = split(2 * c.kv_heads, c.nblk, rows, 16384, 4);
+  const Split p = split(2 * c.kv_heads, c.nblk, rows, 4096, 32, 4);
   return by_type(dt, head_dim, [&](auto t, auto hd) {
     using T = decltype(t);
     k_kv8_store<T, decltype(hd)::value><<<p.grid, kTPB, 0, s>>>(S, c, rows, static_cast<const T*>(k),
@@ -518,7 +526,7 @@ hipError_t launch_kv8_store(sphinx_dtype dt, int head_dim, const Kv8Segs& S, con
 
 hipError_t launch_kv8_load(sphinx_dtype dt, int head_dim, const Kv8Segs& S, const Kv8Slice& c, const Kv8Rows& rows,
                            void* k, void* v, hipStream_t s) {
-  const Split p = split(c.kv_heads, c.nblk, rows, 2048, 1);
+  const Split p = split(c.kv_heads, c.nblk, rows, 2048, 64, 1);
   return by_type(dt, head_dim, [&](auto t, auto hd) {
     using T = decltype(t);
     k_kv8_load<T, decltype(hd)::value>

@@ -165,6 +165,32 @@ def test_listed_whole_blocks(idx, bounds):
     assert np.array_equal(f64(v).reshape(-1, 3, 72)[inside], c.v[idx[inside]])
 
 
+@pytest.mark.parametrize("heads,d", [(32, 64), (24, 72)])
+def test_many_listed_rows_of_many_heads(heads, d):
+    """Enough rows that a worker looks at 32 of them (storing) and at 64 (reading back): whole blocks, runs that start
+    and end anywhere, single and repeated tokens, tokens in front of the slice and behind it."""
+    rng = np.random.default_rng(13)
+    bounds = [0, 1000, 1001, 4097, 7000]
+    some = np.flatnonzero(np.repeat(rng.random(1001) < 0.4, 7)[:7000])
+    runs = np.r_[0:64, 70:200, 1000:1001, 1001:1193, 1200:1264, 1265:4097, 4097:4161, 4170:6990]
+    c = Cache(heads, d, bounds)
+    k, v = (torch.randn(7000, heads * d, device="cuda").bfloat16() for _ in range(2))
+    c.store(k, v, np.arange(7000))
+    for idx in (runs, np.r_[-2, -1, np.repeat(some, 1 + (rng.random(some.size) < 0.1)), 7000, 7003]):
+        n = len(idx)
+        k, v = (torch.randn(n, heads * d, device="cuda").bfloat16() * 3 for _ in range(2))
+        keep = (idx >= 0) & (idx < 7000)
+        i = torch.from_numpy(idx.astype(np.int32)).cuda()
+        B.sphinx_kv8_store(B.BF16, heads, d, k, v, heads * d, i, n, bounds, c.slice)
+        for name, x in (("k", k), ("v", v)):  # the last of repeated tokens counts, as numpy assigns
+            setattr(c, name, O.kv8.write(getattr(c, name), f64(x).reshape(n, heads, d)[keep], idx[keep], bounds))
+        c.check("bf16")
+        ko, vo = c.load("bf16", idx)
+        for out, held in ((ko, c.k), (vo, c.v)):
+            assert np.array_equal(f64(out)[keep].reshape(-1, heads, d), held[idx[keep]])
+            assert (out[torch.from_numpy(~keep).cuda()] == 7).all()
+
+
 def test_load_some_rows():
     rng = np.random.default_rng(9)
     for heads, d, dtype in ((3, 64, "f32"), (2, 72, "bf16")):
