@@ -91,6 +91,10 @@ __device__ __forceinline__ void operand(const uint4& b, float (&f)[16]) {  // wi
 // rounded (the keys' scale goes into the exponent, the values' into P: a
 // product per byte between its conversion and its matrix instruction kept the
 // two from overlapping).
+// bf16 is bound by the cache's bytes: one query against 2^20 keys of 4 heads takes
+// 92 us (5.8 TB/s), 48 sequences of 32 heads on 4 70 us.  f32 is bound by the matrix
+// instructions, next to which little else is issued: 1024 queries against 2048
+// keys of 8 heads 44 us, 4000 against 4000 296 us (111 TFLOP/s).
 template <typename T, int HD, int WAVES>
 __global__ __launch_bounds__(64 * WAVES, sizeof(T) == 2 && HD == 64 && WAVES == 4 ? 3 : 2) void k_kv8_attn_rows(Kv8Attn A, Kv8Slice c, Kv8Plan P, Parts part, int first) {
   constexpr bool F32 = sizeof(T) == 4;
@@ -330,6 +334,10 @@ __global__ __launch_bounds__(64 * WAVES, sizeof(T) == 2 && HD == 64 && WAVES == 
 //    a block's probabilities sum past 2^32; then m moves to that block's
 //    maximum, O and l are rescaled and the block's probabilities are made again
 //    from its bytes.
+// Bound by the chip's power: 9677 queries against 32256 keys of 16 heads take 1.23 ms
+// (1040 TFLOP/s) at 1.70 GHz, matrix cores busy for 51 % of the cycles; 645 queries
+// 103 us at 2.1 GHz and 38 %; head_dim 72 runs at 1.9 GHz and 53 %, a fifth of its
+// products on padding.
 template <int HD>
 struct TileGeo {
   static constexpr int DB = (HD + 31) / 32;   // 32-row blocks of O^T (head_dim 72: of the third, 8 rows count)
@@ -829,7 +837,8 @@ __global__ __launch_bounds__(kTPB, 3) void k_kv8_attn_tiles(Kv8Attn A, Kv8Slice 
 // many chunks) a workgroup of 16 waves, wave w taking chunks w (mod 16).  A
 // lane has one dim; at head_dim 72 eight lanes have a second one.  Bound by the
 // latency of the loads: a wave asks for the maxima, sums and values of eight
-// chunks at once and joins them as it goes.
+// chunks at once and joins them as it goes.  645 queries of 16 heads in eight chunks
+// take 9 us (42 MB moved, mostly through the last-level cache).
 template <typename T, int HD, int WAVES>
 __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void k_kv8_attn_join(Kv8Attn A, int kv_heads, Kv8Plan P, Parts part, int rows) {
   __shared__ float sO[WAVES][HD], sL[WAVES], sM[WAVES];

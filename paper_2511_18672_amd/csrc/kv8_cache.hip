@@ -432,7 +432,8 @@ void k_kv8_store(Kv8Segs S, Kv8Slice c, Kv8Rows rows, const T* __restrict__ k, c
 
 // One workgroup reads the listed rows of one block of one head at a time: the
 // value tile comes into LDS in consecutive 16-byte pieces, a thread takes eight
-// dims of a row.  Bound by bytes.  (A wave per tile, as in the store, was no
+// dims of a row.  Bound by bytes: 32256 tokens of 16 heads of 64 take 30 us (198 MB,
+// 6.6 TB/s, part of it in the last-level cache).  (A wave per tile, as in the store, was no
 // faster: all of 32256 tokens of 16 heads 45 us against 42, 1905 rows 22 us
 // against 17.)
 template <typename T, int HD>
