@@ -92,10 +92,12 @@ __device__ __forceinline__ int xcd_tile(int b, int total) {
 // before their first use.  Callers order the copies themselves: each wave
 // waits for its copies (s_waitcnt vmcnt) before the barrier that publishes
 // them.  The compiler's own vmcnt waits stay correct, since copies it does
-// not see only make them stricter.
+// not see only make them stricter.  An instruction has to stand between the write
+// of M0 and the copy that takes its place from it; the compiler puts one there for
+// the builtin only.
 __device__ __forceinline__ void lds_dma16(const void* gsrc, const void* lds_dst) {
   const uint32_t m0 = (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) char*)lds_dst;
-  asm volatile("s_mov_b32 m0, %1\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(gsrc), "s"(m0) : "memory", "m0");
+  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(gsrc), "s"(m0) : "memory", "m0");
 }
 
 // The same copy from a wave-uniform base address (an SGPR pair) plus a
@@ -103,7 +105,7 @@ __device__ __forceinline__ void lds_dma16(const void* gsrc, const void* lds_dst)
 // arithmetic only.
 __device__ __forceinline__ void lds_dma16_at(const void* sbase, uint32_t voff, const void* lds_dst) {
   const uint32_t m0 = (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) char*)lds_dst;
-  asm volatile("s_mov_b32 m0, %2\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(voff), "s"(sbase), "s"(m0)
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(voff), "s"(sbase), "s"(m0)
                : "memory", "m0");
 }
 
