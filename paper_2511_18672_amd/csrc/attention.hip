@@ -156,14 +156,6 @@ struct Smem {
   char pad[Geo<HD>::PAD + 16];
 };
 
-// acc + p.x + p.y as one v_dot2c with (1, 1) in bf16.  A volatile statement,
-// so that each step's dot product stays in its step: as plain arithmetic the
-// compiler gathers the sixteen of a tile into one chain after the last MFMA.
-__device__ __forceinline__ float rowsum_add(float acc, bf16x2 p) {
-  asm volatile("v_dot2c_f32_bf16_e32 %0, 0x3f803f80, %1" : "+v"(acc) : "v"(__builtin_bit_cast(unsigned, p)));
-  return acc;
-}
-
 __device__ __forceinline__ bf16x8 tr_pair(const char* p0, const char* p1) {
   const v4s a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s*)p0);
   const v4s b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s*)p1);
@@ -342,7 +334,7 @@ __device__ __forceinline__ void region(const char* sK, const char* sV, const Lan
       bf16x2 pr;
       pr[0] = (bf16)ex[st][0];
       pr[1] = (bf16)ex[st][1];
-      psum = rowsum_add(psum, pr);
+      psum = add_pair(psum, pr);
       pn[w][hf][2 * i] = pr[0];
       pn[w][hf][2 * i + 1] = pr[1];
     }

@@ -109,6 +109,19 @@ __device__ __forceinline__ void lds_dma16_at(const void* sbase, uint32_t voff, c
                : "memory", "m0");
 }
 
+// acc + p.x + p.y as one v_dot2c with (1, 1) in bf16.  The empty statement keeps
+// each step's dot product in its step: as plain arithmetic the compiler gathers
+// the sixteen of a tile into one chain after the last MFMA.  The product itself is
+// the builtin, since its sum takes three slots to be there for any other
+// instruction (an overflow check, say): the compiler leaves them free behind the
+// builtin, and does not behind an instruction in inline assembly.
+__device__ __forceinline__ float add_pair(float acc, bf16x2 p) {
+  const bf16x2 ones = {(bf16)1.0f, (bf16)1.0f};
+  acc = __builtin_amdgcn_fdot2_f32_bf16(p, ones, acc, false);
+  asm volatile("" : "+v"(acc));
+  return acc;
+}
+
 __device__ __forceinline__ float bf2f(bf16 v) { return (float)v; }
 __device__ __forceinline__ bf16 f2bf(float v) { return (bf16)v; }  // round to nearest even
 

@@ -354,11 +354,6 @@ struct TileSmem {
 };
 constexpr float kPsumMax = 4294967296.0f;  // 2^32
 
-// acc + p.x + p.y; volatile, so that it stays in its step
-__device__ __forceinline__ float add_pair(float acc, bf16x2 p) {
-  asm volatile("v_dot2c_f32_bf16_e32 %0, 0x3f803f80, %1" : "+v"(acc) : "v"(__builtin_bit_cast(unsigned, p)));
-  return acc;
-}
 __device__ __forceinline__ bf16x2 cvt2(uint32_t w, float scale, bool hi) {
   return hi ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, scale, true)
             : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, scale, false);

@@ -1,0 +1,56 @@
+"""The 8-bit key/value cache through the C ABI: sums that overflow late in a block."""
+import numpy as np
+import pytest
+
+import oracle as O
+
+torch = pytest.importorskip("torch")
+S = pytest.importorskip("paper_2511_18672_amd")
+B = S.binding
+
+from test_gpu_kv8 import TDT, Cache, attend, f64, rows_of, tolerance  # noqa: E402
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("dtype,d", [("bf16", 64), ("bf16", 72), ("f32", 64)])
+@pytest.mark.parametrize("nq", [1, 300])
+@pytest.mark.parametrize("score", [34.0, 192.0])
+def test_one_late_key_of_a_block_that_outweighs_all_others(dtype, d, nq, score):
+    """Scores are 0 but for one token's: 2^192 is past f32's range, 2^34 only past what a block's weights may sum to.
+    The tokens are those whose weights are added last, in a block in front of others and in a segment's last one."""
+    rng = np.random.default_rng(41)
+    for t in (58, 59, 62, 63):
+        for at in (64 + t, 5 * 64 + t):
+            c = Cache(1, d, [0, 384])
+            k = torch.zeros(384, 1, d)
+            k[at, 0, 0] = 32.0 if score < 100 else 192.0  # exact in 8 bits
+            c.store(k.to(TDT[dtype]).cuda(), rows_of(rng, 384, 1, d, dtype))
+            q = torch.zeros(nq, d, dtype=TDT[dtype], device="cuda")
+            q[:, 0] = score / float(k[at, 0, 0])
+            ref, mag, _ = O.kv8.attention(f64(q).reshape(nq, 1, d), c.k, c.v, [0, nq], c.bounds)
+            o = f64(attend(c, q, 1, [0, nq])).reshape(nq, 1, d)
+            err = np.abs(o - ref) - tolerance(dtype, ref, mag, np.zeros_like(mag), 384, d)  # scores are exact
+            assert np.isfinite(o).all() and err.max() <= 0.0, (t, at)
+
+
+@pytest.mark.parametrize("d", [64, 72])
+@pytest.mark.parametrize("score", [66.0, 192.0])
+def test_one_late_key_of_a_block_in_16_bit_attention(d, score):
+    """The same through sphinx_varlen_attention."""
+    rng = np.random.default_rng(42)
+    v = rows_of(rng, 384, 1, d, "bf16").view(384, d)
+    q = torch.zeros(300, d, dtype=torch.bfloat16, device="cuda")
+    q[:, 0] = 1.0
+    for t in range(50, 64):
+        for at in (64 + t, 5 * 64 + t):
+            k = torch.zeros(384, d, dtype=torch.bfloat16, device="cuda")
+            k[at, 0] = score
+            o = torch.empty_like(q)
+            B.sphinx_varlen_attention(B.BF16, 1, d, q, d, k, v, d, o, [0, 300], [0, 384])
+            shape = (-1, 1, d)
+            ref, mag, _ = O.kv8.attention(f64(q).reshape(shape), f64(k).reshape(shape), f64(v).reshape(shape), [0, 300],
+                                          [0, 384])
+            o = f64(o).reshape(shape)
+            err = np.abs(o - ref) - tolerance("bf16", ref, mag, np.zeros_like(mag), 384, d)
+            assert np.isfinite(o).all() and err.max() <= 0.0, (t, at)
