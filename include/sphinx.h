@@ -446,8 +446,10 @@ sphinx_status sphinx_kv8_load(sphinx_dtype dtype, int32_t kv_heads, int32_t head
  * zeros.  heads is a multiple of kv_heads; query head h uses key/value head
  * h / (heads / kv_heads).  q (dev, row j at element j*ldq) must already be
  * multiplied by log2(e)/sqrt(d).
- *   dtype: SPHINX_BF16 (head_dim 64 or 72; probabilities rounded to bf16, sums
- *          in fp32, o rounded to bf16) or SPHINX_F32 (head_dim 64).
+ *   dtype: SPHINX_BF16 (head_dim 64 or 72; sums in fp32, o rounded to bf16;
+ *          probabilities rounded to bf16 as in sphinx_varlen_attention, or to 16
+ *          bits where few queries share a segment and key/value head) or
+ *          SPHINX_F32 (head_dim 64).
  * o: dev, row j at element j*heads*head_dim.  ldq >= heads*head_dim and a
  * multiple of 8; heads*head_dim <= 65536; pointers 16-byte aligned.  ws: dev,
  * 256-byte aligned, sphinx_kv8_attention_workspace_bytes bytes (which covers

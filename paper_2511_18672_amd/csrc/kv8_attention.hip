@@ -86,8 +86,12 @@ __device__ __forceinline__ void operand(const uint4& b, float (&f)[16]) {  // wi
 //  * P^T needs no move: score register 8 hf + j of tile kb belongs to the key
 //    that byte 8 hf + j of the values' chunk (db, kb) holds;
 //  * O^T = V^T P^T leaves the row on the lane.
-// bf16: 32x32x16 products, P rounded to bf16 for the product, the row sum adding
-// the same rounded values; f32: 32x32x2 products of the unscaled bytes, nothing
+// bf16: 32x32x16 products, P as the sum of two bf16 numbers, which is off by at most
+// 2^-15 of it, so that o's own rounding is all that a result shows.  (One bf16 number
+// costs errors of 1.2e-3 to 1.5e-3 beside o's 1.7e-3 and saves half of the V^T P^T
+// products and the splitting, next to which the bytes come: one query against 2^20
+// keys 102.5 instead of 105.2 us, 32 queries of 16 heads against 32256 keys 22.9
+// instead of 24.3, one against 1500 8.7 instead of 9.8.)  f32: 32x32x2 products of the unscaled bytes, nothing
 // rounded (the keys' scale goes into the exponent, the values' into P: a
 // product per byte between its conversion and its matrix instruction kept the
 // two from overlapping).
@@ -255,22 +259,29 @@ __global__ __launch_bounds__(64 * WAVES, sizeof(T) == 2 && HD == 64 && WAVES == 
           oacc[1] = __builtin_amdgcn_mfma_f32_32x32x2f32(v1[r], sc[kb][r], oacc[1], 0, 0, 0);
         }
       } else {
-        const bf16x2 ones = {(bf16)1.0f, (bf16)1.0f};
-        bf16x8 pf[2];
+        // p in two parts: its upper 16 bits, and the rest rounded to bf16
+        bf16x8 pf[2], pl[2];
 #pragma unroll
         for (int r = 0; r < 16; r += 2) {
-          const bf16x2 pr = {(bf16)fast_exp2(sc[kb][r] - at), (bf16)fast_exp2(sc[kb][r + 1] - at)};
-          ps = __builtin_amdgcn_fdot2_f32_bf16(pr, ones, ps, false);
-          pf[r >> 3][r & 7] = pr[0];
-          pf[r >> 3][(r & 7) + 1] = pr[1];
+          const float p0 = fast_exp2(sc[kb][r] - at), p1 = fast_exp2(sc[kb][r + 1] - at);
+          const uint32_t u0 = __float_as_uint(p0), u1 = __float_as_uint(p1);
+          const bf16x2 hi = __builtin_bit_cast(bf16x2, __builtin_amdgcn_perm(u1, u0, 0x07060302));
+          pf[r >> 3][r & 7] = hi[0];
+          pf[r >> 3][(r & 7) + 1] = hi[1];
+          pl[r >> 3][r & 7] = (bf16)(p0 - __uint_as_float(u0 & 0xffff0000u));
+          pl[r >> 3][(r & 7) + 1] = (bf16)(p1 - __uint_as_float(u1 & 0xffff0000u));
+          ps += p0;
+          ps += p1;
         }
 #pragma unroll
         for (int db = 0; db < DB; ++db) {
           bf16x8 vf[2];
           operand(vc[db][kb], vs, vf);
 #pragma unroll
-          for (int hf = 0; hf < 2; ++hf)
+          for (int hf = 0; hf < 2; ++hf) {
             oacc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[hf], pf[hf], oacc[db], 0, 0, 0);
+            oacc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[hf], pl[hf], oacc[db], 0, 0, 0);
+          }
         }
       }
     }
@@ -333,7 +344,11 @@ __global__ __launch_bounds__(64 * WAVES, sizeof(T) == 2 && HD == 64 && WAVES == 
 //    at 0 (or at the first block's maximum, if that is not in [-24, 24]) until
 //    a block's probabilities sum past 2^32; then m moves to that block's
 //    maximum, O and l are rescaled and the block's probabilities are made again
-//    from its bytes.
+//    from its bytes;
+//  * P is rounded to bf16, once for the product and for the row sum: in two parts,
+//    as the 32-row tiles take it, half as many products again would bound the
+//    kernel.  Against 64 bits o is off by 2.2e-3 of its size (rms); its own
+//    rounding gives 1.7e-3.
 // Bound by the chip's power: 9677 queries against 32256 keys of 16 heads take 1.23 ms
 // (1040 TFLOP/s) at 1.70 GHz, matrix cores busy for 51 % of the cycles; 645 queries
 // 103 us at 2.1 GHz and 38 %; head_dim 72 runs at 1.9 GHz and 53 %, a fifth of its

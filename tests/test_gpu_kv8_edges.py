@@ -1,4 +1,4 @@
-"""The 8-bit key/value cache through the C ABI: sums that overflow late in a block."""
+"""The 8-bit key/value cache through the C ABI: sums that overflow late in a block, and weights that bf16 misses."""
 import numpy as np
 import pytest
 
@@ -54,3 +54,26 @@ def test_one_late_key_of_a_block_in_16_bit_attention(d, score):
             o = f64(o).reshape(shape)
             err = np.abs(o - ref) - tolerance("bf16", ref, mag, np.zeros_like(mag), 384, d)
             assert np.isfinite(o).all() and err.max() <= 0.0, (t, at)
+
+
+@pytest.mark.parametrize("d,nq,nk", [(64, 1, 512), (64, 40, 512), (64, 3, 2100), (72, 2, 512), (72, 1, 2100)])
+def test_weights_of_few_queries_are_not_rounded_to_bf16(d, nq, nk):
+    """Half of the keys weigh 2^-s and have the value 1, half weigh 1 and have what 8 bits hold of -2^-s, so that o nearly
+    cancels and its own rounding is small: what is left is how far the weight 2^-s is off.  As a sum of two bf16 numbers it is off
+    by 2^-15 of itself at most (a part that bf16 cuts off is below 2^-7, and half a step of that is 2^-8 of it), which
+    moves o by half of it; bf16 alone misses some of these weights by 2^-9 and more."""
+    rng = np.random.default_rng(43)
+    for n16 in range(1, 16):
+        c = Cache(1, d, [0, nk])
+        k, v = torch.zeros(nk, 1, d), torch.zeros(nk, 1, d)
+        low = torch.from_numpy(rng.permutation(nk) % 2 == 0)
+        k[low, 0, 0] = -n16 / 16.0  # exact in 8 bits, and so are the scores
+        v[:] = torch.where(low, 1.0, -float(O.kv8.round_e4m3(2.0 ** (-n16 / 16.0))))[:, None, None]
+        c.store(k.bfloat16().cuda(), v.bfloat16().cuda())
+        q = torch.zeros(nq, d, dtype=torch.bfloat16, device="cuda")
+        q[:, 0] = 1.0
+        ref, mag, _ = O.kv8.attention(f64(q).reshape(nq, 1, d), c.k, c.v, [0, nq], c.bounds)
+        o = f64(attend(c, q, 1, [0, nq])).reshape(nq, 1, d)
+        # o's rounding, the weights' (numerator), the exponential's and the sums' in fp32
+        bound = 2.0 ** -8 * np.abs(ref) + (2.0 ** -15 + 2.02 * (2.0 ** -22 + (nk + 8) * 2.0 ** -24)) * mag
+        assert (np.abs(o - ref) <= bound).all(), (n16, np.abs(o - ref).max(), bound.max())
