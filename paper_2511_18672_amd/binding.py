@@ -367,7 +367,16 @@ def sphinx_refine_step_cached(desc: ModelDesc, reqs, idx, n: int, cu_host: np.nd
 
 
 def _host_cu(cu) -> np.ndarray:
-    return np.ascontiguousarray(cu, dtype=np.int32)
+    a = np.asarray(cu)
+    if a.dtype != np.int32:
+        if a.dtype.kind not in "iu":
+            raise ValueError(f"token bounds and counts are integers, not {a.dtype}")
+        if a.size and (int(a.min()) < -(1 << 31) or int(a.max()) >= 1 << 31):
+            raise ValueError("token bounds and counts do not fit 32 bits")
+        a = a.astype(np.int32)
+    if a.ndim != 1:
+        raise ValueError(f"token bounds and counts are a row of integers, not {a.shape}")
+    return a
 
 
 def _here(stream, *tensors) -> Optional[int]:
@@ -392,10 +401,31 @@ def _check_idx(idx, n: int):
                          f"{n} int32 in a row are needed")
 
 
+def _check_rows(name: str, t, dtype: int, n: int, ld: int, width: int):
+    """Refuses a tensor of another type than the code names, or without memory for n rows of `width` elements, each ld
+    behind the one before."""
+    import torch
+
+    if t.dtype is not (torch.bfloat16 if dtype == BF16 else torch.float32) and dtype in (F32, BF16):
+        raise ValueError(f"{name} is {t.dtype}, the call names another type")
+    need = (n - 1) * ld + width
+    if n > 0 and not (t.is_contiguous() and t.numel() >= need):
+        have = t.untyped_storage().nbytes() // t.element_size() - t.storage_offset()
+        if have < need:
+            raise ValueError(f"{name} has memory for {have} elements; {n} rows of {width}, each {ld} behind the one "
+                             f"before, take {need}")
+
+
+def _check_bytes(*tensors):
+    for t in tensors:
+        if not t.is_contiguous():
+            raise ValueError(f"slices and workspaces are bytes in a row, not strides {t.stride()}")
+
+
 def sphinx_kv8_bytes(kv_heads: int, head_dim: int, cu_kv) -> int:
     """Bytes of one slice of the 8-bit cache (cu_kv: host int sequence of token bounds, as in the calls below)."""
     cu, out = _host_cu(cu_kv), c_size_t()
-    _check("sphinx_kv8_bytes", lib().sphinx_kv8_bytes(kv_heads, head_dim, cu.ctypes.data, cu.size - 1,
+    _check("sphinx_kv8_bytes", lib().sphinx_kv8_bytes(kv_heads, head_dim, cu.tobytes(), cu.size - 1,
                                                       ctypes.byref(out)))
     return out.value
 
@@ -404,18 +434,24 @@ def sphinx_kv8_store(dtype: int, kv_heads: int, head_dim: int, k, v, ld: int, id
     """Quantises rows j < n of k and v into the slice `cache` (zeroed before its first use) at tokens idx[j]
     (ascending; None: token j)."""
     _check_idx(idx, n)
+    _check_rows("k", k, dtype, n, ld, kv_heads * head_dim)
+    _check_rows("v", v, dtype, n, ld, kv_heads * head_dim)
+    _check_bytes(cache)
     cu, s = _host_cu(cu_kv), _here(stream, k, v, idx, cache)
     _check("sphinx_kv8_store", lib().sphinx_kv8_store(
-        dtype, kv_heads, head_dim, k.data_ptr(), v.data_ptr(), ld, _ptr(idx), n, cu.ctypes.data, cu.size - 1,
+        dtype, kv_heads, head_dim, k.data_ptr(), v.data_ptr(), ld, _ptr(idx), n, cu.tobytes(), cu.size - 1,
         cache.data_ptr(), cache.nbytes, s))
 
 
 def sphinx_kv8_load(dtype: int, kv_heads: int, head_dim: int, cache, cu_kv, idx, n: int, k, v, ld: int, stream=None):
     """Rows j < n of k and v <- the values of tokens idx[j] (ascending; None: token j)."""
     _check_idx(idx, n)
+    _check_rows("k", k, dtype, n, ld, kv_heads * head_dim)
+    _check_rows("v", v, dtype, n, ld, kv_heads * head_dim)
+    _check_bytes(cache)
     cu, s = _host_cu(cu_kv), _here(stream, k, v, idx, cache)
     _check("sphinx_kv8_load", lib().sphinx_kv8_load(
-        dtype, kv_heads, head_dim, cache.data_ptr(), cache.nbytes, cu.ctypes.data, cu.size - 1, _ptr(idx), n,
+        dtype, kv_heads, head_dim, cache.data_ptr(), cache.nbytes, cu.tobytes(), cu.size - 1, _ptr(idx), n,
         k.data_ptr(), v.data_ptr(), ld, s))
 
 
@@ -424,7 +460,7 @@ def sphinx_kv8_attention_workspace_bytes(dtype: int, heads: int, kv_heads: int, 
     if cq.size != ck.size:
         raise ValueError("cu_q and cu_kv differ in length")
     _check("sphinx_kv8_attention_workspace_bytes", lib().sphinx_kv8_attention_workspace_bytes(
-        dtype, heads, kv_heads, head_dim, cq.ctypes.data, ck.ctypes.data, cq.size - 1, ctypes.byref(out)))
+        dtype, heads, kv_heads, head_dim, cq.tobytes(), ck.tobytes(), cq.size - 1, ctypes.byref(out)))
     return out.value
 
 
@@ -436,10 +472,14 @@ def sphinx_kv8_attention(dtype: int, heads: int, kv_heads: int, head_dim: int, q
     kl = None if kv_len is None else _host_cu(kv_len)
     if cq.size != ck.size or (kl is not None and kl.size != ck.size - 1):
         raise ValueError("cu_q, cu_kv and kv_len differ in length")
+    n, width = int(cq[-1]) if cq.size else 0, heads * head_dim
+    _check_rows("q", q, dtype, n, ldq, width)
+    _check_rows("o", o, dtype, n, width, width)
+    _check_bytes(cache, ws)
     s = _here(stream, q, cache, o, ws)
     _check("sphinx_kv8_attention", lib().sphinx_kv8_attention(
-        dtype, heads, kv_heads, head_dim, q.data_ptr(), ldq, cache.data_ptr(), cache.nbytes, cq.ctypes.data,
-        ck.ctypes.data, None if kl is None else kl.ctypes.data, cq.size - 1, o.data_ptr(), ws.data_ptr(), ws.nbytes,
+        dtype, heads, kv_heads, head_dim, q.data_ptr(), ldq, cache.data_ptr(), cache.nbytes, cq.tobytes(),
+        ck.tobytes(), None if kl is None else kl.tobytes(), cq.size - 1, o.data_ptr(), ws.data_ptr(), ws.nbytes,
         s))
 
 
@@ -460,6 +500,10 @@ def sphinx_refine_kv8_workspace_bytes(desc: ModelDesc, reqs, max_sel: int) -> in
 def sphinx_refine_step_kv8(desc: ModelDesc, reqs, idx, n: int, cu_host: np.ndarray, tau, c1, c2, x, kv_cache, ws,
                            stream=None):
     """sphinx_refine_step_cached with the 8-bit cache."""
+    if kv_cache is not None and not isinstance(kv_cache, int):
+        need = sphinx_kv8_cache_bytes(desc, reqs)
+        if kv_cache.nbytes < need:
+            raise ValueError(f"the cache has {kv_cache.nbytes} bytes, these requests take {need}")
     cu = np.ascontiguousarray(cu_host, dtype=np.int32)
     _check("sphinx_refine_step_kv8", lib().sphinx_refine_step_kv8(
         ctypes.byref(desc), reqs, len(reqs), _ptr(idx), n, _ptr(cu), _ptr(tau), _ptr(c1), _ptr(c2), _ptr(x),
