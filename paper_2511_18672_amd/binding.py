@@ -380,7 +380,7 @@ def _host_cu(cu) -> np.ndarray:
 
 
 def _here(stream, *tensors) -> Optional[int]:
-    """The stream of a call on the current device; tensors that are not on it are refused."""
+    """The stream of a call on the current device; tensors and streams that are not on it are refused."""
     import torch
 
     dev = torch.cuda.current_device()
@@ -391,7 +391,11 @@ def _here(stream, *tensors) -> Optional[int]:
         # the handle alone, where torch offers it: a Stream object takes 1 us of a 7 us call
         raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
         return raw(dev) if raw is not None else torch.cuda.current_stream(dev).cuda_stream
-    return stream if isinstance(stream, int) else stream.cuda_stream
+    if isinstance(stream, int):
+        return stream
+    if stream.device_index != dev:
+        raise ValueError(f"stream of cuda:{stream.device_index}, the current device is cuda:{dev}")
+    return stream.cuda_stream
 
 
 def _check_idx(idx, n: int):

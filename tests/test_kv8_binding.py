@@ -107,3 +107,14 @@ def test_a_cache_of_too_few_bytes_for_its_requests_is_refused():
     with pytest.raises(ValueError, match="bytes"):
         S.sphinx_refine_step_kv8(desc, reqs, x, 5, np.array([0, 5]), x, x, x, x, torch.zeros(need - 1, dtype=torch.uint8),
                                  torch.zeros(256, dtype=torch.uint8), 0)
+
+
+def test_streams_of_another_device_are_refused(monkeypatch):
+    class Stream:
+        def __init__(self, device_index):
+            self.device_index, self.cuda_stream = device_index, 77
+
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 1)
+    with pytest.raises(ValueError, match="stream of cuda:0"):
+        B._here(Stream(0))
+    assert B._here(Stream(1)) == 77 and B._here(5) == 5
