@@ -454,10 +454,12 @@ sphinx_status sphinx_kv8_load(sphinx_dtype dtype, int32_t kv_heads, int32_t head
  * multiple of 8; heads*head_dim <= 65536; pointers 16-byte aligned.  ws: dev,
  * 256-byte aligned, sphinx_kv8_attention_workspace_bytes bytes (which covers
  * every kv_len), not shared with work that may run at the same time.  Enqueues
- * a kernel or two, synchronizes nothing and may be captured in a graph.  Sums
- * stay finite for values up to 2^64 in magnitude.  Scores q.k past the range of
- * f32: -inf weighs nothing, +inf and NaN make their query's o NaN, and so does a
- * query whose scores are all -inf. */
+ * a kernel or two, synchronizes nothing and may be captured in a graph.  A call
+ * repeats bit for bit; how it is divided depends on the sizes of all its
+ * segments, so a segment's o may differ by roundings from what it is in a call
+ * with other segments.  Sums stay finite for values up to 2^64 in magnitude.
+ * Scores q.k past the range of f32: -inf weighs nothing, +inf and NaN make their
+ * query's o NaN, and so does a query whose scores are all -inf. */
 sphinx_status sphinx_kv8_attention_workspace_bytes(sphinx_dtype dtype, int32_t heads, int32_t kv_heads,
                                                    int32_t head_dim, const int32_t* cu_q, const int32_t* cu_kv,
                                                    int32_t nseg, size_t* bytes);
@@ -472,7 +474,8 @@ sphinx_status sphinx_kv8_attention(sphinx_dtype dtype, int32_t heads, int32_t kv
  * sphinx_kv8_store (idx ascending), and its rows attend to the tokens of their
  * request through sphinx_kv8_attention.  A factorised model reads the slice
  * back into the workspace (sphinx_kv8_load) for its spatial and temporal
- * attention.  Models with head_dim 64 or 72 (f32: 64); SPHINX_E_UNSUPPORTED
+ * attention.  A request's latents may differ by roundings from those that it has
+ * in a call of its own (see sphinx_kv8_attention).  Models with head_dim 64 or 72 (f32: 64); SPHINX_E_UNSUPPORTED
  * otherwise.  The workspace is larger than sphinx_refine_step's. */
 sphinx_status sphinx_kv8_cache_bytes(const sphinx_model_desc* m, const sphinx_request* reqs, int32_t R,
                                      size_t* bytes);

@@ -3,8 +3,9 @@
 // A slice holds the keys and values of one denoiser block: kv_heads heads of d
 // dims (64 or 72) for the tokens of up to SPHINX_MAX_REQUESTS segments.  The
 // tokens of a segment are grouped in blocks of 64 from its first one, so a
-// block never holds two segments' tokens and results do not depend on what a
-// segment is packed with.  Block b of head h is a tile of 64 d bytes of keys
+// block never holds two segments' tokens and what a segment's part of the cache
+// holds does not depend on what it is packed with.  (How an attention call is
+// divided does, and so the order of its sums: kv8_rules.hpp.)  Block b of head h is a tile of 64 d bytes of keys
 // and one of 64 d bytes of values at (h nblk + b) 2 64 d; behind all tiles,
 // from a 256-byte boundary, one byte per (head, block, keys | values) holds the
 // block's scale 2^(byte - 127).  A zeroed slice holds zeros.

@@ -1,4 +1,5 @@
-"""The 8-bit key/value cache through the C ABI: sums that overflow late in a block, and weights that bf16 misses."""
+"""The 8-bit key/value cache through the C ABI: sums that overflow late in a block, weights that bf16 misses, segments
+packed and alone."""
 import numpy as np
 import pytest
 
@@ -8,7 +9,8 @@ torch = pytest.importorskip("torch")
 S = pytest.importorskip("paper_2511_18672_amd")
 B = S.binding
 
-from test_gpu_kv8 import TDT, Cache, attend, f64, rows_of, tolerance  # noqa: E402
+from test_gpu_kv8 import TDT, Cache, attend, check_attention, f64, filled, queries, rows_of, tolerance  # noqa: E402
+from test_kv8_rules import plan  # noqa: E402
 
 pytestmark = pytest.mark.gpu
 
@@ -77,3 +79,24 @@ def test_weights_of_few_queries_are_not_rounded_to_bf16(d, nq, nk):
         # o's rounding, the weights' (numerator), the exponential's and the sums' in fp32
         bound = 2.0 ** -8 * np.abs(ref) + (2.0 ** -15 + 2.02 * (2.0 ** -22 + (nk + 8) * 2.0 ** -24)) * mag
         assert (np.abs(o - ref) <= bound).all(), (n16, np.abs(o - ref).max(), bound.max())
+
+
+@pytest.mark.parametrize("dtype,d", [("bf16", 64), ("bf16", 72), ("f32", 64)])
+def test_a_segment_packed_and_alone_is_the_same_up_to_rounding(dtype, d):
+    """One query against 2100 keys, alone and beside 700 queries against 5000: another tile height and other chunks, so
+    other sums and other roundings of the weights.  Each is held to the bound of its roundings, and what the segment's
+    part of the cache holds is the same."""
+    rng = np.random.default_rng(44)
+    bf = dtype == "bf16"
+    alone_plan, packed_plan = plan(2, [1], [2100], bf, d), plan(2, [700, 1], [5000, 2100], bf, d)
+    assert alone_plan[1][0] != packed_plan[1][1] and (not bf or (alone_plan[0], packed_plan[0]) == (32, 128))
+    packed = filled(rng, 2, d, [0, 2100, 7100], dtype)
+    alone = Cache(2, d, [0, 2100])
+    k, v = packed.load(dtype)
+    alone.store(k[:2100].view(2100, 2, d), v[:2100].view(2100, 2, d), ld=2 * d)
+    assert np.array_equal(alone.k, packed.k[:2100]) and np.array_equal(alone.v, packed.v[:2100])
+    q = queries(rng, 701, 2, d, dtype)
+    a = check_attention(alone, q[:1], 2, [0, 1])
+    b = check_attention(packed, q, 2, [0, 1, 701])[:1]
+    ref, mag, big = O.kv8.attention(f64(q[:1]).reshape(1, 2, d), alone.k, alone.v, [0, 1], alone.bounds)
+    assert (np.abs(a - b) <= 2 * tolerance(dtype, ref, mag, big, 2100, d)).all()
