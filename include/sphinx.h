@@ -399,11 +399,14 @@ sphinx_status sphinx_scatter_masked(const sphinx_request* reqs, int32_t R, const
  * exactly.
  *
  * The caller owns a slice (sphinx_kv8_bytes bytes, 16-byte aligned) and clears
- * it to zero bytes before its first use: a cleared slice holds zeros.  Its bytes
- * are in an order of the library's own.  Slices of the same cu_kv, kv_heads and
- * head_dim may follow each other in memory (the size is a multiple of 256).  The
- * calls below take the bytes at hand (slice_bytes) and return
- * SPHINX_E_WORKSPACE where a slice needs more.
+ * it to zero bytes before its first use, and before other sequences take its
+ * tokens: a cleared slice holds zeros.  (All rows of a block count for its scale,
+ * also those that no query looks at yet: a new sequence's first tokens would be
+ * kept in steps of the largest old values of their block, until those are
+ * written over.)  Its bytes are in an order of the library's own.  Slices of the
+ * same cu_kv, kv_heads and head_dim may follow each other in memory (the size is
+ * a multiple of 256).  The calls below take the bytes at hand (slice_bytes) and
+ * return SPHINX_E_WORKSPACE where a slice needs more.
  * ------------------------------------------------------------------------ */
 #define SPHINX_KV8_BLOCK 64
 

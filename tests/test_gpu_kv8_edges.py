@@ -1,5 +1,5 @@
-"""The 8-bit key/value cache through the C ABI: sums that overflow late in a block, weights that bf16 misses, segments
-packed and alone."""
+"""The 8-bit key/value cache through the C ABI where it can go wrong: sums that overflow late in a block, weights that
+bf16 misses, segments packed and alone, a slice that is used again, offsets past 32 bits."""
 import numpy as np
 import pytest
 
@@ -100,3 +100,100 @@ def test_a_segment_packed_and_alone_is_the_same_up_to_rounding(dtype, d):
     b = check_attention(packed, q, 2, [0, 1, 701])[:1]
     ref, mag, big = O.kv8.attention(f64(q[:1]).reshape(1, 2, d), alone.k, alone.v, [0, 1], alone.bounds)
     assert (np.abs(a - b) <= 2 * tolerance(dtype, ref, mag, big, 2100, d)).all()
+
+
+@pytest.mark.parametrize("cleared", [True, False])
+def test_a_new_sequence_in_an_old_ones_slice(cleared):
+    """Cleared before, a block's first tokens are kept as if they were alone; otherwise the old rows behind them, which
+    kv_len leaves out, still count for the scale."""
+    rng = np.random.default_rng(45)
+    c = Cache(2, 64, [0, 64])
+    old = rows_of(rng, 64, 2, 64, "bf16") * 256
+    c.store(old, old)
+    if cleared:
+        c.slice.zero_()
+        c.k[:], c.v[:] = 0.0, 0.0
+    new = torch.from_numpy(rng.standard_normal((5, 2, 64)).astype(np.float32)).bfloat16().cuda()
+    c.store(new, new)
+    c.check("f32")
+    alone = O.kv8.quantise(f64(new), [0, 5])
+    assert np.array_equal(c.k[:5], alone) == cleared
+    check_attention(c, queries(rng, 1, 2, 64, "bf16"), 2, [0, 1], [5])
+
+
+def test_the_tall_kernel_past_32_bit_offsets():
+    """2^23 + 100 tokens of five heads (5.4 GB), 200 queries: the 128-row kernel.  All but a few rows are zero, so a
+    zero key weighs 2^0; half of the queries score far past what a block's weights may sum to at the far end, where
+    the block's scores are made again from its bytes."""
+    n, heads = (1 << 23) + 100, 5
+    rng = np.random.default_rng(46)
+    assert plan(heads, [200], [n])[0] == 128
+    size = B.sphinx_kv8_bytes(heads, 64, [0, n])
+    assert size > 1 << 32
+    cache = torch.zeros(size, dtype=torch.uint8, device="cuda")
+    idx = np.array([0, 1 << 22, n - 170, n - 70, n - 2, n - 1], np.int32)
+    k, v = (rng.standard_normal((6, heads, 64)) for _ in range(2))
+    k, v = (torch.from_numpy(x.astype(np.float32)).bfloat16().cuda() for x in (k * 4, v * 1e6))
+    B.sphinx_kv8_store(B.BF16, heads, 64, k, v, heads * 64, torch.from_numpy(idx).cuda(), 6, [0, n], cache)
+    bounds = [0, 1, 2, 3, 4, 6]  # the last two share a block
+    K, V = O.kv8.quantise(f64(k), bounds), O.kv8.quantise(f64(v), bounds)
+    q = queries(rng, 200, heads, 64, "bf16") * 3
+    q[::2] *= 8
+    o = torch.empty(200, heads * 64, dtype=torch.bfloat16, device="cuda")
+    ws = torch.empty(B.sphinx_kv8_attention_workspace_bytes(B.BF16, heads, heads, 64, [0, 200], [0, n]),
+                     dtype=torch.uint8, device="cuda")
+    B.sphinx_kv8_attention(B.BF16, heads, heads, 64, q, heads * 64, cache, [0, n], None, o, [0, 200], ws)
+    qq = f64(q).reshape(200, heads, 64)
+    s = np.einsum("qhd,thd->qht", qq, K)
+    assert s.max() > 100.0
+    top = np.maximum(s.max(2, keepdims=True), 0.0)
+    w = np.exp2(s - top)
+    den = w.sum(2) + (n - 6) * np.exp2(-top[..., 0])
+    ref = np.einsum("qht,thd->qhd", w, V) / den[..., None]
+    mag = np.einsum("qht,thd->qhd", w, np.abs(V)) / den[..., None]
+    big = np.einsum("qhd,thd->qht", np.abs(qq), np.abs(K)).max(2)[..., None]
+    # fp32 sums of 2^23 equal numbers, added in runs of at most 2^17 blocks, take 2^-7 of the sum, and weights 2^-8;
+    # a score is off by 66 roundings of sum |q k|
+    err = np.abs(f64(o).reshape(200, heads, 64) - ref)
+    assert (err <= mag * (2.0 ** -6 + 2.02 * np.log(2.0) * 66 * 2.0 ** -24 * big) + 2.0 ** -8 * np.abs(ref)).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_whole_slices_past_32_bit_offsets(dtype):
+    """All rows of 2^24 + 70 tokens of two heads (4.3 GB) stored and read back: the first blocks, some in the middle and
+    the last ones, the partial one among them, are what the oracle holds."""
+    n, heads = (1 << 24) + 70, 2
+    size = B.sphinx_kv8_bytes(heads, 64, [0, n])
+    assert size > 1 << 32
+    cache = torch.zeros(size, dtype=torch.uint8, device="cuda")
+    code = B.BF16 if dtype == "bf16" else B.F32
+    gen = torch.Generator(device="cuda").manual_seed(5)
+    k, v = (torch.randn(n, heads * 64, generator=gen, device="cuda", dtype=TDT[dtype]) for _ in range(2))
+    B.sphinx_kv8_store(code, heads, 64, k, v, heads * 64, None, n, [0, n], cache)
+    spans = [(0, 128), (1 << 23, (1 << 23) + 128), ((1 << 24) - 128, n)]
+    want = [[O.kv8.quantise(f64(x[a:b]).reshape(-1, heads, 64), [0, b - a]) for a, b in spans] for x in (k, v)]
+    k.fill_(7.0)
+    v.fill_(7.0)
+    B.sphinx_kv8_load(code, heads, 64, cache, [0, n], None, n, k, v, heads * 64)
+    for x, held in zip((k, v), want):
+        for (a, b), h in zip(spans, held):
+            assert np.array_equal(f64(x[a:b]).reshape(-1, heads, 64), h), (a, b)
+
+
+@pytest.mark.parametrize("d,nq", [(64, 1), (64, 40), (64, 300), (72, 2), (72, 300)])
+def test_weights_that_bf16_holds(d, nq):
+    """Whole scores, so that every weight is a power of two, and values of both signs that nearly cancel, so that o's own
+    rounding is small: what is left is fp32 sums.  A weight that is wrong by 2^-10 of itself would show."""
+    rng = np.random.default_rng(47)
+    nk = 1000
+    c = Cache(2, d, [0, nk])
+    k = torch.zeros(nk, 2, d)
+    k[:, :, 0] = torch.from_numpy(-rng.integers(0, 8, (nk, 2)).astype(np.float32))
+    v = torch.from_numpy(rng.choice([-1.0, 1.0], (nk, 2, d)).astype(np.float32))
+    c.store(k.bfloat16().cuda(), v.bfloat16().cuda())
+    q = torch.zeros(nq, 2 * d, dtype=torch.bfloat16, device="cuda")
+    q[:, 0], q[:, d] = 1.0, 1.0
+    ref, mag, _ = O.kv8.attention(f64(q).reshape(nq, 2, d), c.k, c.v, [0, nq], c.bounds)
+    o = f64(attend(c, q, 2, [0, nq])).reshape(nq, 2, d)
+    bound = 2.0 ** -8 * np.abs(ref) + 2.02 * (2.0 ** -22 + (nk + 8) * 2.0 ** -24) * mag
+    assert (np.abs(o - ref) <= bound).all() and bound.mean() < 2.0 ** -10 / 2
