@@ -26,9 +26,12 @@ struct Kv8Plan {
 
 constexpr int kKv8Cus = 256;
 // 32-row tiles: as many workgroups as run at once (three per CU at bf16 and
-// head_dim 64, two else), with a block for each of their waves at least.
+// head_dim 64, two else).  Chunks are evened out below their limit, which is four
+// blocks at least, one for each wave: a segment's chunks (but its last) hold more
+// than half of the limit, so three blocks at least.
 constexpr int kKv8ItemsRows = 3 * kKv8Cus, kKv8MinChunkRows = 4;
-// 128-row tiles: cut into this many workgroups at most, of eight blocks at least.
+// 128-row tiles: cut into this many workgroups at most, with a limit of eight blocks
+// at least, so that a segment's chunks (but its last) hold five at least.
 constexpr int kKv8ItemsTiles = 6 * kKv8Cus, kKv8MinChunkTiles = 8;
 
 inline int kv8_tiles(int64_t rows, int tile) { return (int)((rows + tile - 1) / tile); }
@@ -117,9 +120,10 @@ inline Kv8Plan plan_kv8(bool bf16, int kv_heads, int head_dim, int nseg, const i
 }
 
 // Partial rows that no plan for these segments passes, with any klen up to the
-// given one.  A chunk of several holds more than half of four blocks; 32-row
-// tiles: a segment is cut into pieces of more than half of work / items blocks,
-// so at most twice the items leave partial rows; each item leaves one tile's.
+// given one.  No limit of a chunk is below four blocks, so a segment has no more
+// chunks than fours of blocks.  32-row tiles: a cut segment has less than twice
+// its blocks over the limit as chunks, so less than twice the items leave partial
+// rows; each item leaves one tile's.
 inline int64_t kv8_most_parts(int kv_heads, int nseg, const int64_t* rows, const int* klen) {
   int64_t by_chunk = 0, by_item = 0;
   for (int i = 0; i < nseg; ++i) {

@@ -101,3 +101,25 @@ def test_largest_calls_stay_in_range():
     assert chunks[0] == 1 and size[0] == 1 << 25 and item[1] == 1 << 24 and part[1] == 0
     tile, size, chunks, item, row, part = plan(1, [1], [(1 << 31) - 1])
     assert chunks[0] * int(size[0]) >= 1 << 25 and part[1] == chunks[0] <= most(1, [1], [(1 << 31) - 1])
+
+
+@pytest.mark.parametrize("bf16,head_dim", [(True, 64), (True, 72), (False, 64)])
+@pytest.mark.parametrize("seed", range(10))
+def test_chunks_hold_more_than_half_of_the_least_limit(seed, bf16, head_dim):
+    """More than half of four blocks, or of eight in 128-row tiles; and no more chunks than fours of blocks."""
+    rng = np.random.default_rng(1000 + seed)
+    n = int(rng.integers(1, 65))
+    heads = int(rng.choice([1, 2, 8, 16]))
+    rows = np.exp(rng.uniform(0, np.log(rng.choice([4, 300, 3000])), n)).astype(np.int64)
+    klen = np.exp(rng.uniform(0, np.log(rng.choice([400, 3000, 1000000])), n)).astype(np.int64)
+    for m in (n, 1, min(2, n)):
+        tile, size, chunks, _, _, _ = plan(heads, rows[:m], klen[:m], bf16, head_dim)
+        split = chunks > 1
+        assert (size[split] >= (3 if tile == 32 else 5)).all()
+        assert (chunks <= np.maximum(1, ((klen[:m] + 63) // 64 + 3) // 4)).all()
+
+
+def test_the_chunks_that_the_limits_leave():
+    assert plan(8, [1, 1], [33 * 64, 5 * 64])[1:3][0][1] == 3  # five blocks as three and two
+    tile, size, *_ = plan(1, [300], [33 * 64])
+    assert tile == 128 and size[0] == 7
