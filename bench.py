@@ -505,7 +505,8 @@ def main():
                 "kernel": (f"k_attn_bf16_dma{'' if hd == 64 else hd} (varlen flash attention, head_dim {hd})"
                            if wl.model.dtype == "bf16" else "k_attn_f32") if args.attention == "joint"
                 else "attention class: k_attn_bf16_dma per frame and k_attn_temporal per position, alternating",
-                **({"kernel": f"k_kv8_attn_tiles (attention over the 8-bit cache, head_dim {hd})"}
+                **({"kernel": "attention over the 8-bit cache: k_kv8_attn_tiles for many queries of a bf16 model, "
+                              f"k_kv8_attn_rows otherwise, and k_kv8_attn_join (head_dim {hd})"}
                    if args.cache_dtype == "fp8" and args.attention == "joint" else {}),
                 "algorithmic_flop_per_launch": attn_flop}
     step_flop = L * (attn_flop + sum(gemm_flop.values()))

@@ -286,7 +286,8 @@ __device__ __forceinline__ void saturate(Piece<T>& p) {  // finite ones to 448 t
 // old tiles in.  A wave and not a workgroup per tile: a workgroup spends the way
 // of a row to its bytes on barriers.  bf16 has to fit 128 registers, so that four
 // waves per SIMD wait for memory at once: 9677 listed of 32256 tokens, 16 heads
-// of 64, caches not at hand: 56 -> 44, with the old tile past the registers us; all of them: 55 -> 48.
+// of 64, caches not at hand, 56 -> 50 us, and 44 since the old tile goes to LDS past
+// the registers; all of them 55 -> 48.
 template <typename T, int HD>
 __global__ __launch_bounds__(kTPB, sizeof(T) == 2 ? 4 : 2)
 void k_kv8_store(Kv8Segs S, Kv8Slice c, Kv8Rows rows, const T* __restrict__ k, const T* __restrict__ v, int group,

@@ -67,19 +67,20 @@ inline Kv8Plan plan_kv8(bool bf16, int kv_heads, int head_dim, int nseg, const i
   if (p.tile == 32) {
     int64_t units = 0;
     for (int i = 0; i < nseg; ++i) units += (int64_t)kv8_tiles(rows[i], 32) * kv_heads;
-    // Small calls: eight waves take up to four blocks each, at about 1.5 us a block,
-    // which is less than a second kernel costs (one query against 4096 keys of 8
-    // heads, eight blocks a wave: 16.0 us whole, 12.6 us cut and joined).
-    if (bf16 && units <= kKv8Cus && longest <= 32) {
+    // Small calls: eight waves take up to three blocks each, at about 1.7 us a block,
+    // in one launch instead of two.  One query of 8 heads, calls in a stream, whole
+    // and cut: 1100 keys 8.8 us and 10.6, 1500 keys 9.9 and 10.7, 2048 keys 11.3 and
+    // 10.6; the kernels of a captured graph, without the caller's time for a second
+    // launch: 7.9 and 7.3, 9.1 and 7.8, 10.5 and 8.1.
+    if (bf16 && units <= kKv8Cus && longest <= 24) {
       p.waves = 8;
       cut_kv8(p, kv_heads, nseg, rows, klen, longest);
       return p;
     }
     // Chunks of equal work for all workgroups that run at once, counting that cutting
-    // leaves half a chunk per tile on average.  fp32 is bound by the matrix cores,
-    // which one workgroup keeps nearly as busy as two: tiles that fill the chip
-    // are not cut for a second (1024 queries against 2048 keys of 8 heads, 256
-    // tiles: 50 us in two chunks, 48 us whole).
+    // leaves half a chunk per tile on average.  fp32: where tiles fill the chip, one
+    // workgroup per CU, a cut for a second one gains less than its join costs (1024
+    // queries against 2048 keys of 8 heads, 256 tiles: 50 us in two chunks, 48 us whole).
     const int64_t slots = bf16 && head_dim == 64 ? kKv8ItemsRows : !bf16 && units >= kKv8Cus ? kKv8Cus : 2 * kKv8Cus;
     const int64_t pieces = bf16 ? std::max(slots - units / 2, slots / 2) : slots;
     cut_kv8(p, kv_heads, nseg, rows, klen,
