@@ -347,8 +347,7 @@ __device__ __forceinline__ void region(const char* sK, const char* sV, const Lan
   for (int w = 0; w < 2; ++w)
 #pragma unroll
     for (int hf = 0; hf < 2; ++hf) asm volatile("" : "+v"(pn[w][hf]));
-  asm volatile("" : "+v"(psum));
-  psum_out = psum;
+  psum_out = pair_sum(psum);
 }
 
 // Probabilities exp2(s - delta) of a tile's shifted scores, rounded to bf16 in

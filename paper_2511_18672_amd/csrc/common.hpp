@@ -109,16 +109,21 @@ __device__ __forceinline__ void lds_dma16_at(const void* sbase, uint32_t voff, c
                : "memory", "m0");
 }
 
-// acc + p.x + p.y as one v_dot2c with (1, 1) in bf16.  The empty statement keeps
-// each step's dot product in its step: as plain arithmetic the compiler gathers
-// the sixteen of a tile into one chain after the last MFMA.  The product itself is
-// the builtin, since its sum takes three slots to be there for any other
-// instruction (an overflow check, say): the compiler leaves them free behind the
-// builtin, and does not behind an instruction in inline assembly.
+// acc + p.x + p.y as one v_dot2c with (1, 1) in bf16.  A volatile statement,
+// so that each step's dot product stays in its step: as plain arithmetic the
+// compiler gathers the sixteen of a tile into one chain after the last MFMA, and
+// around the builtin, pinned by an empty statement, it orders a step's
+// instructions so that the headline's attention takes 1.5 % longer.
 __device__ __forceinline__ float add_pair(float acc, bf16x2 p) {
-  const bf16x2 ones = {(bf16)1.0f, (bf16)1.0f};
-  acc = __builtin_amdgcn_fdot2_f32_bf16(p, ones, acc, false);
-  asm volatile("" : "+v"(acc));
+  asm volatile("v_dot2c_f32_bf16_e32 %0, 0x3f803f80, %1" : "+v"(acc) : "v"(__builtin_bit_cast(unsigned, p)));
+  return acc;
+}
+// The sum of such a chain, for any other instruction to read: it takes three slots
+// to be there, which the compiler leaves free behind the builtin, and not behind an
+// instruction in inline assembly.  (tests/test_device_code.py finds a reader that
+// does without.)
+__device__ __forceinline__ float pair_sum(float acc) {
+  asm volatile("s_nop 2" : "+v"(acc));
   return acc;
 }
 

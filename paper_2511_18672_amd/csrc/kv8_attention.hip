@@ -595,7 +595,7 @@ __global__ __launch_bounds__(kTPB, 3) void k_kv8_attn_tiles(Kv8Attn A, Kv8Slice 
     pf[0][1] = q0[1];
     pf[1][0] = q1[0];
     pf[1][1] = q1[1];
-    return psum;
+    return pair_sum(psum);
   };
   auto settle = [&](f32x16& a, f32x16& b) {
     if (shifted)
@@ -696,7 +696,7 @@ __global__ __launch_bounds__(kTPB, 3) void k_kv8_attn_tiles(Kv8Attn A, Kv8Slice 
     for (int w = 0; w < 2; ++w)
 #pragma unroll
       for (int hf = 0; hf < 2; ++hf) asm volatile("" : "+v"(pn[w][hf]));
-    asm volatile("" : "+v"(psum));
+    psum = pair_sum(psum);
     if (__ballot(!(psum <= kPsumMax)) != 0) psum = rebase(t, pn);
     l_run += psum;
     barrier();
@@ -805,6 +805,7 @@ __global__ __launch_bounds__(kTPB, 3) void k_kv8_attn_tiles(Kv8Attn A, Kv8Slice 
       pb[1][r >> 3][r & 7] = y[0];
       pb[1][r >> 3][(r & 7) + 1] = y[1];
     }
+    psum = pair_sum(psum);
     pv(vr, pa);
     if (__ballot(!(psum <= kPsumMax)) != 0) psum = rebase(t, pb);
     l_run += psum;
