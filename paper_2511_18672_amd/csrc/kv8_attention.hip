@@ -91,14 +91,15 @@ __device__ __forceinline__ void operand(const uint4& b, float (&f)[16]) {  // wi
 // costs errors of 1.2e-3 to 1.5e-3 beside o's 1.7e-3 and saves half of the V^T P^T
 // products and the splitting, next to which the bytes come: one query against 2^20
 // keys 102.5 instead of 105.2 us, 32 queries of 16 heads against 32256 keys 22.9
-// instead of 24.3, one against 1500 8.7 instead of 9.8.)  f32: 32x32x2 products of the unscaled bytes, nothing
-// rounded (the keys' scale goes into the exponent, the values' into P: a
-// product per byte between its conversion and its matrix instruction kept the
-// two from overlapping).
+// instead of 24.3, one against 1500 8.7 instead of 9.8.)
+// f32: 32x32x2 products of the unscaled bytes, nothing rounded (the keys' scale goes
+// into the exponent, the values' into P: a product per byte between its conversion
+// and its matrix instruction kept the two from overlapping).
 // bf16 is bound by the cache's bytes: one query against 2^20 keys of 4 heads takes
-// 92 us (5.8 TB/s), 48 sequences of 32 heads on 4 70 us.  f32 is bound by the matrix
-// instructions, next to which little else is issued: 1024 queries against 2048
-// keys of 8 heads 44 us, 4000 against 4000 296 us (111 TFLOP/s).
+// 95 us (5.6 TB/s), 48 sequences of 32 heads on 4 73 us.  f32 is bound by the matrix
+// instructions and what stands between them in the one wave of a SIMD: 1024 queries
+// against 2048 keys of 8 heads take 44 us, the matrix cores busy for 52 % of it, 4000
+// against 4000 296 us (111 TFLOP/s).
 template <typename T, int HD, int WAVES>
 __global__ __launch_bounds__(64 * WAVES, sizeof(T) == 2 && HD == 64 && WAVES == 4 ? 3 : 2) void k_kv8_attn_rows(Kv8Attn A, Kv8Slice c, Kv8Plan P, Parts part, int first) {
   constexpr bool F32 = sizeof(T) == 4;
