@@ -393,8 +393,9 @@ def _here(stream, *tensors) -> Optional[int]:
         return raw(dev) if raw is not None else torch.cuda.current_stream(dev).cuda_stream
     if isinstance(stream, int):
         return stream
-    if stream.device_index != dev:
-        raise ValueError(f"stream of cuda:{stream.device_index}, the current device is cuda:{dev}")
+    at = getattr(stream, "device_index", dev)
+    if at != dev:
+        raise ValueError(f"stream of cuda:{at}, the current device is cuda:{dev}")
     return stream.cuda_stream
 
 
