@@ -490,6 +490,108 @@ sphinx_status sphinx_refine_step_kv8(const sphinx_model_desc* m, const sphinx_re
                                      size_t ws_bytes, void* stream);
 
 /* ------------------------------------------------------------------------
+ * Layer norm over rows in segments, forward and backward.  Segment i (a frame,
+ * a request, or any group of rows) has rows [cu[i], cu[i+1]) (host int32
+ * [nseg+1], non-decreasing from 0, 1 <= nseg <= SPHINX_MAX_REQUESTS; segments
+ * may be empty) and a weight and a shift of its own, rows i of w and b (dev,
+ * wdt f32 or bf16, row i at element i*ldw):
+ *   mean = sum(x) / cols, rstd = 1 / sqrt(sum((x - mean)^2) / cols + eps),
+ *   xh = (x - mean) rstd, y = xh w' + b,   w' = w, or 1 + w with plus_one = 1
+ * (the denoiser's modulation: w = scale, b = shift).  w = NULL stands for
+ * w' = 1, b = NULL for b = 0.  1 <= cols <= 16384.  Rows of x, y, dy and dx may
+ * be strided (row j at element j*ld, ld >= cols) and start at any element;
+ * what lies between and behind them is left as it is.  f32 or bf16 each;
+ * computed in fp32 and rounded once.  A row with an infinity or a NaN becomes
+ * NaN and leaves the others alone (in dw and db: its segment's columns).
+ * Nothing is synchronized; the calls may be captured in a graph, and repeat
+ * bit for bit.
+ * ------------------------------------------------------------------------ */
+
+/* y: dev out, ydt.  stats: dev float [rows][2] out (mean, rstd of each row), or
+ * NULL. */
+sphinx_status sphinx_layer_norm(sphinx_dtype xdt, sphinx_dtype wdt, sphinx_dtype ydt, int32_t cols, float eps,
+                                const void* x, int64_t ldx, const void* w, const void* b, int64_t ldw,
+                                int32_t plus_one, const int32_t* cu /*host[nseg+1]*/, int32_t nseg, void* y,
+                                int64_t ldy, float* stats, void* stream);
+
+/* The same with y as a matrix in 8 bits (see below), quantised from fp32. */
+sphinx_status sphinx_layer_norm_q8(sphinx_dtype xdt, sphinx_dtype wdt, int32_t cols, float eps, const void* x,
+                                   int64_t ldx, const void* w, const void* b, int64_t ldw, int32_t plus_one,
+                                   const int32_t* cu, int32_t nseg, uint8_t* q, uint8_t* s, float* stats,
+                                   void* stream);
+
+/* Gradients from x, the forward call's stats and dy (gdt; the gradient of y):
+ *   g = dy w', dx = rstd (g - sum(g)/cols - xh sum(g xh)/cols)  (dev out, gdt)
+ *   dw[i] = sum of dy xh, db[i] = sum of dy over the rows of segment i
+ * (dev float out, row i at element i*ldg; zeros for an empty segment).  dx, dw
+ * and db may each be NULL.  ws: dev, 256-byte aligned, needed for dw and db, not
+ * shared with work that may run at the same time. */
+sphinx_status sphinx_layer_norm_backward_workspace_bytes(int32_t cols, const int32_t* cu, int32_t nseg,
+                                                         size_t* bytes);
+sphinx_status sphinx_layer_norm_backward(sphinx_dtype xdt, sphinx_dtype wdt, sphinx_dtype gdt, int32_t cols,
+                                         const void* x, int64_t ldx, const float* stats, const void* w, int64_t ldw,
+                                         int32_t plus_one, const int32_t* cu, int32_t nseg, const void* dy,
+                                         int64_t lddy, void* dx, int64_t lddx, float* dw, float* db, int64_t ldg,
+                                         void* ws, size_t ws_bytes, void* stream);
+
+/* ------------------------------------------------------------------------
+ * Matrices in 8 bits with a scale for each block of 128, and their products.
+ * A matrix [rows][cols] in 8 bits is
+ *   q [rows][Kp]  e4m3 bytes, Kp = cols rounded up to a multiple of 128 (zeros
+ *                 behind cols),
+ *   s [rows][Sp]  scale bytes, one for each 128 columns, Sp = Kp/128 rounded up
+ *                 to a multiple of 4 (what lies behind Kp/128 is not looked at):
+ *                 byte e + 127 stands for 2^e,
+ * and holds the values q 2^e.  The numbers of a group share a scale: with A
+ * their largest finite magnitude, e is the smallest integer with A <= 448 2^e,
+ * held in -100 .. 119 (-100 for A = 0); a number x becomes e4m3(x 2^-e), rounded
+ * once to nearest even; finite numbers past 448 2^119 saturate, infinities and
+ * NaN become NaN.  Groups are 128 columns of a row, or with square = 1 the
+ * 128 x 128 numbers of a tile (then a matrix and its transpose hold the same
+ * values, as weights should).
+ * ------------------------------------------------------------------------ */
+#define SPHINX_Q8_BLOCK 128
+
+/* Bytes of q and s.  0 <= cols <= 2^23, 0 <= rows <= 2^30. */
+sphinx_status sphinx_q8_bytes(int32_t rows, int32_t cols, size_t* q_bytes, size_t* s_bytes);
+
+/* Quantises x [rows][cols] (dev, f32 or bf16, row j at element j*ldx) into any
+ * of: q and s (groups along its rows); qt and st, the transposed matrix
+ * [cols][rows] in 8 bits (groups of 128 rows of a column); sums (dev float
+ * [cols]), the sums of its columns in fp32, which is a bias gradient.  Outputs
+ * that are NULL are left out.  ws (256-byte aligned) is needed for sums only.
+ * Deterministic; may be captured in a graph. */
+sphinx_status sphinx_q8_quantise_workspace_bytes(int32_t rows, int32_t cols, size_t* bytes);
+sphinx_status sphinx_q8_quantise(sphinx_dtype dtype, const void* x, int64_t ldx, int32_t rows, int32_t cols,
+                                 int32_t square, uint8_t* q, uint8_t* s, uint8_t* qt, uint8_t* st, float* sums,
+                                 void* ws, size_t ws_bytes, void* stream);
+
+typedef SPHINX_ENUM {
+  SPHINX_Q8_STORE = 0, /* out = C */
+  SPHINX_Q8_GELU = 1,  /* out = GELU_tanh(C) */
+  SPHINX_Q8_ADD = 2    /* out = out + C */
+} sphinx_q8_epilogue;
+
+/* C[m][n] = sum_k A[m][k] B[n][k] + bias[n] for matrices in 8 bits A [M][K] and
+ * B [N][K]; out: dev, odt, row m at element m*ldo.  bias: dev [N], bdt, or NULL.
+ * The forward product y = x W^T takes x and W; the gradients are dx = dy W, with
+ * dy and the transposed W, and dW = dy^T x, with the transposed dy and x (their
+ * contraction runs over the rows, so their groups do as well).  K = 0 gives
+ * the bias alone.
+ * Sums are fp32.  odt bf16: the 8-bit matrix cores, which align the products
+ * of 8 consecutive k to the largest of them and drop what lies 2^-13 below it.
+ * odt f32: every product is exact (bf16 matrix cores, at less than half the rate).
+ * A NaN in a row of A or B makes the outputs of that row or column NaN.
+ * ws: dev, 256-byte aligned, sphinx_q8_matmul_workspace_bytes bytes, not shared
+ * with work that may run at the same time.  Deterministic; may be captured in a
+ * graph. */
+sphinx_status sphinx_q8_matmul_workspace_bytes(sphinx_dtype odt, int32_t M, int32_t N, int32_t K, size_t* bytes);
+sphinx_status sphinx_q8_matmul(sphinx_dtype odt, int32_t M, int32_t N, int32_t K, const uint8_t* a, const uint8_t* sa,
+                               const uint8_t* b, const uint8_t* sb, sphinx_dtype bdt, const void* bias,
+                               sphinx_q8_epilogue epilogue, void* out, int64_t ldo, void* ws, size_t ws_bytes,
+                               void* stream);
+
+/* ------------------------------------------------------------------------
  * Mask front-end (Sec. 5.3 spatially selective refinement; Alg. 1
  * laplacian_var, otsu(norm(.)), the opacity mask 1[O < tau_o] and their
  * union): the token mask of every request from the regression output frames

@@ -24,6 +24,8 @@ ATTN_JOINT, ATTN_FACTORISED = 0, 1  # sphinx_attention
 GRID_SHARED, GRID_PER_FRAME = 0, 1  # sphinx_grid
 MAX_REQUESTS = 64
 KV8_BLOCK = 64  # tokens of a block of the 8-bit cache
+Q8_BLOCK = 128  # numbers that share a scale in an 8-bit matrix
+Q8_STORE, Q8_GELU, Q8_ADD = 0, 1, 2  # sphinx_q8_epilogue
 STATUS_NAMES = {0: "SPHINX_OK", 1: "SPHINX_E_INVALID", 2: "SPHINX_E_UNSUPPORTED", 3: "SPHINX_E_WORKSPACE",
                 4: "SPHINX_E_HIP"}
 PARAMS = ["PE_W", "PE_B", "T1_W", "T1_B", "T2_W", "T2_B", "COND_W", "COND_B", "QKV_W", "QKV_B", "O_W", "O_B",
@@ -38,7 +40,10 @@ EXPORTED = ["sphinx_status_string", "sphinx_model_blob_bytes", "sphinx_model_par
             "sphinx_mask_frontend", "sphinx_adaptive_start", "sphinx_select_mask_static", "sphinx_varlen_attention",
             "sphinx_kv8_bytes", "sphinx_kv8_store", "sphinx_kv8_load", "sphinx_kv8_attention_workspace_bytes",
             "sphinx_kv8_attention", "sphinx_kv8_cache_bytes", "sphinx_refine_kv8_workspace_bytes",
-            "sphinx_refine_step_kv8"]
+            "sphinx_refine_step_kv8", "sphinx_layer_norm", "sphinx_layer_norm_q8",
+            "sphinx_layer_norm_backward_workspace_bytes", "sphinx_layer_norm_backward", "sphinx_q8_bytes",
+            "sphinx_q8_quantise_workspace_bytes", "sphinx_q8_quantise", "sphinx_q8_matmul_workspace_bytes",
+            "sphinx_q8_matmul"]
 PEAK_BLOCKS = 2048
 PEAK_CONSTANT, PEAK_RANDOM = 0, 1
 KERNEL_CLASSES = ["select", "gather", "cond", "embed", "ln", "gemm_qkv", "attention", "gemm_out", "gemm_mlp1",
@@ -131,6 +136,21 @@ def lib() -> ctypes.CDLL:
                                                         POINTER(c_size_t)]),
         "sphinx_refine_step_kv8": (c_int32, [POINTER(ModelDesc), POINTER(Request), c_int32, P, c_int32, P, P, P, P, P,
                                              P, P, c_size_t, P]),
+        "sphinx_layer_norm": (c_int32, [c_int32, c_int32, c_int32, c_int32, c_float, P, c_int64, P, P, c_int64, c_int32,
+                                        P, c_int32, P, c_int64, P, P]),
+        "sphinx_layer_norm_q8": (c_int32, [c_int32, c_int32, c_int32, c_float, P, c_int64, P, P, c_int64, c_int32, P,
+                                           c_int32, P, P, P, P]),
+        "sphinx_layer_norm_backward_workspace_bytes": (c_int32, [c_int32, P, c_int32, POINTER(c_size_t)]),
+        "sphinx_layer_norm_backward": (c_int32, [c_int32, c_int32, c_int32, c_int32, P, c_int64, P, P, c_int64,
+                                                 c_int32, P, c_int32, P, c_int64, P, c_int64, P, P, c_int64, P,
+                                                 c_size_t, P]),
+        "sphinx_q8_bytes": (c_int32, [c_int32, c_int32, POINTER(c_size_t), POINTER(c_size_t)]),
+        "sphinx_q8_quantise_workspace_bytes": (c_int32, [c_int32, c_int32, POINTER(c_size_t)]),
+        "sphinx_q8_quantise": (c_int32, [c_int32, P, c_int64, c_int32, c_int32, c_int32, P, P, P, P, P, P, c_size_t,
+                                         P]),
+        "sphinx_q8_matmul_workspace_bytes": (c_int32, [c_int32, c_int32, c_int32, c_int32, POINTER(c_size_t)]),
+        "sphinx_q8_matmul": (c_int32, [c_int32, c_int32, c_int32, c_int32, P, P, P, P, c_int32, P, c_int32, P, c_int64,
+                                       P, c_size_t, P]),
         "sphinx_scatter_masked": (c_int32, [POINTER(Request), c_int32, P, P, c_int32, P, P, c_int32, c_int32, P]),
         "sphinx_mask_frontend_workspace_bytes": (c_int32, [POINTER(Request), c_int32, POINTER(c_size_t)]),
         "sphinx_adaptive_start": (c_int32, [POINTER(Request), c_int32, P, P, ctypes.c_float, POINTER(KLogic), c_int32,
@@ -513,6 +533,155 @@ def sphinx_refine_step_kv8(desc: ModelDesc, reqs, idx, n: int, cu_host: np.ndarr
     _check("sphinx_refine_step_kv8", lib().sphinx_refine_step_kv8(
         ctypes.byref(desc), reqs, len(reqs), _ptr(idx), n, _ptr(cu), _ptr(tau), _ptr(c1), _ptr(c2), _ptr(x),
         _ptr(kv_cache), _ptr(ws), ws.numel() * ws.element_size(), _stream(stream)))
+
+
+def _int32(name: str, v) -> int:
+    v = int(v)
+    if not -(1 << 31) <= v < 1 << 31:
+        raise ValueError(f"{name} = {v} does not fit 32 bits")
+    return v
+
+
+def _check_out(name: str, t, dtype, n: int):
+    """Refuses a tensor of another type, not in a row, or with fewer than n elements."""
+    if t is not None and (t.dtype is not dtype or not t.is_contiguous() or t.numel() < n):
+        raise ValueError(f"{name} holds {t.numel()} values of {t.dtype}, strides {t.stride()}; "
+                         f"{n} {dtype} in a row are needed")
+
+
+def _check_q8(name: str, q, s, rows: int, cols: int):
+    import torch
+
+    if (q is None) != (s is None):
+        raise ValueError(f"{name}: its bytes and its scales come together")
+    nq, ns = sphinx_q8_bytes(rows, cols)
+    _check_out(name, q, torch.uint8, nq)
+    _check_out(name + "'s scales", s, torch.uint8, ns)
+
+
+def _ln_check(xdt: int, wdt: int, cols: int, x, ldx: int, w, b, ldw: int, cu) -> np.ndarray:
+    c = _host_cu(cu)
+    if c.size < 2:
+        raise ValueError("cu needs two bounds at least")
+    _check_rows("x", x, xdt, int(c[-1]), ldx, cols)
+    for name, t in (("w", w), ("b", b)):
+        if t is not None:
+            _check_rows(name, t, wdt, c.size - 1, ldw, cols)
+    return c
+
+
+def sphinx_layer_norm(xdt: int, wdt: int, ydt: int, cols: int, eps: float, x, ldx: int, w, b, ldw: int, plus_one, cu,
+                      y, ldy: int, stats=None, stream=None):
+    """y <- the normalised rows of x, scaled by w (1 + w with plus_one) and shifted by b, a row of each per segment
+    (cu: host int sequence of row bounds; w, b: None for ones and zeros).  stats: float32 [rows][2] or None."""
+    import torch
+
+    c = _ln_check(xdt, wdt, cols, x, ldx, w, b, ldw, cu)
+    _check_rows("y", y, ydt, int(c[-1]), ldy, cols)
+    _check_out("stats", stats, torch.float32, 2 * int(c[-1]))
+    s = _here(stream, x, w, b, y, stats)
+    _check("sphinx_layer_norm", lib().sphinx_layer_norm(
+        xdt, wdt, ydt, cols, eps, _ptr(x), ldx, _ptr(w), _ptr(b), ldw, int(plus_one), c.tobytes(), c.size - 1, _ptr(y),
+        ldy, _ptr(stats), s))
+
+
+def sphinx_layer_norm_q8(xdt: int, wdt: int, cols: int, eps: float, x, ldx: int, w, b, ldw: int, plus_one, cu, q, s,
+                         stats=None, stream=None):
+    """sphinx_layer_norm with its output in 8 bits (q, s as sphinx_q8_bytes(rows, cols) sizes them)."""
+    import torch
+
+    c = _ln_check(xdt, wdt, cols, x, ldx, w, b, ldw, cu)
+    _check_q8("q", q, s, int(c[-1]), cols)
+    _check_out("stats", stats, torch.float32, 2 * int(c[-1]))
+    at = _here(stream, x, w, b, q, s, stats)
+    _check("sphinx_layer_norm_q8", lib().sphinx_layer_norm_q8(
+        xdt, wdt, cols, eps, _ptr(x), ldx, _ptr(w), _ptr(b), ldw, int(plus_one), c.tobytes(), c.size - 1, _ptr(q),
+        _ptr(s), _ptr(stats), at))
+
+
+def sphinx_layer_norm_backward_workspace_bytes(cols: int, cu) -> int:
+    c, out = _host_cu(cu), c_size_t()
+    _check("sphinx_layer_norm_backward_workspace_bytes", lib().sphinx_layer_norm_backward_workspace_bytes(
+        cols, c.tobytes(), c.size - 1, ctypes.byref(out)))
+    return out.value
+
+
+def sphinx_layer_norm_backward(xdt: int, wdt: int, gdt: int, cols: int, x, ldx: int, stats, w, ldw: int, plus_one, cu,
+                               dy, lddy: int, dx, lddx: int, dw, db, ldg: int, ws, stream=None):
+    """dx (None: left out) and, per segment, dw and db (float32; None: left out) from x, the forward call's stats
+    and dy."""
+    import torch
+
+    c = _ln_check(xdt, wdt, cols, x, ldx, w, None, ldw, cu)
+    n = int(c[-1])
+    _check_rows("dy", dy, gdt, n, lddy, cols)
+    _check_out("stats", stats, torch.float32, 2 * n)
+    if dx is not None:
+        _check_rows("dx", dx, gdt, n, lddx, cols)
+    for name, t in (("dw", dw), ("db", db)):
+        if t is not None:
+            _check_rows(name, t, F32, c.size - 1, ldg, cols)
+    if ws is not None:
+        _check_bytes(ws)
+    s = _here(stream, x, stats, w, dy, dx, dw, db, ws)
+    _check("sphinx_layer_norm_backward", lib().sphinx_layer_norm_backward(
+        xdt, wdt, gdt, cols, _ptr(x), ldx, _ptr(stats), _ptr(w), ldw, int(plus_one), c.tobytes(), c.size - 1, _ptr(dy),
+        lddy, _ptr(dx), lddx, _ptr(dw), _ptr(db), ldg, _ptr(ws), 0 if ws is None else ws.nbytes, s))
+
+
+def sphinx_q8_bytes(rows: int, cols: int):
+    """Bytes of an 8-bit matrix [rows][cols] and of its scales."""
+    q, s = c_size_t(), c_size_t()
+    _check("sphinx_q8_bytes", lib().sphinx_q8_bytes(_int32("rows", rows), _int32("cols", cols), ctypes.byref(q),
+                                                    ctypes.byref(s)))
+    return q.value, s.value
+
+
+def sphinx_q8_quantise_workspace_bytes(rows: int, cols: int) -> int:
+    out = c_size_t()
+    _check("sphinx_q8_quantise_workspace_bytes", lib().sphinx_q8_quantise_workspace_bytes(
+        _int32("rows", rows), _int32("cols", cols), ctypes.byref(out)))
+    return out.value
+
+
+def sphinx_q8_quantise(dtype: int, x, ldx: int, rows: int, cols: int, square, q, s, qt=None, st=None, sums=None,
+                       ws=None, stream=None):
+    """x [rows][cols] in 8 bits: q and s; transposed, qt and st; and its column sums.  None: left out."""
+    import torch
+
+    _check_q8("q", q, s, rows, cols)
+    _check_q8("qt", qt, st, cols, rows)
+    _check_rows("x", x, dtype, rows, ldx, cols)
+    _check_out("sums", sums, torch.float32, cols)
+    if ws is not None:
+        _check_bytes(ws)
+    at = _here(stream, x, q, s, qt, st, sums, ws)
+    _check("sphinx_q8_quantise", lib().sphinx_q8_quantise(
+        dtype, _ptr(x), ldx, rows, cols, int(square), _ptr(q), _ptr(s), _ptr(qt), _ptr(st), _ptr(sums), _ptr(ws),
+        0 if ws is None else ws.nbytes, at))
+
+
+def sphinx_q8_matmul_workspace_bytes(odt: int, M: int, N: int, K: int) -> int:
+    out = c_size_t()
+    _check("sphinx_q8_matmul_workspace_bytes", lib().sphinx_q8_matmul_workspace_bytes(
+        odt, _int32("M", M), _int32("N", N), _int32("K", K), ctypes.byref(out)))
+    return out.value
+
+
+def sphinx_q8_matmul(odt: int, M: int, N: int, K: int, a, sa, b, sb, bdt: int, bias, epilogue: int, out, ldo: int, ws,
+                     stream=None):
+    """out [M][N] <- (or with Q8_ADD, +=) A B^T + bias, GELU with Q8_GELU, for 8-bit matrices A [M][K] and B [N][K]."""
+    _check_q8("a", a, sa, M, K)
+    _check_q8("b", b, sb, N, K)
+    if bias is not None:
+        _check_rows("bias", bias, bdt, 1, N, N)
+    _check_rows("out", out, odt, M, ldo, N)
+    if ws is not None:
+        _check_bytes(ws)
+    s = _here(stream, a, sa, b, sb, bias, out, ws)
+    _check("sphinx_q8_matmul", lib().sphinx_q8_matmul(
+        odt, M, N, K, _ptr(a), _ptr(sa), _ptr(b), _ptr(sb), bdt, _ptr(bias), epilogue, _ptr(out), ldo, _ptr(ws),
+        0 if ws is None else ws.nbytes, s))
 
 
 def sphinx_scatter_masked(reqs, x, idx, n: int, wmask, z, dtype: int, layout: int, stream=None):

@@ -1,0 +1,364 @@
+// Layer norm over rows in segments, forward and backward:
+//   m = mean(x), r = 1 / sqrt(mean((x - m)^2) + eps), xh = (x - m) r
+//   y = xh w' + b                                  w' = w or 1 + w, per segment
+//   g = dy w', dx = r (g - mean(g) - xh mean(g xh)), dw = sum dy xh, db = sum dy
+//
+// A row lives in the registers of LPR lanes (16, 64, 256 or 1024), eight
+// consecutive columns each and NI such groups, so HBM is read once and both
+// passes of the variance run over registers.  Everything is in fp32; y and dx
+// are rounded once.  Both directions are bound by HBM.
+#include <algorithm>
+
+#include "q8.hpp"
+
+namespace sphinx {
+
+namespace {
+// Threads of a workgroup, and rows that it holds at a time.
+template <int LPR>
+struct LnCfg {
+  static constexpr int NT = LPR > 256 ? LPR : 256, ROWS = NT / LPR;
+};
+
+// Sum over the LPR lanes of a row, in each of them; every lane of the workgroup
+// calls it where LPR > 64 (red: one float per wave, two sets used in turn).
+template <int LPR>
+__device__ __forceinline__ float ln_sum(float v, float* red) {
+  if constexpr (LPR == 16) return row_sum(v);
+  v = wave_sum(v);
+  if constexpr (LPR > 64) {
+    constexpr int NW = LPR / 64;
+    if (lane_id() == 0) red[threadIdx.x >> 6] = v;
+    __syncthreads();
+    v = 0.0f;
+#pragma unroll
+    for (int i = 0; i < NW; ++i) v += red[i];
+  }
+  return v;
+}
+
+__device__ __forceinline__ int ln_segment(const LnSegs& S, int row) {
+  int lo = 0, hi = S.nseg - 1;
+  while (lo < hi) {  // the last segment that starts at or before the row (empty ones start there as well)
+    const int mid = (lo + hi + 1) >> 1;
+    if (S.cu[mid] <= row) lo = mid; else hi = mid - 1;
+  }
+  return lo;
+}
+
+__device__ __forceinline__ void ln_load_w(const void* w, bool is_bf16, int64_t at, int n, float none, float (&v)[8]) {
+  if (w == nullptr) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = none;
+  } else if (is_bf16) {
+    load8(static_cast<const bf16*>(w) + at, n, v);
+  } else {
+    load8(static_cast<const float*>(w) + at, n, v);
+  }
+}
+
+struct Q8Out {
+  uint8_t* q;
+  uint8_t* s;
+};
+
+// OUT: bf16, float, or Q8Out for rows in 8 bits (16 lanes hold a block of 128 columns).
+template <typename XT, typename OUT, int LPR, int NI>
+__global__ __launch_bounds__(LnCfg<LPR>::NT) void k_layer_norm(LnArgs a, LnSegs S, OUT* __restrict__ y, int64_t ldy,
+                                                               Q8Out qo, float* __restrict__ stats) {
+  typedef LnCfg<LPR> C;
+  __shared__ float red[2][16];
+  const int t = (int)threadIdx.x % LPR, rows = S.cu[S.nseg], cols = a.cols;
+  const int row0 = (int)blockIdx.x * C::ROWS + (int)threadIdx.x / LPR;
+  const bool live = row0 < rows;
+  const int row = min(row0, rows - 1);  // lanes past the end repeat the last row and store nothing
+  const XT* x = static_cast<const XT*>(a.x) + (int64_t)row * a.ldx;
+  float v[NI][8];
+#pragma unroll
+  for (int i = 0; i < NI; ++i) load8(x + 8 * (i * LPR + t), cols - 8 * (i * LPR + t), v[i]);
+  float s = 0.0f;
+#pragma unroll
+  for (int i = 0; i < NI; ++i)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) s += v[i][e];
+  const float mean = ln_sum<LPR>(s, red[0]) / (float)cols;
+  s = 0.0f;
+#pragma unroll
+  for (int i = 0; i < NI; ++i) {
+    const int n = cols - 8 * (i * LPR + t);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      v[i][e] = e < n ? v[i][e] - mean : 0.0f;
+      s = fmaf(v[i][e], v[i][e], s);
+    }
+  }
+  const float rstd = 1.0f / sqrtf(ln_sum<LPR>(s, red[1]) / (float)cols + a.eps);
+  if (stats != nullptr && live && t == 0) {
+    stats[2 * (int64_t)row] = mean;
+    stats[2 * (int64_t)row + 1] = rstd;
+  }
+  const int64_t wr = (int64_t)ln_segment(S, row) * a.ldw;
+  const float one = a.plus_one ? 1.0f : 0.0f;
+#pragma unroll
+  for (int i = 0; i < NI; ++i) {
+    const int c = 8 * (i * LPR + t), n = cols - c;
+    float w[8], b[8], o[8];
+    ln_load_w(a.w, a.w_bf16, wr + c, n, 1.0f - one, w);
+    ln_load_w(a.b, a.w_bf16, wr + c, n, 0.0f, b);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) o[e] = fmaf(v[i][e] * rstd, w[e] + one, b[e]);
+    if constexpr (std::is_same_v<OUT, Q8Out>) {
+      float top = 0.0f;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        if (e >= n) o[e] = 0.0f;
+        top = fmaxf(top, finite_abs(o[e]));
+      }
+      const int sb = q8_scale_byte(row_max(top));
+      const uint2 p = q8_pack8(o, sb);
+      const int64_t ld = (cols + kQ8Block - 1) / kQ8Block * (int64_t)kQ8Block;
+      if (live && c < ld) {
+        *reinterpret_cast<uint2*>(qo.q + row * ld + c) = p;
+        if (t % 16 == 0) qo.s[row * (((ld >> 7) + 3) & ~(int64_t)3) + (c >> 7)] = (uint8_t)sb;
+      }
+    } else {
+      if (live) store8(y + (int64_t)row * ldy + c, n, o);
+    }
+  }
+}
+
+// Rows of a chunk: a workgroup walks over one chunk of one segment's rows and
+// keeps the sums of its columns in registers; the chunks' sums are joined by
+// k_join_parts in a fixed order, so a call repeats bit for bit.
+struct LnChunks {
+  int rows;                             // of a chunk (the segment's last may hold fewer)
+  int first[SPHINX_MAX_REQUESTS + 1];   // chunks of the segments before
+};
+
+template <typename XT, typename GT, int LPR, int NI>
+__global__ __launch_bounds__(LnCfg<LPR>::NT) void k_layer_norm_backward(LnArgs a, LnSegs S, LnChunks P,
+                                                                        const float* __restrict__ stats,
+                                                                        const GT* __restrict__ dy, int64_t lddy,
+                                                                        GT* __restrict__ dx, int64_t lddx,
+                                                                        float* __restrict__ part) {
+  typedef LnCfg<LPR> C;
+  __shared__ float red[4][16];
+  __shared__ float sums[C::ROWS > 1 ? C::NT * NI * 8 : 1];
+  const int t = (int)threadIdx.x % LPR, grp = (int)threadIdx.x / LPR, cols = a.cols;
+  int seg = 0;
+  {
+    int lo = 0, hi = S.nseg - 1;
+    while (lo < hi) {
+      const int mid = (lo + hi + 1) >> 1;
+      if (P.first[mid] <= (int)blockIdx.x) lo = mid; else hi = mid - 1;
+    }
+    seg = lo;
+  }
+  const int r0 = S.cu[seg] + ((int)blockIdx.x - P.first[seg]) * P.rows, r1 = min(r0 + P.rows, S.cu[seg + 1]);
+  const float one = a.plus_one ? 1.0f : 0.0f;
+  float w[NI][8], sw[NI][8], sb[NI][8];
+#pragma unroll
+  for (int i = 0; i < NI; ++i) {
+    const int c = 8 * (i * LPR + t);
+    ln_load_w(a.w, a.w_bf16, seg * a.ldw + c, cols - c, 1.0f - one, w[i]);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      w[i][e] += one;
+      sw[i][e] = sb[i][e] = 0.0f;
+    }
+  }
+  for (int r = r0; r < r1; r += C::ROWS) {  // the same number of turns for every lane
+    const bool live = r + grp < r1;
+    const int row = min(r + grp, r1 - 1);
+    const XT* xr = static_cast<const XT*>(a.x) + (int64_t)row * a.ldx;
+    const GT* gr = dy + (int64_t)row * lddy;
+    const float mean = stats[2 * (int64_t)row], rstd = stats[2 * (int64_t)row + 1];
+    float xh[NI][8], g[NI][8];
+#pragma unroll
+    for (int i = 0; i < NI; ++i) {
+      const int c = 8 * (i * LPR + t);
+      load8(xr + c, cols - c, xh[i]);
+      load8(gr + c, cols - c, g[i]);
+    }
+    float s1 = 0.0f, s2 = 0.0f;
+#pragma unroll
+    for (int i = 0; i < NI; ++i) {
+      const int n = cols - 8 * (i * LPR + t);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        xh[i][e] = e < n ? (xh[i][e] - mean) * rstd : 0.0f;
+        const float d = live ? g[i][e] : 0.0f;
+        sw[i][e] = live ? fmaf(d, xh[i][e], sw[i][e]) : sw[i][e];  // a repeated row adds nothing, NaN or not
+        sb[i][e] += d;
+        g[i][e] *= w[i][e];
+        s1 += e < n ? g[i][e] : 0.0f;
+        s2 = e < n ? fmaf(g[i][e], xh[i][e], s2) : s2;
+      }
+    }
+    if (dx != nullptr) {
+      const int par = LPR > 64 ? 2 * ((r - r0) & 1) : 0;
+      s1 = ln_sum<LPR>(s1, red[par]) / (float)cols;
+      s2 = ln_sum<LPR>(s2, red[par + 1]) / (float)cols;
+      if (live) {
+#pragma unroll
+        for (int i = 0; i < NI; ++i) {
+          const int c = 8 * (i * LPR + t);
+          float o[8];
+#pragma unroll
+          for (int e = 0; e < 8; ++e) o[e] = rstd * (g[i][e] - s1 - xh[i][e] * s2);
+          store8(dx + (int64_t)row * lddx + c, cols - c, o);
+        }
+      }
+    }
+  }
+  if (part == nullptr) return;
+  float* out = part + (int64_t)blockIdx.x * 2 * cols;
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    if constexpr (C::ROWS == 1) {
+#pragma unroll
+      for (int i = 0; i < NI; ++i) {
+        const int c = 8 * (i * LPR + t);
+        store8(out + k * cols + c, cols - c, k == 0 ? sw[i] : sb[i]);
+      }
+    } else {  // the row groups' sums through LDS
+      __syncthreads();
+#pragma unroll
+      for (int i = 0; i < NI; ++i)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sums[grp * (LPR * NI * 8) + 8 * (i * LPR + t) + e] = k == 0 ? sw[i][e] : sb[i][e];
+      __syncthreads();
+      for (int c = (int)threadIdx.x; c < cols; c += C::NT) {
+        float v = 0.0f;
+#pragma unroll
+        for (int j = 0; j < C::ROWS; ++j) v += sums[j * (LPR * NI * 8) + c];
+        out[k * cols + c] = v;
+      }
+    }
+  }
+}
+
+// 64 columns x 16 slices of the parts per workgroup.
+__global__ __launch_bounds__(1024) void k_join_parts(const float* __restrict__ part, int64_t stride, int cols,
+                                                     PartBounds P, float* __restrict__ out, int64_t ldo) {
+  __shared__ float red[16][64];
+  const int lane = (int)threadIdx.x & 63, slice = (int)threadIdx.x >> 6;
+  const int c = (int)blockIdx.x * 64 + lane, seg = (int)blockIdx.y;
+  float v = 0.0f;
+  if (c < cols)
+    for (int p = P.first[seg] + slice; p < P.first[seg + 1]; p += 16) v += part[p * stride + c];
+  red[slice][lane] = v;
+  __syncthreads();
+  if (slice == 0 && c < cols) {
+    v = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) v += red[i][lane];
+    out[seg * ldo + c] = v;
+  }
+}
+
+// Calls f with the lanes per row and groups of eight columns per lane as constants.
+template <typename F>
+void by_cols(int cols, F&& f) {
+  typedef std::integral_constant<int, 16> L16;
+  typedef std::integral_constant<int, 64> L64;
+  typedef std::integral_constant<int, 256> L256;
+  typedef std::integral_constant<int, 1024> L1024;
+  typedef std::integral_constant<int, 1> N1;
+  typedef std::integral_constant<int, 2> N2;
+  typedef std::integral_constant<int, 3> N3;
+  typedef std::integral_constant<int, 4> N4;
+  const int g = (cols + 7) / 8;
+  if (g <= 16) f(L16{}, N1{});
+  else if (g <= 64) f(L64{}, N1{});
+  else if (g <= 128) f(L64{}, N2{});
+  else if (g <= 192) f(L64{}, N3{});
+  else if (g <= 256) f(L64{}, N4{});
+  else if (g <= 512) f(L256{}, N2{});
+  else if (g <= 1024) f(L256{}, N4{});
+  else f(L1024{}, N2{});
+}
+
+LnChunks ln_chunks(int cols, const LnSegs& S) {
+  // about 1024 workgroups, four per CU, of at least one turn each
+  const int per = cols <= 128 ? 16 : cols <= 2048 ? 4 : 1;  // rows of a turn
+  const int64_t rows = S.cu[S.nseg];
+  LnChunks P;
+  P.rows = (int)std::max<int64_t>(per, (rows + 1023) / 1024);
+  P.rows = (P.rows + per - 1) / per * per;
+  P.first[0] = 0;
+  for (int i = 0; i < S.nseg; ++i)
+    P.first[i + 1] = P.first[i] + (int)(((int64_t)S.cu[i + 1] - S.cu[i] + P.rows - 1) / P.rows);
+  return P;
+}
+}  // namespace
+
+hipError_t launch_join_parts(const float* part, int64_t stride, int cols, const PartBounds& P, float* out, int64_t ldo,
+                             hipStream_t st) {
+  k_join_parts<<<dim3((unsigned)((cols + 63) / 64), (unsigned)P.nseg), 1024, 0, st>>>(part, stride, cols, P, out, ldo);
+  return hipGetLastError();
+}
+
+hipError_t launch_layer_norm(sphinx_dtype xdt, sphinx_dtype ydt, const LnArgs& a, const LnSegs& S, void* y,
+                             int64_t ldy, uint8_t* q, uint8_t* s, float* stats, hipStream_t st) {
+  by_cols(a.cols, [&](auto L, auto N) {
+    constexpr int LPR = decltype(L)::value, NI = decltype(N)::value;
+    typedef LnCfg<LPR> C;
+    const int grid = (S.cu[S.nseg] + C::ROWS - 1) / C::ROWS;
+    auto go = [&](auto xt, auto* out) {
+      typedef decltype(xt) XT;
+      typedef std::remove_pointer_t<decltype(out)> OT;
+      k_layer_norm<XT, OT, LPR, NI><<<grid, C::NT, 0, st>>>(a, S, out, ldy, Q8Out{q, s}, stats);
+    };
+    auto by_out = [&](auto xt) {
+      if (q != nullptr) go(xt, (Q8Out*)nullptr);
+      else if (ydt == SPHINX_BF16) go(xt, (bf16*)y);
+      else go(xt, (float*)y);
+    };
+    if (xdt == SPHINX_BF16) by_out(bf16{});
+    else by_out(float{});
+  });
+  return hipGetLastError();
+}
+
+size_t layer_norm_backward_ws_bytes(int cols, const LnSegs& S) {
+  return (size_t)ln_chunks(cols, S).first[S.nseg] * 2 * cols * 4;
+}
+
+hipError_t launch_layer_norm_backward(sphinx_dtype xdt, sphinx_dtype gdt, const LnArgs& a, const LnSegs& S,
+                                      const float* stats, const void* dy, int64_t lddy, void* dx, int64_t lddx,
+                                      float* dw, float* db, int64_t ldg, float* ws, hipStream_t st) {
+  const LnChunks P = ln_chunks(a.cols, S);
+  const int grid = P.first[S.nseg];
+  float* part = dw != nullptr || db != nullptr ? ws : nullptr;
+  if (grid > 0) {
+    by_cols(a.cols, [&](auto L, auto N) {
+      constexpr int LPR = decltype(L)::value, NI = decltype(N)::value;
+      auto go = [&](auto xt, auto gt) {
+        typedef decltype(xt) XT;
+        typedef decltype(gt) GT;
+        k_layer_norm_backward<XT, GT, LPR, NI><<<grid, LnCfg<LPR>::NT, 0, st>>>(
+            a, S, P, stats, (const GT*)dy, lddy, (GT*)dx, lddx, part);
+      };
+      auto by_g = [&](auto xt) {
+        if (gdt == SPHINX_BF16) go(xt, bf16{});
+        else go(xt, float{});
+      };
+      if (xdt == SPHINX_BF16) by_g(bf16{});
+      else by_g(float{});
+    });
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  PartBounds B;
+  B.nseg = S.nseg;
+  for (int i = 0; i <= S.nseg; ++i) B.first[i] = P.first[i];
+  if (dw != nullptr) {
+    const hipError_t e = launch_join_parts(ws, 2 * (int64_t)a.cols, a.cols, B, dw, ldg, st);
+    if (e != hipSuccess) return e;
+  }
+  if (db != nullptr) return launch_join_parts(ws + a.cols, 2 * (int64_t)a.cols, a.cols, B, db, ldg, st);
+  return hipSuccess;
+}
+
+}  // namespace sphinx
