@@ -540,7 +540,7 @@ sphinx_status sphinx_layer_norm_backward(sphinx_dtype xdt, sphinx_dtype wdt, sph
  *   q [rows][Kp]  e4m3 bytes, Kp = cols rounded up to a multiple of 128 (zeros
  *                 behind cols),
  *   s [rows][Sp]  scale bytes, one for each 128 columns, Sp = Kp/128 rounded up
- *                 to a multiple of 4 (what lies behind Kp/128 is not looked at):
+ *                 to a multiple of 16 (what lies behind Kp/128 is not looked at):
  *                 byte e + 127 stands for 2^e,
  * and holds the values q 2^e.  The numbers of a group share a scale: with A
  * their largest finite magnitude, e is the smallest integer with A <= 448 2^e,

@@ -119,7 +119,7 @@ __global__ __launch_bounds__(LnCfg<LPR>::NT) void k_layer_norm(LnArgs a, LnSegs 
       const int64_t ld = (cols + kQ8Block - 1) / kQ8Block * (int64_t)kQ8Block;
       if (live && c < ld) {
         *reinterpret_cast<uint2*>(qo.q + row * ld + c) = p;
-        if (t % 16 == 0) qo.s[row * (((ld >> 7) + 3) & ~(int64_t)3) + (c >> 7)] = (uint8_t)sb;
+        if (t % 16 == 0) qo.s[row * (int64_t)q8_scale_row((int)(ld >> 7)) + (c >> 7)] = (uint8_t)sb;
       }
     } else {
       if (live) store8(y + (int64_t)row * ldy + c, n, o);

@@ -3,7 +3,8 @@
 //
 // A matrix [rows][cols] in 8 bits is rows of Kp = 128 ceil(cols / 128) e4m3
 // bytes (zeros behind cols), and rows of scale bytes, one for each 128 columns,
-// padded to a multiple of four: byte b stands for 2^(b - 127).  Scales are
+// padded to a multiple of sixteen (a row's scales of sixteen blocks are one 16-byte
+// copy): byte b stands for 2^(b - 127).  Scales are
 // powers of two, so that the matrix cores apply them by themselves and exactly;
 // any other scale would cost a multiply-add of every partial sum of 128
 // products, 16 vector instructions beside 128 cycles of a 32x32x64 product.
@@ -17,7 +18,9 @@ constexpr int kQ8Block = 128;
 constexpr int kLnMaxCols = 16384;
 
 inline int64_t q8_row_bytes(int64_t cols) { return (cols + kQ8Block - 1) / kQ8Block * kQ8Block; }
-inline int64_t q8_scale_bytes(int64_t cols) { return ((cols + kQ8Block - 1) / kQ8Block + 3) / 4 * 4; }
+// Bytes of a row's scales, from its number of blocks.
+__host__ __device__ inline int q8_scale_row(int blocks) { return (blocks + 15) & ~15; }
+inline int64_t q8_scale_bytes(int64_t cols) { return q8_scale_row((int)((cols + kQ8Block - 1) / kQ8Block)); }
 
 // Rows [cu[i], cu[i+1]) belong to segment i.
 struct LnSegs {

@@ -17,6 +17,7 @@
 #include <type_traits>
 
 #include "q8.hpp"
+#include "q8_rules.hpp"
 
 namespace sphinx {
 
@@ -27,137 +28,332 @@ typedef int i32x4 __attribute__((ext_vector_type(4)));
 // s_waitcnt immediate: vmcnt(vm) lgkmcnt(0)
 constexpr int wait_vm(int vm) { return 0x0070 | (vm & 15) | ((vm >> 4) << 14); }
 
+// 8 columns n .. n + 7 of row m.
 template <typename OT>
-__device__ __forceinline__ void q8_store4(const Q8Epi& e, int64_t m, int n, int N, f32x4 v) {
+__device__ __forceinline__ void q8_store8(const Q8Epi& e, int64_t m, int n, int N, float (&v)[8]) {
+  if (n >= N) return;
   OT* o = static_cast<OT*>(e.out) + m * e.ldo + n;
+  const int left = N - n;
+  if (e.bias != nullptr) {
+    float b[8];
+    if (e.bias_bf16) load8(static_cast<const bf16*>(e.bias) + n, left, b);
+    else load8(static_cast<const float*>(e.bias) + n, left, b);
 #pragma unroll
-  for (int t = 0; t < 4; ++t) {
-    if (e.bias != nullptr && n + t < N)
-      v[t] += e.bias_bf16 ? (float)static_cast<const bf16*>(e.bias)[n + t] : static_cast<const float*>(e.bias)[n + t];
-    if (e.epi == Q8_EPI_GELU) v[t] = gelu_tanh(v[t]);
+    for (int t = 0; t < 8; ++t) v[t] += b[t];
   }
+  if (e.epi == Q8_EPI_GELU) {
 #pragma unroll
-  for (int t = 0; t < 4; ++t)
-    if (n + t < N) o[t] = (OT)(e.epi == Q8_EPI_ADD ? (float)o[t] + v[t] : v[t]);
+    for (int t = 0; t < 8; ++t) v[t] = gelu_tanh(v[t]);
+  } else if (e.epi == Q8_EPI_ADD) {
+    float b[8];
+    load8(o, left, b);
+#pragma unroll
+    for (int t = 0; t < 8; ++t) v[t] += b[t];
+  }
+  store8(o, left, v);
 }
 
-template <typename OT>
-__global__ __launch_bounds__(256, 2) void k_q8_matmul(const uint8_t* __restrict__ A, const uint8_t* __restrict__ sA,
-                                                      const uint8_t* __restrict__ B, const uint8_t* __restrict__ sB,
-                                                      int M, int N, int KB, Q8Epi e) {
+__device__ __forceinline__ bf16x8 q8_widen(int lo, int hi, float scale) {
+  const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, false);
+  const bf16x2 b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, true);
+  const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, false);
+  const bf16x2 d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, true);
+  return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+}
+
+// Waves in WM x WN, each 32 TI x 32 TJ outputs.
+template <int TI, int TJ, int WM, int WN>
+struct Q8Cfg {
+  static constexpr int NW = WM * WN, NT = 64 * NW, BM = 32 * TI * WM, BN = 32 * TJ * WN;
+  static constexpr int STAGE = (BM + BN) * 128, SCALES = 64 * NW * 16, SMEM = 2 * (STAGE + SCALES);
+  static constexpr int COPIES = (BM + BN) / 8 / NW;  // 8-row copies per wave and stage
+  static_assert(COPIES * 8 * NW == BM + BN, "every wave copies as many rows");
+  static_assert(BM % 64 == 0 && BM + BN <= 64 * NW, "one copy of 64 rows' scales per wave, of one operand");
+};
+
+// Tile (m0, n0) over the blocks k0 .. k1 - 1 of the contraction (k0 a multiple
+// of 4); part != NULL: the sums go there, [M][N], as they are.
+template <typename OT, int TI, int TJ, int WM, int WN>
+__device__ __forceinline__ void q8_tile(const uint8_t* __restrict__ A, const uint8_t* __restrict__ sA,
+                                        const uint8_t* __restrict__ B, const uint8_t* __restrict__ sB, int M, int N,
+                                        int KB, const Q8Epi& e, unsigned char* smem, int m0, int n0, int k0, int k1,
+                                        float* part) {
+  typedef Q8Cfg<TI, TJ, WM, WN> C;
   constexpr bool kWide = std::is_same_v<OT, float>;  // fp32 outputs
-  constexpr int BM = 128, BN = 128, STAGE = (BM + BN) * 128, COPIES = (BM + BN) / 8 / 4;
-  __shared__ __attribute__((aligned(1024))) unsigned char smem[2 * STAGE];
-  const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-  const int r32 = lane & 31, g = lane >> 5;
-  const int nt = (N + BN - 1) / BN;
-  const int tile = xcd_tile((int)blockIdx.x, (int)gridDim.x);
-  const int m0 = tile / nt * BM, n0 = tile % nt * BN;
+  constexpr int BM = C::BM, BN = C::BN, STAGE = C::STAGE, COPIES = C::COPIES, NW = C::NW;
+  const int tid = (int)threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wm = wave / WN, wn = wave % WN, g = lane >> 5, r32 = lane & 31;
   const int64_t ld = (int64_t)KB * kQ8Block;
-  const int lds = (KB + 3) & ~3;
+  const int lds = q8_scale_row(KB);
+  // copy c of this wave fills rows 8q .. 8q+7 of the stage (A rows, then B rows), q = NW c + wave
   const uint8_t* src[COPIES];
   uint32_t voff[COPIES];
 #pragma unroll
-  for (int i = 0; i < COPIES; ++i) {
-    const int qd = wave * COPIES + i, row = 8 * qd + (lane >> 3);
-    const int c = (lane & 7) ^ ((row >> 1) & 7);
-    const bool is_a = 8 * qd < BM;
-    src[i] = is_a ? A + m0 * ld : B + n0 * ld;  // rows past the end repeat the last one
-    voff[i] = (uint32_t)((is_a ? min(row, M - 1 - m0) : min(row - BM, N - 1 - n0)) * ld + 16 * c);
+  for (int c = 0; c < COPIES; ++c) {
+    const int q = NW * c + wave, row = 8 * q + (lane >> 3);
+    const int ch = (lane & 7) ^ ((row >> 1) & 7);
+    const bool is_a = 8 * q < BM;
+    src[c] = is_a ? A + m0 * ld : B + n0 * ld;  // rows past the end repeat the last one
+    voff[c] = (uint32_t)((is_a ? min(row, M - 1 - m0) : min(row - BM, N - 1 - n0)) * ld + 16 * ch);
   }
-  auto copy = [&](int kb) {
-    unsigned char* base = smem + (kb & 1) * STAGE;
-#pragma unroll
-    for (int i = 0; i < COPIES; ++i)
-      lds_dma16_at(src[i] + (int64_t)kb * kQ8Block, voff[i], base + (wave * COPIES + i) * 1024);
+  auto copy = [&](int kt, int slot, int c) {
+    lds_dma16_at(src[c] + (int64_t)kt * kQ8Block, voff[c], smem + slot * STAGE + (NW * c + wave) * 1024);
   };
-  const int a0 = (wave >> 1) * 64, b0 = (wave & 1) * 64;
-  const uint8_t* sa[2];
-  const uint8_t* sb[2];
-#pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    sa[i] = sA + (int64_t)min(m0 + a0 + 32 * i + r32, M - 1) * lds;
-    sb[i] = sB + (int64_t)min(n0 + b0 + 32 * i + r32, N - 1) * lds;
+  const int a0 = wm * 32 * TI, b0 = wn * 32 * TJ;
+  // Scales: 16 bytes of a row are 16 steps; rows of the tile in order (A, then B), two such sets used in turn.  A
+  // lane takes the bytes of four steps at a time, a dword for each row of a fragment.
+  unsigned char* ssm = smem + 2 * STAGE;
+  const uint8_t* ssrc;
+  {
+    const int row = 64 * wave;  // of lane 0; a wave's 64 rows are of one operand (past the tile: of none)
+    const bool is_a = row < BM;
+    const int at = is_a ? min(m0 + row + lane, M - 1) : min(n0 + row - BM + lane, N - 1);
+    ssrc = (is_a ? sA : sB) + (int64_t)at * lds;
   }
-  f32x16 acc[2][2] = {};
-  if (KB > 0) copy(0);
-  for (int kb = 0; kb < KB; ++kb) {
-    const int xa[2] = {sa[0][kb], sa[1][kb]}, xb[2] = {sb[0][kb], sb[1][kb]};
-    __builtin_amdgcn_s_waitcnt(wait_vm(0));  // step kb has landed, and every wave has read step kb - 1
+  auto copy_scales = [&](int chunk) {
+    lds_dma16(ssrc + 16 * min(chunk, lds / 16 - 1), ssm + (chunk & 1) * C::SCALES + wave * 1024);
+  };
+  int sc[TI + TJ], sn[TI + TJ];
+  auto read_scales = [&](int kt) {
+    const unsigned char* p = ssm + (kt >> 4 & 1) * C::SCALES + (kt >> 2 & 3) * 4 + r32 * 16;
+#pragma unroll
+    for (int i = 0; i < TI; ++i) sn[i] = *reinterpret_cast<const int*>(p + (a0 + 32 * i) * 16);
+#pragma unroll
+    for (int j = 0; j < TJ; ++j) sn[TI + j] = *reinterpret_cast<const int*>(p + (BM + b0 + 32 * j) * 16);
+  };
+  int foff[2][2];
+#pragma unroll
+  for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+    for (int h = 0; h < 2; ++h) foff[ks][h] = r32 * 128 + (((4 * ks + 2 * g + h) ^ ((r32 >> 1) & 7)) << 4);
+
+  f32x16 acc[TI][TJ] = {};
+  if (k1 > k0) {
+    copy_scales(k0 >> 4);
+#pragma unroll
+    for (int st = 0; st < 2; ++st)
+#pragma unroll
+      for (int c = 0; c < COPIES; ++c) copy(min(k0 + st, k1 - 1), st, c);
+    __builtin_amdgcn_s_waitcnt(wait_vm(COPIES));  // stage 0 must land
     asm volatile("" ::: "memory");
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
-    if (kb + 1 < KB) copy(kb + 1);
-    const unsigned char* st = smem + (kb & 1) * STAGE;
+    read_scales(k0);
 #pragma unroll
-    for (int ks = 0; ks < 2; ++ks) {
-      i32x4 fa[2][2], fb[2][2];
+    for (int i = 0; i < TI + TJ; ++i) sc[i] = sn[i];
+  }
+  i32x8 fa[2][TI], fb[2][TJ];
+  // fragment r of a k-step: the TJ of B first, then the TI of A
+  auto read = [&](int slot, int ks, int r) {
+    const unsigned char* st = smem + slot * STAGE + (r < TJ ? BM + b0 + 32 * r : a0 + 32 * (r - TJ)) * 128;
+    const i32x4 lo = *reinterpret_cast<const i32x4*>(st + foff[ks][0]);
+    const i32x4 hi = *reinterpret_cast<const i32x4*>(st + foff[ks][1]);
+    const i32x8 v = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+    if (r < TJ) fb[ks][r] = v; else fa[ks][r - TJ] = v;
+  };
+  bf16x8 wb[TJ][4];
+  // a row of a k-step: its TJ products
+  auto row = [&](int ks, int i, auto U) {
+    constexpr int u = decltype(U)::value;
+    if constexpr (!kWide) {
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const int off = r32 * 128 + (((4 * ks + 2 * g + h) ^ ((r32 >> 1) & 7)) << 4);
+      for (int j = 0; j < TJ; ++j)
+        acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(fb[ks][j], fa[ks][i], acc[i][j], 0, 0, u,
+                                                                    sc[TI + j], u, sc[i]);
+    } else {
+      // eight bytes of a lane at a time: the order of the contraction is free, and the same on both sides
+      const float s = __int_as_float((int)(((uint32_t)sc[i] >> (8 * u) & 255u) << 23));
+      if (i == 0) {
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          fa[i][h] = *reinterpret_cast<const i32x4*>(st + (a0 + 32 * i) * 128 + off);
-          fb[i][h] = *reinterpret_cast<const i32x4*>(st + (BM + b0 + 32 * i) * 128 + off);
+        for (int j = 0; j < TJ; ++j) {
+          const float t = __int_as_float((int)(((uint32_t)sc[TI + j] >> (8 * u) & 255u) << 23));
+#pragma unroll
+          for (int p = 0; p < 4; ++p) wb[j][p] = q8_widen(fb[ks][j][2 * p], fb[ks][j][2 * p + 1], t);
         }
       }
-      if constexpr (!kWide) {
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
+      for (int p = 0; p < 4; ++p) {
+        const bf16x8 wa = q8_widen(fa[ks][i][2 * p], fa[ks][i][2 * p + 1], s);
 #pragma unroll
-          for (int j = 0; j < 2; ++j)
-            acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(
-                __builtin_shufflevector(fb[j][0], fb[j][1], 0, 1, 2, 3, 4, 5, 6, 7),
-                __builtin_shufflevector(fa[i][0], fa[i][1], 0, 1, 2, 3, 4, 5, 6, 7), acc[i][j], 0, 0, 0, xb[j], 0, xa[i]);
-      } else {
-        // eight bytes of a lane at a time: the order of the contraction is free, and the same on both sides
-        auto wide = [](int lo, int hi, float scale) {
-          const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, false);
-          const bf16x2 b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, true);
-          const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, false);
-          const bf16x2 d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, true);
-          return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
-        };
-#pragma unroll
-        for (int u = 0; u < 4; ++u) {
-          bf16x8 wa[2], wb[2];
-#pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            wa[i] = wide(fa[i][u >> 1][2 * (u & 1)], fa[i][u >> 1][2 * (u & 1) + 1], two_to(xa[i] - 127));
-            wb[i] = wide(fb[i][u >> 1][2 * (u & 1)], fb[i][u >> 1][2 * (u & 1) + 1], two_to(xb[i] - 127));
-          }
-#pragma unroll
-          for (int i = 0; i < 2; ++i)
-#pragma unroll
-            for (int j = 0; j < 2; ++j)
-              acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wb[j], wa[i], acc[i][j], 0, 0, 0);
-        }
+        for (int j = 0; j < TJ; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wb[j][p], wa, acc[i][j], 0, 0, 0);
       }
     }
+    // the products stay here: without this the compiler sinks them past the copies and the barrier into the next
+    // block, and spills the fragments that they wait with
+#pragma unroll
+    for (int j = 0; j < TJ; ++j) asm volatile("" : "+v"(acc[i][j]));
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  constexpr int LAST = TJ + TI - 1;       // A fragment TI - 1, read at the start of its own k-step
+  constexpr int BR = TI >= 3 ? 1 : 0;     // rows of the second k-step before the barrier
+  constexpr int RR = TI - BR;             // and after it
+  auto step = [&](int kt, auto U) {
+    constexpr int u = decltype(U)::value, s = u & 1;
+#pragma unroll
+    for (int i = 0; i < TI; ++i) {
+      if (i == 0) read(s, 0, LAST);
+      if (i < TJ) read(s, 1, i);
+      if (i >= 1) read(s, 1, TJ + i - 1);
+      if (TI < TJ && i + 1 == TI) read(s, 1, TJ - 1);
+      row(0, i, U);
+    }
+#pragma unroll
+    for (int i = 0; i < TI; ++i) {
+      if (i == 0) read(s, 1, LAST);
+      if (i == BR) {
+        // stage kt+1 has landed, and every wave has read all of stage kt
+        __builtin_amdgcn_s_waitcnt(wait_vm(0));
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+      }
+      if (i >= BR) {
+        // the last stages are refilled with the last one, which is not read again
+        constexpr int CR = RR > 1 ? RR - 1 : 1;
+#pragma unroll
+        for (int c = 0; c < COPIES; ++c)
+          if (c * CR / COPIES == i - BR) copy(min(kt + 2, k1 - 1), s, c);
+        // the next 16 steps' scales, four times over: that costs less than a branch
+        if (u == 1 && i == BR) copy_scales((kt >> 4) + 1);
+        if (u == 3 && i + 1 == TI) read_scales(kt + 1);
+        // the next stage's first k-step over the rows left; fa[r] not before row r + 1
+#pragma unroll
+        for (int r = 0; r < LAST; ++r) {
+          const int even = r * RR / LAST, after = r - TJ + 1 - BR;
+          if ((even > after ? even : after) == i - BR) read(s ^ 1, 0, r);
+        }
+      }
+      row(1, i, U);
+    }
+    if constexpr (u == 3) {
+#pragma unroll
+      for (int i = 0; i < TI + TJ; ++i) sc[i] = sn[i];
+    }
+  };
+  if (k1 > k0) {
+#pragma unroll
+    for (int r = 0; r < LAST; ++r) read(0, 0, r);
+    typedef std::integral_constant<int, 0> U0;
+    typedef std::integral_constant<int, 1> U1;
+    typedef std::integral_constant<int, 2> U2;
+    typedef std::integral_constant<int, 3> U3;
+    int kt = k0;
+    for (; kt + 4 <= k1; kt += 4) {
+      step(kt, U0{});
+      step(kt + 1, U1{});
+      step(kt + 2, U2{});
+      step(kt + 3, U3{});
+    }
+    if (kt < k1) step(kt, U0{});
+    if (kt + 1 < k1) step(kt + 1, U1{});
+    if (kt + 2 < k1) step(kt + 2, U2{});
   }
-  // transposed blocks: lane l holds row l % 32 and, in registers 4q .. 4q+3, columns 8q + 4 (l / 32) .. + 3
+  // the refills of the last stages must land while the workgroup holds its LDS
+  __builtin_amdgcn_s_waitcnt(wait_vm(0));
+  // transposed blocks: lane l holds row l % 32 and, in registers 4q .. 4q+3, columns 8q + 4 (l / 32) .. + 3; the two
+  // halves of the wave swap so that each lane has eight neighbouring columns
 #pragma unroll
-  for (int i = 0; i < 2; ++i) {
+  for (int i = 0; i < TI; ++i) {
     const int m = m0 + a0 + 32 * i + r32;
-    if (m >= M) continue;
 #pragma unroll
-    for (int j = 0; j < 2; ++j)
+    for (int j = 0; j < TJ; ++j)
 #pragma unroll
-      for (int q = 0; q < 4; ++q)
-        q8_store4<OT>(e, m, n0 + b0 + 32 * j + 8 * q + 4 * g, N,
-                      f32x4{acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]});
+      for (int q = 0; q < 4; q += 2) {
+        float v[8];
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+          const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(acc[i][j][4 * q + t]),
+                                                          __float_as_uint(acc[i][j][4 * q + 4 + t]), false, false);
+          v[t] = __uint_as_float(x[0]);
+          v[4 + t] = __uint_as_float(x[1]);
+        }
+        if (m >= M) continue;
+        if (part != nullptr) {
+          const int n = n0 + b0 + 32 * j + 8 * (q + g);
+          store8(part + (int64_t)m * N + n, N - n, v);
+        } else {
+          q8_store8<OT>(e, m, n0 + b0 + 32 * j + 8 * (q + g), N, v);
+        }
+      }
+  }
+}
+
+// Tiles are dealt to the XCDs in contiguous ranges of panels four row tiles
+// high, column by column inside a panel, so that the tiles an XCD runs at a
+// time share few rows of A and B in its L2.  With part != NULL the contraction
+// is cut into gridDim.y pieces of `per` blocks.
+template <typename OT, int TI, int TJ, int WM, int WN>
+__global__ __launch_bounds__(64 * WM * WN, 2) void k_q8_matmul(
+    const uint8_t* __restrict__ A, const uint8_t* __restrict__ sA, const uint8_t* __restrict__ B,
+    const uint8_t* __restrict__ sB, int M, int N, int KB, Q8Epi e, int per, float* __restrict__ part) {
+  typedef Q8Cfg<TI, TJ, WM, WN> C;
+  __shared__ __attribute__((aligned(1024))) unsigned char smem[C::SMEM];
+  const int nt = (N + C::BN - 1) / C::BN, rt = (M + C::BM - 1) / C::BM;
+  const int tile = xcd_tile((int)blockIdx.x, rt * nt);
+  const int panel = tile / (4 * nt), rem = tile - panel * 4 * nt, ph = min(4, rt - 4 * panel);
+  const int k0 = (int)blockIdx.y * per;
+  q8_tile<OT, TI, TJ, WM, WN>(A, sA, B, sB, M, N, KB, e, smem, (4 * panel + rem % ph) * C::BM, (rem / ph) * C::BN, k0,
+                              min(KB, k0 + per), part == nullptr ? nullptr : part + (int64_t)blockIdx.y * M * N);
+}
+
+// The pieces of a cut contraction added in order, and the epilogue.
+template <typename OT>
+__global__ __launch_bounds__(256) void k_q8_join(const float* __restrict__ part, int pieces, int M, int N, Q8Epi e) {
+  const int wide = (N + 7) / 8;
+  const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x, m = at / wide;
+  if (m >= M) return;
+  const int n = (int)(at - m * wide) * 8;
+  const float* p = part + m * N + n;
+  float v[8];
+  load8(p, N - n, v);
+  for (int i = 1; i < pieces; ++i) {
+    float w[8];
+    load8(p + (int64_t)i * M * N, N - n, w);
+#pragma unroll
+    for (int t = 0; t < 8; ++t) v[t] += w[t];
+  }
+  q8_store8<OT>(e, m, n, N, v);
+}
+
+template <typename OT, int TI, int TJ, int WM, int WN>
+void launch_tiles(int M, int N, int KB, const Q8Mat& a, const Q8Mat& b, const Q8Epi& e, int pieces, float* ws,
+                  hipStream_t stream) {
+  typedef Q8Cfg<TI, TJ, WM, WN> C;
+  const int64_t grid = (int64_t)((M + C::BM - 1) / C::BM) * ((N + C::BN - 1) / C::BN);
+  const int per = ((KB + pieces - 1) / pieces + 3) / 4 * 4;
+  k_q8_matmul<OT, TI, TJ, WM, WN><<<dim3((unsigned)grid, (unsigned)pieces), C::NT, 0, stream>>>(
+      a.q, a.s, b.q, b.s, M, N, KB, e, per, pieces > 1 ? ws : nullptr);
+  if (pieces > 1) {
+    const int64_t n = (int64_t)M * ((N + 7) / 8);
+    k_q8_join<OT><<<(unsigned)((n + 255) / 256), 256, 0, stream>>>(ws, pieces, M, N, e);
   }
 }
 }  // namespace
 
-size_t q8_matmul_ws_bytes(sphinx_dtype odt, int M, int N, int K) { return 0; }
+size_t q8_matmul_ws_bytes(sphinx_dtype odt, int M, int N, int K) {
+  const Q8Plan p = plan_q8_matmul(odt == SPHINX_F32, M, N, (K + kQ8Block - 1) / kQ8Block);
+  return p.pieces > 1 ? (size_t)p.pieces * M * N * 4 : 0;
+}
 
 hipError_t launch_q8_matmul(sphinx_dtype odt, int M, int N, int K, const Q8Mat& a, const Q8Mat& b, const Q8Epi& e,
                             float* ws, hipStream_t stream) {
   const int KB = (K + kQ8Block - 1) / kQ8Block;
-  const int64_t grid = (int64_t)((M + 127) / 128) * ((N + 127) / 128);
-  if (odt == SPHINX_BF16) k_q8_matmul<bf16><<<(unsigned)grid, 256, 0, stream>>>(a.q, a.s, b.q, b.s, M, N, KB, e);
-  else k_q8_matmul<float><<<(unsigned)grid, 256, 0, stream>>>(a.q, a.s, b.q, b.s, M, N, KB, e);
+  const Q8Plan p = plan_q8_matmul(odt == SPHINX_F32, M, N, KB);
+  auto go = [&](auto ot) {
+    typedef decltype(ot) OT;
+    switch (p.tile) {
+      case kQ8Tile256:  // fp32 outputs: its fragments in bf16 would spill
+        if constexpr (std::is_same_v<OT, bf16>) launch_tiles<OT, 4, 2, 2, 4>(M, N, KB, a, b, e, p.pieces, ws, stream);
+        break;
+      case kQ8Tile192: launch_tiles<OT, 3, 2, 2, 4>(M, N, KB, a, b, e, p.pieces, ws, stream); break;
+      case kQ8Tile128: launch_tiles<OT, 2, 2, 2, 2>(M, N, KB, a, b, e, p.pieces, ws, stream); break;
+      case kQ8Tile128x64: launch_tiles<OT, 2, 1, 2, 2>(M, N, KB, a, b, e, p.pieces, ws, stream); break;
+      default: launch_tiles<OT, 1, 1, 2, 2>(M, N, KB, a, b, e, p.pieces, ws, stream);
+    }
+  };
+  if (odt == SPHINX_BF16) go(bf16{});
+  else go(float{});
   return hipGetLastError();
 }
 

@@ -25,7 +25,7 @@ __global__ __launch_bounds__(kNT) void k_q8_rows(const T* __restrict__ x, int64_
   const int sb = q8_scale_byte(row_max(top));
   if (row >= rows) return;
   *reinterpret_cast<uint2*>(q + row * wide * kQ8Block + c) = q8_pack8(v, sb);
-  if (t == 0) s[row * ((wide + 3) & ~3) + k] = (uint8_t)sb;
+  if (t == 0) s[row * q8_scale_row(wide) + k] = (uint8_t)sb;
 }
 
 template <typename T, bool SQUARE>
@@ -74,7 +74,7 @@ __global__ __launch_bounds__(kNT) void k_q8_tile(const T* __restrict__ x, int64_
       const int64_t m = m0 + 8 * g + i;
       if (m < rows) {
         *reinterpret_cast<uint2*>(q + m * wide * kQ8Block + c) = q8_pack8(v[i], sb);
-        if (t == 0) s[m * ((wide + 3) & ~3) + tn] = (uint8_t)sb;
+        if (t == 0) s[m * q8_scale_row(wide) + tn] = (uint8_t)sb;
       }
     }
   }
@@ -119,7 +119,7 @@ __global__ __launch_bounds__(kNT) void k_q8_tile(const T* __restrict__ x, int64_
 #pragma unroll
     for (int i = 0; i < 8; ++i) col[i] = v[i][e];
     *reinterpret_cast<uint2*>(&tr[8 * t + e][8 * g]) = q8_pack8(col, sb);
-    if (g == 0 && c + e < cols) st[(int64_t)(c + e) * ((tall + 3) & ~3) + tm] = (uint8_t)sb;
+    if (g == 0 && c + e < cols) st[(int64_t)(c + e) * q8_scale_row(tall) + tm] = (uint8_t)sb;
   }
   __syncthreads();
 #pragma unroll

@@ -29,7 +29,7 @@ def values(q, s, rows, cols):
     wide = (cols + 127) // 128
     v = q[:rows * wide * 128].view(torch.float8_e4m3fn).float().cpu().numpy().astype(np.float64).reshape(rows, wide * 128)
     assert (v[:, cols:] == 0).all()
-    e = s[:rows * ((wide + 3) // 4 * 4)].view(rows, -1)[:, :wide].cpu().numpy().astype(np.int64) - 127
+    e = s[:rows * ((wide + 15) // 16 * 16)].view(rows, -1)[:, :wide].cpu().numpy().astype(np.int64) - 127
     return (v * np.ldexp(1.0, np.repeat(e, 128, axis=1)))[:, :cols]
 
 
@@ -103,7 +103,7 @@ def test_quantise_extreme_numbers():
     q, s = empty(6, 128)
     B.sphinx_q8_quantise(B.F32, torch.from_numpy(x).to(DEV), 128, 6, 128, False, q, s)
     assert np.array_equal(values(q, s, 6, 128), Q.quantise(x.astype(np.float64)), equal_nan=True)
-    assert s.view(-1)[:24].view(6, 4)[:, 0].cpu().tolist() == [246, 27, 127, 128, 27, 27]
+    assert s[:96].view(6, 16)[:, 0].cpu().tolist() == [246, 27, 127, 128, 27, 27]
 
 
 def test_quantise_rounds_ties_to_even():

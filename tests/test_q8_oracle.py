@@ -161,8 +161,8 @@ def test_matmul_of_nothing_is_a_no_op():
 
 
 def test_sizes():
-    assert B.sphinx_q8_bytes(3, 129) == (3 * 256, 3 * 4)
-    assert B.sphinx_q8_bytes(2, 513) == (2 * 640, 2 * 8)
+    assert B.sphinx_q8_bytes(3, 129) == (3 * 256, 3 * 16)
+    assert B.sphinx_q8_bytes(2, 17 * 128 + 1) == (2 * 18 * 128, 2 * 32)
     assert B.sphinx_q8_bytes(0, 5) == (0, 0) and B.sphinx_q8_bytes(5, 0) == (0, 0)
     for bad in ((-1, 1), (1, -1), (1, (1 << 23) + 1)):
         with pytest.raises(S.SphinxError):
@@ -188,18 +188,18 @@ def test_binding_refuses_tensors_of_another_type_or_too_few():
         with pytest.raises(ValueError):
             call(**bad)
     u8 = lambda n: torch.zeros(n, dtype=torch.uint8)  # noqa: E731
-    for q, s in ((u8(511), u8(16)), (u8(512), u8(15)), (u8(512), None), (zeros(512), u8(16)), (u8(1024)[::2], u8(16))):
+    for q, s in ((u8(511), u8(64)), (u8(512), u8(63)), (u8(512), None), (zeros(512), u8(64)), (u8(1024)[::2], u8(64))):
         with pytest.raises(ValueError):
             B.sphinx_q8_quantise(B.BF16, x, 64, 4, 64, False, q, s)
         with pytest.raises(ValueError):
             B.sphinx_layer_norm_q8(B.BF16, B.F32, 64, 1e-6, x, 64, None, None, 64, False, [0, 4], q, s)
         with pytest.raises(ValueError):
-            B.sphinx_q8_matmul(B.BF16, 4, 4, 64, q, s, u8(512), u8(16), B.F32, None, B.Q8_STORE, zeros(4, 4), 4, None)
+            B.sphinx_q8_matmul(B.BF16, 4, 4, 64, q, s, u8(512), u8(64), B.F32, None, B.Q8_STORE, zeros(4, 4), 4, None)
     with pytest.raises(ValueError, match="bias"):
-        B.sphinx_q8_matmul(B.BF16, 4, 4, 64, u8(512), u8(16), u8(512), u8(16), B.F32, zeros(4), B.Q8_STORE,
+        B.sphinx_q8_matmul(B.BF16, 4, 4, 64, u8(512), u8(64), u8(512), u8(64), B.F32, zeros(4), B.Q8_STORE,
                            zeros(4, 4), 4, None)
     with pytest.raises(ValueError, match="out"):
-        B.sphinx_q8_matmul(B.BF16, 4, 4, 64, u8(512), u8(16), u8(512), u8(16), B.F32, None, B.Q8_STORE, zeros(3, 4), 4,
+        B.sphinx_q8_matmul(B.BF16, 4, 4, 64, u8(512), u8(64), u8(512), u8(64), B.F32, None, B.Q8_STORE, zeros(3, 4), 4,
                            None)
     f = torch.float32
     with pytest.raises(ValueError, match="dw"):
