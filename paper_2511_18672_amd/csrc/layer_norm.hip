@@ -135,6 +135,22 @@ struct LnChunks {
   int first[SPHINX_MAX_REQUESTS + 1];   // chunks of the segments before
 };
 
+// Eight elements as they are in memory, zeros behind n.
+template <typename T>
+struct Raw8 {
+  T v[8];
+  __device__ __forceinline__ void load(const T* p, int n) {
+    if (n >= 8) {
+      __builtin_memcpy(v, p, sizeof(v));
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] = i < n ? p[i] : (T)0.0f;
+    }
+  }
+};
+
+// The next row's loads are issued before this row's arithmetic.  Columns behind
+// the last one hold dy = 0, which adds nothing to a sum over the row.
 template <typename XT, typename GT, int LPR, int NI>
 __global__ __launch_bounds__(LnCfg<LPR>::NT) void k_layer_norm_backward(LnArgs a, LnSegs S, LnChunks P,
                                                                         const float* __restrict__ stats,
@@ -157,6 +173,22 @@ __global__ __launch_bounds__(LnCfg<LPR>::NT) void k_layer_norm_backward(LnArgs a
   const int r0 = S.cu[seg] + ((int)blockIdx.x - P.first[seg]) * P.rows, r1 = min(r0 + P.rows, S.cu[seg + 1]);
   const float one = a.plus_one ? 1.0f : 0.0f;
   float w[NI][8], sw[NI][8], sb[NI][8];
+  Raw8<XT> rx[NI];
+  Raw8<GT> rg[NI];
+  float mean, rstd;
+  auto fetch = [&](int row) {
+    const XT* xr = static_cast<const XT*>(a.x) + (int64_t)row * a.ldx;
+    const GT* gr = dy + (int64_t)row * lddy;
+    mean = stats[2 * (int64_t)row];
+    rstd = stats[2 * (int64_t)row + 1];
+#pragma unroll
+    for (int i = 0; i < NI; ++i) {
+      const int c = 8 * (i * LPR + t);
+      rx[i].load(xr + c, cols - c);
+      rg[i].load(gr + c, cols - c);
+    }
+  };
+  fetch(min(r0 + grp, r1 - 1));
 #pragma unroll
   for (int i = 0; i < NI; ++i) {
     const int c = 8 * (i * LPR + t);
@@ -167,47 +199,34 @@ __global__ __launch_bounds__(LnCfg<LPR>::NT) void k_layer_norm_backward(LnArgs a
       sw[i][e] = sb[i][e] = 0.0f;
     }
   }
-  for (int r = r0; r < r1; r += C::ROWS) {  // the same number of turns for every lane
-    const bool live = r + grp < r1;
-    const int row = min(r + grp, r1 - 1);
-    const XT* xr = static_cast<const XT*>(a.x) + (int64_t)row * a.ldx;
-    const GT* gr = dy + (int64_t)row * lddy;
-    const float mean = stats[2 * (int64_t)row], rstd = stats[2 * (int64_t)row + 1];
+  for (int row = r0 + grp; row < r1; row += C::ROWS) {
     float xh[NI][8], g[NI][8];
-#pragma unroll
-    for (int i = 0; i < NI; ++i) {
-      const int c = 8 * (i * LPR + t);
-      load8(xr + c, cols - c, xh[i]);
-      load8(gr + c, cols - c, g[i]);
-    }
     float s1 = 0.0f, s2 = 0.0f;
+    const float r = rstd;
 #pragma unroll
-    for (int i = 0; i < NI; ++i) {
-      const int n = cols - 8 * (i * LPR + t);
+    for (int i = 0; i < NI; ++i)
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        xh[i][e] = e < n ? (xh[i][e] - mean) * rstd : 0.0f;
-        const float d = live ? g[i][e] : 0.0f;
-        sw[i][e] = live ? fmaf(d, xh[i][e], sw[i][e]) : sw[i][e];  // a repeated row adds nothing, NaN or not
+        xh[i][e] = ((float)rx[i].v[e] - mean) * r;
+        const float d = (float)rg[i].v[e];
+        sw[i][e] = fmaf(d, xh[i][e], sw[i][e]);
         sb[i][e] += d;
-        g[i][e] *= w[i][e];
-        s1 += e < n ? g[i][e] : 0.0f;
-        s2 = e < n ? fmaf(g[i][e], xh[i][e], s2) : s2;
+        g[i][e] = d * w[i][e];
+        s1 += g[i][e];
+        s2 = fmaf(g[i][e], xh[i][e], s2);
       }
-    }
+    fetch(min(row + C::ROWS, r1 - 1));
     if (dx != nullptr) {
-      const int par = LPR > 64 ? 2 * ((r - r0) & 1) : 0;
+      const int par = LPR > 64 ? 2 * ((row - r0) & 1) : 0;
       s1 = ln_sum<LPR>(s1, red[par]) / (float)cols;
       s2 = ln_sum<LPR>(s2, red[par + 1]) / (float)cols;
-      if (live) {
 #pragma unroll
-        for (int i = 0; i < NI; ++i) {
-          const int c = 8 * (i * LPR + t);
-          float o[8];
+      for (int i = 0; i < NI; ++i) {
+        const int c = 8 * (i * LPR + t);
+        float o[8];
 #pragma unroll
-          for (int e = 0; e < 8; ++e) o[e] = rstd * (g[i][e] - s1 - xh[i][e] * s2);
-          store8(dx + (int64_t)row * lddx + c, cols - c, o);
-        }
+        for (int e = 0; e < 8; ++e) o[e] = r * (g[i][e] - s1 - xh[i][e] * s2);
+        store8(dx + (int64_t)row * lddx + c, cols - c, o);
       }
     }
   }
@@ -238,22 +257,33 @@ __global__ __launch_bounds__(LnCfg<LPR>::NT) void k_layer_norm_backward(LnArgs a
   }
 }
 
-// 64 columns x 16 slices of the parts per workgroup.
+// 64 columns x 16 slices of the parts per workgroup; out1 takes the columns from
+// `cols` on (a part holds two rows of them), and either may be NULL.
 __global__ __launch_bounds__(1024) void k_join_parts(const float* __restrict__ part, int64_t stride, int cols,
-                                                     PartBounds P, float* __restrict__ out, int64_t ldo) {
+                                                     PartBounds P, float* __restrict__ out0, float* __restrict__ out1,
+                                                     int64_t ldo) {
   __shared__ float red[16][64];
   const int lane = (int)threadIdx.x & 63, slice = (int)threadIdx.x >> 6;
   const int c = (int)blockIdx.x * 64 + lane, seg = (int)blockIdx.y;
-  float v = 0.0f;
-  if (c < cols)
-    for (int p = P.first[seg] + slice; p < P.first[seg + 1]; p += 16) v += part[p * stride + c];
-  red[slice][lane] = v;
+  const bool second = blockIdx.z == 1 || out0 == nullptr;
+  const float* p = part + (second ? cols : 0) + c;
+  float v[4] = {};
+  if (c < cols) {
+    const int end = P.first[seg + 1];
+    int i = P.first[seg] + slice;
+    for (; i + 48 < end; i += 64) {  // four sums, so that four loads are in flight
+#pragma unroll
+      for (int k = 0; k < 4; ++k) v[k] += p[(int64_t)(i + 16 * k) * stride];
+    }
+    for (; i < end; i += 16) v[0] += p[(int64_t)i * stride];
+  }
+  red[slice][lane] = (v[0] + v[1]) + (v[2] + v[3]);
   __syncthreads();
   if (slice == 0 && c < cols) {
-    v = 0.0f;
+    float sum = 0.0f;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) v += red[i][lane];
-    out[seg * ldo + c] = v;
+    for (int i = 0; i < 16; ++i) sum += red[i][lane];
+    (second ? out1 : out0)[seg * ldo + c] = sum;
   }
 }
 
@@ -280,11 +310,11 @@ void by_cols(int cols, F&& f) {
 }
 
 LnChunks ln_chunks(int cols, const LnSegs& S) {
-  // about 1024 workgroups, four per CU, of at least one turn each
+  // about 512 workgroups, two per CU, of at least one turn each
   const int per = cols <= 128 ? 16 : cols <= 2048 ? 4 : 1;  // rows of a turn
   const int64_t rows = S.cu[S.nseg];
   LnChunks P;
-  P.rows = (int)std::max<int64_t>(per, (rows + 1023) / 1024);
+  P.rows = (int)std::max<int64_t>(per, (rows + 511) / 512);
   P.rows = (P.rows + per - 1) / per * per;
   P.first[0] = 0;
   for (int i = 0; i < S.nseg; ++i)
@@ -293,9 +323,10 @@ LnChunks ln_chunks(int cols, const LnSegs& S) {
 }
 }  // namespace
 
-hipError_t launch_join_parts(const float* part, int64_t stride, int cols, const PartBounds& P, float* out, int64_t ldo,
-                             hipStream_t st) {
-  k_join_parts<<<dim3((unsigned)((cols + 63) / 64), (unsigned)P.nseg), 1024, 0, st>>>(part, stride, cols, P, out, ldo);
+hipError_t launch_join_parts(const float* part, int64_t stride, int cols, const PartBounds& P, float* out0,
+                             float* out1, int64_t ldo, hipStream_t st) {
+  const dim3 grid((unsigned)((cols + 63) / 64), (unsigned)P.nseg, out0 != nullptr && out1 != nullptr ? 2 : 1);
+  k_join_parts<<<grid, 1024, 0, st>>>(part, stride, cols, P, out0, out1, ldo);
   return hipGetLastError();
 }
 
@@ -350,15 +381,11 @@ hipError_t launch_layer_norm_backward(sphinx_dtype xdt, sphinx_dtype gdt, const 
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
+  if (dw == nullptr && db == nullptr) return hipSuccess;
   PartBounds B;
   B.nseg = S.nseg;
   for (int i = 0; i <= S.nseg; ++i) B.first[i] = P.first[i];
-  if (dw != nullptr) {
-    const hipError_t e = launch_join_parts(ws, 2 * (int64_t)a.cols, a.cols, B, dw, ldg, st);
-    if (e != hipSuccess) return e;
-  }
-  if (db != nullptr) return launch_join_parts(ws + a.cols, 2 * (int64_t)a.cols, a.cols, B, db, ldg, st);
-  return hipSuccess;
+  return launch_join_parts(ws, 2 * (int64_t)a.cols, a.cols, B, dw, db, ldg, st);
 }
 
 }  // namespace sphinx

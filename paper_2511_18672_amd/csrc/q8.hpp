@@ -46,14 +46,14 @@ size_t layer_norm_backward_ws_bytes(int cols, const LnSegs& S);
 hipError_t launch_layer_norm_backward(sphinx_dtype xdt, sphinx_dtype gdt, const LnArgs& a, const LnSegs& S,
                                       const float* stats, const void* dy, int64_t lddy, void* dx, int64_t lddx,
                                       float* dw, float* db, int64_t ldg, float* ws, hipStream_t st);
-// Sums over parts: out[i][c] = sum over parts p in [first[i], first[i+1]) of part[p * stride + c], c < cols;
-// one output row per segment, in a fixed order.
+// Sums over parts: out0[i][c] = sum over parts p in [first[i], first[i+1]) of part[p * stride + c], c < cols, and out1
+// likewise of the cols behind them; one output row per segment, in a fixed order.  Either may be NULL.
 struct PartBounds {
   int nseg;
   int first[SPHINX_MAX_REQUESTS + 1];
 };
-hipError_t launch_join_parts(const float* part, int64_t stride, int cols, const PartBounds& P, float* out, int64_t ldo,
-                             hipStream_t st);
+hipError_t launch_join_parts(const float* part, int64_t stride, int cols, const PartBounds& P, float* out0,
+                             float* out1, int64_t ldo, hipStream_t st);
 
 // q8_quantise.hip
 hipError_t launch_q8_quantise(sphinx_dtype dt, const void* x, int64_t ldx, int rows, int cols, bool square, uint8_t* q,

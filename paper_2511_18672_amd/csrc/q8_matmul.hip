@@ -28,29 +28,33 @@ typedef int i32x4 __attribute__((ext_vector_type(4)));
 // s_waitcnt immediate: vmcnt(vm) lgkmcnt(0)
 constexpr int wait_vm(int vm) { return 0x0070 | (vm & 15) | ((vm >> 4) << 14); }
 
-// 8 columns n .. n + 7 of row m.
-template <typename OT>
-__device__ __forceinline__ void q8_store8(const Q8Epi& e, int64_t m, int n, int N, float (&v)[8]) {
-  if (n >= N) return;
-  OT* o = static_cast<OT*>(e.out) + m * e.ldo + n;
-  const int left = N - n;
+// Bias and GELU of columns n .. n + 7.
+__device__ __forceinline__ void q8_finish(const Q8Epi& e, int n, int N, float (&v)[8]) {
   if (e.bias != nullptr) {
     float b[8];
-    if (e.bias_bf16) load8(static_cast<const bf16*>(e.bias) + n, left, b);
-    else load8(static_cast<const float*>(e.bias) + n, left, b);
+    if (e.bias_bf16) load8(static_cast<const bf16*>(e.bias) + n, N - n, b);
+    else load8(static_cast<const float*>(e.bias) + n, N - n, b);
 #pragma unroll
     for (int t = 0; t < 8; ++t) v[t] += b[t];
   }
   if (e.epi == Q8_EPI_GELU) {
 #pragma unroll
     for (int t = 0; t < 8; ++t) v[t] = gelu_tanh(v[t]);
-  } else if (e.epi == Q8_EPI_ADD) {
+  }
+}
+
+// Finished columns n .. n + 7 of row m.
+template <typename OT>
+__device__ __forceinline__ void q8_store8(const Q8Epi& e, int64_t m, int n, int N, float (&v)[8]) {
+  if (n >= N) return;
+  OT* o = static_cast<OT*>(e.out) + m * e.ldo + n;
+  if (e.epi == Q8_EPI_ADD) {
     float b[8];
-    load8(o, left, b);
+    load8(o, N - n, b);
 #pragma unroll
     for (int t = 0; t < 8; ++t) v[t] += b[t];
   }
-  store8(o, left, v);
+  store8(o, N - n, v);
 }
 
 __device__ __forceinline__ bf16x8 q8_widen(int lo, int hi, float scale) {
@@ -251,32 +255,95 @@ __device__ __forceinline__ void q8_tile(const uint8_t* __restrict__ A, const uin
   }
   // the refills of the last stages must land while the workgroup holds its LDS
   __builtin_amdgcn_s_waitcnt(wait_vm(0));
+  asm volatile("" ::: "memory");
   // transposed blocks: lane l holds row l % 32 and, in registers 4q .. 4q+3, columns 8q + 4 (l / 32) .. + 3; the two
-  // halves of the wave swap so that each lane has eight neighbouring columns
+  // halves of the wave swap so that each lane has eight neighbouring columns, n0 + b0 + 32 j + 8 (q + g)
+  auto eight = [&](int i, int j, int q, float (&v)[8]) {
 #pragma unroll
-  for (int i = 0; i < TI; ++i) {
-    const int m = m0 + a0 + 32 * i + r32;
+    for (int t = 0; t < 4; ++t) {
+      const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(acc[i][j][4 * q + t]),
+                                                      __float_as_uint(acc[i][j][4 * q + 4 + t]), false, false);
+      v[t] = __uint_as_float(x[0]);
+      v[4 + t] = __uint_as_float(x[1]);
+    }
+  };
+  // bf16 outputs that are added to: the sum is rounded once, so it does not go through LDS in bf16
+  if (!kWide && part == nullptr && e.epi == Q8_EPI_ADD) {
 #pragma unroll
-    for (int j = 0; j < TJ; ++j)
+    for (int i = 0; i < TI; ++i) {
+      const int m = m0 + a0 + 32 * i + r32;
 #pragma unroll
-      for (int q = 0; q < 4; q += 2) {
-        float v[8];
+      for (int j = 0; j < TJ; ++j)
 #pragma unroll
-        for (int t = 0; t < 4; ++t) {
-          const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(acc[i][j][4 * q + t]),
-                                                          __float_as_uint(acc[i][j][4 * q + 4 + t]), false, false);
-          v[t] = __uint_as_float(x[0]);
-          v[4 + t] = __uint_as_float(x[1]);
-        }
-        if (m >= M) continue;
-        if (part != nullptr) {
+        for (int q = 0; q < 4; q += 2) {
+          float v[8];
+          eight(i, j, q, v);
           const int n = n0 + b0 + 32 * j + 8 * (q + g);
-          store8(part + (int64_t)m * N + n, N - n, v);
+          q8_finish(e, n, N, v);
+          if (m < M) q8_store8<OT>(e, m, n, N, v);
+        }
+    }
+    return;
+  }
+  // Rows go out through LDS, 32 at a time in a region of the wave's own, so that a store writes whole lines, which then
+  // bypass the caches (stores of 16-byte pieces of 32 rows, joined in L2, push the operands out of it: M 32256, N 4608,
+  // K 1152 195 us instead of 174; whole lines through L2 209).  Rows that start inside a line, and half lines, go
+  // through L2.
+  __builtin_amdgcn_s_barrier();  // every wave has read its last stage
+  asm volatile("" ::: "memory");
+  auto rows_out = [&](auto ot, auto* out, int64_t ldo, bool finish) {
+    typedef decltype(ot) ST;
+    constexpr int V = 16 / (int)sizeof(ST), PITCH = 32 * TJ * (int)sizeof(ST) + 16;  // values of a piece; bytes of a row
+    constexpr int LPW = 32 * TJ / V, RPP = 64 / LPW;                                // lanes of a row; rows of a store
+    unsigned char* mine = smem + wave * 32 * PITCH;
+    const int c = lane % LPW * V, n = n0 + b0 + c, left = N - n;
+    const bool lines = 32 * TJ * sizeof(ST) >= 128 && (((uintptr_t)out | (uint64_t)ldo * sizeof(ST)) & 127) == 0;
+#pragma unroll
+    for (int i = 0; i < TI; ++i) {
+#pragma unroll
+      for (int j = 0; j < TJ; ++j)
+#pragma unroll
+        for (int q = 0; q < 4; q += 2) {
+          float v[8];
+          eight(i, j, q, v);
+          if (finish) q8_finish(e, n0 + b0 + 32 * j + 8 * (q + g), N, v);
+          ST w[8];
+#pragma unroll
+          for (int t = 0; t < 8; ++t) w[t] = (ST)v[t];
+          __builtin_memcpy(__builtin_assume_aligned(mine + r32 * PITCH + (32 * j + 8 * (q + g)) * sizeof(ST), 16), w,
+                           8 * sizeof(ST));
+        }
+#pragma unroll
+      for (int p = 0; p < 32 / RPP; ++p) {
+        const int r = p * RPP + lane / LPW, m = m0 + a0 + 32 * i + r;
+        ST w[V];
+        __builtin_memcpy(w, __builtin_assume_aligned(mine + r * PITCH + c * sizeof(ST), 16), 16);
+        if (m >= M) continue;
+        ST* o = out + m * ldo + n;
+        if (left >= V) {
+          if (kWide && finish && e.epi == Q8_EPI_ADD) {
+            ST old[V];
+            __builtin_memcpy(old, o, 16);
+#pragma unroll
+            for (int t = 0; t < V; ++t) w[t] = (ST)((float)w[t] + (float)old[t]);
+          }
+          if (lines) {
+            f32x4 z;
+            __builtin_memcpy(&z, w, 16);
+            __builtin_nontemporal_store(z, reinterpret_cast<f32x4*>(o));
+          } else {
+            __builtin_memcpy(o, w, 16);
+          }
         } else {
-          q8_store8<OT>(e, m, n0 + b0 + 32 * j + 8 * (q + g), N, v);
+#pragma unroll
+          for (int t = 0; t < V; ++t)
+            if (t < left) o[t] = kWide && finish && e.epi == Q8_EPI_ADD ? (ST)((float)w[t] + (float)o[t]) : w[t];
         }
       }
-  }
+    }
+  };
+  if (part != nullptr) rows_out(float{}, part, N, false);
+  else rows_out(OT{}, static_cast<OT*>(e.out), e.ldo, true);
 }
 
 // Tiles are dealt to the XCDs in contiguous ranges of panels four row tiles
@@ -313,6 +380,7 @@ __global__ __launch_bounds__(256) void k_q8_join(const float* __restrict__ part,
 #pragma unroll
     for (int t = 0; t < 8; ++t) v[t] += w[t];
   }
+  q8_finish(e, n, N, v);
   q8_store8<OT>(e, m, n, N, v);
 }
 

@@ -160,7 +160,7 @@ hipError_t launch_q8_quantise(sphinx_dtype dt, const void* x, int64_t ldx, int r
   P.nseg = 1;
   P.first[0] = 0;
   P.first[1] = tall;
-  return launch_join_parts(ws, cols, cols, P, sums, cols, stream);
+  return launch_join_parts(ws, cols, cols, P, sums, nullptr, cols, stream);
 }
 
 }  // namespace sphinx
