@@ -166,6 +166,21 @@ def lib() -> ctypes.CDLL:
     return L
 
 
+_torch = None
+_TYPES = {}
+
+
+def _load_torch():
+    """torch, imported once (an import statement in a function takes a tenth of a microsecond), and its types."""
+    global _torch
+    if _torch is None:
+        import torch
+
+        _TYPES.update({F32: torch.float32, BF16: torch.bfloat16, "u8": torch.uint8})
+        _torch = torch
+    return _torch
+
+
 def _check(fn: str, status: int):
     if status != 0:
         raise SphinxError(fn, status)
@@ -401,8 +416,7 @@ def _host_cu(cu) -> np.ndarray:
 
 def _here(stream, *tensors) -> Optional[int]:
     """The stream of a call on the current device; tensors and streams that are not on it are refused."""
-    import torch
-
+    torch = _torch or _load_torch()
     dev = torch.cuda.current_device()
     for t in tensors:
         if t is not None and t.get_device() != dev:
@@ -429,9 +443,9 @@ def _check_idx(idx, n: int):
 def _check_rows(name: str, t, dtype: int, n: int, ld: int, width: int):
     """Refuses a tensor of another type than the code names, or without memory for n rows of `width` elements, each ld
     behind the one before."""
-    import torch
-
-    if t.dtype is not (torch.bfloat16 if dtype == BF16 else torch.float32) and dtype in (F32, BF16):
+    if _torch is None:
+        _load_torch()
+    if t.dtype is not _TYPES.get(dtype, t.dtype):
         raise ValueError(f"{name} is {t.dtype}, the call names another type")
     need = (n - 1) * ld + width
     if n > 0 and not (t.is_contiguous() and t.numel() >= need):
@@ -550,13 +564,15 @@ def _check_out(name: str, t, dtype, n: int):
 
 
 def _check_q8(name: str, q, s, rows: int, cols: int):
-    import torch
-
-    if (q is None) != (s is None):
+    if q is None and s is None:
+        return
+    if q is None or s is None:
         raise ValueError(f"{name}: its bytes and its scales come together")
-    nq, ns = sphinx_q8_bytes(rows, cols)
-    _check_out(name, q, torch.uint8, nq)
-    _check_out(name + "'s scales", s, torch.uint8, ns)
+    if _torch is None:
+        _load_torch()
+    u8, wide = _TYPES["u8"], (cols + 127) // 128  # sizes that the library refuses are refused by the call
+    _check_out(name, q, u8, rows * wide * 128)
+    _check_out(name, s, u8, rows * ((wide + 15) // 16 * 16))
 
 
 def _ln_check(xdt: int, wdt: int, cols: int, x, ldx: int, w, b, ldw: int, cu) -> np.ndarray:
@@ -574,11 +590,9 @@ def sphinx_layer_norm(xdt: int, wdt: int, ydt: int, cols: int, eps: float, x, ld
                       y, ldy: int, stats=None, stream=None):
     """y <- the normalised rows of x, scaled by w (1 + w with plus_one) and shifted by b, a row of each per segment
     (cu: host int sequence of row bounds; w, b: None for ones and zeros).  stats: float32 [rows][2] or None."""
-    import torch
-
     c = _ln_check(xdt, wdt, cols, x, ldx, w, b, ldw, cu)
     _check_rows("y", y, ydt, int(c[-1]), ldy, cols)
-    _check_out("stats", stats, torch.float32, 2 * int(c[-1]))
+    _check_out("stats", stats, _TYPES[F32], 2 * int(c[-1]))
     s = _here(stream, x, w, b, y, stats)
     _check("sphinx_layer_norm", lib().sphinx_layer_norm(
         xdt, wdt, ydt, cols, eps, _ptr(x), ldx, _ptr(w), _ptr(b), ldw, int(plus_one), c.tobytes(), c.size - 1, _ptr(y),
@@ -588,11 +602,9 @@ def sphinx_layer_norm(xdt: int, wdt: int, ydt: int, cols: int, eps: float, x, ld
 def sphinx_layer_norm_q8(xdt: int, wdt: int, cols: int, eps: float, x, ldx: int, w, b, ldw: int, plus_one, cu, q, s,
                          stats=None, stream=None):
     """sphinx_layer_norm with its output in 8 bits (q, s as sphinx_q8_bytes(rows, cols) sizes them)."""
-    import torch
-
     c = _ln_check(xdt, wdt, cols, x, ldx, w, b, ldw, cu)
     _check_q8("q", q, s, int(c[-1]), cols)
-    _check_out("stats", stats, torch.float32, 2 * int(c[-1]))
+    _check_out("stats", stats, _TYPES[F32], 2 * int(c[-1]))
     at = _here(stream, x, w, b, q, s, stats)
     _check("sphinx_layer_norm_q8", lib().sphinx_layer_norm_q8(
         xdt, wdt, cols, eps, _ptr(x), ldx, _ptr(w), _ptr(b), ldw, int(plus_one), c.tobytes(), c.size - 1, _ptr(q),
@@ -610,12 +622,10 @@ def sphinx_layer_norm_backward(xdt: int, wdt: int, gdt: int, cols: int, x, ldx: 
                                dy, lddy: int, dx, lddx: int, dw, db, ldg: int, ws, stream=None):
     """dx (None: left out) and, per segment, dw and db (float32; None: left out) from x, the forward call's stats
     and dy."""
-    import torch
-
     c = _ln_check(xdt, wdt, cols, x, ldx, w, None, ldw, cu)
     n = int(c[-1])
     _check_rows("dy", dy, gdt, n, lddy, cols)
-    _check_out("stats", stats, torch.float32, 2 * n)
+    _check_out("stats", stats, _TYPES[F32], 2 * n)
     if dx is not None:
         _check_rows("dx", dx, gdt, n, lddx, cols)
     for name, t in (("dw", dw), ("db", db)):
@@ -647,12 +657,10 @@ def sphinx_q8_quantise_workspace_bytes(rows: int, cols: int) -> int:
 def sphinx_q8_quantise(dtype: int, x, ldx: int, rows: int, cols: int, square, q, s, qt=None, st=None, sums=None,
                        ws=None, stream=None):
     """x [rows][cols] in 8 bits: q and s; transposed, qt and st; and its column sums.  None: left out."""
-    import torch
-
     _check_q8("q", q, s, rows, cols)
     _check_q8("qt", qt, st, cols, rows)
     _check_rows("x", x, dtype, rows, ldx, cols)
-    _check_out("sums", sums, torch.float32, cols)
+    _check_out("sums", sums, _TYPES[F32], cols)
     if ws is not None:
         _check_bytes(ws)
     at = _here(stream, x, q, s, qt, st, sums, ws)

@@ -108,13 +108,9 @@ __global__ __launch_bounds__(LnCfg<LPR>::NT) void k_layer_norm(LnArgs a, LnSegs 
 #pragma unroll
     for (int e = 0; e < 8; ++e) o[e] = fmaf(v[i][e] * rstd, w[e] + one, b[e]);
     if constexpr (std::is_same_v<OUT, Q8Out>) {
-      float top = 0.0f;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        if (e >= n) o[e] = 0.0f;
-        top = fmaxf(top, finite_abs(o[e]));
-      }
-      const int sb = q8_scale_byte(row_max(top));
+      for (int e = 0; e < 8; ++e) o[e] = e < n ? o[e] : 0.0f;
+      const int sb = q8_scale_byte(row_max(finite_top(o)));
       const uint2 p = q8_pack8(o, sb);
       const int64_t ld = (cols + kQ8Block - 1) / kQ8Block * (int64_t)kQ8Block;
       if (live && c < ld) {

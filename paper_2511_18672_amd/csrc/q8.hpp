@@ -90,9 +90,21 @@ __device__ __forceinline__ int q8_scale_byte(float top) {
   return min(max(e, -100), 119) + 127;
 }
 
-__device__ __forceinline__ float finite_abs(float x) {
-  const float a = fabsf(x);
-  return a < __uint_as_float(0x7f800000u) ? a : 0.0f;  // false for NaN as well
+// Largest finite magnitude of N numbers.  The maximum passes over NaN by itself;
+// only where it meets an infinity (or nothing but NaN) are they looked at one by
+// one.
+template <int N>
+__device__ __forceinline__ float finite_top(const float (&x)[N]) {
+  const float inf = __uint_as_float(0x7f800000u);
+  float top = 0.0f;
+#pragma unroll
+  for (int i = 0; i < N; ++i) top = fmaxf(top, fabsf(x[i]));
+  if (!(top < inf)) {
+    top = 0.0f;
+#pragma unroll
+    for (int i = 0; i < N; ++i) top = fabsf(x[i]) < inf ? fmaxf(top, fabsf(x[i])) : top;
+  }
+  return top;
 }
 
 // Eight values times 2^-e in e4m3, rounded to nearest even; infinities and NaN
@@ -158,7 +170,8 @@ __device__ __forceinline__ void store8(bf16* p, int n, const float (&v)[8]) {
   }
 }
 
-// Sum and maximum over the 16 lanes of a row, in every lane of it.
+// Sum and maximum over the 16 lanes of a row, in every lane of it, and over the
+// lanes at the same place of a wave's four rows.
 __device__ __forceinline__ float row_sum(float v) {
   v += dpp_f<0xB1>(v);
   v += dpp_f<0x4E>(v);
@@ -170,6 +183,19 @@ __device__ __forceinline__ float row_max(float v) {
   v = fmaxf(v, dpp_f<0x4E>(v));
   v = fmaxf(v, dpp_f<0x141>(v));
   return fmaxf(v, dpp_f<0x140>(v));
+}
+
+__device__ __forceinline__ float rows4_sum(float v) {
+  const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = __uint_as_float(a[0]) + __uint_as_float(a[1]);
+  const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return __uint_as_float(b[0]) + __uint_as_float(b[1]);
+}
+__device__ __forceinline__ float rows4_max(float v) {
+  const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+  const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
 }
 
 }  // namespace sphinx

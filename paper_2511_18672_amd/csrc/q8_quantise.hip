@@ -19,23 +19,27 @@ __global__ __launch_bounds__(kNT) void k_q8_rows(const T* __restrict__ x, int64_
   const int t = (int)threadIdx.x & 15, k = (int)(at - row * wide), c = k * kQ8Block + 8 * t;
   float v[8];
   load8(x + min(row, (int64_t)rows - 1) * ldx + c, cols - c, v);
-  float top = 0.0f;
-#pragma unroll
-  for (int e = 0; e < 8; ++e) top = fmaxf(top, finite_abs(v[e]));
-  const int sb = q8_scale_byte(row_max(top));
+  const int sb = q8_scale_byte(row_max(finite_top(v)));
   if (row >= rows) return;
   *reinterpret_cast<uint2*>(q + row * wide * kQ8Block + c) = q8_pack8(v, sb);
   if (t == 0) s[row * q8_scale_row(wide) + k] = (uint8_t)sb;
 }
+
+// Place of 16-byte chunk b of row r in the transposed tile: neighbouring columns
+// of a thread's eight and the sixteen threads of a row fall on all banks, when
+// they are written (8 bytes a lane, rows 8 apart) and when they are read (whole
+// rows).
+__device__ __forceinline__ int tr_at(int r, int b) { return (r + (r >> 6)) * kQ8Block + ((b ^ (r >> 3 & 7)) << 4); }
 
 template <typename T, bool SQUARE>
 __global__ __launch_bounds__(kNT) void k_q8_tile(const T* __restrict__ x, int64_t ldx, int rows, int cols,
                                                  uint8_t* __restrict__ q, uint8_t* __restrict__ s,
                                                  uint8_t* __restrict__ qt, uint8_t* __restrict__ st,
                                                  float* __restrict__ part) {
-  __shared__ float red[16][kQ8Block];
-  __shared__ __attribute__((aligned(16))) unsigned char tr[kQ8Block][kQ8Block + 16];
+  __shared__ __attribute__((aligned(16))) float red[2][4][kQ8Block];  // sums, magnitudes: of a wave's 32 rows
+  __shared__ __attribute__((aligned(16))) unsigned char tr[(kQ8Block + 1) * kQ8Block];
   const int t = (int)threadIdx.x & 15, g = (int)threadIdx.x >> 4;  // columns 8 t .. + 7, rows 8 g .. + 7 of the tile
+  const int wave = (int)threadIdx.x >> 6;
   const int wide = (cols + kQ8Block - 1) / kQ8Block, tall = (rows + kQ8Block - 1) / kQ8Block;
   const int tm = (int)blockIdx.x / wide, tn = (int)blockIdx.x % wide;
   const int m0 = tm * kQ8Block, c = tn * kQ8Block + 8 * t;
@@ -45,89 +49,74 @@ __global__ __launch_bounds__(kNT) void k_q8_tile(const T* __restrict__ x, int64_
     const int m = m0 + 8 * g + i;
     load8(x + (int64_t)min(m, rows - 1) * ldx + c, m < rows ? cols - c : 0, v[i]);
   }
-  int square = 0;
-  if constexpr (SQUARE) {
-    float top = 0.0f;
+  // columns: their sums and largest magnitudes over the wave's rows
+  if (part != nullptr) {
+    float sum[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
+    for (int e = 0; e < 8; ++e) {
+      sum[e] = v[0][e];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) top = fmaxf(top, finite_abs(v[i][e]));
-    top = row_max(top);
-    if (t == 0) red[g][0] = top;
-    __syncthreads();
-    top = 0.0f;
+      for (int i = 1; i < 8; ++i) sum[e] += v[i][e];
+      sum[e] = rows4_sum(sum[e]);
+    }
+    if ((g & 3) == 0) __builtin_memcpy(__builtin_assume_aligned(&red[0][wave][8 * t], 16), sum, 32);
+  }
+  if (SQUARE || qt != nullptr) {
+    float top[8];
 #pragma unroll
-    for (int i = 0; i < 16; ++i) top = fmaxf(top, red[i][0]);
-    square = q8_scale_byte(top);
-    __syncthreads();
+    for (int e = 0; e < 8; ++e) {
+      const float col[8] = {v[0][e], v[1][e], v[2][e], v[3][e], v[4][e], v[5][e], v[6][e], v[7][e]};
+      top[e] = rows4_max(finite_top(col));
+    }
+    if ((g & 3) == 0) __builtin_memcpy(__builtin_assume_aligned(&red[1][wave][8 * t], 16), top, 32);
+  }
+  __syncthreads();
+  if (part != nullptr && (int)threadIdx.x < kQ8Block && tn * kQ8Block + (int)threadIdx.x < cols) {
+    const int k = (int)threadIdx.x;
+    part[(int64_t)tm * cols + tn * kQ8Block + k] = (red[0][0][k] + red[0][1][k]) + (red[0][2][k] + red[0][3][k]);
+  }
+  int sb[8];  // scales of the thread's columns
+  if (SQUARE || qt != nullptr) {
+    float top[8] = {};
+#pragma unroll
+    for (int w = 0; w < 4; ++w)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) top[e] = fmaxf(top[e], red[1][w][8 * t + e]);
+    if constexpr (SQUARE) {
+      const int one = q8_scale_byte(row_max(finite_top(top)));
+#pragma unroll
+      for (int e = 0; e < 8; ++e) sb[e] = one;
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) sb[e] = q8_scale_byte(top[e]);
+    }
   }
   if (q != nullptr) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      int sb = square;
-      if constexpr (!SQUARE) {
-        float top = 0.0f;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) top = fmaxf(top, finite_abs(v[i][e]));
-        sb = q8_scale_byte(row_max(top));
-      }
+      const int rb = SQUARE ? sb[0] : q8_scale_byte(row_max(finite_top(v[i])));
       const int64_t m = m0 + 8 * g + i;
       if (m < rows) {
-        *reinterpret_cast<uint2*>(q + m * wide * kQ8Block + c) = q8_pack8(v[i], sb);
-        if (t == 0) s[m * q8_scale_row(wide) + tn] = (uint8_t)sb;
+        *reinterpret_cast<uint2*>(q + m * wide * kQ8Block + c) = q8_pack8(v[i], rb);
+        if (t == 0) s[m * q8_scale_row(wide) + tn] = (uint8_t)rb;
       }
     }
   }
-  if (part != nullptr) {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      float sum = 0.0f;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) sum += v[i][e];
-      red[g][8 * t + e] = sum;
-    }
-    __syncthreads();
-    if ((int)threadIdx.x < kQ8Block && tn * kQ8Block + (int)threadIdx.x < cols) {
-      float sum = 0.0f;
-#pragma unroll
-      for (int i = 0; i < 16; ++i) sum += red[i][threadIdx.x];
-      part[(int64_t)tm * cols + tn * kQ8Block + threadIdx.x] = sum;
-    }
-    __syncthreads();
-  }
   if (qt == nullptr) return;
-  if constexpr (!SQUARE) {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      float top = 0.0f;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) top = fmaxf(top, finite_abs(v[i][e]));
-      red[g][8 * t + e] = top;
-    }
-    __syncthreads();
-  }
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
-    int sb = square;
-    if constexpr (!SQUARE) {
-      float top = 0.0f;
-#pragma unroll
-      for (int i = 0; i < 16; ++i) top = fmaxf(top, red[i][8 * t + e]);
-      sb = q8_scale_byte(top);
-    }
-    float col[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) col[i] = v[i][e];
-    *reinterpret_cast<uint2*>(&tr[8 * t + e][8 * g]) = q8_pack8(col, sb);
-    if (g == 0 && c + e < cols) st[(int64_t)(c + e) * q8_scale_row(tall) + tm] = (uint8_t)sb;
+    const float col[8] = {v[0][e], v[1][e], v[2][e], v[3][e], v[4][e], v[5][e], v[6][e], v[7][e]};
+    *reinterpret_cast<uint2*>(tr + tr_at(8 * t + e, g >> 1) + 8 * (g & 1)) = q8_pack8(col, sb[e]);
+    if (g == 0 && c + e < cols) st[(int64_t)(c + e) * q8_scale_row(tall) + tm] = (uint8_t)sb[e];
   }
   __syncthreads();
 #pragma unroll
   for (int p = 0; p < 4; ++p) {
-    const int r = p * 32 + ((int)threadIdx.x >> 3), b = 16 * ((int)threadIdx.x & 7);
+    const int r = p * 32 + ((int)threadIdx.x >> 3), b = (int)threadIdx.x & 7;
     const int64_t n = (int64_t)tn * kQ8Block + r;
     if (n < cols)
-      *reinterpret_cast<uint4*>(qt + n * tall * kQ8Block + m0 + b) = *reinterpret_cast<const uint4*>(&tr[r][b]);
+      *reinterpret_cast<uint4*>(qt + n * tall * kQ8Block + m0 + 16 * b) =
+          *reinterpret_cast<const uint4*>(tr + tr_at(r, b));
   }
 }
 }  // namespace
