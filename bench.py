@@ -59,6 +59,8 @@ def parse():
                     help="latent cache with a full step every T steps (0: off, the default workload)")
     ap.add_argument("--cache-dtype", default="model", choices=["model", "fp8"],
                     help="latent cache in the model's type or in 8 bits (needs --cache-period)")
+    ap.add_argument("--product-dtype", default="model", choices=["model", "fp8"],
+                    help="block products in the model's type (the default workload) or in 8 bits; with fp8, dtype says so")
     ap.add_argument("--select-every-step", type=int, default=1,
                     help="1: run mask+compaction in every step (default); 0: only when the active set changes")
     return ap.parse_args()
@@ -414,7 +416,7 @@ def main():
     t_setup = time.perf_counter()
     R = S.from_workload(wl, layout=S.TOKENS if args.layout == "tokens" else S.NCHW,
                         cache_period=args.cache_period, per_frame_grid=args.per_frame_grid,
-                        cache_dtype=args.cache_dtype)
+                        cache_dtype=args.cache_dtype, product_dtype=args.product_dtype)
     R.reset()
     stream = torch.cuda.current_stream()
     D, L, mlp, hd = wl.model.D, wl.model.L, wl.model.mlp, wl.model.head_dim
@@ -522,7 +524,8 @@ def main():
                       "selected_tokens": int(n), "tokens": int(wl.N), "select_every_step": force,
                       "state_layout": args.layout, "cache_period": args.cache_period,
                       "attention": args.attention, "per_frame_grid": args.per_frame_grid,
-                      **({"cache_dtype": args.cache_dtype} if args.cache_dtype != "model" else {})},
+                      **({"cache_dtype": args.cache_dtype} if args.cache_dtype != "model" else {}),
+                      **({"product_dtype": args.product_dtype} if args.product_dtype != "model" else {})},
            "mfma_util_step": round(mfma_util, 4),
            "roofline": roofline, "kernels": kernels,
            "kernels_note": f"per-class HIP-event averages from {n_breakdown} further untimed steps; "

@@ -583,13 +583,40 @@ typedef SPHINX_ENUM {
  * odt f32: every product is exact (bf16 matrix cores, at less than half the rate).
  * A NaN in a row of A or B makes the outputs of that row or column NaN.
  * ws: dev, 256-byte aligned, sphinx_q8_matmul_workspace_bytes bytes, not shared
- * with work that may run at the same time.  Deterministic; may be captured in a
- * graph. */
+ * with work that may run at the same time.  A call repeats bit for bit and may be
+ * captured in a graph; how a contraction is cut depends on all three sizes, so a
+ * row of a product may differ by roundings of its sum from what it is beside
+ * other rows. */
 sphinx_status sphinx_q8_matmul_workspace_bytes(sphinx_dtype odt, int32_t M, int32_t N, int32_t K, size_t* bytes);
 sphinx_status sphinx_q8_matmul(sphinx_dtype odt, int32_t M, int32_t N, int32_t K, const uint8_t* a, const uint8_t* sa,
                                const uint8_t* b, const uint8_t* sb, sphinx_dtype bdt, const void* bias,
                                sphinx_q8_epilogue epilogue, void* out, int64_t ldo, void* ws, size_t ws_bytes,
                                void* stream);
+
+/* The same with C (SPHINX_Q8_STORE) or GELU_tanh(C) (SPHINX_Q8_GELU) as a matrix
+ * [M][N] in 8 bits, groups along its rows, quantised from fp32: what the next
+ * product takes.  Products as for odt bf16. */
+sphinx_status sphinx_q8_matmul_q8(int32_t M, int32_t N, int32_t K, const uint8_t* a, const uint8_t* sa,
+                                  const uint8_t* b, const uint8_t* sb, sphinx_dtype bdt, const void* bias,
+                                  sphinx_q8_epilogue epilogue, uint8_t* q, uint8_t* s, void* stream);
+
+/* The refinement step with its block products in 8 bits (bf16 models).  w8: dev,
+ * 256-byte aligned, sphinx_model_q8_bytes bytes, filled by sphinx_model_q8_pack
+ * from m->weights: the four matrices of every block, in squares of 128 x 128.
+ * sphinx_refine_step_q8 is sphinx_refine_step (kv_cache = NULL),
+ * sphinx_refine_step_cached (kv8 = 0) or sphinx_refine_step_kv8 (kv8 = 1) with
+ * each block's QKV, output and MLP products through w8: their inputs (the
+ * modulated norms, the attention's output, the GELU) are quantised along their
+ * rows.  All else, biases and residual stream among it, is as it was.
+ * SPHINX_E_UNSUPPORTED for f32 models. */
+sphinx_status sphinx_model_q8_bytes(const sphinx_model_desc* m, size_t* bytes);
+sphinx_status sphinx_model_q8_pack(const sphinx_model_desc* m, void* w8, size_t w8_bytes, void* stream);
+sphinx_status sphinx_refine_q8_workspace_bytes(const sphinx_model_desc* m, const sphinx_request* reqs, int32_t R,
+                                               int64_t max_sel, int32_t kv8, size_t* bytes);
+sphinx_status sphinx_refine_step_q8(const sphinx_model_desc* m, const void* w8, size_t w8_bytes,
+                                    const sphinx_request* reqs, int32_t R, const int32_t* idx, int32_t n,
+                                    const int32_t* cu_host, const int32_t* tau, const float* c1, const float* c2,
+                                    float* x, void* kv_cache, int32_t kv8, void* ws, size_t ws_bytes, void* stream);
 
 /* ------------------------------------------------------------------------
  * Mask front-end (Sec. 5.3 spatially selective refinement; Alg. 1

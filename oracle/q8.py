@@ -42,15 +42,12 @@ def exponents(x, square=False):
     x = np.asarray(x, np.float64)
     rows, cols = x.shape
     high = BLOCK if square else 1
-    top = np.abs(np.where(np.isfinite(x), x, 0.0))
-    out = np.empty((rows, cols), np.int64)
-    for i in range(0, rows, high):
-        for j in range(0, cols, BLOCK):
-            part = top[i:i + high, j:j + BLOCK].max()
-            m, p = np.frexp(part / 448.0)  # part = 448 m 2^p, m in [0.5, 1)
-            e = E_MIN if part == 0.0 else int(p) - (1 if m == 0.5 else 0)
-            out[i:i + high, j:j + BLOCK] = min(max(e, E_MIN), E_MAX)
-    return out
+    top = np.zeros((-(-rows // high) * high, -(-cols // BLOCK) * BLOCK))
+    top[:rows, :cols] = np.abs(np.where(np.isfinite(x), x, 0.0))
+    top = top.reshape(top.shape[0] // high, high, -1, BLOCK).max(axis=(1, 3))
+    m, p = np.frexp(top / 448.0)  # top = 448 m 2^p, m in [0.5, 1)
+    e = np.clip(np.where(top == 0.0, E_MIN, np.where(m == 0.5, p - 1, p)), E_MIN, E_MAX).astype(np.int64)
+    return np.repeat(np.repeat(e, high, axis=0), BLOCK, axis=1)[:rows, :cols]
 
 
 def quantise(x, square=False):

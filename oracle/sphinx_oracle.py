@@ -56,7 +56,7 @@ from typing import Dict, List, Optional, Sequence
 
 import numpy as np
 
-from . import kv8
+from . import kv8, q8
 
 T_TRAIN = 1000
 BETA_START = 1e-4
@@ -406,11 +406,15 @@ class Model:
     dtype: str
     weights: Dict[str, np.ndarray]
     attention: str = "joint"
+    products8: bool = False  # block products of 8-bit matrices (weights holds the values of its own)
 
 
-def model_from_workload(wl) -> Model:
-    m = wl.model
-    return Model(m.D, m.heads, m.mlp, m.L, m.dtype, wl.weights, getattr(m, "attention", "joint"))
+def model_from_workload(wl, products8: bool = False) -> Model:
+    m, weights = wl.model, wl.weights
+    if products8:
+        weights = {k: q8.quantise(v, square=True) if k.endswith(("qkv_w", "o_w", "fc1_w", "fc2_w")) else v
+                   for k, v in weights.items()}
+    return Model(m.D, m.heads, m.mlp, m.L, m.dtype, weights, getattr(m, "attention", "joint"), products8)
 
 
 def conditioning(model: Model, tau: np.ndarray) -> np.ndarray:
@@ -444,6 +448,9 @@ def denoise(model: Model, x: np.ndarray, f, y, xx, tau_tok: np.ndarray, seg: np.
     rnd = round_bf16 if (precision == "model" and model.dtype == "bf16") else (lambda a: a)
     # queries are kept in base-2 softmax units: q' = q log2(e)/sqrt(d), and
     # softmax(q k^T / sqrt(d)) = softmax(ln(2) q' k^T)
+    # 8-bit products: their inputs in 8 bits along their rows, straight from the norm and the GELU, and from the
+    # attention's output in the model's type
+    into = q8.quantise if model.products8 else rnd
     qscale, sscale = np.log2(np.e) / np.sqrt(D // H), np.log(2.0)
     # conditioning, per distinct timestep (identical for equal timesteps)
     taus, inv = np.unique(np.asarray(tau_tok), return_inverse=True)
@@ -452,7 +459,7 @@ def denoise(model: Model, x: np.ndarray, f, y, xx, tau_tok: np.ndarray, seg: np.
     for l in range(model.L):
         mod = linear(c, w[f"b{l}.ada_w"], w[f"b{l}.ada_b"])[inv]
         sh1, sc1, g1, sh2, sc2, g2 = (mod[:, i * D:(i + 1) * D] for i in range(6))
-        a = rnd(layer_norm(h) * (1.0 + sc1) + sh1)
+        a = into(layer_norm(h) * (1.0 + sc1) + sh1)
         qkv = linear(a, w[f"b{l}.qkv_w"], w[f"b{l}.qkv_b"])
         q, k, v = rnd(qkv[:, :D] * qscale), rnd(qkv[:, D:2 * D]), rnd(qkv[:, 2 * D:])
         kind = block_attention(model.attention, l)
@@ -478,9 +485,11 @@ def denoise(model: Model, x: np.ndarray, f, y, xx, tau_tok: np.ndarray, seg: np.
                                            np.concatenate([y, kv_pos[1]]), np.concatenate([xx, kv_pos[2]]))
                 gq, gk = both[:x.shape[0]], both[x.shape[0]:]
                 o = rnd(attention_groups(q, cache[l][0], cache[l][1], H, gq, gk, scale=sscale))
+        if model.products8:
+            o = into(o)
         h = h + (1.0 + g1) * linear(o, w[f"b{l}.o_w"], w[f"b{l}.o_b"])
-        a2 = rnd(layer_norm(h) * (1.0 + sc2) + sh2)
-        m = rnd(gelu_tanh(linear(a2, w[f"b{l}.fc1_w"], w[f"b{l}.fc1_b"])))
+        a2 = into(layer_norm(h) * (1.0 + sc2) + sh2)
+        m = into(gelu_tanh(linear(a2, w[f"b{l}.fc1_w"], w[f"b{l}.fc1_b"])))
         h = h + (1.0 + g2) * linear(m, w[f"b{l}.fc2_w"], w[f"b{l}.fc2_b"])
     fm = linear(c, w["fada_w"], w["fada_b"])[inv]
     shf, scf = fm[:, :D], fm[:, D:]
@@ -596,12 +605,12 @@ class Kv8Cache(list):
 
 
 def refine(wl, precision: str = "model", denoiser=None, trace: bool = False, steps: Optional[int] = None,
-           period: int = 0, per_frame_grid: bool = False, cache8: bool = False):
+           period: int = 0, per_frame_grid: bool = False, cache8: bool = False, products8: bool = False):
     """Run the whole partial-denoising loop; returns the final NCHW state (float64)
     and, with trace=True, the list of per-step results.  period > 0 turns on
     the latent cache with a full step every ``period`` steps, cache8 keeps it in
-    8 bits."""
-    model = model_from_workload(wl)
+    8 bits; products8 multiplies the block matrices in 8 bits."""
+    model = model_from_workload(wl, products8)
     plans = plan_steps([r.frames for r in wl.requests], wl.s_start, wl.nsteps, period, per_frame_grid)
     info = token_info(wl.requests)
     state = np.asarray(wl.z0, dtype=np.float64).copy()

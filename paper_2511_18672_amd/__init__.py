@@ -11,7 +11,8 @@ from .binding import (ATTN_FACTORISED, ATTN_JOINT, GRID_PER_FRAME, GRID_SHARED, 
                       Q8_ADD, Q8_BLOCK, Q8_GELU, Q8_STORE, sphinx_layer_norm, sphinx_layer_norm_backward,
                       sphinx_layer_norm_backward_workspace_bytes, sphinx_layer_norm_q8, sphinx_q8_bytes,
                       sphinx_q8_matmul, sphinx_q8_matmul_workspace_bytes, sphinx_q8_quantise,
-                      sphinx_q8_quantise_workspace_bytes,
+                      sphinx_q8_quantise_workspace_bytes, sphinx_q8_matmul_q8, sphinx_model_q8_bytes,
+                      sphinx_model_q8_pack, sphinx_refine_q8_workspace_bytes, sphinx_refine_step_q8,
                       make_requests, model_desc, plan_step, refine_step, scatter_blend, select_mask, sphinx_gather,
                       sphinx_gather_ctx, sphinx_kv_cache_bytes, sphinx_mask_frontend,
                       sphinx_mask_frontend_workspace_bytes, sphinx_model_blob_bytes, sphinx_model_param,
@@ -28,7 +29,8 @@ __all__ = ["ATTN_FACTORISED", "ATTN_JOINT", "GRID_PER_FRAME", "GRID_SHARED", "sp
            "sphinx_refine_kv8_workspace_bytes", "sphinx_refine_step_kv8", "Q8_ADD", "Q8_BLOCK", "Q8_GELU", "Q8_STORE", "sphinx_layer_norm",
            "sphinx_layer_norm_backward", "sphinx_layer_norm_backward_workspace_bytes", "sphinx_layer_norm_q8",
            "sphinx_q8_bytes", "sphinx_q8_matmul", "sphinx_q8_matmul_workspace_bytes", "sphinx_q8_quantise",
-           "sphinx_q8_quantise_workspace_bytes", "sphinx_kv_cache_bytes", "sphinx_mask_frontend",
+           "sphinx_q8_quantise_workspace_bytes", "sphinx_q8_matmul_q8", "sphinx_model_q8_bytes", "sphinx_model_q8_pack",
+           "sphinx_refine_q8_workspace_bytes", "sphinx_refine_step_q8", "sphinx_kv_cache_bytes", "sphinx_mask_frontend",
            "sphinx_mask_frontend_workspace_bytes", "sphinx_model_blob_bytes", "sphinx_model_param",
            "sphinx_peak_mfma", "sphinx_plan_cache", "sphinx_plan_step", "sphinx_refine_step",
            "sphinx_refine_step_cached", "sphinx_refine_workspace_bytes", "sphinx_scatter_blend",

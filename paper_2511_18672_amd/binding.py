@@ -43,7 +43,8 @@ EXPORTED = ["sphinx_status_string", "sphinx_model_blob_bytes", "sphinx_model_par
             "sphinx_refine_step_kv8", "sphinx_layer_norm", "sphinx_layer_norm_q8",
             "sphinx_layer_norm_backward_workspace_bytes", "sphinx_layer_norm_backward", "sphinx_q8_bytes",
             "sphinx_q8_quantise_workspace_bytes", "sphinx_q8_quantise", "sphinx_q8_matmul_workspace_bytes",
-            "sphinx_q8_matmul"]
+            "sphinx_q8_matmul", "sphinx_q8_matmul_q8", "sphinx_model_q8_bytes", "sphinx_model_q8_pack",
+            "sphinx_refine_q8_workspace_bytes", "sphinx_refine_step_q8"]
 PEAK_BLOCKS = 2048
 PEAK_CONSTANT, PEAK_RANDOM = 0, 1
 KERNEL_CLASSES = ["select", "gather", "cond", "embed", "ln", "gemm_qkv", "attention", "gemm_out", "gemm_mlp1",
@@ -151,6 +152,13 @@ def lib() -> ctypes.CDLL:
         "sphinx_q8_matmul_workspace_bytes": (c_int32, [c_int32, c_int32, c_int32, c_int32, POINTER(c_size_t)]),
         "sphinx_q8_matmul": (c_int32, [c_int32, c_int32, c_int32, c_int32, P, P, P, P, c_int32, P, c_int32, P, c_int64,
                                        P, c_size_t, P]),
+        "sphinx_q8_matmul_q8": (c_int32, [c_int32, c_int32, c_int32, P, P, P, P, c_int32, P, c_int32, P, P, P]),
+        "sphinx_model_q8_bytes": (c_int32, [POINTER(ModelDesc), POINTER(c_size_t)]),
+        "sphinx_model_q8_pack": (c_int32, [POINTER(ModelDesc), P, c_size_t, P]),
+        "sphinx_refine_q8_workspace_bytes": (c_int32, [POINTER(ModelDesc), POINTER(Request), c_int32, c_int64, c_int32,
+                                                       POINTER(c_size_t)]),
+        "sphinx_refine_step_q8": (c_int32, [POINTER(ModelDesc), P, c_size_t, POINTER(Request), c_int32, P, c_int32, P,
+                                            P, P, P, P, P, c_int32, P, c_size_t, P]),
         "sphinx_scatter_masked": (c_int32, [POINTER(Request), c_int32, P, P, c_int32, P, P, c_int32, c_int32, P]),
         "sphinx_mask_frontend_workspace_bytes": (c_int32, [POINTER(Request), c_int32, POINTER(c_size_t)]),
         "sphinx_adaptive_start": (c_int32, [POINTER(Request), c_int32, P, P, ctypes.c_float, POINTER(KLogic), c_int32,
@@ -690,6 +698,52 @@ def sphinx_q8_matmul(odt: int, M: int, N: int, K: int, a, sa, b, sb, bdt: int, b
     _check("sphinx_q8_matmul", lib().sphinx_q8_matmul(
         odt, M, N, K, _ptr(a), _ptr(sa), _ptr(b), _ptr(sb), bdt, _ptr(bias), epilogue, _ptr(out), ldo, _ptr(ws),
         0 if ws is None else ws.nbytes, s))
+
+
+def sphinx_q8_matmul_q8(M: int, N: int, K: int, a, sa, b, sb, bdt: int, bias, epilogue: int, q, s, stream=None):
+    """The 8-bit matrix q, s [M][N] <- A B^T + bias (Q8_STORE), or its GELU (Q8_GELU)."""
+    _check_q8("a", a, sa, M, K)
+    _check_q8("b", b, sb, N, K)
+    if bias is not None:
+        _check_rows("bias", bias, bdt, 1, N, N)
+    _check_q8("q", q, s, M, N)
+    at = _here(stream, a, sa, b, sb, bias, q, s)
+    _check("sphinx_q8_matmul_q8", lib().sphinx_q8_matmul_q8(
+        M, N, K, _ptr(a), _ptr(sa), _ptr(b), _ptr(sb), bdt, _ptr(bias), epilogue, _ptr(q), _ptr(s), at))
+
+
+def sphinx_model_q8_bytes(desc: ModelDesc) -> int:
+    out = c_size_t()
+    _check("sphinx_model_q8_bytes", lib().sphinx_model_q8_bytes(ctypes.byref(desc), ctypes.byref(out)))
+    return out.value
+
+
+def sphinx_model_q8_pack(desc: ModelDesc, w8, stream=None):
+    """The block matrices of desc.weights in 8 bits into w8 (bytes, sphinx_model_q8_bytes)."""
+    _check_bytes(w8)
+    _check("sphinx_model_q8_pack", lib().sphinx_model_q8_pack(ctypes.byref(desc), _ptr(w8), w8.nbytes,
+                                                              _here(stream, w8)))
+
+
+def sphinx_refine_q8_workspace_bytes(desc: ModelDesc, reqs, max_sel: int, kv8: bool = False) -> int:
+    out = c_size_t()
+    _check("sphinx_refine_q8_workspace_bytes", lib().sphinx_refine_q8_workspace_bytes(
+        ctypes.byref(desc), reqs, len(reqs), max_sel, int(kv8), ctypes.byref(out)))
+    return out.value
+
+
+def sphinx_refine_step_q8(desc: ModelDesc, w8, reqs, idx, n: int, cu_host: np.ndarray, tau, c1, c2, x, kv_cache,
+                          kv8: bool, ws, stream=None):
+    """sphinx_refine_step (kv_cache None), _cached or (kv8) _kv8 with the block products in 8 bits."""
+    if kv_cache is not None and not isinstance(kv_cache, int):
+        need = (sphinx_kv8_cache_bytes if kv8 else sphinx_kv_cache_bytes)(desc, reqs)
+        if kv_cache.nbytes < need:
+            raise ValueError(f"the cache has {kv_cache.nbytes} bytes, these requests take {need}")
+    cu = np.ascontiguousarray(cu_host, dtype=np.int32)
+    _check_bytes(w8, ws)
+    _check("sphinx_refine_step_q8", lib().sphinx_refine_step_q8(
+        ctypes.byref(desc), _ptr(w8), w8.nbytes, reqs, len(reqs), _ptr(idx), n, _ptr(cu), _ptr(tau), _ptr(c1),
+        _ptr(c2), _ptr(x), _ptr(kv_cache), int(kv8), _ptr(ws), ws.nbytes, _stream(stream)))
 
 
 def sphinx_scatter_masked(reqs, x, idx, n: int, wmask, z, dtype: int, layout: int, stream=None):

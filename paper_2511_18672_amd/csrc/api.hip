@@ -9,6 +9,7 @@
 
 #include "kernels.hpp"
 #include "kv8.hpp"
+#include "q8.hpp"
 #include "sphinx_prof.h"
 
 using namespace sphinx;
@@ -775,14 +776,39 @@ size_t kv8_refine_extra(const sphinx_model_desc& m, const ReqTable& T, int64_t s
   return align256(kv8_attention_ws_bytes(m.heads, m.head_dim, 1, T.R, nq, klen));
 }
 
+// Block matrices in 8 bits: per block QKV, output, MLP1 and MLP2, bytes and scales.
+struct Q8Model {
+  size_t q[4], s[4], block;  // offsets inside a block, and its bytes
+  int rows[4], cols[4];
+};
+Q8Model q8_model(const sphinx_model_desc& m) {
+  Q8Model w = {{}, {}, 0, {3 * m.D, m.D, m.mlp, m.D}, {m.D, m.D, m.D, m.mlp}};
+  for (int i = 0; i < 4; ++i) {
+    w.q[i] = w.block;
+    w.s[i] = w.q[i] + align256((size_t)w.rows[i] * q8_row_bytes(w.cols[i]));
+    w.block = w.s[i] + align256((size_t)w.rows[i] * q8_scale_bytes(w.cols[i]));
+  }
+  return w;
+}
+sphinx_status q8_model_check(const sphinx_model_desc* m) {
+  const sphinx_status st = check_model(m);
+  if (st != SPHINX_OK) return st;
+  return m->dtype == SPHINX_BF16 ? SPHINX_OK : SPHINX_E_UNSUPPORTED;
+}
+// Workspace of the products' inputs in 8 bits, behind the rest.
+size_t q8_refine_extra(const sphinx_model_desc& m, int64_t sel) {
+  const int wide = std::max(m.D, m.mlp);
+  return align256((size_t)sel * q8_row_bytes(wide)) + align256((size_t)sel * q8_scale_bytes(wide));
+}
+
 // One denoiser pass plus the DDIM update over the n forwarded rows; with a
 // cache (kv_cache != NULL) every block stores the rows' keys and values and
 // attends over all tokens of each request through the cache, which holds the
-// model's dtype or (kv8) 8 bits.
+// model's dtype or (kv8) 8 bits.  w8 != NULL: the block products in 8 bits.
 sphinx_status refine_impl(const sphinx_model_desc* m, const sphinx_request* reqs, int32_t R, const int32_t* idx,
                           int32_t n_sel, const int32_t* cu_sel_host, const int32_t* tau, const float* c1,
                           const float* c2, float* x_sel, void* kv_cache, bool kv8, void* ws, size_t ws_bytes,
-                          void* stream) {
+                          void* stream, const void* w8 = nullptr) {
   sphinx_status st = check_model(m);
   if (st == SPHINX_OK && kv8) st = kv8_model_check(m);
   if (st != SPHINX_OK) return st;
@@ -814,7 +840,8 @@ sphinx_status refine_impl(const sphinx_model_desc* m, const sphinx_request* reqs
       if (T.frames[r] > 64) return SPHINX_E_UNSUPPORTED;
   }
   const RefineWs W = refine_layout(*m, T, G, n_sel);
-  if (ws_bytes < W.total + (kv8 ? kv8_refine_extra(*m, T, n_sel) : 0)) return SPHINX_E_WORKSPACE;
+  const size_t q8_at = W.total + (kv8 ? kv8_refine_extra(*m, T, n_sel) : 0);
+  if (ws_bytes < q8_at + (w8 != nullptr ? q8_refine_extra(*m, n_sel) : 0)) return SPHINX_E_WORKSPACE;
   const bool cached = kv_cache != nullptr;
 
   // segments: requests with forwarded tokens, most keys first for the attention schedule
@@ -873,6 +900,24 @@ sphinx_status refine_impl(const sphinx_model_desc* m, const sphinx_request* reqs
   void* qkv = base + W.big;
   void* obuf = base + W.big + (size_t)n * 3 * D * esize(dt);
   void* mbuf = base + W.big;
+
+  // block products in 8 bits: their input, and matrix i of block l
+  const Q8Model W8 = q8_model(*m);
+  uint8_t* in_q = base + q8_at;
+  uint8_t* in_s = in_q + align256((size_t)n * q8_row_bytes(std::max(D, (int)m->mlp)));
+  uint8_t* mid_s = static_cast<uint8_t*>(mbuf) + align256((size_t)n * q8_row_bytes(m->mlp));  // fits: big holds bf16
+  auto q8_matrix = [&](int i, int l) {
+    const uint8_t* b = static_cast<const uint8_t*>(w8) + l * W8.block;
+    return Q8Mat{b + W8.q[i], b + W8.s[i]};
+  };
+  auto q8_norm = [&](int sh_off, int sc_off) {
+    const LnSegs one{1, {0, n}};
+    const LnArgs a{h, D, mod + sc_off, mod + sh_off, ldm, false, true, D, 1e-6f, crow};
+    return launch_layer_norm(SPHINX_F32, dt, a, one, nullptr, 0, in_q, in_s, nullptr, s);
+  };
+  auto q8_product = [&](Q8Kind kind, int i, int l, const Q8Epi& e) {
+    return launch_q8_matmul(kind, n, W8.rows[i], W8.cols[i], Q8Mat{in_q, in_s}, q8_matrix(i, l), e, nullptr, s);
+  };
 
   // factorised: frame segments (host copy of the per-frame counts: one stream
   // synchronisation) and the token -> row map of the temporal blocks
@@ -937,14 +982,18 @@ sphinx_status refine_impl(const sphinx_model_desc* m, const sphinx_request* reqs
     const int c0 = 6 * D * l;
     {
       Bracket br(SPHINX_K_LN, s);
-      SPHINX_TRY(launch_ln_mod(h, n, D, mod, ldm, c0, c0 + D, crow, abuf, dt, s));
+      if (w8 != nullptr) SPHINX_TRY(q8_norm(c0, c0 + D));
+      else SPHINX_TRY(launch_ln_mod(h, n, D, mod, ldm, c0, c0 + D, crow, abuf, dt, s));
     }
     {
       Bracket br(SPHINX_K_GEMM_QKV, s);
       // q leaves the projection scaled by log2(e)/sqrt(head_dim), rounded once:
       // attention scores then come out of q k^T in base-2 units
       GemmEpi e_qkv{qkv, 3 * D, nullptr, 0, nullptr, D, kLog2e / std::sqrt((float)m->head_dim)};
-      SPHINX_TRY(launch_gemm(EPI_BIAS, dt, abuf, P(SPHINX_P_QKV_W, l), P(SPHINX_P_QKV_B, l), n, 3 * D, D, e_qkv, s));
+      if (w8 != nullptr)
+        SPHINX_TRY(q8_product(kQ8Bf16, 0, l, Q8Epi{Q8_EPI_STORE, P(SPHINX_P_QKV_B, l), true, qkv, 3 * D, nullptr,
+                                                   nullptr, 0, nullptr, D, e_qkv.qscale}));
+      else SPHINX_TRY(launch_gemm(EPI_BIAS, dt, abuf, P(SPHINX_P_QKV_W, l), P(SPHINX_P_QKV_B, l), n, 3 * D, D, e_qkv, s));
     }
     AttnIO io{qkv, static_cast<const unsigned char*>(qkv) + (size_t)D * esize(dt),
               static_cast<const unsigned char*>(qkv) + 2 * (size_t)D * esize(dt), obuf, 3 * D, 3 * D};
@@ -989,21 +1038,33 @@ sphinx_status refine_impl(const sphinx_model_desc* m, const sphinx_request* reqs
     {
       Bracket br(SPHINX_K_GEMM_OUT, s);
       GemmEpi e_o{h, D, mod + c0 + 2 * D, ldm, crow};
-      SPHINX_TRY(launch_gemm(EPI_GATED, dt, obuf, P(SPHINX_P_O_W, l), P(SPHINX_P_O_B, l), n, D, D, e_o, s));
+      if (w8 != nullptr) {
+        SPHINX_TRY(launch_q8_quantise(dt, obuf, D, n, D, false, in_q, in_s, nullptr, nullptr, nullptr, nullptr, s));
+        SPHINX_TRY(q8_product(kQ8Gated, 1, l, Q8Epi{Q8_EPI_STORE, P(SPHINX_P_O_B, l), true, h, D, nullptr, e_o.gate,
+                                                    ldm, crow, 0, 0.0f}));
+      } else SPHINX_TRY(launch_gemm(EPI_GATED, dt, obuf, P(SPHINX_P_O_W, l), P(SPHINX_P_O_B, l), n, D, D, e_o, s));
     }
     {
       Bracket br(SPHINX_K_LN, s);
-      SPHINX_TRY(launch_ln_mod(h, n, D, mod, ldm, c0 + 3 * D, c0 + 4 * D, crow, abuf, dt, s));
+      if (w8 != nullptr) SPHINX_TRY(q8_norm(c0 + 3 * D, c0 + 4 * D));
+      else SPHINX_TRY(launch_ln_mod(h, n, D, mod, ldm, c0 + 3 * D, c0 + 4 * D, crow, abuf, dt, s));
     }
     {
       Bracket br(SPHINX_K_GEMM_MLP1, s);
       GemmEpi e_1{mbuf, m->mlp, nullptr, 0, nullptr};
-      SPHINX_TRY(launch_gemm(EPI_GELU, dt, abuf, P(SPHINX_P_FC1_W, l), P(SPHINX_P_FC1_B, l), n, m->mlp, D, e_1, s));
+      if (w8 != nullptr)  // into the memory of the activations in bf16, so that its input stays whole
+        SPHINX_TRY(q8_product(kQ8Bytes, 2, l, Q8Epi{Q8_EPI_GELU, P(SPHINX_P_FC1_B, l), true, mbuf, 0, mid_s, nullptr, 0,
+                                                    nullptr, 0, 0.0f}));
+      else SPHINX_TRY(launch_gemm(EPI_GELU, dt, abuf, P(SPHINX_P_FC1_W, l), P(SPHINX_P_FC1_B, l), n, m->mlp, D, e_1, s));
     }
     {
       Bracket br(SPHINX_K_GEMM_MLP2, s);
       GemmEpi e_2{h, D, mod + c0 + 5 * D, ldm, crow};
-      SPHINX_TRY(
+      if (w8 != nullptr)
+        SPHINX_TRY(launch_q8_matmul(kQ8Gated, n, D, m->mlp, Q8Mat{static_cast<uint8_t*>(mbuf), mid_s}, q8_matrix(3, l),
+                                    Q8Epi{Q8_EPI_STORE, P(SPHINX_P_FC2_B, l), true, h, D, nullptr, e_2.gate, ldm, crow,
+                                          0, 0.0f}, nullptr, s));
+      else SPHINX_TRY(
           launch_gemm(EPI_GATED, dt, mbuf, P(SPHINX_P_FC2_W, l), P(SPHINX_P_FC2_B, l), n, D, m->mlp, e_2, s));
     }
   }
@@ -1067,6 +1128,55 @@ sphinx_status sphinx_refine_kv8_workspace_bytes(const sphinx_model_desc* m, cons
   if (st != SPHINX_OK) return st;
   *bytes += kv8_refine_extra(*m, T, std::max<int64_t>(max_sel, 1));
   return SPHINX_OK;
+}
+
+sphinx_status sphinx_model_q8_bytes(const sphinx_model_desc* m, size_t* bytes) {
+  const sphinx_status st = q8_model_check(m);
+  if (st != SPHINX_OK) return st;
+  if (bytes == nullptr) return SPHINX_E_INVALID;
+  *bytes = (size_t)m->L * q8_model(*m).block;
+  return SPHINX_OK;
+}
+
+sphinx_status sphinx_model_q8_pack(const sphinx_model_desc* m, void* w8, size_t w8_bytes, void* stream) {
+  const sphinx_status st = q8_model_check(m);
+  if (st != SPHINX_OK) return st;
+  if (w8 == nullptr || m->weights == nullptr || !aligned(w8, 256) || !aligned(m->weights, 256)) return SPHINX_E_INVALID;
+  const Q8Model W = q8_model(*m);
+  if (w8_bytes < (size_t)m->L * W.block) return SPHINX_E_WORKSPACE;
+  const Blob B = blob_layout(*m);
+  const sphinx_param p[4] = {SPHINX_P_QKV_W, SPHINX_P_O_W, SPHINX_P_FC1_W, SPHINX_P_FC2_W};
+  for (int l = 0; l < m->L; ++l)
+    for (int i = 0; i < 4; ++i) {
+      uint8_t* out = static_cast<uint8_t*>(w8) + l * W.block;
+      SPHINX_TRY(launch_q8_quantise(m->dtype, static_cast<const unsigned char*>(m->weights) + B.at(p[i], l), W.cols[i],
+                                    W.rows[i], W.cols[i], true, out + W.q[i], out + W.s[i], nullptr, nullptr, nullptr,
+                                    nullptr, (hipStream_t)stream));
+    }
+  return SPHINX_OK;
+}
+
+sphinx_status sphinx_refine_q8_workspace_bytes(const sphinx_model_desc* m, const sphinx_request* reqs, int32_t R,
+                                               int64_t max_sel, int32_t kv8, size_t* bytes) {
+  if (kv8 != 0 && kv8 != 1) return SPHINX_E_INVALID;
+  sphinx_status st = q8_model_check(m);
+  if (st != SPHINX_OK) return st;
+  st = kv8 != 0 ? sphinx_refine_kv8_workspace_bytes(m, reqs, R, max_sel, bytes)
+                : sphinx_refine_workspace_bytes(m, reqs, R, max_sel, bytes);
+  if (st == SPHINX_OK) *bytes += q8_refine_extra(*m, std::max<int64_t>(max_sel, 1));
+  return st;
+}
+
+sphinx_status sphinx_refine_step_q8(const sphinx_model_desc* m, const void* w8, size_t w8_bytes,
+                                    const sphinx_request* reqs, int32_t R, const int32_t* idx, int32_t n,
+                                    const int32_t* cu_host, const int32_t* tau, const float* c1, const float* c2,
+                                    float* x, void* kv_cache, int32_t kv8, void* ws, size_t ws_bytes, void* stream) {
+  if ((kv8 != 0 && kv8 != 1) || (kv8 == 1 && kv_cache == nullptr)) return SPHINX_E_INVALID;
+  const sphinx_status st = q8_model_check(m);
+  if (st != SPHINX_OK) return st;
+  if (w8 == nullptr || !aligned(w8, 256)) return SPHINX_E_INVALID;
+  if (w8_bytes < (size_t)m->L * q8_model(*m).block) return SPHINX_E_WORKSPACE;
+  return refine_impl(m, reqs, R, idx, n, cu_host, tau, c1, c2, x, kv_cache, kv8 != 0, ws, ws_bytes, stream, w8);
 }
 
 sphinx_status sphinx_varlen_attention(sphinx_dtype dtype, int32_t heads, int32_t head_dim, const void* q,

@@ -59,7 +59,7 @@ sphinx_status sphinx_layer_norm(sphinx_dtype xdt, sphinx_dtype wdt, sphinx_dtype
   if (!(eps >= 0.0f) || ldy < cols || !aligned(y, 16) || !aligned(stats, 16)) return SPHINX_E_INVALID;
   if (S.cu[nseg] == 0) return SPHINX_OK;
   if (y == nullptr) return SPHINX_E_INVALID;
-  const LnArgs a{x, ldx, w, b, ldw, wdt == SPHINX_BF16, plus_one != 0, cols, eps};
+  const LnArgs a{x, ldx, w, b, ldw, wdt == SPHINX_BF16, plus_one != 0, cols, eps, nullptr};
   return hip_status(launch_layer_norm(xdt, ydt, a, S, y, ldy, nullptr, nullptr, stats, (hipStream_t)stream));
 }
 
@@ -73,7 +73,7 @@ sphinx_status sphinx_layer_norm_q8(sphinx_dtype xdt, sphinx_dtype wdt, int32_t c
   if (!(eps >= 0.0f) || !aligned(q, 16) || !aligned(s, 16) || !aligned(stats, 16)) return SPHINX_E_INVALID;
   if (S.cu[nseg] == 0) return SPHINX_OK;
   if (q == nullptr || s == nullptr) return SPHINX_E_INVALID;
-  const LnArgs a{x, ldx, w, b, ldw, wdt == SPHINX_BF16, plus_one != 0, cols, eps};
+  const LnArgs a{x, ldx, w, b, ldw, wdt == SPHINX_BF16, plus_one != 0, cols, eps, nullptr};
   return hip_status(launch_layer_norm(xdt, SPHINX_BF16, a, S, nullptr, 0, q, s, stats, (hipStream_t)stream));
 }
 
@@ -108,7 +108,7 @@ sphinx_status sphinx_layer_norm_backward(sphinx_dtype xdt, sphinx_dtype wdt, sph
     if (need > 0 && ws == nullptr) return SPHINX_E_INVALID;
     if (ws_bytes < need) return SPHINX_E_WORKSPACE;
   }
-  const LnArgs a{x, ldx, w, nullptr, ldw, wdt == SPHINX_BF16, plus_one != 0, cols, 0.0f};
+  const LnArgs a{x, ldx, w, nullptr, ldw, wdt == SPHINX_BF16, plus_one != 0, cols, 0.0f, nullptr};
   return hip_status(launch_layer_norm_backward(xdt, gdt, a, S, stats, dy, lddy, dx, lddx, dw, db, ldg,
                                                static_cast<float*>(ws), (hipStream_t)stream));
 }
@@ -182,8 +182,27 @@ sphinx_status sphinx_q8_matmul(sphinx_dtype odt, int32_t M, int32_t N, int32_t K
   if (out == nullptr || (K > 0 && (!a || !sa || !b || !sb)) || (need > 0 && ws == nullptr)) return SPHINX_E_INVALID;
   if (ws_bytes < need) return SPHINX_E_WORKSPACE;
   const Q8Epi e{(int)epilogue, bias, bdt == SPHINX_BF16, out, ldo};
-  return hip_status(launch_q8_matmul(odt, M, N, K, Q8Mat{a, sa}, Q8Mat{b, sb}, e, static_cast<float*>(ws),
+  return hip_status(launch_q8_matmul(odt == SPHINX_F32 ? kQ8F32 : kQ8Bf16, M, N, K, Q8Mat{a, sa}, Q8Mat{b, sb}, e, static_cast<float*>(ws),
                                      (hipStream_t)stream));
+}
+
+sphinx_status sphinx_q8_matmul_q8(int32_t M, int32_t N, int32_t K, const uint8_t* a, const uint8_t* sa,
+                                  const uint8_t* b, const uint8_t* sb, sphinx_dtype bdt, const void* bias,
+                                  sphinx_q8_epilogue epilogue, uint8_t* q, uint8_t* s, void* stream) {
+  if (!valid_dtype(bdt)) return SPHINX_E_UNSUPPORTED;
+  sphinx_status st = q8_size_check(M, K);
+  if (st == SPHINX_OK) st = q8_size_check(N, K);
+  if (st == SPHINX_OK) st = q8_size_check(M, N);
+  if (st != SPHINX_OK) return st;
+  if (epilogue != SPHINX_Q8_STORE && epilogue != SPHINX_Q8_GELU) return SPHINX_E_INVALID;
+  if (!aligned(a, 16) || !aligned(sa, 16) || !aligned(b, 16) || !aligned(sb, 16) || !aligned(bias, 16) ||
+      !aligned(q, 16) || !aligned(s, 16))
+    return SPHINX_E_INVALID;
+  if (M == 0 || N == 0) return SPHINX_OK;
+  if (!q || !s || (K > 0 && (!a || !sa || !b || !sb))) return SPHINX_E_INVALID;
+  Q8Epi e{(int)epilogue, bias, bdt == SPHINX_BF16, q, 0};
+  e.scales = s;
+  return hip_status(launch_q8_matmul(kQ8Bytes, M, N, K, Q8Mat{a, sa}, Q8Mat{b, sb}, e, nullptr, (hipStream_t)stream));
 }
 
 }  // extern "C"

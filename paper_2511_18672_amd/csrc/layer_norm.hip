@@ -97,7 +97,7 @@ __global__ __launch_bounds__(LnCfg<LPR>::NT) void k_layer_norm(LnArgs a, LnSegs 
     stats[2 * (int64_t)row] = mean;
     stats[2 * (int64_t)row + 1] = rstd;
   }
-  const int64_t wr = (int64_t)ln_segment(S, row) * a.ldw;
+  const int64_t wr = (int64_t)(a.row_of != nullptr ? a.row_of[row] : ln_segment(S, row)) * a.ldw;
   const float one = a.plus_one ? 1.0f : 0.0f;
 #pragma unroll
   for (int i = 0; i < NI; ++i) {

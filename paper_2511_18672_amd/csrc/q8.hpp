@@ -11,6 +11,7 @@
 #pragma once
 
 #include "kernels.hpp"
+#include "q8_rules.hpp"
 
 namespace sphinx {
 
@@ -37,6 +38,7 @@ struct LnArgs {
   bool w_bf16, plus_one;
   int cols;
   float eps;
+  const int32_t* row_of;  // row of w and b that each row takes, instead of its segment's (forward only), or NULL
 };
 
 // layer_norm.hip.  One of y (rows at ldy) and q/s is given; stats may be NULL.
@@ -59,7 +61,7 @@ hipError_t launch_join_parts(const float* part, int64_t stride, int cols, const 
 hipError_t launch_q8_quantise(sphinx_dtype dt, const void* x, int64_t ldx, int rows, int cols, bool square, uint8_t* q,
                               uint8_t* s, uint8_t* qt, uint8_t* st, float* sums, float* ws, hipStream_t stream);
 
-// q8_matmul.hip: out[M][N] = A[M][K] B[N][K]^T
+// q8_matmul.hip: C[M][N] = A[M][K] B[N][K]^T + bias
 enum { Q8_EPI_STORE = 0, Q8_EPI_GELU = 1, Q8_EPI_ADD = 2 };
 struct Q8Mat {
   const uint8_t* q;
@@ -69,11 +71,18 @@ struct Q8Epi {
   int epi;
   const void* bias;  // NULL: none
   bool bias_bf16;
-  void* out;
+  void* out;         // outputs of the given type; kQ8Gated: the fp32 residual; kQ8Bytes: rows of e4m3 bytes
   int64_t ldo;
+  uint8_t* scales;      // kQ8Bytes: its scales
+  const float* gate;    // kQ8Gated: out += (1 + gate[row_of[m]][n]) C, rows of gate at ldg
+  int64_t ldg;
+  const int32_t* row_of;
+  int qcols;            // columns [0, qcols) are multiplied by qscale (qcols a multiple of 8)
+  float qscale;
 };
 size_t q8_matmul_ws_bytes(sphinx_dtype odt, int M, int N, int K);
-hipError_t launch_q8_matmul(sphinx_dtype odt, int M, int N, int K, const Q8Mat& a, const Q8Mat& b, const Q8Epi& e,
+// ws: q8_matmul_ws_bytes for kQ8Bf16 and kQ8F32, not looked at for the others.
+hipError_t launch_q8_matmul(Q8Kind kind, int M, int N, int K, const Q8Mat& a, const Q8Mat& b, const Q8Epi& e,
                             float* ws, hipStream_t stream);
 
 // ---------------------------------------------------------------------------

@@ -17,7 +17,6 @@
 #include <type_traits>
 
 #include "q8.hpp"
-#include "q8_rules.hpp"
 
 namespace sphinx {
 
@@ -28,7 +27,7 @@ typedef int i32x4 __attribute__((ext_vector_type(4)));
 // s_waitcnt immediate: vmcnt(vm) lgkmcnt(0)
 constexpr int wait_vm(int vm) { return 0x0070 | (vm & 15) | ((vm >> 4) << 14); }
 
-// Bias and GELU of columns n .. n + 7.
+// Bias, scale and GELU of columns n .. n + 7.
 __device__ __forceinline__ void q8_finish(const Q8Epi& e, int n, int N, float (&v)[8]) {
   if (e.bias != nullptr) {
     float b[8];
@@ -40,6 +39,10 @@ __device__ __forceinline__ void q8_finish(const Q8Epi& e, int n, int N, float (&
   if (e.epi == Q8_EPI_GELU) {
 #pragma unroll
     for (int t = 0; t < 8; ++t) v[t] = gelu_tanh(v[t]);
+  }
+  if (n < e.qcols) {
+#pragma unroll
+    for (int t = 0; t < 8; ++t) v[t] *= e.qscale;
   }
 }
 
@@ -75,16 +78,77 @@ struct Q8Cfg {
   static_assert(BM % 64 == 0 && BM + BN <= 64 * NW, "one copy of 64 rows' scales per wave, of one operand");
 };
 
+// Outputs as a matrix in 8 bits, quantised from fp32: a block of 128 columns is
+// two waves' (TJ = 2), which tell each other their rows' largest magnitudes.
+template <int TI, int TJ, int WN, typename A, typename F>
+__device__ __forceinline__ void q8_rows_in_8_bits(A& acc, F& eight, const Q8Epi& e, unsigned char* smem, int m0, int n0,
+                                                  int M, int N, int wave) {
+  static_assert(TJ == 2 && WN % 2 == 0, "64 columns a wave");
+  const int lane = (int)threadIdx.x & 63, g = lane >> 5, r32 = lane & 31;
+  const int Np = (N + kQ8Block - 1) / kQ8Block * kQ8Block;
+  constexpr int PITCH = 64 + 16;
+  unsigned char* mine = smem + wave * 32 * PITCH;
+  float* tops = reinterpret_cast<float*>(smem + 16 * 32 * PITCH) + wave * 32 * TI;
+  const float* other = tops + ((wave & 1) != 0 ? -32 * TI : 32 * TI);
+  float top[TI];
+#pragma unroll
+  for (int i = 0; i < TI; ++i) {
+    float all[32];
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+      for (int q = 0; q < 4; q += 2) {
+        float v[8];
+        const int n = n0 + 32 * j + 8 * (q + g);
+        eight(i, j, q, v);
+        q8_finish(e, n, N, v);
+#pragma unroll
+        for (int t = 0; t < 8; ++t) {
+          v[t] = n + t < N ? v[t] : 0.0f;
+          all[16 * j + 4 * q + t] = acc[i][j][4 * q + t] = v[t];
+        }
+      }
+    top[i] = finite_top(all);
+    const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(top[i]), __float_as_uint(top[i]), false, false);
+    top[i] = fmaxf(__uint_as_float(x[0]), __uint_as_float(x[1]));
+    if (g == 0) tops[32 * i + r32] = top[i];
+  }
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < TI; ++i) {
+    const int sb = q8_scale_byte(fmaxf(top[i], other[32 * i + r32]));
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+      for (int q = 0; q < 4; q += 2) {
+        float v[8];
+#pragma unroll
+        for (int t = 0; t < 8; ++t) v[t] = acc[i][j][4 * q + t];
+        *reinterpret_cast<uint2*>(mine + r32 * PITCH + 32 * j + 8 * (q + g)) = q8_pack8(v, sb);
+      }
+    const int m = m0 + 32 * i + r32;
+    if ((wave & 1) == 0 && g == 0 && m < M && n0 < Np)
+      e.scales[(int64_t)m * q8_scale_row(Np / kQ8Block) + n0 / kQ8Block] = (uint8_t)sb;
+#pragma unroll
+    for (int p = 0; p < 2; ++p) {
+      const int r = 16 * p + (lane >> 2), c = 16 * (lane & 3), row = m0 + 32 * i + r;
+      const uint4 w = *reinterpret_cast<const uint4*>(mine + r * PITCH + c);
+      if (row < M && n0 < Np) *reinterpret_cast<uint4*>(static_cast<uint8_t*>(e.out) + (int64_t)row * Np + n0 + c) = w;
+    }
+  }
+}
+
 // Tile (m0, n0) over the blocks k0 .. k1 - 1 of the contraction (k0 a multiple
 // of 4); part != NULL: the sums go there, [M][N], as they are.
-template <typename OT, int TI, int TJ, int WM, int WN>
+template <Q8Kind KIND, int TI, int TJ, int WM, int WN>
 __device__ __forceinline__ void q8_tile(const uint8_t* __restrict__ A, const uint8_t* __restrict__ sA,
                                         const uint8_t* __restrict__ B, const uint8_t* __restrict__ sB, int M, int N,
                                         int KB, const Q8Epi& e, unsigned char* smem, int m0, int n0, int k0, int k1,
                                         float* part) {
   typedef Q8Cfg<TI, TJ, WM, WN> C;
-  constexpr bool kWide = std::is_same_v<OT, float>;  // fp32 outputs
-  constexpr int BM = C::BM, BN = C::BN, STAGE = C::STAGE, COPIES = C::COPIES, NW = C::NW;
+  constexpr bool kWide = KIND == kQ8F32;
+  typedef std::conditional_t<KIND == kQ8Bf16, bf16, float> OT;
+  constexpr int BM = C::BM, STAGE = C::STAGE, COPIES = C::COPIES, NW = C::NW;
   const int tid = (int)threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wm = wave / WN, wn = wave % WN, g = lane >> 5, r32 = lane & 31;
@@ -268,7 +332,7 @@ __device__ __forceinline__ void q8_tile(const uint8_t* __restrict__ A, const uin
     }
   };
   // bf16 outputs that are added to: the sum is rounded once, so it does not go through LDS in bf16
-  if (!kWide && part == nullptr && e.epi == Q8_EPI_ADD) {
+  if (KIND == kQ8Bf16 && part == nullptr && e.epi == Q8_EPI_ADD) {
 #pragma unroll
     for (int i = 0; i < TI; ++i) {
       const int m = m0 + a0 + 32 * i + r32;
@@ -291,6 +355,10 @@ __device__ __forceinline__ void q8_tile(const uint8_t* __restrict__ A, const uin
   // through L2.
   __builtin_amdgcn_s_barrier();  // every wave has read its last stage
   asm volatile("" ::: "memory");
+  if constexpr (KIND == kQ8Bytes) {
+    q8_rows_in_8_bits<TI, TJ, WN>(acc, eight, e, smem, m0 + a0, n0 + b0, M, N, wave);
+    return;
+  }
   auto rows_out = [&](auto ot, auto* out, int64_t ldo, bool finish) {
     typedef decltype(ot) ST;
     constexpr int V = 16 / (int)sizeof(ST), PITCH = 32 * TJ * (int)sizeof(ST) + 16;  // values of a piece; bytes of a row
@@ -320,7 +388,14 @@ __device__ __forceinline__ void q8_tile(const uint8_t* __restrict__ A, const uin
         __builtin_memcpy(w, __builtin_assume_aligned(mine + r * PITCH + c * sizeof(ST), 16), 16);
         if (m >= M) continue;
         ST* o = out + m * ldo + n;
-        if (left >= V) {
+        if (KIND == kQ8Gated) {  // N is a multiple of 4 here
+          if (left < V) continue;
+          const f32x4 gv = *reinterpret_cast<const f32x4*>(e.gate + e.row_of[m] * e.ldg + n);
+          f32x4 hv = *reinterpret_cast<const f32x4*>(o);
+#pragma unroll
+          for (int t = 0; t < 4; ++t) hv[t] = fmaf(1.0f + gv[t], (float)w[t], hv[t]);
+          *reinterpret_cast<f32x4*>(o) = hv;
+        } else if (left >= V) {
           if (kWide && finish && e.epi == Q8_EPI_ADD) {
             ST old[V];
             __builtin_memcpy(old, o, 16);
@@ -350,7 +425,7 @@ __device__ __forceinline__ void q8_tile(const uint8_t* __restrict__ A, const uin
 // high, column by column inside a panel, so that the tiles an XCD runs at a
 // time share few rows of A and B in its L2.  With part != NULL the contraction
 // is cut into gridDim.y pieces of `per` blocks.
-template <typename OT, int TI, int TJ, int WM, int WN>
+template <Q8Kind KIND, int TI, int TJ, int WM, int WN>
 __global__ __launch_bounds__(64 * WM * WN, 2) void k_q8_matmul(
     const uint8_t* __restrict__ A, const uint8_t* __restrict__ sA, const uint8_t* __restrict__ B,
     const uint8_t* __restrict__ sB, int M, int N, int KB, Q8Epi e, int per, float* __restrict__ part) {
@@ -360,7 +435,7 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void k_q8_matmul(
   const int tile = xcd_tile((int)blockIdx.x, rt * nt);
   const int panel = tile / (4 * nt), rem = tile - panel * 4 * nt, ph = min(4, rt - 4 * panel);
   const int k0 = (int)blockIdx.y * per;
-  q8_tile<OT, TI, TJ, WM, WN>(A, sA, B, sB, M, N, KB, e, smem, (4 * panel + rem % ph) * C::BM, (rem / ph) * C::BN, k0,
+  q8_tile<KIND, TI, TJ, WM, WN>(A, sA, B, sB, M, N, KB, e, smem, (4 * panel + rem % ph) * C::BM, (rem / ph) * C::BN, k0,
                               min(KB, k0 + per), part == nullptr ? nullptr : part + (int64_t)blockIdx.y * M * N);
 }
 
@@ -384,44 +459,55 @@ __global__ __launch_bounds__(256) void k_q8_join(const float* __restrict__ part,
   q8_store8<OT>(e, m, n, N, v);
 }
 
-template <typename OT, int TI, int TJ, int WM, int WN>
+template <Q8Kind KIND, int TI, int TJ, int WM, int WN>
 void launch_tiles(int M, int N, int KB, const Q8Mat& a, const Q8Mat& b, const Q8Epi& e, int pieces, float* ws,
                   hipStream_t stream) {
   typedef Q8Cfg<TI, TJ, WM, WN> C;
   const int64_t grid = (int64_t)((M + C::BM - 1) / C::BM) * ((N + C::BN - 1) / C::BN);
   const int per = ((KB + pieces - 1) / pieces + 3) / 4 * 4;
-  k_q8_matmul<OT, TI, TJ, WM, WN><<<dim3((unsigned)grid, (unsigned)pieces), C::NT, 0, stream>>>(
+  k_q8_matmul<KIND, TI, TJ, WM, WN><<<dim3((unsigned)grid, (unsigned)pieces), C::NT, 0, stream>>>(
       a.q, a.s, b.q, b.s, M, N, KB, e, per, pieces > 1 ? ws : nullptr);
-  if (pieces > 1) {
+  if constexpr (KIND == kQ8Bf16 || KIND == kQ8F32) {
+    typedef std::conditional_t<KIND == kQ8Bf16, bf16, float> OT;
     const int64_t n = (int64_t)M * ((N + 7) / 8);
-    k_q8_join<OT><<<(unsigned)((n + 255) / 256), 256, 0, stream>>>(ws, pieces, M, N, e);
+    if (pieces > 1) k_q8_join<OT><<<(unsigned)((n + 255) / 256), 256, 0, stream>>>(ws, pieces, M, N, e);
   }
 }
 }  // namespace
 
 size_t q8_matmul_ws_bytes(sphinx_dtype odt, int M, int N, int K) {
-  const Q8Plan p = plan_q8_matmul(odt == SPHINX_F32, M, N, (K + kQ8Block - 1) / kQ8Block);
-  return p.pieces > 1 ? (size_t)p.pieces * M * N * 4 : 0;
+  const int KB = (K + kQ8Block - 1) / kQ8Block;
+  const Q8Kind kind = odt == SPHINX_F32 ? kQ8F32 : kQ8Bf16;
+  int pieces = 1;  // of whichever epilogue
+  for (bool gelu : {false, true}) pieces = std::max(pieces, plan_q8_matmul(kind, gelu, M, N, KB).pieces);
+  return pieces > 1 ? (size_t)pieces * M * N * 4 : 0;
 }
 
-hipError_t launch_q8_matmul(sphinx_dtype odt, int M, int N, int K, const Q8Mat& a, const Q8Mat& b, const Q8Epi& e,
+hipError_t launch_q8_matmul(Q8Kind kind, int M, int N, int K, const Q8Mat& a, const Q8Mat& b, const Q8Epi& e,
                             float* ws, hipStream_t stream) {
   const int KB = (K + kQ8Block - 1) / kQ8Block;
-  const Q8Plan p = plan_q8_matmul(odt == SPHINX_F32, M, N, KB);
-  auto go = [&](auto ot) {
-    typedef decltype(ot) OT;
+  const Q8Plan p = plan_q8_matmul(kind, e.epi == Q8_EPI_GELU, M, N, KB);
+  auto go = [&](auto k) {
+    constexpr Q8Kind KIND = decltype(k)::value;
     switch (p.tile) {
-      case kQ8Tile256:  // fp32 outputs: its fragments in bf16 would spill
-        if constexpr (std::is_same_v<OT, bf16>) launch_tiles<OT, 4, 2, 2, 4>(M, N, KB, a, b, e, p.pieces, ws, stream);
+      case kQ8Tile256:  // not for fp32 outputs, whose fragments in bf16 would spill
+        if constexpr (KIND != kQ8F32) launch_tiles<KIND, 4, 2, 2, 4>(M, N, KB, a, b, e, p.pieces, ws, stream);
         break;
-      case kQ8Tile192: launch_tiles<OT, 3, 2, 2, 4>(M, N, KB, a, b, e, p.pieces, ws, stream); break;
-      case kQ8Tile128: launch_tiles<OT, 2, 2, 2, 2>(M, N, KB, a, b, e, p.pieces, ws, stream); break;
-      case kQ8Tile128x64: launch_tiles<OT, 2, 1, 2, 2>(M, N, KB, a, b, e, p.pieces, ws, stream); break;
-      default: launch_tiles<OT, 1, 1, 2, 2>(M, N, KB, a, b, e, p.pieces, ws, stream);
+      case kQ8Tile192: launch_tiles<KIND, 3, 2, 2, 4>(M, N, KB, a, b, e, p.pieces, ws, stream); break;
+      case kQ8Tile128: launch_tiles<KIND, 2, 2, 2, 2>(M, N, KB, a, b, e, p.pieces, ws, stream); break;
+      case kQ8Tile128x64:
+        if constexpr (KIND != kQ8Bytes) launch_tiles<KIND, 2, 1, 2, 2>(M, N, KB, a, b, e, p.pieces, ws, stream);
+        break;
+      default:
+        if constexpr (KIND != kQ8Bytes) launch_tiles<KIND, 1, 1, 2, 2>(M, N, KB, a, b, e, p.pieces, ws, stream);
     }
   };
-  if (odt == SPHINX_BF16) go(bf16{});
-  else go(float{});
+  switch (kind) {
+    case kQ8Bf16: go(std::integral_constant<Q8Kind, kQ8Bf16>{}); break;
+    case kQ8F32: go(std::integral_constant<Q8Kind, kQ8F32>{}); break;
+    case kQ8Gated: go(std::integral_constant<Q8Kind, kQ8Gated>{}); break;
+    default: go(std::integral_constant<Q8Kind, kQ8Bytes>{});
+  }
   return hipGetLastError();
 }
 

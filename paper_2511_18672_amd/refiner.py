@@ -16,6 +16,10 @@ and every step runs ``sphinx_gather_ctx``, ``sphinx_refine_step_cached`` and
 ``cache_dtype="fp8"`` keeps the cache in 8 bits with a scale per block of 64
 tokens and head (``sphinx_refine_step_kv8``): half the bytes of a bf16 cache.
 
+``product_dtype="fp8"`` runs the block products of a bf16 model in 8 bits with a
+scale per block of 128 (``sphinx_refine_step_q8``), with or without a cache; the
+weights are quantised once, by ``sphinx_model_q8_pack``.
+
 The fp32 state of record and the noise live token-major by default (token t's
 16 values contiguous at 16*t), so each gathered or scattered token is one
 contiguous row; the NCHW latents are converted once at ``reset`` and back in
@@ -72,11 +76,16 @@ class Refiner:
     def __init__(self, requests: Sequence, cfg, blob: torch.Tensor, s_start: np.ndarray, nsteps: np.ndarray,
                  u: np.ndarray, thr: np.ndarray, z0: np.ndarray, eps: np.ndarray, device="cuda",
                  max_sel: Optional[int] = None, layout: int = B.TOKENS, cache_period: int = 0,
-                 per_frame_grid: bool = False, cache_dtype: str = "model"):
+                 per_frame_grid: bool = False, cache_dtype: str = "model",
+                 product_dtype: str = "model"):
         if cache_dtype not in ("model", "fp8"):
             raise ValueError(f"cache_dtype {cache_dtype!r}: 'model' or 'fp8'")
         if cache_dtype != "model" and cache_period <= 0:
             raise ValueError("cache_dtype needs a cache: set cache_period")
+        if product_dtype not in ("model", "fp8"):
+            raise ValueError(f"product_dtype {product_dtype!r}: 'model' or 'fp8'")
+        if product_dtype != "model" and cfg.dtype != "bf16":
+            raise ValueError("products in 8 bits need a bf16 model")
         if not torch.cuda.is_available():
             raise RuntimeError("Refiner needs a GPU: the selective-refinement step has no CPU path")
         B.lib()
@@ -116,8 +125,15 @@ class Refiner:
         self.x_sel = torch.empty(16 * self.max_sel, dtype=torch.float32, device=dev)
         self.ws_sel = torch.empty(B.sphinx_select_workspace_bytes(self.N), dtype=torch.uint8, device=dev)
         self.kv8 = cache_dtype == "fp8"
-        ws_bytes = B.sphinx_refine_kv8_workspace_bytes if self.kv8 else B.sphinx_refine_workspace_bytes
-        self.ws = torch.empty(ws_bytes(self.desc, self.reqs, self.max_sel), dtype=torch.uint8, device=dev)
+        self.w8 = None
+        if product_dtype == "fp8":
+            self.w8 = torch.empty(B.sphinx_model_q8_bytes(self.desc), dtype=torch.uint8, device=dev)
+            B.sphinx_model_q8_pack(self.desc, self.w8)
+            ws_bytes = B.sphinx_refine_q8_workspace_bytes(self.desc, self.reqs, self.max_sel, self.kv8)
+        else:
+            ws_bytes = (B.sphinx_refine_kv8_workspace_bytes if self.kv8 else B.sphinx_refine_workspace_bytes)(
+                self.desc, self.reqs, self.max_sel)
+        self.ws = torch.empty(ws_bytes, dtype=torch.uint8, device=dev)
         self.total_steps = int(np.max(nsteps))
         self.grid = B.GRID_PER_FRAME if per_frame_grid else B.GRID_SHARED
         plans = [B.sphinx_plan_step(self.reqs, s_start, nsteps, i, self.grid) for i in range(self.total_steps)]
@@ -219,8 +235,12 @@ class Refiner:
         P = self.plan
         B.sphinx_gather(self.reqs, self.layout, self.z, B.F32, self.eps, self.dt, self.idx, n, P["a"][k],
                         P["b"][k], self.x_sel, stream)
-        B.sphinx_refine_step(self.desc, self.reqs, self.idx, n, self.cu_host, P["tau"][k], P["c1"][k],
-                             P["c2"][k], self.x_sel, self.ws, stream)
+        if self.w8 is not None:
+            B.sphinx_refine_step_q8(self.desc, self.w8, self.reqs, self.idx, n, self.cu_host, P["tau"][k], P["c1"][k],
+                                    P["c2"][k], self.x_sel, None, False, self.ws, stream)
+        else:
+            B.sphinx_refine_step(self.desc, self.reqs, self.idx, n, self.cu_host, P["tau"][k], P["c1"][k],
+                                 P["c2"][k], self.x_sel, self.ws, stream)
         B.sphinx_scatter_blend(self.reqs, self.x_sel, self.idx, n, self.z, B.F32, self.layout, self.z, B.F32,
                                self.layout, stream)
         return n
@@ -240,9 +260,13 @@ class Refiner:
             return 0
         B.sphinx_gather_ctx(self.reqs, self.layout, self.z, B.F32, self.eps, self.dt, idx_f, n_f, self.mask,
                             P["a"][k], P["b"][k], C["a_ctx"][k], C["b_ctx"][k], self.x_sel, stream)
-        refine = B.sphinx_refine_step_kv8 if self.kv8 else B.sphinx_refine_step_cached
-        refine(self.desc, self.reqs, idx_f, n_f, cu_f, P["tau"][k], P["c1"][k], P["c2"][k], self.x_sel, self.kv_cache,
-               self.ws, stream)
+        if self.w8 is not None:
+            B.sphinx_refine_step_q8(self.desc, self.w8, self.reqs, idx_f, n_f, cu_f, P["tau"][k], P["c1"][k],
+                                    P["c2"][k], self.x_sel, self.kv_cache, self.kv8, self.ws, stream)
+        else:
+            refine = B.sphinx_refine_step_kv8 if self.kv8 else B.sphinx_refine_step_cached
+            refine(self.desc, self.reqs, idx_f, n_f, cu_f, P["tau"][k], P["c1"][k], P["c2"][k], self.x_sel,
+                   self.kv_cache, self.ws, stream)
         B.sphinx_scatter_masked(self.reqs, self.x_sel, idx_f, n_f, self.mask, self.z, B.F32, self.layout, stream)
         return n
 

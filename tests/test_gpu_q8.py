@@ -169,6 +169,17 @@ def test_product(M, N, K, odt):
     assert (np.abs(host(product(odt, a, b, M, N, K, epilogue=B.Q8_ADD, before=before, ld=1)) - total) <= tol1).all()
 
 
+@pytest.mark.parametrize("odt", ["f32", "bf16"])
+def test_tiles_of_every_size_add_up_alike(odt):
+    """Products whose contraction is not cut give the same bits for a row whatever the rows and columns beside it, so
+    whatever the tile (64x64 to 256x256)."""
+    M, N, K = 9000, 2304, 300
+    a, b = pack(numbers(M, K, 1)), pack(numbers(N, K, 2))
+    full = product(odt, a, b, M, N, K)
+    for m, n in ((1, 2304), (70, 64), (400, 2304), (1500, 1000), (9000, 200), (4000, 2304)):
+        assert torch.equal(product(odt, a, b, m, n, K), full[:m, :n]), (m, n)
+
+
 def test_product_without_a_contraction_is_the_bias():
     u8 = torch.empty(0, dtype=torch.uint8, device=DEV)
     bias = dev(np.arange(70.0))
