@@ -60,7 +60,7 @@ def parse():
     ap.add_argument("--cache-dtype", default="model", choices=["model", "fp8"],
                     help="latent cache in the model's type or in 8 bits (needs --cache-period)")
     ap.add_argument("--product-dtype", default="model", choices=["model", "fp8"],
-                    help="block products in the model's type (the default workload) or in 8 bits; with fp8, dtype says so")
+                    help="QKV and MLP products in the model's type (the default workload) or in 8 bits")
     ap.add_argument("--select-every-step", type=int, default=1,
                     help="1: run mask+compaction in every step (default); 0: only when the active set changes")
     return ap.parse_args()

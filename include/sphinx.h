@@ -600,15 +600,15 @@ sphinx_status sphinx_q8_matmul_q8(int32_t M, int32_t N, int32_t K, const uint8_t
                                   const uint8_t* b, const uint8_t* sb, sphinx_dtype bdt, const void* bias,
                                   sphinx_q8_epilogue epilogue, uint8_t* q, uint8_t* s, void* stream);
 
-/* The refinement step with its block products in 8 bits (bf16 models).  w8: dev,
- * 256-byte aligned, sphinx_model_q8_bytes bytes, filled by sphinx_model_q8_pack
- * from m->weights: the four matrices of every block, in squares of 128 x 128.
- * sphinx_refine_step_q8 is sphinx_refine_step (kv_cache = NULL),
- * sphinx_refine_step_cached (kv8 = 0) or sphinx_refine_step_kv8 (kv8 = 1) with
- * each block's QKV, output and MLP products through w8: their inputs (the
- * modulated norms, the attention's output, the GELU) are quantised along their
- * rows.  All else, biases and residual stream among it, is as it was.
- * SPHINX_E_UNSUPPORTED for f32 models. */
+/* The refinement step with block products in 8 bits (bf16 models): the QKV
+ * projection and both MLP layers, whose inputs, the modulated norms and the
+ * GELU, are quantised along their rows by the kernel that computes them.  w8:
+ * dev, 256-byte aligned, sphinx_model_q8_bytes bytes, filled by
+ * sphinx_model_q8_pack from m->weights: those three matrices of every block, in
+ * squares of 128 x 128.  sphinx_refine_step_q8 is sphinx_refine_step (kv_cache =
+ * NULL), sphinx_refine_step_cached (kv8 = 0) or sphinx_refine_step_kv8 (kv8 = 1)
+ * with these products; all else is as it was.  SPHINX_E_UNSUPPORTED for f32
+ * models. */
 sphinx_status sphinx_model_q8_bytes(const sphinx_model_desc* m, size_t* bytes);
 sphinx_status sphinx_model_q8_pack(const sphinx_model_desc* m, void* w8, size_t w8_bytes, void* stream);
 sphinx_status sphinx_refine_q8_workspace_bytes(const sphinx_model_desc* m, const sphinx_request* reqs, int32_t R,

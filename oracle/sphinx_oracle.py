@@ -406,13 +406,13 @@ class Model:
     dtype: str
     weights: Dict[str, np.ndarray]
     attention: str = "joint"
-    products8: bool = False  # block products of 8-bit matrices (weights holds the values of its own)
+    products8: bool = False  # QKV and MLP products of 8-bit matrices (weights holds the values of theirs)
 
 
 def model_from_workload(wl, products8: bool = False) -> Model:
     m, weights = wl.model, wl.weights
     if products8:
-        weights = {k: q8.quantise(v, square=True) if k.endswith(("qkv_w", "o_w", "fc1_w", "fc2_w")) else v
+        weights = {k: q8.quantise(v, square=True) if k.endswith(("qkv_w", "fc1_w", "fc2_w")) else v
                    for k, v in weights.items()}
     return Model(m.D, m.heads, m.mlp, m.L, m.dtype, weights, getattr(m, "attention", "joint"), products8)
 
@@ -448,8 +448,7 @@ def denoise(model: Model, x: np.ndarray, f, y, xx, tau_tok: np.ndarray, seg: np.
     rnd = round_bf16 if (precision == "model" and model.dtype == "bf16") else (lambda a: a)
     # queries are kept in base-2 softmax units: q' = q log2(e)/sqrt(d), and
     # softmax(q k^T / sqrt(d)) = softmax(ln(2) q' k^T)
-    # 8-bit products: their inputs in 8 bits along their rows, straight from the norm and the GELU, and from the
-    # attention's output in the model's type
+    # 8-bit products (QKV and MLP): their inputs in 8 bits along their rows, straight from the norm and the GELU
     into = q8.quantise if model.products8 else rnd
     qscale, sscale = np.log2(np.e) / np.sqrt(D // H), np.log(2.0)
     # conditioning, per distinct timestep (identical for equal timesteps)
@@ -485,8 +484,6 @@ def denoise(model: Model, x: np.ndarray, f, y, xx, tau_tok: np.ndarray, seg: np.
                                            np.concatenate([y, kv_pos[1]]), np.concatenate([xx, kv_pos[2]]))
                 gq, gk = both[:x.shape[0]], both[x.shape[0]:]
                 o = rnd(attention_groups(q, cache[l][0], cache[l][1], H, gq, gk, scale=sscale))
-        if model.products8:
-            o = into(o)
         h = h + (1.0 + g1) * linear(o, w[f"b{l}.o_w"], w[f"b{l}.o_b"])
         a2 = into(layer_norm(h) * (1.0 + sc2) + sh2)
         m = into(gelu_tanh(linear(a2, w[f"b{l}.fc1_w"], w[f"b{l}.fc1_b"])))
@@ -609,7 +606,7 @@ def refine(wl, precision: str = "model", denoiser=None, trace: bool = False, ste
     """Run the whole partial-denoising loop; returns the final NCHW state (float64)
     and, with trace=True, the list of per-step results.  period > 0 turns on
     the latent cache with a full step every ``period`` steps, cache8 keeps it in
-    8 bits; products8 multiplies the block matrices in 8 bits."""
+    8 bits; products8 takes the QKV and MLP products in 8 bits."""
     model = model_from_workload(wl, products8)
     plans = plan_steps([r.frames for r in wl.requests], wl.s_start, wl.nsteps, period, per_frame_grid)
     info = token_info(wl.requests)

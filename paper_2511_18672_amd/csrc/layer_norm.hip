@@ -3,7 +3,7 @@
 //   y = xh w' + b                                  w' = w or 1 + w, per segment
 //   g = dy w', dx = r (g - mean(g) - xh mean(g xh)), dw = sum dy xh, db = sum dy
 //
-// A row lives in the registers of LPR lanes (16, 64, 256 or 1024), eight
+// A row lives in the registers of LPR lanes (16, 64, 256 or 512), eight
 // consecutive columns each and NI such groups, so HBM is read once and both
 // passes of the variance run over registers.  Everything is in fp32; y and dx
 // are rounded once.  Both directions are bound by HBM.
@@ -73,9 +73,22 @@ __global__ __launch_bounds__(LnCfg<LPR>::NT) void k_layer_norm(LnArgs a, LnSegs 
   const bool live = row0 < rows;
   const int row = min(row0, rows - 1);  // lanes past the end repeat the last row and store nothing
   const XT* x = static_cast<const XT*>(a.x) + (int64_t)row * a.ldx;
-  float v[NI][8];
+  // short rows: everything that they need is on its way before the first sum is waited for.  Longer ones would pay for
+  // it with waves (3000 x 8192 in bf16 21.3 -> 23.3 us)
+  constexpr bool kEarly = NI <= 2 && LPR <= 64;
+  float v[NI][8], w[NI][8], b[NI][8];
 #pragma unroll
   for (int i = 0; i < NI; ++i) load8(x + 8 * (i * LPR + t), cols - 8 * (i * LPR + t), v[i]);
+  const int64_t wr = (int64_t)(a.row_of != nullptr ? a.row_of[row] : ln_segment(S, row)) * a.ldw;
+  const float one = a.plus_one ? 1.0f : 0.0f;
+  auto weights = [&](int i) {
+    const int c = 8 * (i * LPR + t);
+    ln_load_w(a.w, a.w_bf16, wr + c, cols - c, 1.0f - one, w[i]);
+    ln_load_w(a.b, a.w_bf16, wr + c, cols - c, 0.0f, b[i]);
+  };
+  if constexpr (kEarly)
+#pragma unroll
+    for (int i = 0; i < NI; ++i) weights(i);
   float s = 0.0f;
 #pragma unroll
   for (int i = 0; i < NI; ++i)
@@ -97,16 +110,13 @@ __global__ __launch_bounds__(LnCfg<LPR>::NT) void k_layer_norm(LnArgs a, LnSegs 
     stats[2 * (int64_t)row] = mean;
     stats[2 * (int64_t)row + 1] = rstd;
   }
-  const int64_t wr = (int64_t)(a.row_of != nullptr ? a.row_of[row] : ln_segment(S, row)) * a.ldw;
-  const float one = a.plus_one ? 1.0f : 0.0f;
 #pragma unroll
   for (int i = 0; i < NI; ++i) {
     const int c = 8 * (i * LPR + t), n = cols - c;
-    float w[8], b[8], o[8];
-    ln_load_w(a.w, a.w_bf16, wr + c, n, 1.0f - one, w);
-    ln_load_w(a.b, a.w_bf16, wr + c, n, 0.0f, b);
+    if constexpr (!kEarly) weights(i);
+    float o[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) o[e] = fmaf(v[i][e] * rstd, w[e] + one, b[e]);
+    for (int e = 0; e < 8; ++e) o[e] = fmaf(v[i][e] * rstd, w[i][e] + one, b[i][e]);
     if constexpr (std::is_same_v<OUT, Q8Out>) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) o[e] = e < n ? o[e] : 0.0f;
@@ -284,12 +294,14 @@ __global__ __launch_bounds__(1024) void k_join_parts(const float* __restrict__ p
 }
 
 // Calls f with the lanes per row and groups of eight columns per lane as constants.
+// `sums`: the columns' sums take registers as well (backward), so that four groups of columns per lane would leave one
+// wave per SIMD.
 template <typename F>
-void by_cols(int cols, F&& f) {
+void by_cols(int cols, bool sums, F&& f) {
   typedef std::integral_constant<int, 16> L16;
   typedef std::integral_constant<int, 64> L64;
   typedef std::integral_constant<int, 256> L256;
-  typedef std::integral_constant<int, 1024> L1024;
+  typedef std::integral_constant<int, 512> L512;
   typedef std::integral_constant<int, 1> N1;
   typedef std::integral_constant<int, 2> N2;
   typedef std::integral_constant<int, 3> N3;
@@ -299,15 +311,17 @@ void by_cols(int cols, F&& f) {
   else if (g <= 64) f(L64{}, N1{});
   else if (g <= 128) f(L64{}, N2{});
   else if (g <= 192) f(L64{}, N3{});
+  else if (sums && g <= 256) f(L256{}, N1{});
   else if (g <= 256) f(L64{}, N4{});
   else if (g <= 512) f(L256{}, N2{});
   else if (g <= 1024) f(L256{}, N4{});
-  else f(L1024{}, N2{});
+  else f(L512{}, N4{});
 }
 
 LnChunks ln_chunks(int cols, const LnSegs& S) {
-  // about 512 workgroups, two per CU, of at least one turn each
-  const int per = cols <= 128 ? 16 : cols <= 2048 ? 4 : 1;  // rows of a turn
+  // about 512 workgroups, two per CU, of at least one turn each (1024: 32256 x 1024 in bf16 38 -> 43 us, 9677 x 1024
+  // 17 -> 20, since twice as many sums are written and joined)
+  const int per = cols <= 128 ? 16 : cols <= 1536 ? 4 : 1;  // rows of a turn
   const int64_t rows = S.cu[S.nseg];
   LnChunks P;
   P.rows = (int)std::max<int64_t>(per, (rows + 511) / 512);
@@ -328,7 +342,7 @@ hipError_t launch_join_parts(const float* part, int64_t stride, int cols, const 
 
 hipError_t launch_layer_norm(sphinx_dtype xdt, sphinx_dtype ydt, const LnArgs& a, const LnSegs& S, void* y,
                              int64_t ldy, uint8_t* q, uint8_t* s, float* stats, hipStream_t st) {
-  by_cols(a.cols, [&](auto L, auto N) {
+  by_cols(a.cols, false, [&](auto L, auto N) {
     constexpr int LPR = decltype(L)::value, NI = decltype(N)::value;
     typedef LnCfg<LPR> C;
     const int grid = (S.cu[S.nseg] + C::ROWS - 1) / C::ROWS;
@@ -359,7 +373,7 @@ hipError_t launch_layer_norm_backward(sphinx_dtype xdt, sphinx_dtype gdt, const 
   const int grid = P.first[S.nseg];
   float* part = dw != nullptr || db != nullptr ? ws : nullptr;
   if (grid > 0) {
-    by_cols(a.cols, [&](auto L, auto N) {
+    by_cols(a.cols, true, [&](auto L, auto N) {
       constexpr int LPR = decltype(L)::value, NI = decltype(N)::value;
       auto go = [&](auto xt, auto gt) {
         typedef decltype(xt) XT;

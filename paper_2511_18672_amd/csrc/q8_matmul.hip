@@ -138,6 +138,61 @@ __device__ __forceinline__ void q8_rows_in_8_bits(A& acc, F& eight, const Q8Epi&
   }
 }
 
+// out += (1 + gate) C on an fp32 residual whose N is a multiple of 4.  Rows of the
+// residual are read one set of 32 ahead of their use; a wave's rows mostly have
+// one row of gates, which is then read once.
+template <int TI, int TJ, typename A, typename F>
+__device__ __forceinline__ void q8_rows_gated(A& acc, F& eight, const Q8Epi& e, unsigned char* smem, int m0, int n0,
+                                              int M, int N, int wave) {
+  constexpr int PITCH = 32 * TJ * 4 + 16, LPW = 8 * TJ, RPP = 64 / LPW, P = 32 / RPP;
+  const int lane = (int)threadIdx.x & 63, g = lane >> 5, r32 = lane & 31;
+  unsigned char* mine = smem + wave * 32 * PITCH;
+  const int c = lane % LPW * 4, n = min(n0 + c, N - 4), sub = lane / LPW;
+  const bool in = n0 + c < N;
+  float* out = static_cast<float*>(e.out) + n;
+  f32x4 h[2][P];
+  auto load = [&](int i) {
+#pragma unroll
+    for (int p = 0; p < P; ++p)
+      h[i & 1][p] = *reinterpret_cast<const f32x4*>(out + (int64_t)min(m0 + 32 * i + p * RPP + sub, M - 1) * e.ldo);
+  };
+  load(0);
+  const int first = e.row_of[min(m0, M - 1)];
+  bool same = true;
+#pragma unroll
+  for (int i = 0; i < TI; ++i) same = same && e.row_of[min(m0 + 32 * i + r32, M - 1)] == first;
+  auto rows = [&](auto SAME) {
+    f32x4 gate;
+    if constexpr (decltype(SAME)::value) gate = *reinterpret_cast<const f32x4*>(e.gate + first * e.ldg + n);
+#pragma unroll
+    for (int i = 0; i < TI; ++i) {
+      if (i + 1 < TI) load(i + 1);
+#pragma unroll
+      for (int j = 0; j < TJ; ++j)
+#pragma unroll
+        for (int q = 0; q < 4; q += 2) {
+          float v[8];
+          eight(i, j, q, v);
+          q8_finish(e, n0 + 32 * j + 8 * (q + g), N, v);
+          __builtin_memcpy(__builtin_assume_aligned(mine + r32 * PITCH + (32 * j + 8 * (q + g)) * 4, 16), v, 32);
+        }
+#pragma unroll
+      for (int p = 0; p < P; ++p) {
+        const int r = p * RPP + sub, m = m0 + 32 * i + r;
+        const f32x4 v = *reinterpret_cast<const f32x4*>(mine + r * PITCH + c * 4);
+        if constexpr (!decltype(SAME)::value)
+          gate = *reinterpret_cast<const f32x4*>(e.gate + e.row_of[min(m, M - 1)] * e.ldg + n);
+        f32x4 o;
+#pragma unroll
+        for (int t = 0; t < 4; ++t) o[t] = fmaf(1.0f + gate[t], v[t], h[i & 1][p][t]);
+        if (in && m < M) *reinterpret_cast<f32x4*>(out + (int64_t)m * e.ldo) = o;
+      }
+    }
+  };
+  if (__ballot(same) == ~0ull) rows(std::true_type{});
+  else rows(std::false_type{});
+}
+
 // Tile (m0, n0) over the blocks k0 .. k1 - 1 of the contraction (k0 a multiple
 // of 4); part != NULL: the sums go there, [M][N], as they are.
 template <Q8Kind KIND, int TI, int TJ, int WM, int WN>
@@ -355,6 +410,10 @@ __device__ __forceinline__ void q8_tile(const uint8_t* __restrict__ A, const uin
   // through L2.
   __builtin_amdgcn_s_barrier();  // every wave has read its last stage
   asm volatile("" ::: "memory");
+  if constexpr (KIND == kQ8Gated) {
+    q8_rows_gated<TI, TJ>(acc, eight, e, smem, m0 + a0, n0 + b0, M, N, wave);
+    return;
+  }
   if constexpr (KIND == kQ8Bytes) {
     q8_rows_in_8_bits<TI, TJ, WN>(acc, eight, e, smem, m0 + a0, n0 + b0, M, N, wave);
     return;
@@ -388,14 +447,7 @@ __device__ __forceinline__ void q8_tile(const uint8_t* __restrict__ A, const uin
         __builtin_memcpy(w, __builtin_assume_aligned(mine + r * PITCH + c * sizeof(ST), 16), 16);
         if (m >= M) continue;
         ST* o = out + m * ldo + n;
-        if (KIND == kQ8Gated) {  // N is a multiple of 4 here
-          if (left < V) continue;
-          const f32x4 gv = *reinterpret_cast<const f32x4*>(e.gate + e.row_of[m] * e.ldg + n);
-          f32x4 hv = *reinterpret_cast<const f32x4*>(o);
-#pragma unroll
-          for (int t = 0; t < 4; ++t) hv[t] = fmaf(1.0f + gv[t], (float)w[t], hv[t]);
-          *reinterpret_cast<f32x4*>(o) = hv;
-        } else if (left >= V) {
+        if (left >= V) {
           if (kWide && finish && e.epi == Q8_EPI_ADD) {
             ST old[V];
             __builtin_memcpy(old, o, 16);

@@ -16,7 +16,7 @@ and every step runs ``sphinx_gather_ctx``, ``sphinx_refine_step_cached`` and
 ``cache_dtype="fp8"`` keeps the cache in 8 bits with a scale per block of 64
 tokens and head (``sphinx_refine_step_kv8``): half the bytes of a bf16 cache.
 
-``product_dtype="fp8"`` runs the block products of a bf16 model in 8 bits with a
+``product_dtype="fp8"`` runs the QKV and MLP products of a bf16 model in 8 bits with a
 scale per block of 128 (``sphinx_refine_step_q8``), with or without a cache; the
 weights are quantised once, by ``sphinx_model_q8_pack``.
 

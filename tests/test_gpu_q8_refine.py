@@ -1,4 +1,4 @@
-"""Products that leave a matrix in 8 bits, and the refinement step with its block products in 8 bits."""
+"""Products that leave a matrix in 8 bits, and the refinement step with its QKV and MLP products in 8 bits."""
 import dataclasses
 
 import numpy as np
@@ -88,7 +88,7 @@ def test_weights_are_quantised_in_squares(model):
     R = S.from_workload(wl, product_dtype="fp8")
     w8, at, cfg = R.w8.cpu(), 0, wl.model
     for l in range(cfg.L):
-        for name in ("qkv_w", "o_w", "fc1_w", "fc2_w"):
+        for name in ("qkv_w", "fc1_w", "fc2_w"):
             w = np.asarray(wl.weights[f"b{l}.{name}"], np.float64)
             nq, ns = B.sphinx_q8_bytes(*w.shape)
             q = w8[at:at + nq]
@@ -119,12 +119,11 @@ def test_loop_against_the_oracle(model, kw):
 @pytest.mark.parametrize("model", list(MODELS))
 def test_one_step_of_one_block_against_the_oracle(model):
     """A number x is quantised in steps of D = 2^-3.5 |x| (between 2^-4 and 2^-3), which is an error of variance D^2/12.
-    Only the attention's output comes to its quantisation in bf16: there the GPU's number and the oracle's may differ by
-    a step of bf16, d = 2^-7.5 |x| (where they do not round alike, less than half of the time: the probabilities are
-    rounded to bf16 before they are averaged), and then fall to different sides of a border with probability d/D: an
-    error of variance d D / 2 at most.  Its ratio to D^2/12 is 6 d/D = 6/16, the ratio of the two rms sqrt(6/16) < 0.62.
-    The other three products' inputs are quantised from fp32 and share borders but for one in 10^4, so that with the
-    noise of four products in the second rms and a part of one in the first, the ratio is below 0.62 in every case."""
+    The GPU's number and the oracle's differ by some d, and fall to different sides of a border with probability d/D: an
+    error of variance d D, 12 d/D of the other.  The first norm's input is fp32 throughout: d/D below 10^-4.  The second
+    norm's comes through an attention in bf16 (o is rounded: d = 2^-8 of its part of the residual stream at most) and
+    the GELU's through it and a product: even if that were all of them, 12 d/D = 12 2^-8 2^3.5 = 0.53, of the roundings
+    of two of the three inputs.  The ratio of the rms is then below sqrt(0.53 2/3) < 0.6."""
     wl = workload(model)
     wl = dataclasses.replace(wl, model=dataclasses.replace(wl.model, L=1))
     R = S.from_workload(wl, product_dtype="fp8")
@@ -134,7 +133,7 @@ def test_one_step_of_one_block_against_the_oracle(model):
     ref, plain = (O.refine(wl, precision="model", products8=p, steps=1) for p in (True, False))
     a, b = (float(np.sqrt(((got - x) ** 2).mean())) for x in (ref, plain))
     print(f"[q8 step {model}] rms to the 8-bit oracle {a:.3e}, to the other one {b:.3e}", flush=True)
-    assert a <= 0.62 * b
+    assert a <= 0.6 * b
 
 
 def test_the_loop_repeats_bit_for_bit():
