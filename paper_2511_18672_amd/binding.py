@@ -175,15 +175,17 @@ def lib() -> ctypes.CDLL:
 
 
 _torch = None
+_raw_stream = None
 _TYPES = {}
 
 
 def _load_torch():
     """torch, imported once (an import statement in a function takes a tenth of a microsecond), and its types."""
-    global _torch
+    global _torch, _raw_stream
     if _torch is None:
         import torch
 
+        _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
         _TYPES.update({F32: torch.float32, BF16: torch.bfloat16, "u8": torch.uint8})
         _torch = torch
     return _torch
@@ -431,8 +433,7 @@ def _here(stream, *tensors) -> Optional[int]:
             raise ValueError(f"tensor on {t.device}, the current device is cuda:{dev}")
     if stream is None:
         # the handle alone, where torch offers it: a Stream object takes 1 us of a 7 us call
-        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
-        return raw(dev) if raw is not None else torch.cuda.current_stream(dev).cuda_stream
+        return _raw_stream(dev) if _raw_stream is not None else torch.cuda.current_stream(dev).cuda_stream
     if isinstance(stream, int):
         return stream
     at = getattr(stream, "device_index", dev)
@@ -564,59 +565,77 @@ def _int32(name: str, v) -> int:
     return v
 
 
-def _check_out(name: str, t, dtype, n: int):
-    """Refuses a tensor of another type, not in a row, or with fewer than n elements."""
-    if t is not None and (t.dtype is not dtype or not t.is_contiguous() or t.numel() < n):
+def _rows(name: str, t, dtype: int, n: int, ld: int, width: int) -> Optional[int]:
+    """The address of a tensor that _check_rows takes (None: NULL)."""
+    if t is None:
+        return None
+    if t.dtype is not _TYPES.get(dtype) or t.numel() < (n - 1) * ld + width or not t.is_contiguous():
+        _check_rows(name, t, dtype, n, ld, width)
+    return t.data_ptr()
+
+
+def _flat(name: str, t, dtype, n: int) -> Optional[int]:
+    """The address of a tensor of n elements or more in a row, of the given type (None: NULL)."""
+    if t is None:
+        return None
+    if t.dtype is not _TYPES.get(dtype) or t.numel() < n or not t.is_contiguous():
+        if _torch is None:
+            _load_torch()
+            return _flat(name, t, dtype, n)
         raise ValueError(f"{name} holds {t.numel()} values of {t.dtype}, strides {t.stride()}; "
-                         f"{n} {dtype} in a row are needed")
+                         f"{n} {_TYPES[dtype]} in a row are needed")
+    return t.data_ptr()
 
 
-def _check_q8(name: str, q, s, rows: int, cols: int):
+def _q8(name: str, q, s, rows: int, cols: int):
+    """The addresses of an 8-bit matrix's bytes and scales (both None: NULL)."""
     if q is None and s is None:
-        return
+        return None, None
     if q is None or s is None:
         raise ValueError(f"{name}: its bytes and its scales come together")
-    if _torch is None:
-        _load_torch()
-    u8, wide = _TYPES["u8"], (cols + 127) // 128  # sizes that the library refuses are refused by the call
-    _check_out(name, q, u8, rows * wide * 128)
-    _check_out(name, s, u8, rows * ((wide + 15) // 16 * 16))
+    wide = (cols + 127) // 128  # sizes that the library refuses are refused by the call
+    return _flat(name, q, "u8", rows * wide * 128), _flat(name, s, "u8", rows * ((wide + 15) // 16 * 16))
 
 
-def _ln_check(xdt: int, wdt: int, cols: int, x, ldx: int, w, b, ldw: int, cu) -> np.ndarray:
+def _ws(ws):
+    if ws is None:
+        return None, 0
+    if not ws.is_contiguous():
+        _check_bytes(ws)
+    return ws.data_ptr(), ws.nbytes
+
+
+def _bounds(cu):
+    """Row bounds of segments: their bytes, the number of segments and of rows."""
     c = _host_cu(cu)
     if c.size < 2:
         raise ValueError("cu needs two bounds at least")
-    _check_rows("x", x, xdt, int(c[-1]), ldx, cols)
-    for name, t in (("w", w), ("b", b)):
-        if t is not None:
-            _check_rows(name, t, wdt, c.size - 1, ldw, cols)
-    return c
+    return c.tobytes(), c.size - 1, int(c[-1])
 
 
 def sphinx_layer_norm(xdt: int, wdt: int, ydt: int, cols: int, eps: float, x, ldx: int, w, b, ldw: int, plus_one, cu,
                       y, ldy: int, stats=None, stream=None):
     """y <- the normalised rows of x, scaled by w (1 + w with plus_one) and shifted by b, a row of each per segment
     (cu: host int sequence of row bounds; w, b: None for ones and zeros).  stats: float32 [rows][2] or None."""
-    c = _ln_check(xdt, wdt, cols, x, ldx, w, b, ldw, cu)
-    _check_rows("y", y, ydt, int(c[-1]), ldy, cols)
-    _check_out("stats", stats, _TYPES[F32], 2 * int(c[-1]))
+    c, nseg, n = _bounds(cu)
+    px, pw = _rows("x", x, xdt, n, ldx, cols), _rows("w", w, wdt, nseg, ldw, cols)
+    pb, py = _rows("b", b, wdt, nseg, ldw, cols), _rows("y", y, ydt, n, ldy, cols)
+    ps = _flat("stats", stats, F32, 2 * n)
     s = _here(stream, x, w, b, y, stats)
-    _check("sphinx_layer_norm", lib().sphinx_layer_norm(
-        xdt, wdt, ydt, cols, eps, _ptr(x), ldx, _ptr(w), _ptr(b), ldw, int(plus_one), c.tobytes(), c.size - 1, _ptr(y),
-        ldy, _ptr(stats), s))
+    _check("sphinx_layer_norm", lib().sphinx_layer_norm(xdt, wdt, ydt, cols, eps, px, ldx, pw, pb, ldw, int(plus_one),
+                                                        c, nseg, py, ldy, ps, s))
 
 
 def sphinx_layer_norm_q8(xdt: int, wdt: int, cols: int, eps: float, x, ldx: int, w, b, ldw: int, plus_one, cu, q, s,
                          stats=None, stream=None):
     """sphinx_layer_norm with its output in 8 bits (q, s as sphinx_q8_bytes(rows, cols) sizes them)."""
-    c = _ln_check(xdt, wdt, cols, x, ldx, w, b, ldw, cu)
-    _check_q8("q", q, s, int(c[-1]), cols)
-    _check_out("stats", stats, _TYPES[F32], 2 * int(c[-1]))
+    c, nseg, n = _bounds(cu)
+    px, pw = _rows("x", x, xdt, n, ldx, cols), _rows("w", w, wdt, nseg, ldw, cols)
+    pb, ps = _rows("b", b, wdt, nseg, ldw, cols), _flat("stats", stats, F32, 2 * n)
+    pq, pqs = _q8("q", q, s, n, cols)
     at = _here(stream, x, w, b, q, s, stats)
-    _check("sphinx_layer_norm_q8", lib().sphinx_layer_norm_q8(
-        xdt, wdt, cols, eps, _ptr(x), ldx, _ptr(w), _ptr(b), ldw, int(plus_one), c.tobytes(), c.size - 1, _ptr(q),
-        _ptr(s), _ptr(stats), at))
+    _check("sphinx_layer_norm_q8", lib().sphinx_layer_norm_q8(xdt, wdt, cols, eps, px, ldx, pw, pb, ldw, int(plus_one),
+                                                              c, nseg, pq, pqs, ps, at))
 
 
 def sphinx_layer_norm_backward_workspace_bytes(cols: int, cu) -> int:
@@ -630,21 +649,15 @@ def sphinx_layer_norm_backward(xdt: int, wdt: int, gdt: int, cols: int, x, ldx: 
                                dy, lddy: int, dx, lddx: int, dw, db, ldg: int, ws, stream=None):
     """dx (None: left out) and, per segment, dw and db (float32; None: left out) from x, the forward call's stats
     and dy."""
-    c = _ln_check(xdt, wdt, cols, x, ldx, w, None, ldw, cu)
-    n = int(c[-1])
-    _check_rows("dy", dy, gdt, n, lddy, cols)
-    _check_out("stats", stats, _TYPES[F32], 2 * n)
-    if dx is not None:
-        _check_rows("dx", dx, gdt, n, lddx, cols)
-    for name, t in (("dw", dw), ("db", db)):
-        if t is not None:
-            _check_rows(name, t, F32, c.size - 1, ldg, cols)
-    if ws is not None:
-        _check_bytes(ws)
+    c, nseg, n = _bounds(cu)
+    px, pw = _rows("x", x, xdt, n, ldx, cols), _rows("w", w, wdt, nseg, ldw, cols)
+    ps, pg = _flat("stats", stats, F32, 2 * n), _rows("dy", dy, gdt, n, lddy, cols)
+    pdx, pdw = _rows("dx", dx, gdt, n, lddx, cols), _rows("dw", dw, F32, nseg, ldg, cols)
+    pdb, (pws, nws) = _rows("db", db, F32, nseg, ldg, cols), _ws(ws)
     s = _here(stream, x, stats, w, dy, dx, dw, db, ws)
     _check("sphinx_layer_norm_backward", lib().sphinx_layer_norm_backward(
-        xdt, wdt, gdt, cols, _ptr(x), ldx, _ptr(stats), _ptr(w), ldw, int(plus_one), c.tobytes(), c.size - 1, _ptr(dy),
-        lddy, _ptr(dx), lddx, _ptr(dw), _ptr(db), ldg, _ptr(ws), 0 if ws is None else ws.nbytes, s))
+        xdt, wdt, gdt, cols, px, ldx, ps, pw, ldw, int(plus_one), c, nseg, pg, lddy, pdx, lddx, pdw, pdb, ldg, pws, nws,
+        s))
 
 
 def sphinx_q8_bytes(rows: int, cols: int):
@@ -665,16 +678,12 @@ def sphinx_q8_quantise_workspace_bytes(rows: int, cols: int) -> int:
 def sphinx_q8_quantise(dtype: int, x, ldx: int, rows: int, cols: int, square, q, s, qt=None, st=None, sums=None,
                        ws=None, stream=None):
     """x [rows][cols] in 8 bits: q and s; transposed, qt and st; and its column sums.  None: left out."""
-    _check_q8("q", q, s, rows, cols)
-    _check_q8("qt", qt, st, cols, rows)
-    _check_rows("x", x, dtype, rows, ldx, cols)
-    _check_out("sums", sums, _TYPES[F32], cols)
-    if ws is not None:
-        _check_bytes(ws)
+    pq, ps = _q8("q", q, s, rows, cols)
+    pqt, pst = _q8("qt", qt, st, cols, rows)
+    px, pm, (pws, nws) = _rows("x", x, dtype, rows, ldx, cols), _flat("sums", sums, F32, cols), _ws(ws)
     at = _here(stream, x, q, s, qt, st, sums, ws)
-    _check("sphinx_q8_quantise", lib().sphinx_q8_quantise(
-        dtype, _ptr(x), ldx, rows, cols, int(square), _ptr(q), _ptr(s), _ptr(qt), _ptr(st), _ptr(sums), _ptr(ws),
-        0 if ws is None else ws.nbytes, at))
+    _check("sphinx_q8_quantise", lib().sphinx_q8_quantise(dtype, px, ldx, rows, cols, int(square), pq, ps, pqt, pst, pm,
+                                                          pws, nws, at))
 
 
 def sphinx_q8_matmul_workspace_bytes(odt: int, M: int, N: int, K: int) -> int:
@@ -687,29 +696,19 @@ def sphinx_q8_matmul_workspace_bytes(odt: int, M: int, N: int, K: int) -> int:
 def sphinx_q8_matmul(odt: int, M: int, N: int, K: int, a, sa, b, sb, bdt: int, bias, epilogue: int, out, ldo: int, ws,
                      stream=None):
     """out [M][N] <- (or with Q8_ADD, +=) A B^T + bias, GELU with Q8_GELU, for 8-bit matrices A [M][K] and B [N][K]."""
-    _check_q8("a", a, sa, M, K)
-    _check_q8("b", b, sb, N, K)
-    if bias is not None:
-        _check_rows("bias", bias, bdt, 1, N, N)
-    _check_rows("out", out, odt, M, ldo, N)
-    if ws is not None:
-        _check_bytes(ws)
+    (pa, psa), (pb, psb) = _q8("a", a, sa, M, K), _q8("b", b, sb, N, K)
+    pbias, po, (pws, nws) = _rows("bias", bias, bdt, 1, N, N), _rows("out", out, odt, M, ldo, N), _ws(ws)
     s = _here(stream, a, sa, b, sb, bias, out, ws)
-    _check("sphinx_q8_matmul", lib().sphinx_q8_matmul(
-        odt, M, N, K, _ptr(a), _ptr(sa), _ptr(b), _ptr(sb), bdt, _ptr(bias), epilogue, _ptr(out), ldo, _ptr(ws),
-        0 if ws is None else ws.nbytes, s))
+    _check("sphinx_q8_matmul", lib().sphinx_q8_matmul(odt, M, N, K, pa, psa, pb, psb, bdt, pbias, epilogue, po, ldo, pws,
+                                                      nws, s))
 
 
 def sphinx_q8_matmul_q8(M: int, N: int, K: int, a, sa, b, sb, bdt: int, bias, epilogue: int, q, s, stream=None):
     """The 8-bit matrix q, s [M][N] <- A B^T + bias (Q8_STORE), or its GELU (Q8_GELU)."""
-    _check_q8("a", a, sa, M, K)
-    _check_q8("b", b, sb, N, K)
-    if bias is not None:
-        _check_rows("bias", bias, bdt, 1, N, N)
-    _check_q8("q", q, s, M, N)
+    (pa, psa), (pb, psb), (pq, ps) = _q8("a", a, sa, M, K), _q8("b", b, sb, N, K), _q8("q", q, s, M, N)
+    pbias = _rows("bias", bias, bdt, 1, N, N)
     at = _here(stream, a, sa, b, sb, bias, q, s)
-    _check("sphinx_q8_matmul_q8", lib().sphinx_q8_matmul_q8(
-        M, N, K, _ptr(a), _ptr(sa), _ptr(b), _ptr(sb), bdt, _ptr(bias), epilogue, _ptr(q), _ptr(s), at))
+    _check("sphinx_q8_matmul_q8", lib().sphinx_q8_matmul_q8(M, N, K, pa, psa, pb, psb, bdt, pbias, epilogue, pq, ps, at))
 
 
 def sphinx_model_q8_bytes(desc: ModelDesc) -> int:

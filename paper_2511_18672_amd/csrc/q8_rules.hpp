@@ -9,8 +9,9 @@
 namespace sphinx {
 
 // Tiles of outputs: 256x256 and 192x256 in eight waves, one per CU; 128x128 and
-// 128x64 (two per CU) and 64x64 (four) in four waves.
-enum Q8Tile { kQ8Tile256, kQ8Tile192, kQ8Tile128, kQ8Tile128x64, kQ8Tile64 };
+// 128x64 (two per CU) and 64x64 (four) in four waves; up to 16 rows by 16
+// columns.
+enum Q8Tile { kQ8Tile256, kQ8Tile192, kQ8Tile128, kQ8Tile128x64, kQ8Tile64, kQ8Few };
 
 // What becomes of the outputs: bf16 or fp32 values, an fp32 residual that they
 // are added to through a gate, or a matrix in 8 bits.
@@ -46,6 +47,7 @@ inline const Q8TileCost& q8_tile_cost(bool f32, int tile) {
 inline Q8Plan plan_q8_matmul(Q8Kind kind, bool gelu, int M, int N, int KB) {
   const bool f32 = kind == kQ8F32, whole_k = kind == kQ8Gated || kind == kQ8Bytes;
   Q8Plan best = {kQ8Tile128, 1};
+  if (!whole_k && M <= 16) return Q8Plan{kQ8Few, 1};
   double us = 1e30;
   for (int t = 0; t < (kind == kQ8Bytes ? 3 : 5); ++t) {
     const Q8TileCost& c = q8_tile_cost(f32, t);
