@@ -499,9 +499,10 @@ sphinx_status sphinx_refine_step_kv8(const sphinx_model_desc* m, const sphinx_re
  *   xh = (x - mean) rstd, y = xh w' + b,   w' = w, or 1 + w with plus_one = 1
  * (the denoiser's modulation: w = scale, b = shift).  w = NULL stands for
  * w' = 1, b = NULL for b = 0.  1 <= cols <= 16384.  Rows of x, y, dy and dx may
- * be strided (row j at element j*ld, ld >= cols) and start at any element;
- * what lies between and behind them is left as it is.  f32 or bf16 each;
- * computed in fp32 and rounded once.  A row with an infinity or a NaN becomes
+ * be strided (row j at element j*ld, ld >= cols), at most 2^30 of them; what lies
+ * between and behind them is left as it is.  f32 or bf16 each; computed in fp32
+ * and rounded once.  y may be x, and dx may be dy, of the same type and stride;
+ * other outputs overlap nothing.  A row with an infinity or a NaN becomes
  * NaN and leaves the others alone (in dw and db: its segment's columns).
  * Nothing is synchronized; the calls may be captured in a graph, and repeat
  * bit for bit.
@@ -552,7 +553,8 @@ sphinx_status sphinx_layer_norm_backward(sphinx_dtype xdt, sphinx_dtype wdt, sph
  * ------------------------------------------------------------------------ */
 #define SPHINX_Q8_BLOCK 128
 
-/* Bytes of q and s.  0 <= cols <= 2^23, 0 <= rows <= 2^30. */
+/* Bytes of q and s.  0 <= cols <= 2^23, 0 <= rows <= 2^28, fewer than 2^24 tiles
+ * of 128 x 128 (of a product's outputs as well). */
 sphinx_status sphinx_q8_bytes(int32_t rows, int32_t cols, size_t* q_bytes, size_t* s_bytes);
 
 /* Quantises x [rows][cols] (dev, f32 or bf16, row j at element j*ldx) into any

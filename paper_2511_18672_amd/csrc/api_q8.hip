@@ -21,6 +21,7 @@ sphinx_status ln_segs(int32_t cols, const int32_t* cu, int32_t nseg, LnSegs* S) 
     if (cu[i + 1] < cu[i]) return SPHINX_E_INVALID;
     S->cu[i + 1] = cu[i + 1];
   }
+  if (cu[nseg] > (1 << 30)) return SPHINX_E_UNSUPPORTED;  // rows are stepped over in 32 bits
   return SPHINX_OK;
 }
 
@@ -39,10 +40,15 @@ sphinx_status ln_check(sphinx_dtype xdt, sphinx_dtype wdt, int32_t cols, const v
 
 sphinx_status q8_size_check(int32_t rows, int32_t cols) {
   if (rows < 0 || cols < 0) return SPHINX_E_INVALID;
-  // blocks are counted in 32 bits, and a tile's rows are addressed with 32-bit byte offsets
+  // a tile's rows are addressed with 32-bit byte offsets, and a launch has less than 2^32 threads (2^24 tiles of
+  // 128 x 128 hold 256 GB)
   const int64_t wide = ((int64_t)cols + 127) / 128, tall = ((int64_t)rows + 127) / 128;
-  if (cols > (1 << 23) || rows > (1 << 30) || wide * tall >= ((int64_t)1 << 31)) return SPHINX_E_UNSUPPORTED;
+  if (cols > (1 << 23) || rows > (1 << 28) || wide * tall >= (1 << 24)) return SPHINX_E_UNSUPPORTED;
   return SPHINX_OK;
+}
+// Outputs of a product, whose columns may be as many as B's rows.
+sphinx_status q8_outputs_check(int32_t M, int32_t N) {
+  return (((int64_t)M + 127) / 128) * (((int64_t)N + 127) / 128) < (1 << 24) ? SPHINX_OK : SPHINX_E_UNSUPPORTED;
 }
 }  // namespace
 
@@ -135,7 +141,7 @@ sphinx_status sphinx_q8_quantise(sphinx_dtype dtype, const void* x, int64_t ldx,
                                  void* ws, size_t ws_bytes, void* stream) {
   if (!valid_dtype(dtype)) return SPHINX_E_UNSUPPORTED;
   sphinx_status r = q8_size_check(rows, cols);
-  if (r == SPHINX_OK) r = q8_size_check(cols, rows);
+  if (r == SPHINX_OK && qt != nullptr) r = q8_size_check(cols, rows);
   if (r != SPHINX_OK) return r;
   if (ldx < cols || (square != 0 && square != 1)) return SPHINX_E_INVALID;
   if (!aligned(x, 16) || !aligned(q, 16) || !aligned(s, 16) || !aligned(qt, 16) || !aligned(st, 16) ||
@@ -159,7 +165,7 @@ sphinx_status sphinx_q8_matmul_workspace_bytes(sphinx_dtype odt, int32_t M, int3
   if (!valid_dtype(odt)) return SPHINX_E_UNSUPPORTED;
   sphinx_status st = q8_size_check(M, K);
   if (st == SPHINX_OK) st = q8_size_check(N, K);
-  if (st == SPHINX_OK) st = q8_size_check(M, N);
+  if (st == SPHINX_OK) st = q8_outputs_check(M, N);
   if (st != SPHINX_OK) return st;
   if (bytes == nullptr) return SPHINX_E_INVALID;
   *bytes = M == 0 || N == 0 ? 0 : q8_matmul_ws_bytes(odt, M, N, K);

@@ -64,14 +64,14 @@ struct Q8Out {
 
 // OUT: bf16, float, or Q8Out for rows in 8 bits (16 lanes hold a block of 128 columns).
 template <typename XT, typename OUT, int LPR, int NI>
-__global__ __launch_bounds__(LnCfg<LPR>::NT) void k_layer_norm(LnArgs a, LnSegs S, OUT* __restrict__ y, int64_t ldy,
+__global__ __launch_bounds__(LnCfg<LPR>::NT) void k_layer_norm(LnArgs a, LnSegs S, OUT* y, int64_t ldy,
                                                                Q8Out qo, float* __restrict__ stats) {
   typedef LnCfg<LPR> C;
   __shared__ float red[2][16];
   const int t = (int)threadIdx.x % LPR, rows = S.cu[S.nseg], cols = a.cols;
-  const int row0 = (int)blockIdx.x * C::ROWS + (int)threadIdx.x / LPR;
+  const int64_t row0 = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * C::ROWS + (int)threadIdx.x / LPR;
   const bool live = row0 < rows;
-  const int row = min(row0, rows - 1);  // lanes past the end repeat the last row and store nothing
+  const int row = live ? (int)row0 : rows - 1;  // lanes past the end repeat the last row and store nothing
   const XT* x = static_cast<const XT*>(a.x) + (int64_t)row * a.ldx;
   // short rows: everything that they need is on its way before the first sum is waited for.  Longer ones would pay for
   // it with waves (3000 x 8192 in bf16 21.3 -> 23.3 us)
@@ -155,17 +155,20 @@ struct Raw8 {
   }
 };
 
-// The next row's loads are issued before this row's arithmetic.  Columns behind
-// the last one hold dy = 0, which adds nothing to a sum over the row.
+// The next row's loads are issued before this row's arithmetic (also where dx
+// is dy: they are other rows).  Columns behind the last one hold dy = 0, which
+// adds nothing to a sum over the row.  The widest rows read their weights from
+// LDS each time, since the registers do not hold them (3000 x 10000 148 -> 74 us).
 template <typename XT, typename GT, int LPR, int NI>
 __global__ __launch_bounds__(LnCfg<LPR>::NT) void k_layer_norm_backward(LnArgs a, LnSegs S, LnChunks P,
                                                                         const float* __restrict__ stats,
-                                                                        const GT* __restrict__ dy, int64_t lddy,
-                                                                        GT* __restrict__ dx, int64_t lddx,
+                                                                        const GT* dy, int64_t lddy,
+                                                                        GT* dx, int64_t lddx,
                                                                         float* __restrict__ part) {
   typedef LnCfg<LPR> C;
   __shared__ float red[4][16];
-  __shared__ float sums[C::ROWS > 1 ? C::NT * NI * 8 : 1];
+  constexpr bool kWeightsInLds = LPR == 512;
+  __shared__ __attribute__((aligned(16))) float sums[C::ROWS > 1 ? C::NT * NI * 8 : kWeightsInLds ? LPR * NI * 8 : 1];
   const int t = (int)threadIdx.x % LPR, grp = (int)threadIdx.x / LPR, cols = a.cols;
   int seg = 0;
   {
@@ -178,7 +181,7 @@ __global__ __launch_bounds__(LnCfg<LPR>::NT) void k_layer_norm_backward(LnArgs a
   }
   const int r0 = S.cu[seg] + ((int)blockIdx.x - P.first[seg]) * P.rows, r1 = min(r0 + P.rows, S.cu[seg + 1]);
   const float one = a.plus_one ? 1.0f : 0.0f;
-  float w[NI][8], sw[NI][8], sb[NI][8];
+  float w[kWeightsInLds ? 1 : NI][8], sw[NI][8], sb[NI][8];
   Raw8<XT> rx[NI];
   Raw8<GT> rg[NI];
   float mean, rstd;
@@ -198,29 +201,34 @@ __global__ __launch_bounds__(LnCfg<LPR>::NT) void k_layer_norm_backward(LnArgs a
 #pragma unroll
   for (int i = 0; i < NI; ++i) {
     const int c = 8 * (i * LPR + t);
-    ln_load_w(a.w, a.w_bf16, seg * a.ldw + c, cols - c, 1.0f - one, w[i]);
+    float (&wi)[8] = w[kWeightsInLds ? 0 : i];
+    ln_load_w(a.w, a.w_bf16, seg * a.ldw + c, cols - c, 1.0f - one, wi);
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      w[i][e] += one;
+      wi[e] += one;
       sw[i][e] = sb[i][e] = 0.0f;
     }
+    if constexpr (kWeightsInLds) __builtin_memcpy(__builtin_assume_aligned(sums + c, 16), wi, 32);  // read by this lane
   }
   for (int row = r0 + grp; row < r1; row += C::ROWS) {
     float xh[NI][8], g[NI][8];
     float s1 = 0.0f, s2 = 0.0f;
     const float r = rstd;
 #pragma unroll
-    for (int i = 0; i < NI; ++i)
+    for (int i = 0; i < NI; ++i) {
+      float (&wi)[8] = w[kWeightsInLds ? 0 : i];
+      if constexpr (kWeightsInLds) __builtin_memcpy(wi, __builtin_assume_aligned(sums + 8 * (i * LPR + t), 16), 32);
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         xh[i][e] = ((float)rx[i].v[e] - mean) * r;
         const float d = (float)rg[i].v[e];
         sw[i][e] = fmaf(d, xh[i][e], sw[i][e]);
         sb[i][e] += d;
-        g[i][e] = d * w[i][e];
+        g[i][e] = d * wi[e];
         s1 += g[i][e];
         s2 = fmaf(g[i][e], xh[i][e], s2);
       }
+    }
     fetch(min(row + C::ROWS, r1 - 1));
     if (dx != nullptr) {
       const int par = LPR > 64 ? 2 * ((row - r0) & 1) : 0;
@@ -345,7 +353,7 @@ hipError_t launch_layer_norm(sphinx_dtype xdt, sphinx_dtype ydt, const LnArgs& a
   by_cols(a.cols, false, [&](auto L, auto N) {
     constexpr int LPR = decltype(L)::value, NI = decltype(N)::value;
     typedef LnCfg<LPR> C;
-    const int grid = (S.cu[S.nseg] + C::ROWS - 1) / C::ROWS;
+    const dim3 grid = long_grid(((int64_t)S.cu[S.nseg] + C::ROWS - 1) / C::ROWS);
     auto go = [&](auto xt, auto* out) {
       typedef decltype(xt) XT;
       typedef std::remove_pointer_t<decltype(out)> OT;

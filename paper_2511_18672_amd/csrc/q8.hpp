@@ -23,6 +23,12 @@ inline int64_t q8_row_bytes(int64_t cols) { return (cols + kQ8Block - 1) / kQ8Bl
 __host__ __device__ inline int q8_scale_row(int blocks) { return (blocks + 15) & ~15; }
 inline int64_t q8_scale_bytes(int64_t cols) { return q8_scale_row((int)((cols + kQ8Block - 1) / kQ8Block)); }
 
+// A grid of n workgroups or more, numbered y * gridDim.x + x: a dimension has less than 2^32 threads.
+inline dim3 long_grid(int64_t n) {
+  const int64_t wide = 1 << 20;
+  return n <= wide ? dim3((unsigned)n) : dim3((unsigned)wide, (unsigned)((n + wide - 1) / wide));
+}
+
 // Rows [cu[i], cu[i+1]) belong to segment i.
 struct LnSegs {
   int nseg;

@@ -14,7 +14,7 @@ constexpr int kNT = 256;
 template <typename T>
 __global__ __launch_bounds__(kNT) void k_q8_rows(const T* __restrict__ x, int64_t ldx, int rows, int cols, int wide,
                                                  uint8_t* __restrict__ q, uint8_t* __restrict__ s) {
-  const int64_t at = (int64_t)blockIdx.x * (kNT / 16) + (threadIdx.x >> 4);  // block of the matrix
+  const int64_t at = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * (kNT / 16) + (threadIdx.x >> 4);  // block of 128
   const int64_t row = at / wide;
   const int t = (int)threadIdx.x & 15, k = (int)(at - row * wide), c = k * kQ8Block + 8 * t;
   float v[8];
@@ -130,7 +130,7 @@ hipError_t launch_q8_quantise(sphinx_dtype dt, const void* x, int64_t ldx, int r
       const T* in = static_cast<const T*>(x);
       if (!square && qt == nullptr && sums == nullptr) {
         const int64_t grid = ((int64_t)rows * wide + kNT / 16 - 1) / (kNT / 16);
-        k_q8_rows<T><<<(unsigned)grid, kNT, 0, stream>>>(in, ldx, rows, cols, wide, q, s);
+        k_q8_rows<T><<<long_grid(grid), kNT, 0, stream>>>(in, ldx, rows, cols, wide, q, s);
       } else if (square) {
         k_q8_tile<T, true><<<(unsigned)(wide * tall), kNT, 0, stream>>>(in, ldx, rows, cols, q, s, qt, st,
                                                                         sums != nullptr ? ws : nullptr);

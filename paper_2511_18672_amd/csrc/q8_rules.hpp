@@ -47,11 +47,12 @@ inline const Q8TileCost& q8_tile_cost(bool f32, int tile) {
 inline Q8Plan plan_q8_matmul(Q8Kind kind, bool gelu, int M, int N, int KB) {
   const bool f32 = kind == kQ8F32, whole_k = kind == kQ8Gated || kind == kQ8Bytes;
   Q8Plan best = {kQ8Tile128, 1};
-  if (!whole_k && M <= 16) return Q8Plan{kQ8Few, 1};
+  if (!whole_k && M <= 16 && N <= (1 << 22)) return Q8Plan{kQ8Few, 1};
   double us = 1e30;
   for (int t = 0; t < (kind == kQ8Bytes ? 3 : 5); ++t) {
     const Q8TileCost& c = q8_tile_cost(f32, t);
     const int64_t tiles = (int64_t)((M + c.rows - 1) / c.rows) * ((N + c.cols - 1) / c.cols);
+    if (tiles >= (1 << 23)) continue;  // more threads than a launch can have
     for (int pieces = 1; pieces <= (whole_k ? 1 : 16); pieces *= 2) {
       const int per = pieces == 1 ? KB : ((KB + pieces - 1) / pieces + 3) / 4 * 4;
       if (pieces > 1 && ((pieces - 1) * per >= KB || per < 8)) break;  // no empty piece

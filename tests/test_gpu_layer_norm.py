@@ -251,3 +251,53 @@ def test_a_stream_of_its_own_and_a_graph():
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(outs, want))
+
+
+@pytest.mark.parametrize("cols", [40, 700, 1100, 3000, 9000])
+@pytest.mark.parametrize("name", ["f32", "bf16"])
+def test_in_place(cols, name):
+    """y in the place of x, dx in the place of dy."""
+    t = with_stats(inputs([50, 0, 33], cols, name, "f32"), name)
+    code = TYPE[name][1]
+    ref = run_backward(t, cols, name, "f32", name, True)
+    ws = torch.empty(B.sphinx_layer_norm_backward_workspace_bytes(cols, t["cu"]), dtype=torch.uint8, device=DEV)
+    dw, db = torch.empty(3, cols, device=DEV), torch.empty(3, cols, device=DEV)
+    B.sphinx_layer_norm_backward(code, B.F32, code, cols, t["x"], cols, t["stats"], t["w"], cols, True, t["cu"], t["g"],
+                                 cols, t["g"], cols, dw, db, cols, ws)
+    assert torch.equal(t["g"], ref["dx"]) and torch.equal(dw, ref["dw"]) and torch.equal(db, ref["db"])
+    y = torch.empty_like(t["x"])
+    args = (code, B.F32, code, cols, 1e-6, t["x"], cols, t["w"], t["b"], cols, False, t["cu"])
+    B.sphinx_layer_norm(*args, y, cols)
+    B.sphinx_layer_norm(*args, t["x"], cols)
+    assert torch.equal(t["x"], y)
+
+
+def test_offsets_past_32_bits():
+    """More than 2^31 elements: the last rows are what they are in a call of their own."""
+    rows, cols, last = 136000, 16384, 300
+    x = torch.empty(rows, cols, dtype=torch.bfloat16, device=DEV)
+    x.normal_(generator=torch.Generator(DEV).manual_seed(1))
+    w = torch.rand(1, cols, device=DEV)
+    y, q = torch.empty_like(x), torch.empty(rows * cols, dtype=torch.uint8, device=DEV)
+    s = torch.empty(rows * cols // 128, dtype=torch.uint8, device=DEV)
+    stats = torch.empty(rows, 2, device=DEV)
+    few = [torch.empty(last, cols, dtype=torch.bfloat16, device=DEV), torch.empty(last, 2, device=DEV),
+           torch.empty(last * cols, dtype=torch.uint8, device=DEV), torch.empty(last * cols // 128, dtype=torch.uint8,
+                                                                                device=DEV)]
+    call = (B.BF16, B.F32, B.BF16, cols, 1e-6)
+    B.sphinx_layer_norm(*call, x, cols, w, None, cols, False, [0, rows], y, cols, stats)
+    B.sphinx_layer_norm_q8(B.BF16, B.F32, cols, 1e-6, x, cols, w, None, cols, False, [0, rows], q, s)
+    end = x[-last:].clone()
+    B.sphinx_layer_norm(*call, end, cols, w, None, cols, False, [0, last], few[0], cols, few[1])
+    B.sphinx_layer_norm_q8(B.BF16, B.F32, cols, 1e-6, end, cols, w, None, cols, False, [0, last], few[2], few[3])
+    assert torch.equal(y[-last:], few[0]) and torch.equal(stats[-last:], few[1])
+    assert torch.equal(q[-last * cols:], few[2]) and torch.equal(s[-last * cols // 128:], few[3])
+    # backward, y as the gradient: two segments, of which the second is the last rows
+    ws = torch.empty(B.sphinx_layer_norm_backward_workspace_bytes(cols, [0, rows - last, rows]), dtype=torch.uint8,
+                     device=DEV)
+    w2, dx = torch.cat([w, w]), torch.empty_like(x)
+    B.sphinx_layer_norm_backward(B.BF16, B.F32, B.BF16, cols, x, cols, stats, w2, cols, False, [0, rows - last, rows], y,
+                                 cols, dx, cols, None, None, cols, ws)
+    B.sphinx_layer_norm_backward(B.BF16, B.F32, B.BF16, cols, end, cols, few[1], w, cols, False, [0, last], few[0], cols,
+                                 few[0], cols, None, None, cols, None)
+    assert torch.equal(dx[-last:], few[0])

@@ -245,6 +245,38 @@ def test_product_repeats_on_streams_and_in_graphs(odt):
             assert torch.equal(got, product(odt, pack(host(x)), b, M, N, K))
 
 
+def test_offsets_past_32_bits():
+    """Matrices of more than 2^32 bytes: their last rows and columns are what they are in a call of their own."""
+    M, K, N, last = 131072 + 700, 33000, 96, 300
+    x = torch.empty(M, K, dtype=torch.bfloat16, device=DEV)
+    x.normal_(generator=torch.Generator(DEV).manual_seed(1))
+    a = empty(M, K, 0)
+    B.sphinx_q8_quantise(B.BF16, x, K, M, K, False, *a)
+    end = x[-last:].contiguous()
+    few = empty(last, K, 0)
+    B.sphinx_q8_quantise(B.BF16, end, K, last, K, False, *few)
+    wide = (K + 127) // 128
+    assert torch.equal(a[0][-last * wide * 128:], few[0])
+    scales = lambda t: t.view(-1, (wide + 15) // 16 * 16)[:, :wide]  # noqa: E731
+    assert torch.equal(scales(a[1])[-last:], scales(few[1]))
+    t, tall = empty(K, M, 0), (M + 127) // 128
+    B.sphinx_q8_quantise(B.BF16, x, K, M, K, False, None, None, *t)
+    del x
+    b = pack(numbers(N, K, 3))
+    # (not to the bit: beside few rows the contraction is cut)
+    c, size = Q.matmul(values(*few, last, K), values(*b, N, K))
+    tol = tolerance("bf16", c, size, K)
+    assert (np.abs(host(product("bf16", a, b, M, N, K)[-last:]) - c) <= tol).all()
+    assert (np.abs(host(product("bf16", b, a, N, M, K)[:, -last:]) - c.T) <= tol.T).all()  # on the other side
+    # the transposed copy's last column is the first one's of the columns reversed
+    v = t[0].view(K, tall * 128)[-1, :M].view(torch.float8_e4m3fn).float()
+    e = torch.exp2(t[1].view(K, -1)[-1, :tall].float() - 127).repeat_interleave(128)[:M]
+    r = a[0].view(M, wide * 128)[:, K - 1].view(torch.float8_e4m3fn).float()
+    f = torch.exp2(scales(a[1])[:, -1].float() - 127)
+    # one number in two groupings: each within half a step (2^-4 of it, or 2^-10 of its unit)
+    assert ((v * e - r * f).abs() <= 2.0 ** -3 * (r * f).abs() * 1.1 + 2.0 ** -9 * torch.maximum(e, f)).all()
+
+
 def test_a_linear_layer_with_its_norm_forward_and_backward():
     """norm -> 8 bits -> product + bias, and back: every gradient against the oracle's, which starts from the values
     that the 8-bit matrices hold."""

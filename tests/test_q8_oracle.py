@@ -84,7 +84,7 @@ def norm(xdt=1, wdt=0, ydt=1, cols=64, eps=1e-6, x=P, ldx=64, w=P, b=P, ldw=64, 
     (dict(cols=16385, ldx=20000, ldw=20000, ldy=20000), UNSUPPORTED), (dict(eps=-1.0), INVALID),
     (dict(eps=float("nan")), INVALID), (dict(x=None), INVALID), (dict(x=P + 8), INVALID), (dict(ldx=63), INVALID),
     (dict(ldw=63), INVALID), (dict(one=2), INVALID), (dict(bounds=(0,)), INVALID), (dict(bounds=(1, 4)), INVALID),
-    (dict(bounds=(0, 4, 3)), INVALID), (dict(bounds=tuple(range(66))), UNSUPPORTED), (dict(y=None), INVALID),
+    (dict(bounds=(0, 4, 3)), INVALID), (dict(bounds=(0, (1 << 30) + 1)), UNSUPPORTED), (dict(bounds=tuple(range(66))), UNSUPPORTED), (dict(y=None), INVALID),
     (dict(y=P + 4), INVALID), (dict(ldy=1), INVALID), (dict(stats=P + 8), INVALID), (dict(w=P + 2), INVALID),
 ])
 def test_norm_refuses(bad, want):
@@ -129,7 +129,8 @@ def quant(dt=1, x=P, ldx=200, rows=100, cols=200, square=0, q=P, s=P, qt=P, st=P
     (dict(rows=-1), INVALID), (dict(cols=-1, ldx=0), INVALID), (dict(square=2), INVALID), (dict(s=None), INVALID),
     (dict(st=None), INVALID), (dict(q=None, qt=None, sums=None), INVALID), (dict(q=P + 8), INVALID),
     (dict(ws=None), INVALID), (dict(ws_bytes=799), WORKSPACE), (dict(ws=P + 16), INVALID),
-    (dict(cols=(1 << 23) + 1, ldx=1 << 24), UNSUPPORTED), (dict(rows=1 << 30, cols=1 << 10, ldx=1 << 10), UNSUPPORTED),
+    (dict(cols=(1 << 23) + 1, ldx=1 << 24), UNSUPPORTED), (dict(rows=1 << 28, cols=1 << 10, ldx=1 << 10), UNSUPPORTED), (dict(rows=(1 << 28) + 1), UNSUPPORTED),
+    (dict(rows=(1 << 23) + 1), UNSUPPORTED),
 ])
 def test_quantise_refuses(bad, want):
     assert quant(**bad) == want
@@ -149,10 +150,51 @@ def product(odt=1, M=5, N=6, K=7, a=P, sa=P, b=P, sb=P, bdt=0, bias=P, epi=0, ou
     (dict(K=(1 << 23) + 1), UNSUPPORTED), (dict(a=None), INVALID), (dict(sb=None), INVALID), (dict(a=P + 8), INVALID),
     (dict(epi=3), INVALID), (dict(epi=-1), INVALID), (dict(out=None), INVALID), (dict(ldo=5), INVALID),
     (dict(out=P + 8), INVALID), (dict(bias=P + 4), INVALID), (dict(ws=P + 64), INVALID),
-    (dict(M=1 << 30, N=1 << 23, ldo=1 << 23), UNSUPPORTED),
+    (dict(M=1 << 28, N=1 << 23, ldo=1 << 23), UNSUPPORTED), (dict(M=(1 << 28) + 1), UNSUPPORTED),
 ])
 def test_matmul_refuses(bad, want):
     assert product(**bad) == want
+
+
+def product8(M=5, N=6, K=7, a=P, sa=P, b=P, sb=P, bdt=0, bias=P, epi=0, q=P, s=P):
+    return status("sphinx_q8_matmul_q8", M, N, K, a, sa, b, sb, bdt, bias, epi, q, s, None)
+
+
+@pytest.mark.parametrize("bad, want", [
+    (dict(bdt=2), UNSUPPORTED), (dict(N=-1), INVALID), (dict(a=None), INVALID), (dict(sb=P + 8), INVALID),
+    (dict(epi=2), INVALID), (dict(q=None), INVALID), (dict(s=None), INVALID), (dict(q=P + 4), INVALID),
+    (dict(bias=P + 2), INVALID), (dict(N=(1 << 23) + 1), UNSUPPORTED), (dict(K=(1 << 23) + 1), UNSUPPORTED),
+])
+def test_matmul_into_8_bits_refuses(bad, want):
+    assert product8(**bad) == want
+
+
+def test_the_8_bit_step_refuses():
+    import workloads as W
+
+    reqs = B.make_requests([W.Request(1, 4, 4)])
+    good = W.ModelCfg(D=128, heads=2, head_dim=64, mlp=256, L=2, dtype="bf16")
+    f32 = W.ModelCfg(D=128, heads=2, head_dim=64, mlp=256, L=2, dtype="f32")
+    with pytest.raises(S.SphinxError):
+        B.sphinx_model_q8_bytes(B.model_desc(f32, P))
+    with pytest.raises(S.SphinxError):
+        B.sphinx_refine_q8_workspace_bytes(B.model_desc(f32, P), reqs, 4)
+    desc = B.model_desc(good, P)
+    # a block: QKV, MLP1 and MLP2, each with a row of 16 scale bytes per row
+    assert B.sphinx_model_q8_bytes(desc) == 2 * ((384 * 128 + 384 * 16) + (256 * 128 + 256 * 16) + (128 * 256 + 128 * 16))
+    plain, more = B.sphinx_refine_workspace_bytes(desc, reqs, 4), B.sphinx_refine_q8_workspace_bytes(desc, reqs, 4)
+    assert more >= plain + 4 * 128 + 4 * 16
+    bounds = np.array([0, 4], np.int32)
+
+    def step(w8=P, w8_bytes=1 << 30, cache=None, kv8=0, ws_bytes=1 << 30, d=desc):
+        import ctypes
+
+        return status("sphinx_refine_step_q8", ctypes.byref(d), w8, w8_bytes, reqs, 1, P, 4, bounds.ctypes.data, P, P, P,
+                      P, cache, kv8, P, ws_bytes, None)
+
+    assert step(w8=None) == INVALID and step(w8=P + 16) == INVALID and step(w8_bytes=100) == WORKSPACE
+    assert step(kv8=1) == INVALID and step(kv8=2) == INVALID and step(ws_bytes=plain) == WORKSPACE
+    assert step(d=B.model_desc(f32, P)) == UNSUPPORTED
 
 
 def test_matmul_of_nothing_is_a_no_op():
@@ -164,7 +206,7 @@ def test_sizes():
     assert B.sphinx_q8_bytes(3, 129) == (3 * 256, 3 * 16)
     assert B.sphinx_q8_bytes(2, 17 * 128 + 1) == (2 * 18 * 128, 2 * 32)
     assert B.sphinx_q8_bytes(0, 5) == (0, 0) and B.sphinx_q8_bytes(5, 0) == (0, 0)
-    for bad in ((-1, 1), (1, -1), (1, (1 << 23) + 1)):
+    for bad in ((-1, 1), (1, -1), (1, (1 << 23) + 1), ((1 << 28) + 1, 1)):
         with pytest.raises(S.SphinxError):
             B.sphinx_q8_bytes(*bad)
     with pytest.raises(ValueError, match="32 bits"):
