@@ -28,24 +28,60 @@ typedef int i32x4 __attribute__((ext_vector_type(4)));
 // s_waitcnt immediate: vmcnt(vm) lgkmcnt(0)
 constexpr int wait_vm(int vm) { return 0x0070 | (vm & 15) | ((vm >> 4) << 14); }
 
-// Bias, scale and GELU of columns n .. n + 7.
-__device__ __forceinline__ void q8_finish(const Q8Epi& e, int n, int N, float (&v)[8]) {
-  if (e.bias != nullptr) {
-    float b[8];
-    if (e.bias_bf16) load8(static_cast<const bf16*>(e.bias) + n, N - n, b);
-    else load8(static_cast<const float*>(e.bias) + n, N - n, b);
-#pragma unroll
-    for (int t = 0; t < 8; ++t) v[t] += b[t];
-  }
-  if (e.epi == Q8_EPI_GELU) {
+// What follows the sums (they start at the bias): nothing, GELU, or the scale of
+// the columns before qcols.  A constant, so that the epilogue has no branches.
+enum { Q8_THEN_NOTHING = 0, Q8_THEN_GELU = 1, Q8_THEN_SCALE = 2 };
+
+template <int THEN>
+__device__ __forceinline__ void q8_finish(const Q8Epi& e, int n, float (&v)[8]) {
+  if constexpr (THEN == Q8_THEN_GELU) {
 #pragma unroll
     for (int t = 0; t < 8; ++t) v[t] = gelu_tanh(v[t]);
   }
-  if (n < e.qcols) {
+  if constexpr (THEN == Q8_THEN_SCALE) {
+    const float qs = n < e.qcols ? e.qscale : 1.0f;
 #pragma unroll
-    for (int t = 0; t < 8; ++t) v[t] *= e.qscale;
+    for (int t = 0; t < 8; ++t) v[t] *= qs;
   }
 }
+
+// Biases of four columns from n0 + 8 k + n on, for each k (zeros without one), as
+// they are in memory until value() is asked for: all loads are on their way
+// before the first is waited for.
+template <int C>
+struct Q8Bias {
+  f32x4 raw[C] = {};
+  bool is_bf16 = false;
+  __device__ __forceinline__ void load(const Q8Epi& e, int n, int N) {
+    if (e.bias == nullptr) return;
+    const bf16* h = static_cast<const bf16*>(e.bias);
+    const float* f = static_cast<const float*>(e.bias);
+    // across the last column: one by one, and the last one's for those behind it, which are not stored
+    const bool whole = __ballot(n + 8 * (C - 1) + 4 <= N) == ~0ull;
+    is_bf16 = e.bias_bf16;
+#pragma unroll
+    for (int k = 0; k < C; ++k) {
+      if (whole) {
+        if (is_bf16) __builtin_memcpy(&raw[k], h + n + 8 * k, 8);
+        else __builtin_memcpy(&raw[k], f + n + 8 * k, 16);
+      } else if (is_bf16) {
+        bf16x4 v;
+#pragma unroll
+        for (int t = 0; t < 4; ++t) v[t] = h[min(n + 8 * k + t, N - 1)];
+        __builtin_memcpy(&raw[k], &v, 8);
+      } else {
+#pragma unroll
+        for (int t = 0; t < 4; ++t) raw[k][t] = f[min(n + 8 * k + t, N - 1)];
+      }
+    }
+  }
+  __device__ __forceinline__ f32x4 value(int k) const {
+    if (!is_bf16) return raw[k];
+    bf16x4 h;
+    __builtin_memcpy(&h, &raw[k], 8);
+    return f32x4{(float)h[0], (float)h[1], (float)h[2], (float)h[3]};
+  }
+};
 
 // Finished columns n .. n + 7 of row m.
 template <typename OT>
@@ -81,7 +117,7 @@ struct Q8Cfg {
 
 // Outputs as a matrix in 8 bits, quantised from fp32: a block of 128 columns is
 // two waves' (TJ = 2), which tell each other their rows' largest magnitudes.
-template <int TI, int TJ, int WN, typename A, typename F>
+template <int TI, int TJ, int WN, int THEN, typename A, typename F>
 __device__ __forceinline__ void q8_rows_in_8_bits(A& acc, F& eight, const Q8Epi& e, unsigned char* smem, int m0, int n0,
                                                   int M, int N, int wave) {
   static_assert(TJ == 2 && WN % 2 == 0, "64 columns a wave");
@@ -102,7 +138,7 @@ __device__ __forceinline__ void q8_rows_in_8_bits(A& acc, F& eight, const Q8Epi&
         float v[8];
         const int n = n0 + 32 * j + 8 * (q + g);
         eight(i, j, q, v);
-        q8_finish(e, n, N, v);
+        q8_finish<THEN>(e, n, v);
 #pragma unroll
         for (int t = 0; t < 8; ++t) {
           v[t] = n + t < N ? v[t] : 0.0f;
@@ -174,7 +210,6 @@ __device__ __forceinline__ void q8_rows_gated(A& acc, F& eight, const Q8Epi& e, 
         for (int q = 0; q < 4; q += 2) {
           float v[8];
           eight(i, j, q, v);
-          q8_finish(e, n0 + 32 * j + 8 * (q + g), N, v);
           __builtin_memcpy(__builtin_assume_aligned(mine + r32 * PITCH + (32 * j + 8 * (q + g)) * 4, 16), v, 32);
         }
 #pragma unroll
@@ -252,7 +287,10 @@ __device__ __forceinline__ void q8_tile(const uint8_t* __restrict__ A, const uin
 #pragma unroll
     for (int h = 0; h < 2; ++h) foff[ks][h] = r32 * 128 + (((4 * ks + 2 * g + h) ^ ((r32 >> 1) & 7)) << 4);
 
-  f32x16 acc[TI][TJ] = {};
+  // transposed blocks: lane l holds row l % 32 and, in registers 4q .. 4q+3, columns 8q + 4 (l / 32) .. + 3.  The sums
+  // start at the bias (of pieces, where they are joined).
+  Q8Bias<4 * TJ> bias;
+  if (part == nullptr) bias.load(e, n0 + b0 + 4 * g, N);
   if (k1 > k0) {
     copy_scales(k0 >> 4);
 #pragma unroll
@@ -267,6 +305,17 @@ __device__ __forceinline__ void q8_tile(const uint8_t* __restrict__ A, const uin
 #pragma unroll
     for (int i = 0; i < TI + TJ; ++i) sc[i] = sn[i];
   }
+  f32x16 acc[TI][TJ];
+#pragma unroll
+  for (int j = 0; j < TJ; ++j)
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const f32x4 v = bias.value(4 * j + q);
+#pragma unroll
+      for (int t = 0; t < 4; ++t)
+#pragma unroll
+        for (int i = 0; i < TI; ++i) acc[i][j][4 * q + t] = v[t];
+    }
   i32x8 fa[2][TI], fb[2][TJ];
   // fragment r of a k-step: the TJ of B first, then the TI of A
   auto read = [&](int slot, int ks, int r) {
@@ -376,8 +425,7 @@ __device__ __forceinline__ void q8_tile(const uint8_t* __restrict__ A, const uin
   // the refills of the last stages must land while the workgroup holds its LDS
   __builtin_amdgcn_s_waitcnt(wait_vm(0));
   asm volatile("" ::: "memory");
-  // transposed blocks: lane l holds row l % 32 and, in registers 4q .. 4q+3, columns 8q + 4 (l / 32) .. + 3; the two
-  // halves of the wave swap so that each lane has eight neighbouring columns, n0 + b0 + 32 j + 8 (q + g)
+  // the two halves of the wave swap so that each lane has eight neighbouring columns, n0 + b0 + 32 j + 8 (q + g)
   auto eight = [&](int i, int j, int q, float (&v)[8]) {
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
@@ -398,9 +446,7 @@ __device__ __forceinline__ void q8_tile(const uint8_t* __restrict__ A, const uin
         for (int q = 0; q < 4; q += 2) {
           float v[8];
           eight(i, j, q, v);
-          const int n = n0 + b0 + 32 * j + 8 * (q + g);
-          q8_finish(e, n, N, v);
-          if (m < M) q8_store8<OT>(e, m, n, N, v);
+          if (m < M) q8_store8<OT>(e, m, n0 + b0 + 32 * j + 8 * (q + g), N, v);
         }
     }
     return;
@@ -416,11 +462,16 @@ __device__ __forceinline__ void q8_tile(const uint8_t* __restrict__ A, const uin
     return;
   }
   if constexpr (KIND == kQ8Bytes) {
-    q8_rows_in_8_bits<TI, TJ, WN>(acc, eight, e, smem, m0 + a0, n0 + b0, M, N, wave);
+    if (e.epi == Q8_EPI_GELU)
+      q8_rows_in_8_bits<TI, TJ, WN, Q8_THEN_GELU>(acc, eight, e, smem, m0 + a0, n0 + b0, M, N, wave);
+    else
+      q8_rows_in_8_bits<TI, TJ, WN, Q8_THEN_NOTHING>(acc, eight, e, smem, m0 + a0, n0 + b0, M, N, wave);
     return;
   }
-  auto rows_out = [&](auto ot, auto* out, int64_t ldo, bool finish) {
-    typedef decltype(ot) ST;
+  auto rows_out = [&](auto* out, int64_t ldo, auto then, auto add) {
+    typedef std::remove_pointer_t<decltype(out)> ST;
+    constexpr int THEN = decltype(then)::value;
+    constexpr bool ADD = decltype(add)::value;
     constexpr int V = 16 / (int)sizeof(ST), PITCH = 32 * TJ * (int)sizeof(ST) + 16;  // values of a piece; bytes of a row
     constexpr int LPW = 32 * TJ / V, RPP = 64 / LPW;                                // lanes of a row; rows of a store
     unsigned char* mine = smem + wave * 32 * PITCH;
@@ -434,7 +485,7 @@ __device__ __forceinline__ void q8_tile(const uint8_t* __restrict__ A, const uin
         for (int q = 0; q < 4; q += 2) {
           float v[8];
           eight(i, j, q, v);
-          if (finish) q8_finish(e, n0 + b0 + 32 * j + 8 * (q + g), N, v);
+          q8_finish<THEN>(e, n0 + b0 + 32 * j, v);  // 32 columns are all before qcols or none
           ST w[8];
 #pragma unroll
           for (int t = 0; t < 8; ++t) w[t] = (ST)v[t];
@@ -449,7 +500,7 @@ __device__ __forceinline__ void q8_tile(const uint8_t* __restrict__ A, const uin
         if (m >= M) continue;
         ST* o = out + m * ldo + n;
         if (left >= V) {
-          if (kWide && finish && e.epi == Q8_EPI_ADD) {
+          if constexpr (ADD) {
             ST old[V];
             __builtin_memcpy(old, o, 16);
 #pragma unroll
@@ -465,13 +516,18 @@ __device__ __forceinline__ void q8_tile(const uint8_t* __restrict__ A, const uin
         } else {
 #pragma unroll
           for (int t = 0; t < V; ++t)
-            if (t < left) o[t] = kWide && finish && e.epi == Q8_EPI_ADD ? (ST)((float)w[t] + (float)o[t]) : w[t];
+            if (t < left) o[t] = ADD ? (ST)((float)w[t] + (float)o[t]) : w[t];
         }
       }
     }
   };
-  if (part != nullptr) rows_out(float{}, part, N, false);
-  else rows_out(OT{}, static_cast<OT*>(e.out), e.ldo, true);
+  typedef std::integral_constant<int, Q8_THEN_NOTHING> Nothing;
+  OT* out = static_cast<OT*>(e.out);
+  if (part != nullptr) rows_out(part, N, Nothing{}, std::false_type{});
+  else if (e.epi == Q8_EPI_GELU) rows_out(out, e.ldo, std::integral_constant<int, Q8_THEN_GELU>{}, std::false_type{});
+  else if (kWide && e.epi == Q8_EPI_ADD) rows_out(out, e.ldo, Nothing{}, std::bool_constant<kWide>{});
+  else if (!kWide && e.qcols > 0) rows_out(out, e.ldo, std::integral_constant<int, Q8_THEN_SCALE>{}, std::false_type{});
+  else rows_out(out, e.ldo, Nothing{}, std::false_type{});
 }
 
 // Tiles are dealt to the XCDs in contiguous ranges of panels four row tiles
@@ -508,7 +564,15 @@ __global__ __launch_bounds__(256) void k_q8_join(const float* __restrict__ part,
 #pragma unroll
     for (int t = 0; t < 8; ++t) v[t] += w[t];
   }
-  q8_finish(e, n, N, v);
+  if (e.bias != nullptr) {
+    float b[8];
+    if (e.bias_bf16) load8(static_cast<const bf16*>(e.bias) + n, N - n, b);
+    else load8(static_cast<const float*>(e.bias) + n, N - n, b);
+#pragma unroll
+    for (int t = 0; t < 8; ++t) v[t] += b[t];
+  }
+  if (e.epi == Q8_EPI_GELU) q8_finish<Q8_THEN_GELU>(e, n, v);
+  else if (e.qcols > 0) q8_finish<Q8_THEN_SCALE>(e, n, v);
   q8_store8<OT>(e, m, n, N, v);
 }
 

@@ -30,27 +30,32 @@ struct Q8TileCost {
   double block, alone;  // a block where every slot, and where one of a CU, has a tile
 };
 
-// Fitted on products of M 64 to 32256, N 64 to 8192 and K 200 to 32256, each in
-// a stream of equal launches: 5 to 11 % rms.
-inline const Q8TileCost& q8_tile_cost(bool f32, int tile) {
-  static const Q8TileCost bf16[] = {{256, 256, 1, 7.3, 3.0, 1.40, 1.38}, {192, 256, 1, 6.9, 2.1, 1.07, 0.89},
-                                    {128, 128, 2, 4.4, 0.7, 0.86, 0.52}, {128, 64, 2, 4.2, 0.2, 0.63, 0.44},
-                                    {64, 64, 4, 4.1, 0.2, 0.80, 0.22}};
-  static const Q8TileCost wide[] = {{256, 256, 1, 1e9, 0, 0, 0},         {192, 256, 1, 8.7, 1.6, 2.01, 1.69},
-                                    {128, 128, 2, 6.1, 1.1, 1.45, 0.75}, {128, 64, 2, 3.9, 0.7, 0.89, 0.52},
-                                    {64, 64, 4, 3.9, 0.5, 1.00, 0.32}};
-  return f32 ? wide[tile] : bf16[tile];
+// Fitted on 24 products (17 where the kind asks for whole blocks of columns) of
+// M 64 to 32256, N 64 to 8192 and K 200 to 32256 with a bias, each in a stream of
+// equal launches: 5 to 15 % rms.  The choice by them costs 1 % on average against
+// the fastest of the tiles, and 15 % at most (fp32, 4800 x 1152 x 1152: 23 us, 20).
+inline const Q8TileCost& q8_tile_cost(Q8Kind kind, int tile) {
+  static const Q8TileCost cost[4][5] = {
+      {{256, 256, 1, 9.1, 2.8, 1.35, 1.09}, {192, 256, 1, 7.7, 2.0, 1.10, 0.87}, {128, 128, 2, 5.5, 0.9, 0.86, 0.50},
+       {128, 64, 2, 4.4, 0.4, 0.67, 0.42}, {64, 64, 4, 4.1, 0.3, 0.84, 0.30}},
+      {{256, 256, 1, 1e9, 0.0, 0.0, 0.0}, {192, 256, 1, 11.1, 1.6, 2.01, 1.61}, {128, 128, 2, 7.8, 1.1, 1.44, 0.71},
+       {128, 64, 2, 5.0, 0.7, 0.89, 0.48}, {64, 64, 4, 4.4, 0.5, 1.06, 0.36}},
+      {{256, 256, 1, 15.5, 2.8, 2.54, 1.10}, {192, 256, 1, 12.6, 2.0, 1.55, 0.89}, {128, 128, 2, 8.0, 0.9, 1.13, 0.55},
+       {128, 64, 2, 4.5, 0.4, 0.74, 0.51}, {64, 64, 4, 3.4, 0.3, 0.94, 0.37}},
+      {{256, 256, 1, 10.4, 2.8, 1.54, 1.14}, {192, 256, 1, 8.8, 2.0, 1.13, 0.93}, {128, 128, 2, 5.0, 0.9, 0.95, 0.57},
+       {}, {}}};
+  return cost[kind][tile];
 }
 
 // Only bf16 and fp32 outputs have a second kernel that joins pieces; outputs in
 // 8 bits need tiles of whole blocks of 128 columns.
 inline Q8Plan plan_q8_matmul(Q8Kind kind, bool gelu, int M, int N, int KB) {
-  const bool f32 = kind == kQ8F32, whole_k = kind == kQ8Gated || kind == kQ8Bytes;
+  const bool whole_k = kind == kQ8Gated || kind == kQ8Bytes;
   Q8Plan best = {kQ8Tile128, 1};
   if (!whole_k && M <= 16 && N <= (1 << 22)) return Q8Plan{kQ8Few, 1};
   double us = 1e30;
   for (int t = 0; t < (kind == kQ8Bytes ? 3 : 5); ++t) {
-    const Q8TileCost& c = q8_tile_cost(f32, t);
+    const Q8TileCost& c = q8_tile_cost(kind, t);
     const int64_t tiles = (int64_t)((M + c.rows - 1) / c.rows) * ((N + c.cols - 1) / c.cols);
     if (tiles >= (1 << 23)) continue;  // more threads than a launch can have
     for (int pieces = 1; pieces <= (whole_k ? 1 : 16); pieces *= 2) {
