@@ -122,23 +122,30 @@ __device__ __forceinline__ float finite_top(const float (&x)[N]) {
   return top;
 }
 
-// Eight values times 2^-e in e4m3, rounded to nearest even; infinities and NaN
-// become NaN.  At the largest scale finite values may lie past 448, where the
+// N values (4 or 8) times 2^-e in e4m3, rounded to nearest even; infinities and
+// NaN become NaN.  At the largest scale finite values may lie past 448, where the
 // hardware would give NaN: they saturate.
-__device__ __forceinline__ uint2 q8_pack8(const float (&x)[8], int sbyte) {
+template <int N>
+__device__ __forceinline__ void q8_pack(const float (&x)[N], int sbyte, uint32_t (&w)[N / 4]) {
   const float inv = two_to(127 - sbyte);
-  float v[8];
+  float v[N];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) v[i] = x[i] * inv;
+  for (int i = 0; i < N; ++i) v[i] = x[i] * inv;
   if (sbyte == 119 + 127) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
+    for (int i = 0; i < N; ++i)
       if (fabsf(v[i]) < __uint_as_float(0x7f800000u)) v[i] = fminf(fmaxf(v[i], -448.0f), 448.0f);
   }
-  int lo = __builtin_amdgcn_cvt_pk_fp8_f32(v[0], v[1], 0, false), hi = __builtin_amdgcn_cvt_pk_fp8_f32(v[4], v[5], 0, false);
-  lo = __builtin_amdgcn_cvt_pk_fp8_f32(v[2], v[3], lo, true);
-  hi = __builtin_amdgcn_cvt_pk_fp8_f32(v[6], v[7], hi, true);
-  return make_uint2((uint32_t)lo, (uint32_t)hi);
+#pragma unroll
+  for (int i = 0; i < N; i += 4) {
+    const int k = __builtin_amdgcn_cvt_pk_fp8_f32(v[i], v[i + 1], 0, false);
+    w[i / 4] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(v[i + 2], v[i + 3], k, true);
+  }
+}
+__device__ __forceinline__ uint2 q8_pack8(const float (&x)[8], int sbyte) {
+  uint32_t w[2];
+  q8_pack(x, sbyte, w);
+  return make_uint2(w[0], w[1]);
 }
 
 // Elements p[0 .. n) as floats, zeros behind them (n may be past 8 or below 1).

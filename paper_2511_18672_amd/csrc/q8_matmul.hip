@@ -1,9 +1,12 @@
 // Product of two matrices in 8 bits with power-of-two scales per block of 128
-// (q8.hpp has the layout): out[M][N] = sum_k A[m][k] B[n][k], + bias, GELU or
-// added to out.  A workgroup computes a tile of 128 x 128 outputs in four waves
-// of 64 x 64; K steps of 128 bytes are copied straight to LDS, two of them in
-// flight.  16-byte chunk c of row r sits at c ^ ((r >> 1) & 7), so that the 16
-// rows of a pass of a 16-byte LDS read fall on all banks.
+// (q8.hpp has the layout): out[M][N] = sum_k A[m][k] B[n][k], + bias, GELU, added
+// to out, or left in 8 bits.  A workgroup computes a tile of 64 x 64 to 256 x 256
+// outputs in four or eight waves (q8_rules.hpp chooses).  K steps of 128 bytes are
+// copied straight to LDS into one of two stages, the next one's while this one is
+// read; a wave's fragments of the next 64 bytes are read between its products, and
+// one barrier a step frees a stage.  16-byte chunk c of row r sits at
+// c ^ ((r >> 1) & 7), so that the 16 rows of a pass of a 16-byte LDS read fall on
+// all banks.
 //
 // bf16 outputs: v_mfma_scale_f32_32x32x64_f8f6f4 on the bytes, the scales in the
 // instruction.  Its sums are fp32, but inside a group of eight products what lies
@@ -12,7 +15,16 @@
 // rounding of a bf16 output.
 // fp32 outputs: the numbers are made bf16 with their scale, which is exact
 // (v_cvt_scalef32_pk_bf16_fp8), and go through v_mfma_f32_32x32x16_bf16, whose
-// products are exact and sums fp32.
+// products are exact and sums fp32 (1e-7).
+//
+// 8192 x 8192 x 8192: 410-418 us, 2630-2690 TFLOP/s (a loop of the instruction on
+// registers alone 3300-3850, by the power that the numbers take); fp32 outputs
+// 850-880 us, 1250-1290 (the same loop of bf16 products 1410 in a library product).
+// Short contractions are bound by what a tile costs besides its steps: 9677 x 4096
+// x 1024 into bf16 takes 56 us in a stream of such calls, of which 40 are left
+// without the epilogue's LDS rounds and stores (62 behind a norm, with GELU, with
+// the matrix cores busy 27 % of them);
+// 32256 x 4608 x 1152 takes 220, of which 58 would be the store alone at 5 TB/s.
 #include <algorithm>
 #include <type_traits>
 

@@ -1,14 +1,23 @@
 // Quantisation in blocks of 128 (q8.hpp has the layout): along the rows, along
 // the columns into a transposed copy, or in squares, in one pass over x, with
 // the column sums on the way.  A tile of 128 x 128 values sits in the registers
-// of a workgroup, eight rows of eight columns each thread; the transposed bytes
-// go through LDS.  Bound by HBM.
+// of a workgroup, four rows of eight columns each thread; the transposed bytes
+// go through LDS.  Bound by HBM: rows alone 5.4-5.8 TB/s (32256 x 4096 in bf16
+// 71-73 us); 9677 x 4096 in bf16 both ways 32.7 us, the transposed copy alone 25.0
+// (4.9 and 4.8 TB/s; the columns' magnitudes have to be known before the first
+// byte of a tile leaves it, so a tile's loads and stores overlap only with those
+// of the other workgroups of its CU).
 #include "q8.hpp"
 
 namespace sphinx {
 
 namespace {
 constexpr int kNT = 256;
+// Rows of eight columns that a thread of a tile holds, and a tile's threads.  With
+// eight rows the chain of a thread's work shows where there are few tiles: 1333 x
+// 1152 in bf16 both ways 8.5 us, 6.2 with four (7.4 with two), 9677 x 4096 34.2 and
+// 32.7 (45.5).
+constexpr int kTileR = 4, kTileNT = kQ8Block * kQ8Block / (8 * kTileR);
 
 // The rows of a matrix alone: 16 lanes hold a block of 128 columns.
 template <typename T>
@@ -27,26 +36,29 @@ __global__ __launch_bounds__(kNT) void k_q8_rows(const T* __restrict__ x, int64_
 
 // Place of 16-byte chunk b of row r in the transposed tile: neighbouring columns
 // of a thread's eight and the sixteen threads of a row fall on all banks, when
-// they are written (8 bytes a lane, rows 8 apart) and when they are read (whole
+// they are written (4 bytes a lane, rows 8 apart) and when they are read (whole
 // rows).
 __device__ __forceinline__ int tr_at(int r, int b) { return (r + (r >> 6)) * kQ8Block + ((b ^ (r >> 3 & 7)) << 4); }
 
 template <typename T, bool SQUARE>
-__global__ __launch_bounds__(kNT) void k_q8_tile(const T* __restrict__ x, int64_t ldx, int rows, int cols,
+__global__ __launch_bounds__(kTileNT) void k_q8_tile(const T* __restrict__ x, int64_t ldx, int rows, int cols,
                                                  uint8_t* __restrict__ q, uint8_t* __restrict__ s,
                                                  uint8_t* __restrict__ qt, uint8_t* __restrict__ st,
                                                  float* __restrict__ part) {
-  __shared__ __attribute__((aligned(16))) float red[2][4][kQ8Block];  // sums, magnitudes: of a wave's 32 rows
+  constexpr int R = kTileR, W = kTileNT / 64;
+  __shared__ __attribute__((aligned(16))) float red[2][W][kQ8Block];  // sums, magnitudes: of a wave's 4 R rows
   __shared__ __attribute__((aligned(16))) unsigned char tr[(kQ8Block + 1) * kQ8Block];
-  const int t = (int)threadIdx.x & 15, g = (int)threadIdx.x >> 4;  // columns 8 t .. + 7, rows 8 g .. + 7 of the tile
+  const int t = (int)threadIdx.x & 15, g = (int)threadIdx.x >> 4;  // columns 8 t .. + 7, rows R g .. + R - 1 of the tile
   const int wave = (int)threadIdx.x >> 6;
   const int wide = (cols + kQ8Block - 1) / kQ8Block, tall = (rows + kQ8Block - 1) / kQ8Block;
-  const int tm = (int)blockIdx.x / wide, tn = (int)blockIdx.x % wide;
+  const int at = (int)(blockIdx.y * gridDim.x + blockIdx.x);  // of less than 2^24 tiles
+  if (at >= wide * tall) return;
+  const int tm = at / wide, tn = at % wide;
   const int m0 = tm * kQ8Block, c = tn * kQ8Block + 8 * t;
-  float v[8][8];
+  float v[R][8];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const int m = m0 + 8 * g + i;
+  for (int i = 0; i < R; ++i) {
+    const int m = m0 + R * g + i;
     load8(x + (int64_t)min(m, rows - 1) * ldx + c, m < rows ? cols - c : 0, v[i]);
   }
   // columns: their sums and largest magnitudes over the wave's rows
@@ -56,7 +68,7 @@ __global__ __launch_bounds__(kNT) void k_q8_tile(const T* __restrict__ x, int64_
     for (int e = 0; e < 8; ++e) {
       sum[e] = v[0][e];
 #pragma unroll
-      for (int i = 1; i < 8; ++i) sum[e] += v[i][e];
+      for (int i = 1; i < R; ++i) sum[e] += v[i][e];
       sum[e] = rows4_sum(sum[e]);
     }
     if ((g & 3) == 0) __builtin_memcpy(__builtin_assume_aligned(&red[0][wave][8 * t], 16), sum, 32);
@@ -65,7 +77,9 @@ __global__ __launch_bounds__(kNT) void k_q8_tile(const T* __restrict__ x, int64_
     float top[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      const float col[8] = {v[0][e], v[1][e], v[2][e], v[3][e], v[4][e], v[5][e], v[6][e], v[7][e]};
+      float col[R];
+#pragma unroll
+      for (int i = 0; i < R; ++i) col[i] = v[i][e];
       top[e] = rows4_max(finite_top(col));
     }
     if ((g & 3) == 0) __builtin_memcpy(__builtin_assume_aligned(&red[1][wave][8 * t], 16), top, 32);
@@ -73,13 +87,16 @@ __global__ __launch_bounds__(kNT) void k_q8_tile(const T* __restrict__ x, int64_
   __syncthreads();
   if (part != nullptr && (int)threadIdx.x < kQ8Block && tn * kQ8Block + (int)threadIdx.x < cols) {
     const int k = (int)threadIdx.x;
-    part[(int64_t)tm * cols + tn * kQ8Block + k] = (red[0][0][k] + red[0][1][k]) + (red[0][2][k] + red[0][3][k]);
+    float sum = red[0][0][k] + red[0][1][k];
+#pragma unroll
+    for (int w = 2; w < W; w += 2) sum += red[0][w][k] + red[0][w + 1][k];
+    part[(int64_t)tm * cols + tn * kQ8Block + k] = sum;
   }
   int sb[8];  // scales of the thread's columns
   if (SQUARE || qt != nullptr) {
     float top[8] = {};
 #pragma unroll
-    for (int w = 0; w < 4; ++w)
+    for (int w = 0; w < W; ++w)
 #pragma unroll
       for (int e = 0; e < 8; ++e) top[e] = fmaxf(top[e], red[1][w][8 * t + e]);
     if constexpr (SQUARE) {
@@ -93,9 +110,9 @@ __global__ __launch_bounds__(kNT) void k_q8_tile(const T* __restrict__ x, int64_
   }
   if (q != nullptr) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
+    for (int i = 0; i < R; ++i) {
       const int rb = SQUARE ? sb[0] : q8_scale_byte(row_max(finite_top(v[i])));
-      const int64_t m = m0 + 8 * g + i;
+      const int64_t m = m0 + R * g + i;
       if (m < rows) {
         *reinterpret_cast<uint2*>(q + m * wide * kQ8Block + c) = q8_pack8(v[i], rb);
         if (t == 0) s[m * q8_scale_row(wide) + tn] = (uint8_t)rb;
@@ -105,14 +122,18 @@ __global__ __launch_bounds__(kNT) void k_q8_tile(const T* __restrict__ x, int64_
   if (qt == nullptr) return;
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
-    const float col[8] = {v[0][e], v[1][e], v[2][e], v[3][e], v[4][e], v[5][e], v[6][e], v[7][e]};
-    *reinterpret_cast<uint2*>(tr + tr_at(8 * t + e, g >> 1) + 8 * (g & 1)) = q8_pack8(col, sb[e]);
+    float col[R];
+    uint32_t w[1];
+#pragma unroll
+    for (int i = 0; i < R; ++i) col[i] = v[i][e];
+    q8_pack(col, sb[e], w);
+    *reinterpret_cast<uint32_t*>(tr + tr_at(8 * t + e, g >> 2) + 4 * (g & 3)) = w[0];
     if (g == 0 && c + e < cols) st[(int64_t)(c + e) * q8_scale_row(tall) + tm] = (uint8_t)sb[e];
   }
   __syncthreads();
 #pragma unroll
-  for (int p = 0; p < 4; ++p) {
-    const int r = p * 32 + ((int)threadIdx.x >> 3), b = (int)threadIdx.x & 7;
+  for (int p = 0; p < R / 2; ++p) {
+    const int r = p * (kTileNT / 8) + ((int)threadIdx.x >> 3), b = (int)threadIdx.x & 7;
     const int64_t n = (int64_t)tn * kQ8Block + r;
     if (n < cols)
       *reinterpret_cast<uint4*>(qt + n * tall * kQ8Block + m0 + 16 * b) =
@@ -128,15 +149,15 @@ hipError_t launch_q8_quantise(sphinx_dtype dt, const void* x, int64_t ldx, int r
     auto go = [&](auto t) {
       typedef decltype(t) T;
       const T* in = static_cast<const T*>(x);
+      const dim3 tiles = long_grid((int64_t)wide * tall);
+      float* part = sums != nullptr ? ws : nullptr;
       if (!square && qt == nullptr && sums == nullptr) {
         const int64_t grid = ((int64_t)rows * wide + kNT / 16 - 1) / (kNT / 16);
         k_q8_rows<T><<<long_grid(grid), kNT, 0, stream>>>(in, ldx, rows, cols, wide, q, s);
       } else if (square) {
-        k_q8_tile<T, true><<<(unsigned)(wide * tall), kNT, 0, stream>>>(in, ldx, rows, cols, q, s, qt, st,
-                                                                        sums != nullptr ? ws : nullptr);
+        k_q8_tile<T, true><<<tiles, kTileNT, 0, stream>>>(in, ldx, rows, cols, q, s, qt, st, part);
       } else {
-        k_q8_tile<T, false><<<(unsigned)(wide * tall), kNT, 0, stream>>>(in, ldx, rows, cols, q, s, qt, st,
-                                                                         sums != nullptr ? ws : nullptr);
+        k_q8_tile<T, false><<<tiles, kTileNT, 0, stream>>>(in, ldx, rows, cols, q, s, qt, st, part);
       }
     };
     if (dt == SPHINX_BF16) go(bf16{});
