@@ -144,6 +144,13 @@ struct LnChunks {
   int first[SPHINX_MAX_REQUESTS + 1];   // chunks of the segments before
 };
 
+struct LnSums {
+  float* dw;  // rows of weight and bias gradients per segment, at ld; either may be NULL
+  float* db;
+  int64_t ld;
+  int blocks;  // workgroups that sum columns
+};
+
 // Eight elements as they are in memory, zeros behind n.
 template <typename T>
 struct Raw8 {
@@ -158,31 +165,107 @@ struct Raw8 {
   }
 };
 
+// Sums over all rows of a segment for 32 of its columns, from the statistics of
+// the forward pass alone: 4 lanes of eight columns, 64 slices of the rows, eight
+// rows in flight, joined in a fixed order.  buf: 8 floats a thread.  At least 32
+// columns: the last ones' workgroup overlaps the one before, so that all loads are
+// whole.
+template <typename XT, typename GT>
+__device__ __forceinline__ void ln_column_sums(const LnArgs& a, int r0, int r1, int c0,
+                                               const float* __restrict__ stats, const GT* dy, int64_t lddy,
+                                               float* dw, float* db, float* buf) {
+  constexpr int NT = 256, U = 8;
+  const int first = c0;
+  c0 = min(c0, a.cols - 32);
+  const int c = c0 + 8 * ((int)threadIdx.x & 3), slice = (int)threadIdx.x >> 2;
+  const XT* x = static_cast<const XT*>(a.x) + c;
+  float sum[2][8] = {};
+  for (int row = r0 + slice; row < r1; row += NT / 4 * U) {
+    Raw8<XT> rx[U];
+    Raw8<GT> rg[U];
+    float2 st[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int64_t at = min(row + NT / 4 * u, r1 - 1);
+      st[u] = *reinterpret_cast<const float2*>(stats + 2 * at);
+      rx[u].load(x + at * a.ldx, 8);
+      rg[u].load(dy + at * lddy + c, 8);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (row + NT / 4 * u < r1) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const float d = (float)rg[u].v[e];
+          sum[0][e] = fmaf(d, ((float)rx[u].v[e] - st[u].x) * st[u].y, sum[0][e]);
+          sum[1][e] += d;
+        }
+      }
+    }
+  }
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    float* out = k == 0 ? dw : db;
+    if (out == nullptr) continue;
+    // 64 slices of 32 columns, then 8 of them
+    __builtin_memcpy(__builtin_assume_aligned(buf + 8 * (int)threadIdx.x, 16), sum[k], 32);
+    __syncthreads();
+    float v = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v += buf[32 * (8 * ((int)threadIdx.x >> 5) + i) + ((int)threadIdx.x & 31)];
+    __syncthreads();
+    buf[threadIdx.x] = v;
+    __syncthreads();
+    const int col = c0 + (int)threadIdx.x;
+    if ((int)threadIdx.x < 32 && col >= first) {
+      v = 0.0f;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v += buf[32 * i + (int)threadIdx.x];
+      out[col] = v;
+    }
+    __syncthreads();
+  }
+}
+
 // The next row's loads are issued before this row's arithmetic (also where dx
 // is dy: they are other rows).  Columns behind the last one hold dy = 0, which
 // adds nothing to a sum over the row.  The widest rows read their weights from
 // LDS each time, since the registers do not hold them (3000 x 10000 148 -> 74 us).
-template <typename XT, typename GT, int LPR, int NI>
+// ONE: the first to.blocks workgroups sum columns into to.dw and to.db, and the
+// others, a chunk each, leave the sums alone (part is not used).
+template <typename XT, typename GT, int LPR, int NI, bool ONE>
 __global__ __launch_bounds__(LnCfg<LPR>::NT) void k_layer_norm_backward(LnArgs a, LnSegs S, LnChunks P,
                                                                         const float* __restrict__ stats,
                                                                         const GT* dy, int64_t lddy,
                                                                         GT* dx, int64_t lddx,
-                                                                        float* __restrict__ part) {
+                                                                        float* __restrict__ part, LnSums to) {
   typedef LnCfg<LPR> C;
   __shared__ float red[4][16];
   constexpr bool kWeightsInLds = LPR == 512;
   __shared__ __attribute__((aligned(16))) float sums[C::ROWS > 1 ? C::NT * NI * 8 : kWeightsInLds ? LPR * NI * 8 : 1];
   const int t = (int)threadIdx.x % LPR, grp = (int)threadIdx.x / LPR, cols = a.cols;
+  int chunk = (int)blockIdx.x;
+  if constexpr (ONE) {
+    static_assert(C::NT == 256 && C::ROWS > 1, "sums hold eight floats of 256 threads");
+    if (chunk < to.blocks) {
+      const int groups = (cols + 31) / 32, of = chunk / groups;
+      ln_column_sums<XT, GT>(a, S.cu[of], S.cu[of + 1], 32 * (chunk - of * groups), stats, dy, lddy,
+                             to.dw == nullptr ? nullptr : to.dw + of * to.ld,
+                             to.db == nullptr ? nullptr : to.db + of * to.ld, sums);
+      return;
+    }
+    chunk -= to.blocks;
+  }
   int seg = 0;
   {
     int lo = 0, hi = S.nseg - 1;
     while (lo < hi) {
       const int mid = (lo + hi + 1) >> 1;
-      if (P.first[mid] <= (int)blockIdx.x) lo = mid; else hi = mid - 1;
+      if (P.first[mid] <= chunk) lo = mid; else hi = mid - 1;
     }
     seg = lo;
   }
-  const int r0 = S.cu[seg] + ((int)blockIdx.x - P.first[seg]) * P.rows, r1 = min(r0 + P.rows, S.cu[seg + 1]);
+  const int r0 = S.cu[seg] + (chunk - P.first[seg]) * P.rows, r1 = min(r0 + P.rows, S.cu[seg + 1]);
   const float one = a.plus_one ? 1.0f : 0.0f;
   float w[kWeightsInLds ? 1 : NI][8], sw[NI][8], sb[NI][8];
   Raw8<XT> rx[NI];
@@ -225,8 +308,10 @@ __global__ __launch_bounds__(LnCfg<LPR>::NT) void k_layer_norm_backward(LnArgs a
       for (int e = 0; e < 8; ++e) {
         xh[i][e] = ((float)rx[i].v[e] - mean) * r;
         const float d = (float)rg[i].v[e];
-        sw[i][e] = fmaf(d, xh[i][e], sw[i][e]);
-        sb[i][e] += d;
+        if constexpr (!ONE) {
+          sw[i][e] = fmaf(d, xh[i][e], sw[i][e]);
+          sb[i][e] += d;
+        }
         g[i][e] = d * wi[e];
         s1 += g[i][e];
         s2 = fmaf(g[i][e], xh[i][e], s2);
@@ -247,7 +332,7 @@ __global__ __launch_bounds__(LnCfg<LPR>::NT) void k_layer_norm_backward(LnArgs a
       }
     }
   }
-  if (part == nullptr) return;
+  if (ONE || part == nullptr) return;
   float* out = part + (int64_t)blockIdx.x * 2 * cols;
 #pragma unroll
   for (int k = 0; k < 2; ++k) {
@@ -383,14 +468,55 @@ hipError_t launch_layer_norm_backward(sphinx_dtype xdt, sphinx_dtype gdt, const 
   const LnChunks P = ln_chunks(a.cols, S);
   const int grid = P.first[S.nseg];
   float* part = dw != nullptr || db != nullptr ? ws : nullptr;
+  // Small calls sum the columns beside the rows, in workgroups of their own that read x and dy again, instead of
+  // joining chunks in a second launch: 1000 x 1024 in bf16 11.7 -> 8.6 us a call (12.3 -> 9.2 where x and dy come from
+  // HBM), 2048 x 1024 in eight segments 11.4 -> 8.4 (11.9 -> 8.5).  A workgroup's share is a segment's rows (1500 x 333
+  // in fp32 from HBM 12.6 -> 13.6, 2000 x 1024 from the caches 14.0 -> 15.4), and the second reading has to find them in
+  // the caches (4000 x 1024 in bf16 in four segments, 16.4 MB, 11.4 -> 12.3).
+  const int64_t rows = S.cu[S.nseg];
+  int longest = 0;
+  for (int i = 0; i < S.nseg; ++i) longest = std::max(longest, S.cu[i + 1] - S.cu[i]);
+  const int xb = xdt == SPHINX_BF16 ? 2 : 4, gb = gdt == SPHINX_BF16 ? 2 : 4;
+  if ((dw != nullptr || db != nullptr) && a.cols >= 32 && a.cols <= 1536 && longest <= 1024 &&
+      rows * a.cols * (xb + gb) <= (12 << 20)) {
+    // rows that dx overlaps are summed before it is written
+    auto apart = [&](const void* p, int64_t ld, int bytes) {
+      auto end = [&](const void* q, int64_t l, int b) { return (uintptr_t)q + ((rows - 1) * l + a.cols) * b; };
+      return dx == nullptr || rows == 0 || end(p, ld, bytes) <= (uintptr_t)dx || end(dx, lddx, gb) <= (uintptr_t)p;
+    };
+    const bool one = apart(a.x, a.ldx, xb) && apart(dy, lddy, gb);
+    by_cols(a.cols, true, [&](auto L, auto N) {
+      constexpr int LPR = decltype(L)::value, NI = decltype(N)::value;
+      if constexpr (LPR <= 64 && NI <= 3) {
+        auto go = [&](auto xt, auto gt) {
+          typedef decltype(xt) XT;
+          typedef decltype(gt) GT;
+          auto launch = [&](int blocks, int chunks) {
+            k_layer_norm_backward<XT, GT, LPR, NI, true><<<(unsigned)(blocks + chunks), LnCfg<LPR>::NT, 0, st>>>(
+                a, S, P, stats, (const GT*)dy, lddy, (GT*)dx, lddx, nullptr, LnSums{dw, db, ldg, blocks});
+          };
+          const int blocks = (a.cols + 31) / 32 * S.nseg, chunks = dx != nullptr ? grid : 0;
+          launch(blocks, one ? chunks : 0);
+          if (!one && chunks > 0) launch(0, chunks);
+        };
+        auto by_g = [&](auto xt) {
+          if (gdt == SPHINX_BF16) go(xt, bf16{});
+          else go(xt, float{});
+        };
+        if (xdt == SPHINX_BF16) by_g(bf16{});
+        else by_g(float{});
+      }
+    });
+    return hipGetLastError();
+  }
   if (grid > 0) {
     by_cols(a.cols, true, [&](auto L, auto N) {
       constexpr int LPR = decltype(L)::value, NI = decltype(N)::value;
       auto go = [&](auto xt, auto gt) {
         typedef decltype(xt) XT;
         typedef decltype(gt) GT;
-        k_layer_norm_backward<XT, GT, LPR, NI><<<grid, LnCfg<LPR>::NT, 0, st>>>(
-            a, S, P, stats, (const GT*)dy, lddy, (GT*)dx, lddx, part);
+        k_layer_norm_backward<XT, GT, LPR, NI, false><<<grid, LnCfg<LPR>::NT, 0, st>>>(
+            a, S, P, stats, (const GT*)dy, lddy, (GT*)dx, lddx, part, LnSums{});
       };
       auto by_g = [&](auto xt) {
         if (gdt == SPHINX_BF16) go(xt, bf16{});

@@ -181,6 +181,24 @@ def test_backward(lens, cols, x, w, g):
     check_backward(t, cols, g, plus_one, run_backward(t, cols, x, w, g, plus_one, ld=3))
 
 
+# around the limits of the calls whose columns are summed beside the rows: 32 to 1536 columns, 1024 rows of a segment,
+# 12 MB of x and dy
+@pytest.mark.parametrize("lens, cols", [([70], 31), ([70], 32), ([1024], 33), ([1025], 33), ([700, 0, 1024, 1], 32),
+                                        ([1600], 100), ([1600, 3], 500), ([1700], 1000), ([1600], 1200), ([64], 1536),
+                                        ([9] * 64, 95), ([1000, 0, 1000, 1000], 1200)])
+@pytest.mark.parametrize("x, w, g", [("f32", "bf16", "f32"), ("bf16", "f32", "bf16")])
+def test_backward_of_calls_small_and_not(lens, cols, x, w, g):
+    t = with_stats(inputs(lens, cols, x, w), g)
+    out = run_backward(t, cols, x, w, g, True, ld=5)
+    check_backward(t, cols, g, True, out)
+    # dx in the place of dy takes the sums from what dy held
+    ws = torch.empty(B.sphinx_layer_norm_backward_workspace_bytes(cols, t["cu"]), dtype=torch.uint8, device=DEV)
+    dw = torch.empty(len(lens), cols, device=DEV)
+    B.sphinx_layer_norm_backward(TYPE[x][1], TYPE[w][1], TYPE[g][1], cols, t["x"], cols, t["stats"], t["w"], cols, True,
+                                 t["cu"], t["g"], cols, t["g"], cols, dw, None, cols, ws)
+    assert torch.equal(t["g"], out["dx"]) and torch.equal(dw, out["dw"][:, :cols])
+
+
 def test_backward_outputs_left_out_and_calls_repeated():
     t = with_stats(inputs([700, 0, 41], 520, "bf16", "f32"), "bf16")
     full = run_backward(t, 520, "bf16", "f32", "bf16", True)
