@@ -150,7 +150,7 @@ hipError_t launch_q8_quantise(sphinx_dtype dt, const void* x, int64_t ldx, int r
       typedef decltype(t) T;
       const T* in = static_cast<const T*>(x);
       const dim3 tiles = long_grid((int64_t)wide * tall);
-      float* part = sums != nullptr ? ws : nullptr;
+      float* part = sums != nullptr && tall > 1 ? ws : sums;  // one tile's sums are the sums
       if (!square && qt == nullptr && sums == nullptr) {
         const int64_t grid = ((int64_t)rows * wide + kNT / 16 - 1) / (kNT / 16);
         k_q8_rows<T><<<long_grid(grid), kNT, 0, stream>>>(in, ldx, rows, cols, wide, q, s);
@@ -165,7 +165,7 @@ hipError_t launch_q8_quantise(sphinx_dtype dt, const void* x, int64_t ldx, int r
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
-  if (sums == nullptr) return hipSuccess;
+  if (sums == nullptr || tall == 1) return hipSuccess;
   PartBounds P;
   P.nseg = 1;
   P.first[0] = 0;
