@@ -207,23 +207,9 @@ __device__ __forceinline__ void ln_column_sums(const LnArgs& a, int r0, int r1, 
   for (int k = 0; k < 2; ++k) {
     float* out = k == 0 ? dw : db;
     if (out == nullptr) continue;
-    // 64 slices of 32 columns, then 8 of them
-    __builtin_memcpy(__builtin_assume_aligned(buf + 8 * (int)threadIdx.x, 16), sum[k], 32);
-    __syncthreads();
-    float v = 0.0f;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v += buf[32 * (8 * ((int)threadIdx.x >> 5) + i) + ((int)threadIdx.x & 31)];
-    __syncthreads();
-    buf[threadIdx.x] = v;
-    __syncthreads();
+    const float v = join_slices<NT>(sum[k], buf);
     const int col = c0 + (int)threadIdx.x;
-    if ((int)threadIdx.x < 32 && col >= first) {
-      v = 0.0f;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) v += buf[32 * i + (int)threadIdx.x];
-      out[col] = v;
-    }
-    __syncthreads();
+    if ((int)threadIdx.x < 32 && col >= first) out[col] = v;
   }
 }
 

@@ -220,4 +220,25 @@ __device__ __forceinline__ float rows4_max(float v) {
   return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
 }
 
+// Sums over slices of rows: thread t of NT holds columns 8 (t % 4) .. + 7 of slice t / 4; the first 32 threads get the
+// column of their number, added in a fixed order.  buf: 8 floats a thread.
+template <int NT>
+__device__ __forceinline__ float join_slices(const float (&sum)[8], float* buf) {
+  const int t = (int)threadIdx.x;
+  __syncthreads();
+  __builtin_memcpy(__builtin_assume_aligned(buf + 8 * t, 16), sum, 32);
+  __syncthreads();
+  float v = 0.0f;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) v += buf[32 * (8 * (t >> 5) + i) + (t & 31)];
+  __syncthreads();
+  buf[t] = v;
+  __syncthreads();
+  v = 0.0f;
+  if (t < 32)
+#pragma unroll
+    for (int i = 0; i < NT / 32; ++i) v += buf[32 * i + t];
+  return v;
+}
+
 }  // namespace sphinx

@@ -40,18 +40,52 @@ __global__ __launch_bounds__(kNT) void k_q8_rows(const T* __restrict__ x, int64_
 // rows).
 __device__ __forceinline__ int tr_at(int r, int b) { return (r + (r >> 6)) * kQ8Block + ((b ^ (r >> 3 & 7)) << 4); }
 
+// Sums over all rows for 32 of the columns, eight rows in flight.  The last ones'
+// workgroup overlaps the one before, so that all loads are whole.
+template <typename T>
+__device__ __forceinline__ void q8_column_sums(const T* __restrict__ x, int64_t ldx, int rows, int cols, int first,
+                                               float* __restrict__ sums, float* buf) {
+  constexpr int U = 8, S = kTileNT / 4;
+  const int c0 = min(first, cols - 32);
+  const T* p = x + c0 + 8 * ((int)threadIdx.x & 3);
+  float sum[8] = {};
+  for (int row = (int)threadIdx.x >> 2; row < rows; row += S * U) {
+    float v[U][8];
+#pragma unroll
+    for (int u = 0; u < U; ++u) load8(p + (int64_t)min(row + S * u, rows - 1) * ldx, 8, v[u]);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (row + S * u < rows) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sum[e] += v[u][e];
+      }
+    }
+  }
+  const float v = join_slices<kTileNT>(sum, buf);
+  const int col = c0 + (int)threadIdx.x;
+  if ((int)threadIdx.x < 32 && col >= first) sums[col] = v;
+}
+
+// The first sum_blocks workgroups sum 32 columns each into sums; the others have a
+// tile each, and leave its columns' sums in part, if it is given.
 template <typename T, bool SQUARE>
 __global__ __launch_bounds__(kTileNT) void k_q8_tile(const T* __restrict__ x, int64_t ldx, int rows, int cols,
                                                  uint8_t* __restrict__ q, uint8_t* __restrict__ s,
                                                  uint8_t* __restrict__ qt, uint8_t* __restrict__ st,
-                                                 float* __restrict__ part) {
+                                                 float* __restrict__ part, float* __restrict__ sums,
+                                                 int sum_blocks) {
   constexpr int R = kTileR, W = kTileNT / 64;
   __shared__ __attribute__((aligned(16))) float red[2][W][kQ8Block];  // sums, magnitudes: of a wave's 4 R rows
   __shared__ __attribute__((aligned(16))) unsigned char tr[(kQ8Block + 1) * kQ8Block];
   const int t = (int)threadIdx.x & 15, g = (int)threadIdx.x >> 4;  // columns 8 t .. + 7, rows R g .. + R - 1 of the tile
   const int wave = (int)threadIdx.x >> 6;
   const int wide = (cols + kQ8Block - 1) / kQ8Block, tall = (rows + kQ8Block - 1) / kQ8Block;
-  const int at = (int)(blockIdx.y * gridDim.x + blockIdx.x);  // of less than 2^24 tiles
+  int at = (int)(blockIdx.y * gridDim.x + blockIdx.x);  // of less than 2^24 tiles
+  if (at < sum_blocks) {
+    q8_column_sums(x, ldx, rows, cols, 32 * at, sums, reinterpret_cast<float*>(tr));
+    return;
+  }
+  at -= sum_blocks;
   if (at >= wide * tall) return;
   const int tm = at / wide, tn = at % wide;
   const int m0 = tm * kQ8Block, c = tn * kQ8Block + 8 * t;
@@ -145,19 +179,27 @@ __global__ __launch_bounds__(kTileNT) void k_q8_tile(const T* __restrict__ x, in
 hipError_t launch_q8_quantise(sphinx_dtype dt, const void* x, int64_t ldx, int rows, int cols, bool square, uint8_t* q,
                               uint8_t* s, uint8_t* qt, uint8_t* st, float* sums, float* ws, hipStream_t stream) {
   const int wide = (cols + kQ8Block - 1) / kQ8Block, tall = (rows + kQ8Block - 1) / kQ8Block;
+  // A second launch joins the tiles' sums, except where one tile's are the sums, and where small inputs are read again
+  // for them beside the tiles: 1333 x 840 in bf16 10.5 -> 7.0 us a call (10.2 -> 7.3 from HBM), 2000 x 1024 10.4 -> 7.1
+  // (fp32 from HBM 10.3 -> 8.2).  It loses to the join where they do not stay in the caches (2048 x 4096 in bf16 12.2 ->
+  // 15.0) and where a workgroup has many rows to add (4096 x 1024 from HBM 10.5 -> 12.4).
+  const bool beside = sums != nullptr && tall > 1 && cols >= 32 && rows <= 2048 &&
+                      (int64_t)rows * cols * (dt == SPHINX_BF16 ? 2 : 4) <= (8 << 20);
+  const bool join = sums != nullptr && tall != 1 && !beside;
   if (rows > 0) {
     auto go = [&](auto t) {
       typedef decltype(t) T;
       const T* in = static_cast<const T*>(x);
-      const dim3 tiles = long_grid((int64_t)wide * tall);
-      float* part = sums != nullptr && tall > 1 ? ws : sums;  // one tile's sums are the sums
+      const int sum_blocks = beside ? (cols + 31) / 32 : 0;
+      const dim3 tiles = long_grid((int64_t)wide * tall + sum_blocks);
+      float* part = join ? ws : beside ? nullptr : sums;
       if (!square && qt == nullptr && sums == nullptr) {
         const int64_t grid = ((int64_t)rows * wide + kNT / 16 - 1) / (kNT / 16);
         k_q8_rows<T><<<long_grid(grid), kNT, 0, stream>>>(in, ldx, rows, cols, wide, q, s);
       } else if (square) {
-        k_q8_tile<T, true><<<tiles, kTileNT, 0, stream>>>(in, ldx, rows, cols, q, s, qt, st, part);
+        k_q8_tile<T, true><<<tiles, kTileNT, 0, stream>>>(in, ldx, rows, cols, q, s, qt, st, part, sums, sum_blocks);
       } else {
-        k_q8_tile<T, false><<<tiles, kTileNT, 0, stream>>>(in, ldx, rows, cols, q, s, qt, st, part);
+        k_q8_tile<T, false><<<tiles, kTileNT, 0, stream>>>(in, ldx, rows, cols, q, s, qt, st, part, sums, sum_blocks);
       }
     };
     if (dt == SPHINX_BF16) go(bf16{});
@@ -165,7 +207,7 @@ hipError_t launch_q8_quantise(sphinx_dtype dt, const void* x, int64_t ldx, int r
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
-  if (sums == nullptr || tall == 1) return hipSuccess;
+  if (!join) return hipSuccess;
   PartBounds P;
   P.nseg = 1;
   P.first[0] = 0;

@@ -92,6 +92,27 @@ def test_quantise(rows, cols, name, square):
         assert np.array_equal(values(*a, r, c), values(*b, r, c), equal_nan=True)
 
 
+# around the limits of the inputs whose columns are summed beside the tiles: 129 to 2048 rows, 32 columns, 8 MB
+@pytest.mark.parametrize("rows, cols", [(129, 31), (129, 32), (129, 33), (2048, 40), (2049, 40), (1024, 2048),
+                                        (1025, 2048), (1025, 4096)])
+@pytest.mark.parametrize("name", ["f32", "bf16"])
+def test_column_sums_of_inputs_small_and_not(rows, cols, name):
+    buf = torch.full((rows, cols + 3), GUARD, dtype=TYPE[name][0], device=DEV)
+    buf[:, :cols] = dev(numbers(rows, cols), name)
+    x = host(buf[:, :cols])
+    ws = torch.full((B.sphinx_q8_quantise_workspace_bytes(rows, cols),), 255, dtype=torch.uint8, device=DEV)
+    # 16 rows of a thread, 8 slices and 16 groups of them, or what test_quantise counts
+    lim = U * (8 + 16 + rows / 128 + 17) * np.abs(x).sum(axis=0)
+    for square in (False, True):
+        sums = torch.full((cols + 3,), GUARD, device=DEV)
+        q, s = empty(rows, cols)
+        B.sphinx_q8_quantise(TYPE[name][1], buf, cols + 3, rows, cols, square, q, s, None, None, sums, ws)
+        assert (np.abs(host(sums)[:cols] - x.sum(axis=0)) <= lim).all() and (sums[cols:] == GUARD).all()
+        alone = torch.empty(cols, device=DEV)
+        B.sphinx_q8_quantise(TYPE[name][1], buf, cols + 3, rows, cols, square, None, None, None, None, alone, ws)
+        assert torch.equal(alone, sums[:cols])
+
+
 def test_quantise_extreme_numbers():
     x = np.zeros((6, 128), np.float32)
     x[0, :4] = 3e38, -3.3e38, 1e38, 1.0     # past 448 2^119: saturates
