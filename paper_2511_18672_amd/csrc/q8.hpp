@@ -87,7 +87,7 @@ struct Q8Epi {
   float qscale;
 };
 size_t q8_matmul_ws_bytes(sphinx_dtype odt, int M, int N, int K);
-// ws: q8_matmul_ws_bytes for kQ8Bf16 and kQ8F32, not looked at for the others.
+// ws: q8_matmul_ws_bytes for kQ8Bf16 and kQ8F32; NULL: the contraction is not cut.  The other kinds never are.
 hipError_t launch_q8_matmul(Q8Kind kind, int M, int N, int K, const Q8Mat& a, const Q8Mat& b, const Q8Epi& e,
                             float* ws, hipStream_t stream);
 

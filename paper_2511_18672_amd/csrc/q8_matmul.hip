@@ -684,7 +684,7 @@ size_t q8_matmul_ws_bytes(sphinx_dtype odt, int M, int N, int K) {
 hipError_t launch_q8_matmul(Q8Kind kind, int M, int N, int K, const Q8Mat& a, const Q8Mat& b, const Q8Epi& e,
                             float* ws, hipStream_t stream) {
   const int KB = (K + kQ8Block - 1) / kQ8Block;
-  const Q8Plan p = plan_q8_matmul(kind, e.epi == Q8_EPI_GELU, M, N, KB);
+  const Q8Plan p = plan_q8_matmul(kind, e.epi == Q8_EPI_GELU, M, N, KB, ws == nullptr);
   auto go = [&](auto k) {
     constexpr Q8Kind KIND = decltype(k)::value;
     if constexpr (KIND == kQ8Bf16 || KIND == kQ8F32) {

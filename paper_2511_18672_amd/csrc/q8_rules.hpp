@@ -48,11 +48,13 @@ inline const Q8TileCost& q8_tile_cost(Q8Kind kind, int tile) {
 }
 
 // Only bf16 and fp32 outputs have a second kernel that joins pieces; outputs in
-// 8 bits need tiles of whole blocks of 128 columns.
-inline Q8Plan plan_q8_matmul(Q8Kind kind, bool gelu, int M, int N, int KB) {
-  const bool whole_k = kind == kQ8Gated || kind == kQ8Bytes;
+// 8 bits need tiles of whole blocks of 128 columns.  whole: there is no workspace for
+// pieces (the refinement step's QKV product, whose contraction of up to 16 blocks is
+// not worth cutting: with a workspace the plan would be the same).
+inline Q8Plan plan_q8_matmul(Q8Kind kind, bool gelu, int M, int N, int KB, bool whole = false) {
+  const bool values = kind == kQ8Bf16 || kind == kQ8F32, whole_k = whole || !values;
   Q8Plan best = {kQ8Tile128, 1};
-  if (!whole_k && M <= 16 && N <= (1 << 22)) return Q8Plan{kQ8Few, 1};
+  if (values && M <= 16 && N <= (1 << 22)) return Q8Plan{kQ8Few, 1};
   double us = 1e30;
   for (int t = 0; t < (kind == kQ8Bytes ? 3 : 5); ++t) {
     const Q8TileCost& c = q8_tile_cost(kind, t);
