@@ -83,7 +83,8 @@ struct Q8Epi {
   const float* gate;    // kQ8Gated: out += (1 + gate[row_of[m]][n]) C, rows of gate at ldg
   int64_t ldg;
   const int32_t* row_of;
-  int qcols;            // columns [0, qcols) are multiplied by qscale (qcols a multiple of 8)
+  int qcols;            // kQ8Bf16 stored: columns [0, qcols) are multiplied by qscale (qcols a multiple of 32, which a
+                        // tile's epilogue takes at a time); the contraction is not cut
   float qscale;
 };
 size_t q8_matmul_ws_bytes(sphinx_dtype odt, int M, int N, int K);

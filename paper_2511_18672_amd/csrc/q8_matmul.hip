@@ -584,7 +584,6 @@ __global__ __launch_bounds__(256) void k_q8_join(const float* __restrict__ part,
     for (int t = 0; t < 8; ++t) v[t] += b[t];
   }
   if (e.epi == Q8_EPI_GELU) q8_finish<Q8_THEN_GELU>(e, n, v);
-  else if (e.qcols > 0) q8_finish<Q8_THEN_SCALE>(e, n, v);
   q8_store8<OT>(e, m, n, N, v);
 }
 
@@ -684,7 +683,8 @@ size_t q8_matmul_ws_bytes(sphinx_dtype odt, int M, int N, int K) {
 hipError_t launch_q8_matmul(Q8Kind kind, int M, int N, int K, const Q8Mat& a, const Q8Mat& b, const Q8Epi& e,
                             float* ws, hipStream_t stream) {
   const int KB = (K + kQ8Block - 1) / kQ8Block;
-  const Q8Plan p = plan_q8_matmul(kind, e.epi == Q8_EPI_GELU, M, N, KB, ws == nullptr);
+  if (e.qcols % 32 != 0 || (e.qcols > 0 && (kind != kQ8Bf16 || e.epi != Q8_EPI_STORE))) return hipErrorInvalidValue;
+  const Q8Plan p = plan_q8_matmul(kind, e.epi == Q8_EPI_GELU, M, N, KB, ws == nullptr || e.qcols > 0);
   auto go = [&](auto k) {
     constexpr Q8Kind KIND = decltype(k)::value;
     if constexpr (KIND == kQ8Bf16 || KIND == kQ8F32) {

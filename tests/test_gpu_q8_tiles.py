@@ -204,3 +204,17 @@ def test_scales_from_end_to_end(tile, M, N, odt):
     va, vb = held(*a, M, K), held(*b, N, K).T.contiguous()
     c, size = va @ vb, va.abs() @ vb.abs()
     assert within(product(odt, a, b, M, N, K, ld=3), c, sum_error(K, size, odt == "bf16"), HALF[odt])
+
+
+def test_scaled_columns_of_a_long_contraction():
+    """Values that would be cut, where there is a workspace, are not where columns are scaled."""
+    M, N, K, scale = 70, 130, 40 * 128 - 3, 0.25
+    assert plan(L.BF16, False, M, N, 40)[1] > 1
+    a, b, c, size = operands(M, N, K)
+    ws = torch.full((B.sphinx_q8_matmul_workspace_bytes(B.BF16, M, N, K),), 255, dtype=torch.uint8, device=DEV)
+    out = torch.empty(M, N, dtype=torch.bfloat16, device=DEV)
+    assert L.launch(B.lib(), L.BF16, M, N, K, a, b, ws, torch.cuda.current_stream().cuda_stream, out=out, ldo=N,
+                    qcols=96, qscale=scale) == 0
+    times = torch.ones(N, dtype=torch.float64, device=DEV)
+    times[:96] = scale
+    assert within(out, c * times, sum_error(K, size) * times, HALF["bf16"]) and (ws == 255).all()

@@ -75,3 +75,15 @@ def test_structures_of_the_launcher_are_the_tests_own(tmp_path):
            os.path.join(ROOT, "paper_2511_18672_amd", "csrc"), str(src)]
     r = subprocess.run(cmd, capture_output=True, text=True)
     assert r.returncode == 0, r.stderr
+
+
+def test_the_launcher_refuses_scaled_columns_that_end_inside_32():
+    """A tile's epilogue scales 32 columns or none.  Refused before any HIP call."""
+    S = pytest.importorskip("paper_2511_18672_amd")
+    if not os.path.exists(S.binding.LIB_PATH):
+        pytest.skip("libsphinx.so not built")
+    call = lambda kind=q8_launch.BF16, **e: q8_launch.launch(  # noqa: E731
+        S.lib(), kind, 100, 96, 64, (1 << 20, 1 << 20), (1 << 20, 1 << 20), out=1 << 20, ldo=96, qscale=0.5, **e)
+    invalid = 1  # hipErrorInvalidValue
+    assert call(qcols=8) == invalid and call(qcols=40) == invalid
+    assert call(qcols=32, epi=q8_launch.GELU) == invalid and call(q8_launch.F32, qcols=32) == invalid
