@@ -685,26 +685,32 @@ hipError_t launch_q8_matmul(Q8Kind kind, int M, int N, int K, const Q8Mat& a, co
   const int KB = (K + kQ8Block - 1) / kQ8Block;
   if (e.qcols % 32 != 0 || (e.qcols > 0 && (kind != kQ8Bf16 || e.epi != Q8_EPI_STORE))) return hipErrorInvalidValue;
   const Q8Plan p = plan_q8_matmul(kind, e.epi == Q8_EPI_GELU, M, N, KB, ws == nullptr || e.qcols > 0);
+  bool launched = false;
   auto go = [&](auto k) {
     constexpr Q8Kind KIND = decltype(k)::value;
-    if constexpr (KIND == kQ8Bf16 || KIND == kQ8F32) {
+    auto tiles = [&](auto tile, auto ti, auto tj, auto wn) {  // waves 2 x wn, each 32 ti x 32 tj outputs
+      if constexpr (q8_has_tile(KIND, decltype(tile)::value)) {
+        if (p.tile != decltype(tile)::value) return;
+        launch_tiles<KIND, decltype(ti)::value, decltype(tj)::value, 2, decltype(wn)::value>(M, N, KB, a, b, e, p.pieces,
+                                                                                             ws, stream);
+        launched = true;
+      }
+    };
+    if constexpr (q8_has_tile(KIND, kQ8Few)) {
       if (p.tile == kQ8Few) {
         k_q8_matmul_few<KIND><<<(unsigned)((N + 15) / 16), 512, 0, stream>>>(a.q, a.s, b.q, b.s, M, N, KB, e);
-        return;
+        launched = true;
       }
     }
-    switch (p.tile) {
-      case kQ8Tile256:  // not for fp32 outputs, whose fragments in bf16 would spill
-        if constexpr (KIND != kQ8F32) launch_tiles<KIND, 4, 2, 2, 4>(M, N, KB, a, b, e, p.pieces, ws, stream);
-        break;
-      case kQ8Tile192: launch_tiles<KIND, 3, 2, 2, 4>(M, N, KB, a, b, e, p.pieces, ws, stream); break;
-      case kQ8Tile128: launch_tiles<KIND, 2, 2, 2, 2>(M, N, KB, a, b, e, p.pieces, ws, stream); break;
-      case kQ8Tile128x64:
-        if constexpr (KIND != kQ8Bytes) launch_tiles<KIND, 2, 1, 2, 2>(M, N, KB, a, b, e, p.pieces, ws, stream);
-        break;
-      default:
-        if constexpr (KIND != kQ8Bytes) launch_tiles<KIND, 1, 1, 2, 2>(M, N, KB, a, b, e, p.pieces, ws, stream);
-    }
+    typedef std::integral_constant<int, 1> I1;
+    typedef std::integral_constant<int, 2> I2;
+    typedef std::integral_constant<int, 3> I3;
+    typedef std::integral_constant<int, 4> I4;
+    tiles(std::integral_constant<Q8Tile, kQ8Tile256>{}, I4{}, I2{}, I4{});
+    tiles(std::integral_constant<Q8Tile, kQ8Tile192>{}, I3{}, I2{}, I4{});
+    tiles(std::integral_constant<Q8Tile, kQ8Tile128>{}, I2{}, I2{}, I2{});
+    tiles(std::integral_constant<Q8Tile, kQ8Tile128x64>{}, I2{}, I1{}, I2{});
+    tiles(std::integral_constant<Q8Tile, kQ8Tile64>{}, I1{}, I1{}, I2{});
   };
   switch (kind) {
     case kQ8Bf16: go(std::integral_constant<Q8Kind, kQ8Bf16>{}); break;
@@ -712,7 +718,7 @@ hipError_t launch_q8_matmul(Q8Kind kind, int M, int N, int K, const Q8Mat& a, co
     case kQ8Gated: go(std::integral_constant<Q8Kind, kQ8Gated>{}); break;
     default: go(std::integral_constant<Q8Kind, kQ8Bytes>{});
   }
-  return hipGetLastError();
+  return launched ? hipGetLastError() : hipErrorInvalidValue;
 }
 
 }  // namespace sphinx

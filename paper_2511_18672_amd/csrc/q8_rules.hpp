@@ -38,7 +38,7 @@ inline const Q8TileCost& q8_tile_cost(Q8Kind kind, int tile) {
   static const Q8TileCost cost[4][5] = {
       {{256, 256, 1, 9.1, 2.8, 1.35, 1.09}, {192, 256, 1, 7.7, 2.0, 1.10, 0.87}, {128, 128, 2, 5.5, 0.9, 0.86, 0.50},
        {128, 64, 2, 4.4, 0.4, 0.67, 0.42}, {64, 64, 4, 4.1, 0.3, 0.84, 0.30}},
-      {{256, 256, 1, 1e9, 0.0, 0.0, 0.0}, {192, 256, 1, 11.1, 1.6, 2.01, 1.61}, {128, 128, 2, 7.8, 1.1, 1.44, 0.71},
+      {{}, {192, 256, 1, 11.1, 1.6, 2.01, 1.61}, {128, 128, 2, 7.8, 1.1, 1.44, 0.71},
        {128, 64, 2, 5.0, 0.7, 0.89, 0.48}, {64, 64, 4, 4.4, 0.5, 1.06, 0.36}},
       {{256, 256, 1, 15.5, 2.8, 2.54, 1.10}, {192, 256, 1, 12.6, 2.0, 1.55, 0.89}, {128, 128, 2, 8.0, 0.9, 1.13, 0.55},
        {128, 64, 2, 4.5, 0.4, 0.74, 0.51}, {64, 64, 4, 3.4, 0.3, 0.94, 0.37}},
@@ -47,16 +47,23 @@ inline const Q8TileCost& q8_tile_cost(Q8Kind kind, int tile) {
   return cost[kind][tile];
 }
 
-// Only bf16 and fp32 outputs have a second kernel that joins pieces; outputs in
-// 8 bits need tiles of whole blocks of 128 columns.  whole: there is no workspace for
-// pieces (the refinement step's QKV product, whose contraction of up to 16 blocks is
-// not worth cutting: with a workspace the plan would be the same).
+// fp32 outputs have no 256x256, whose fragments in bf16 would spill; outputs in 8 bits
+// need tiles of whole blocks of 128 columns; few rows have a kernel for values only.
+constexpr bool q8_has_tile(Q8Kind kind, Q8Tile t) {
+  if (t == kQ8Few) return kind == kQ8Bf16 || kind == kQ8F32;
+  return kind == kQ8F32 ? t != kQ8Tile256 : kind != kQ8Bytes || t <= kQ8Tile128;
+}
+
+// Only bf16 and fp32 outputs have a second kernel that joins pieces.  whole: there is
+// no workspace for them (the refinement step's QKV product, whose contraction of up to
+// 16 blocks is not worth cutting: with a workspace the plan would be the same).
 inline Q8Plan plan_q8_matmul(Q8Kind kind, bool gelu, int M, int N, int KB, bool whole = false) {
   const bool values = kind == kQ8Bf16 || kind == kQ8F32, whole_k = whole || !values;
   Q8Plan best = {kQ8Tile128, 1};
   if (values && M <= 16 && N <= (1 << 22)) return Q8Plan{kQ8Few, 1};
   double us = 1e30;
-  for (int t = 0; t < (kind == kQ8Bytes ? 3 : 5); ++t) {
+  for (int t = 0; t < 5; ++t) {
+    if (!q8_has_tile(kind, (Q8Tile)t)) continue;
     const Q8TileCost& c = q8_tile_cost(kind, t);
     const int64_t tiles = (int64_t)((M + c.rows - 1) / c.rows) * ((N + c.cols - 1) / c.cols);
     if (tiles >= (1 << 23)) continue;  // more threads than a launch can have

@@ -18,6 +18,7 @@ extern "C" int plan(int kind, int gelu, int M, int N, int KB, int whole) {
   const sphinx::Q8Plan p = sphinx::plan_q8_matmul((sphinx::Q8Kind)kind, gelu != 0, M, N, KB, whole != 0);
   return p.tile * 100 + p.pieces;
 }
+extern "C" int has(int kind, int tile) { return sphinx::q8_has_tile((sphinx::Q8Kind)kind, (sphinx::Q8Tile)tile); }
 // Row counts up to `rows` at which the plan with a workspace is another one than without.
 extern "C" int differing(int kind, int gelu, int rows, int N, int KB) {
   int n = 0;
@@ -57,6 +58,18 @@ def test_no_pieces_without_a_workspace(kind):
         assert free[1] > 1 or free[0] == tile  # the same tile, where the contraction would not have been cut
         cut += free[1] > 1
     assert (cut > 100) == (kind in (BF16, F32))
+
+
+def test_plans_name_tiles_that_the_launcher_has():
+    rng = np.random.default_rng(2)
+    have = {kind: {t for t in range(6) if lib().has(kind, t)} for kind in range(4)}
+    assert have == {BF16: {0, 1, 2, 3, 4, 5}, F32: {1, 2, 3, 4, 5}, GATED: {0, 1, 2, 3, 4}, BYTES: {0, 1, 2}}
+    for kind in have:
+        seen = set()
+        for _ in range(4000):
+            M, N, KB = (int(np.exp(rng.uniform(0, np.log(hi)))) for hi in (1 << 18, 1 << 14, 4000))
+            seen.add(plan(kind, rng.random() < 0.5, M, N, KB, rng.random() < 0.5)[0])
+        assert seen == have[kind]
 
 
 def test_the_refinement_steps_products_lose_nothing_by_it():
