@@ -456,6 +456,8 @@ def _check_rows(name: str, t, dtype: int, n: int, ld: int, width: int):
         _load_torch()
     if t.dtype is not _TYPES.get(dtype, t.dtype):
         raise ValueError(f"{name} is {t.dtype}, the call names another type")
+    if not -(1 << 63) <= ld < 1 << 63:
+        raise ValueError(f"{name}: rows {ld} elements apart do not fit 64 bits")
     need = (n - 1) * ld + width
     if n > 0 and not (t.is_contiguous() and t.numel() >= need):
         have = t.untyped_storage().nbytes() // t.element_size() - t.storage_offset()
@@ -565,11 +567,18 @@ def _int32(name: str, v) -> int:
     return v
 
 
+def _fit32(v: int):
+    """Refuses sizes and codes, or'ed together, of which one does not fit 32 bits (negative ones that do are for the
+    library to refuse): the C types would take what is left of them."""
+    if v >> 31 not in (0, -1):
+        raise ValueError("a size or a code does not fit 32 bits")
+
+
 def _rows(name: str, t, dtype: int, n: int, ld: int, width: int) -> Optional[int]:
     """The address of a tensor that _check_rows takes (None: NULL)."""
     if t is None:
         return None
-    if t.dtype is not _TYPES.get(dtype) or t.numel() < (n - 1) * ld + width or not t.is_contiguous():
+    if ld < 0 or t.dtype is not _TYPES.get(dtype) or t.numel() < (n - 1) * ld + width or not t.is_contiguous():
         _check_rows(name, t, dtype, n, ld, width)
     return t.data_ptr()
 
@@ -617,6 +626,7 @@ def sphinx_layer_norm(xdt: int, wdt: int, ydt: int, cols: int, eps: float, x, ld
                       y, ldy: int, stats=None, stream=None):
     """y <- the normalised rows of x, scaled by w (1 + w with plus_one) and shifted by b, a row of each per segment
     (cu: host int sequence of row bounds; w, b: None for ones and zeros).  stats: float32 [rows][2] or None."""
+    _fit32(xdt | wdt | ydt | cols)
     c, nseg, n = _bounds(cu)
     px, pw = _rows("x", x, xdt, n, ldx, cols), _rows("w", w, wdt, nseg, ldw, cols)
     pb, py = _rows("b", b, wdt, nseg, ldw, cols), _rows("y", y, ydt, n, ldy, cols)
@@ -629,6 +639,7 @@ def sphinx_layer_norm(xdt: int, wdt: int, ydt: int, cols: int, eps: float, x, ld
 def sphinx_layer_norm_q8(xdt: int, wdt: int, cols: int, eps: float, x, ldx: int, w, b, ldw: int, plus_one, cu, q, s,
                          stats=None, stream=None):
     """sphinx_layer_norm with its output in 8 bits (q, s as sphinx_q8_bytes(rows, cols) sizes them)."""
+    _fit32(xdt | wdt | cols)
     c, nseg, n = _bounds(cu)
     px, pw = _rows("x", x, xdt, n, ldx, cols), _rows("w", w, wdt, nseg, ldw, cols)
     pb, ps = _rows("b", b, wdt, nseg, ldw, cols), _flat("stats", stats, F32, 2 * n)
@@ -641,7 +652,7 @@ def sphinx_layer_norm_q8(xdt: int, wdt: int, cols: int, eps: float, x, ldx: int,
 def sphinx_layer_norm_backward_workspace_bytes(cols: int, cu) -> int:
     c, out = _host_cu(cu), c_size_t()
     _check("sphinx_layer_norm_backward_workspace_bytes", lib().sphinx_layer_norm_backward_workspace_bytes(
-        cols, c.tobytes(), c.size - 1, ctypes.byref(out)))
+        _int32("cols", cols), c.tobytes(), c.size - 1, ctypes.byref(out)))
     return out.value
 
 
@@ -649,6 +660,7 @@ def sphinx_layer_norm_backward(xdt: int, wdt: int, gdt: int, cols: int, x, ldx: 
                                dy, lddy: int, dx, lddx: int, dw, db, ldg: int, ws, stream=None):
     """dx (None: left out) and, per segment, dw and db (float32; None: left out) from x, the forward call's stats
     and dy."""
+    _fit32(xdt | wdt | gdt | cols)
     c, nseg, n = _bounds(cu)
     px, pw = _rows("x", x, xdt, n, ldx, cols), _rows("w", w, wdt, nseg, ldw, cols)
     ps, pg = _flat("stats", stats, F32, 2 * n), _rows("dy", dy, gdt, n, lddy, cols)
@@ -678,6 +690,7 @@ def sphinx_q8_quantise_workspace_bytes(rows: int, cols: int) -> int:
 def sphinx_q8_quantise(dtype: int, x, ldx: int, rows: int, cols: int, square, q, s, qt=None, st=None, sums=None,
                        ws=None, stream=None):
     """x [rows][cols] in 8 bits: q and s; transposed, qt and st; and its column sums.  None: left out."""
+    _fit32(dtype | rows | cols)
     pq, ps = _q8("q", q, s, rows, cols)
     pqt, pst = _q8("qt", qt, st, cols, rows)
     px, pm, (pws, nws) = _rows("x", x, dtype, rows, ldx, cols), _flat("sums", sums, F32, cols), _ws(ws)
@@ -696,6 +709,7 @@ def sphinx_q8_matmul_workspace_bytes(odt: int, M: int, N: int, K: int) -> int:
 def sphinx_q8_matmul(odt: int, M: int, N: int, K: int, a, sa, b, sb, bdt: int, bias, epilogue: int, out, ldo: int, ws,
                      stream=None):
     """out [M][N] <- (or with Q8_ADD, +=) A B^T + bias, GELU with Q8_GELU, for 8-bit matrices A [M][K] and B [N][K]."""
+    _fit32(odt | bdt | epilogue | M | N | K)
     (pa, psa), (pb, psb) = _q8("a", a, sa, M, K), _q8("b", b, sb, N, K)
     pbias, po, (pws, nws) = _rows("bias", bias, bdt, 1, N, N), _rows("out", out, odt, M, ldo, N), _ws(ws)
     s = _here(stream, a, sa, b, sb, bias, out, ws)
@@ -705,6 +719,7 @@ def sphinx_q8_matmul(odt: int, M: int, N: int, K: int, a, sa, b, sb, bdt: int, b
 
 def sphinx_q8_matmul_q8(M: int, N: int, K: int, a, sa, b, sb, bdt: int, bias, epilogue: int, q, s, stream=None):
     """The 8-bit matrix q, s [M][N] <- A B^T + bias (Q8_STORE), or its GELU (Q8_GELU)."""
+    _fit32(bdt | epilogue | M | N | K)
     (pa, psa), (pb, psb), (pq, ps) = _q8("a", a, sa, M, K), _q8("b", b, sb, N, K), _q8("q", q, s, M, N)
     pbias = _rows("bias", bias, bdt, 1, N, N)
     at = _here(stream, a, sa, b, sb, bias, q, s)
