@@ -610,7 +610,7 @@ sphinx_status sphinx_q8_matmul_q8(int32_t M, int32_t N, int32_t K, const uint8_t
  * squares of 128 x 128.  sphinx_refine_step_q8 is sphinx_refine_step (kv_cache =
  * NULL), sphinx_refine_step_cached (kv8 = 0) or sphinx_refine_step_kv8 (kv8 = 1)
  * with these products; all else is as it was.  SPHINX_E_UNSUPPORTED for f32
- * models. */
+ * models and for mlp past 2^23. */
 sphinx_status sphinx_model_q8_bytes(const sphinx_model_desc* m, size_t* bytes);
 sphinx_status sphinx_model_q8_pack(const sphinx_model_desc* m, void* w8, size_t w8_bytes, void* stream);
 sphinx_status sphinx_refine_q8_workspace_bytes(const sphinx_model_desc* m, const sphinx_request* reqs, int32_t R,

@@ -795,7 +795,7 @@ Q8Model q8_model(const sphinx_model_desc& m) {
 sphinx_status q8_model_check(const sphinx_model_desc* m) {
   const sphinx_status st = check_model(m);
   if (st != SPHINX_OK) return st;
-  return m->dtype == SPHINX_BF16 ? SPHINX_OK : SPHINX_E_UNSUPPORTED;
+  return m->dtype == SPHINX_BF16 && m->mlp <= kQ8MaxCols ? SPHINX_OK : SPHINX_E_UNSUPPORTED;
 }
 // Workspace of the modulated norms in 8 bits, behind the rest.
 size_t q8_refine_extra(const sphinx_model_desc& m, int64_t sel) {

@@ -40,10 +40,9 @@ sphinx_status ln_check(sphinx_dtype xdt, sphinx_dtype wdt, int32_t cols, const v
 
 sphinx_status q8_size_check(int32_t rows, int32_t cols) {
   if (rows < 0 || cols < 0) return SPHINX_E_INVALID;
-  // a tile's rows are addressed with 32-bit byte offsets, and a launch has less than 2^32 threads (2^24 tiles of
-  // 128 x 128 hold 256 GB)
+  // a launch has less than 2^32 threads (2^24 tiles of 128 x 128 hold 256 GB)
   const int64_t wide = ((int64_t)cols + 127) / 128, tall = ((int64_t)rows + 127) / 128;
-  if (cols > (1 << 23) || rows > (1 << 28) || wide * tall >= (1 << 24)) return SPHINX_E_UNSUPPORTED;
+  if (cols > kQ8MaxCols || rows > (1 << 28) || wide * tall >= (1 << 24)) return SPHINX_E_UNSUPPORTED;
   return SPHINX_OK;
 }
 // Outputs of a product, whose columns may be as many as B's rows.

@@ -16,6 +16,7 @@
 namespace sphinx {
 
 constexpr int kQ8Block = 128;
+constexpr int kQ8MaxCols = 1 << 23;  // a tile's rows are addressed with 32-bit byte offsets
 constexpr int kLnMaxCols = 16384;
 
 inline int64_t q8_row_bytes(int64_t cols) { return (cols + kQ8Block - 1) / kQ8Block * kQ8Block; }

@@ -71,3 +71,24 @@ def test_workspace_sizes():
     for cols in (P32 + 64, 64 - P32):
         with pytest.raises(ValueError, match="32 bits"):
             B.sphinx_layer_norm_backward_workspace_bytes(cols, (0, 2))
+
+
+@pytest.mark.parametrize("mlp, fits", [(1 << 23, True), ((1 << 23) + 128, False), (1 << 26, False)])
+def test_models_whose_rows_are_longer_than_an_8_bit_matrix_has(mlp, fits):
+    """A product's tile addresses its rows with 32-bit offsets: matrices in 8 bits have at most 2^23 columns, those of a
+    model as well."""
+    import ctypes
+
+    import workloads as W
+
+    desc = B.model_desc(W.ModelCfg(D=128, heads=2, head_dim=64, mlp=mlp, L=1, dtype="bf16"), 1 << 20)
+    reqs = B.make_requests([W.Request(1, 4, 4)])
+    calls = [lambda: B.sphinx_model_q8_bytes(desc), lambda: B.sphinx_refine_q8_workspace_bytes(desc, reqs, 4)]
+    for call in calls:
+        if fits:
+            assert call() > 0
+        else:
+            with pytest.raises(S.SphinxError, match="UNSUPPORTED"):
+                call()
+    pack = B.lib().sphinx_model_q8_pack(ctypes.byref(desc), 1 << 20, 0, None)
+    assert B.STATUS_NAMES[pack] == ("SPHINX_E_WORKSPACE" if fits else "SPHINX_E_UNSUPPORTED")
