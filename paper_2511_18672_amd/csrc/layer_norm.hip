@@ -214,8 +214,9 @@ __device__ __forceinline__ void ln_column_sums(const LnArgs& a, int r0, int r1, 
 }
 
 // The next row's loads are issued before this row's arithmetic (also where dx
-// is dy: they are other rows).  Columns behind the last one hold dy = 0 and xh = 0,
-// which add nothing to a sum over the row.  The widest rows read their weights from
+// is dy: they are other rows).  Columns behind the last one hold x = 0 and dy = 0,
+// which add nothing to a sum over the row while mean * rstd is finite; where it is
+// not, they are left out.  The widest rows read their weights from
 // LDS each time, since the registers do not hold them (3000 x 10000 148 -> 74 us).
 // ONE: the first to.blocks workgroups sum columns into to.dw and to.db, and the
 // others, a chunk each, leave the sums alone (part is not used).
@@ -291,14 +292,8 @@ __global__ __launch_bounds__(LnCfg<LPR>::NT) void k_layer_norm_backward(LnArgs a
       float (&wi)[8] = w[kWeightsInLds ? 0 : i];
       if constexpr (kWeightsInLds) __builtin_memcpy(wi, __builtin_assume_aligned(sums + 8 * (i * LPR + t), 16), 32);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) xh[i][e] = ((float)rx[i].v[e] - mean) * r;
-      // behind the last column (0 - mean) r may be infinite, and 0 times it NaN
-      if (8 * (i + 1) * LPR > cols) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) xh[i][e] = 8 * (i * LPR + t) + e < cols ? xh[i][e] : 0.0f;
-      }
-#pragma unroll
       for (int e = 0; e < 8; ++e) {
+        xh[i][e] = ((float)rx[i].v[e] - mean) * r;
         const float d = (float)rg[i].v[e];
         if constexpr (!ONE) {
           sw[i][e] = fmaf(d, xh[i][e], sw[i][e]);
@@ -309,8 +304,19 @@ __global__ __launch_bounds__(LnCfg<LPR>::NT) void k_layer_norm_backward(LnArgs a
         s2 = fmaf(g[i][e], xh[i][e], s2);
       }
     }
+    // rare, and cheaper than a selection per number; behind the loads, but where the registers do not hold both
+    const bool far = !(fabsf(mean * r) < __uint_as_float(0x7f800000u));
+    auto inside = [&]() {
+      s2 = 0.0f;
+#pragma unroll
+      for (int i = 0; i < NI; ++i)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) s2 = 8 * (i * LPR + t) + e < cols ? fmaf(g[i][e], xh[i][e], s2) : s2;
+    };
+    if (kWeightsInLds && far) inside();
     fetch(min(row + C::ROWS, r1 - 1));
     if (dx != nullptr) {
+      if (!kWeightsInLds && far) inside();
       const int par = LPR > 64 ? 2 * ((row - r0) & 1) : 0;
       s1 = ln_sum<LPR>(s1, red[par]) / (float)cols;
       s2 = ln_sum<LPR>(s2, red[par + 1]) / (float)cols;
