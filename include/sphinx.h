@@ -503,7 +503,12 @@ sphinx_status sphinx_refine_step_kv8(const sphinx_model_desc* m, const sphinx_re
  * between and behind them is left as it is.  f32 or bf16 each; computed in fp32
  * and rounded once.  y may be x, and dx may be dy, of the same type and stride;
  * other outputs overlap nothing.  A row with an infinity or a NaN becomes
- * NaN and leaves the others alone (in dw and db: its segment's columns).
+ * NaN and leaves the others alone (in dw and db: its segment's columns), as does a
+ * constant row with eps = 0 (0/0).  Every other row of numbers up to 2^127 has
+ * finite statistics and, with finite w and b, y, also where a sum or a square on
+ * the way passes fp32's largest; gradients take numbers up to 2^126, and a sum of
+ * theirs that passes fp32's largest is infinite.  Differences from the mean below
+ * 2^-63 count as none beside eps (with eps = 0 they are lost).
  * Nothing is synchronized; the calls may be captured in a graph, and repeat
  * bit for bit.
  * ------------------------------------------------------------------------ */

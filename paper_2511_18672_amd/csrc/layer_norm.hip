@@ -79,15 +79,17 @@ __global__ __launch_bounds__(LnCfg<LPR>::NT) void k_layer_norm(LnArgs a, LnSegs 
   // short rows: everything that they need is on its way before the first sum is waited for.  Longer ones would pay for
   // it with waves (3000 x 8192 in bf16 21.3 -> 23.3 us)
   constexpr bool kEarly = NI <= 2 && LPR <= 64;
+  constexpr int kFull = LPR > 64 && NI == 4 ? 2 : NI - 1;  // groups of columns that by_cols fills
+  auto left = [&](int i) { return i < kFull ? 8 : cols - 8 * (i * LPR + t); };
   float v[NI][8], w[NI][8], b[NI][8];
 #pragma unroll
-  for (int i = 0; i < NI; ++i) load8(x + 8 * (i * LPR + t), cols - 8 * (i * LPR + t), v[i]);
+  for (int i = 0; i < NI; ++i) load8(x + 8 * (i * LPR + t), left(i), v[i]);
   const int64_t wr = (int64_t)(a.row_of != nullptr ? a.row_of[row] : ln_segment(S, row)) * a.ldw;
   const float one = a.plus_one ? 1.0f : 0.0f;
   auto weights = [&](int i) {
     const int c = 8 * (i * LPR + t);
-    ln_load_w(a.w, a.w_bf16, wr + c, cols - c, 1.0f - one, w[i]);
-    ln_load_w(a.b, a.w_bf16, wr + c, cols - c, 0.0f, b[i]);
+    ln_load_w(a.w, a.w_bf16, wr + c, left(i), 1.0f - one, w[i]);
+    ln_load_w(a.b, a.w_bf16, wr + c, left(i), 0.0f, b[i]);
   };
   if constexpr (kEarly)
 #pragma unroll
@@ -101,39 +103,93 @@ __global__ __launch_bounds__(LnCfg<LPR>::NT) void k_layer_norm(LnArgs a, LnSegs 
   s = 0.0f;
 #pragma unroll
   for (int i = 0; i < NI; ++i) {
-    const int n = cols - 8 * (i * LPR + t);
+    const int n = left(i);
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       v[i][e] = e < n ? v[i][e] - mean : 0.0f;
       s = fmaf(v[i][e], v[i][e], s);
     }
   }
-  const float rstd = 1.0f / sqrtf(ln_sum<LPR>(s, red[1]) / (float)cols + a.eps);
-  if (stats != nullptr && live && t == 0) {
-    stats[2 * (int64_t)row] = mean;
-    stats[2 * (int64_t)row + 1] = rstd;
-  }
-#pragma unroll
-  for (int i = 0; i < NI; ++i) {
-    const int c = 8 * (i * LPR + t), n = cols - c;
-    if constexpr (!kEarly) weights(i);
+  const float var = ln_sum<LPR>(s, red[1]) / (float)cols, inf = __uint_as_float(0x7f800000u);
+  const uint64_t far_rows = __ballot(!(var < inf));
+  const bool near = live && var < inf;
+  auto keep = [&](bool store, int to, float m, float r) {
+    if (stats != nullptr && store) {
+      stats[2 * (int64_t)to] = m;
+      stats[2 * (int64_t)to + 1] = r;
+    }
+  };
+  // columns c .. c + 7 from their differences from the mean
+  auto put = [&](bool store, int to, int c, int n, const float (&d)[8], float r, const float (&wc)[8], const float (&bc)[8]) {
     float o[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) o[e] = fmaf(v[i][e] * rstd, w[i][e] + one, b[i][e]);
+    for (int e = 0; e < 8; ++e) o[e] = fmaf(d[e] * r, wc[e] + one, bc[e]);
     if constexpr (std::is_same_v<OUT, Q8Out>) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) o[e] = e < n ? o[e] : 0.0f;
       const int sb = q8_scale_byte(row_max(finite_top(o)));
       const uint2 p = q8_pack8(o, sb);
       const int64_t ld = (cols + kQ8Block - 1) / kQ8Block * (int64_t)kQ8Block;
-      if (live && c < ld) {
-        *reinterpret_cast<uint2*>(qo.q + row * ld + c) = p;
-        if (t % 16 == 0) qo.s[row * (int64_t)q8_scale_row((int)(ld >> 7)) + (c >> 7)] = (uint8_t)sb;
+      if (store && c < ld) {
+        *reinterpret_cast<uint2*>(qo.q + to * ld + c) = p;
+        if (c % 128 == 0) qo.s[to * (int64_t)q8_scale_row((int)(ld >> 7)) + (c >> 7)] = (uint8_t)sb;
       }
     } else {
-      if (live) store8(y + (int64_t)row * ldy + c, n, o);
+      if (store) store8(y + (int64_t)to * ldy + c, n, o);
     }
+  };
+  const float rstd = 1.0f / sqrtf(var + a.eps);
+  keep(near && t == 0, row, mean, rstd);
+#pragma unroll
+  for (int i = 0; i < NI; ++i) {
+    if constexpr (!kEarly) weights(i);
+    put(near, row, 8 * (i * LPR + t), left(i), v[i], rstd, w[i], b[i]);
   }
+  if (far_rows == 0) return;
+  // A row whose sum, or that of its squares, passes fp32's largest (or that holds an infinity or a NaN, which stay NaN) is
+  // taken again from memory in units of 2^80: its numbers are below 2^48 then, and their squares' sum below 2^110.  All
+  // lanes of the row come here, behind the rest, so that other rows neither wait nor keep registers for it.
+  const float down = two_to(-80), up = two_to(80);
+  int tid = (int)threadIdx.x;
+  asm volatile("" : "+v"(tid));  // all else is found again
+  if ((far_rows >> (tid & 63) & 1) == 0) return;
+  const int64_t r0 = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * C::ROWS + tid / LPR;
+  const bool alive = r0 < rows;
+  const int again = alive ? (int)r0 : rows - 1, first = 8 * (tid % LPR);
+  const XT* xa = static_cast<const XT*>(a.x) + (int64_t)again * a.ldx;
+  auto each = [&](float m, auto f) {
+#pragma unroll 1
+    for (int i = 0; i < NI; ++i) {
+      const int c = 8 * LPR * i + first, n = cols - c;
+      float u[8];
+      load8(xa + c, n, u);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) u[e] = e < n ? u[e] * down - m : 0.0f;
+      f(c, u);
+    }
+  };
+  s = 0.0f;
+  each(0.0f, [&](int, const float (&u)[8]) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) s += u[e];
+  });
+  const float m = ln_sum<LPR>(s, red[0]) / (float)cols;
+  s = 0.0f;
+  each(m, [&](int, const float (&u)[8]) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) s = fmaf(u[e], u[e], s);
+  });
+  const float far = ln_sum<LPR>(s, red[1]) / (float)cols, whole = far * up * up;
+  // where only a sum was too large, the variance is taken back; where that is below 2^-96, no difference is left here
+  const float r = whole < inf ? fminf(up / sqrtf(whole + a.eps), 0x1p127f) : 1.0f / sqrtf(far + a.eps * down * down);
+  keep(alive && first == 0, again, m * up, whole < inf ? 1.0f / sqrtf(whole + a.eps) : r * down);
+  const int64_t wa = (int64_t)(a.row_of != nullptr ? a.row_of[again] : ln_segment(S, again)) * a.ldw;
+  each(m, [&](int c, const float (&u)[8]) {
+    float wc[8], bc[8];
+    ln_load_w(a.w, a.w_bf16, wa + c, cols - c, 1.0f - one, wc);
+    ln_load_w(a.b, a.w_bf16, wa + c, cols - c, 0.0f, bc);
+    put(alive, again, c, cols - c, u, r, wc, bc);
+  });
 }
 
 // Rows of a chunk: a workgroup walks over one chunk of one segment's rows and
@@ -389,7 +445,7 @@ __global__ __launch_bounds__(1024) void k_join_parts(const float* __restrict__ p
 
 // Calls f with the lanes per row and groups of eight columns per lane as constants.
 // `sums`: the columns' sums take registers as well (backward), so that four groups of columns per lane would leave one
-// wave per SIMD.
+// wave per SIMD.  All groups but the last (of 256 and 512 lanes with four, the last two) are full.
 template <typename F>
 void by_cols(int cols, bool sums, F&& f) {
   typedef std::integral_constant<int, 16> L16;
