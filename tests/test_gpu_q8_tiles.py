@@ -218,3 +218,42 @@ def test_scaled_columns_of_a_long_contraction():
     times = torch.ones(N, dtype=torch.float64, device=DEV)
     times[:96] = scale
     assert within(out, c * times, sum_error(K, size) * times, HALF["bf16"]) and (ws == 255).all()
+
+
+def test_one_step_in_large_tiles_against_the_oracle():
+    """One block over all tokens of six requests, whose QKV product takes 256x256, the first MLP layer 192x256 and the second
+    128x128.  Nearer to the oracle with 8-bit products than to the one without, by the ratio that test_gpu_q8_refine
+    derives for such a step from the shares of numbers that two roundings to 8 bits can disagree on."""
+    import oracle as O
+    import workloads as W
+
+    cfg = W.ModelCfg(D=1024, heads=16, head_dim=64, mlp=2048, L=1, dtype="bf16")
+    wl = W.custom("q8_large_tiles", cfg, [W.Request(1, 40, 100)] * 5 + [W.Request(1, 2, 6)], [1.0] * 6, [0.5] * 6, [2] * 6)
+    R = S.from_workload(wl, product_dtype="fp8")
+    R.reset()
+    n = R.step(0)
+    assert n == 5003
+    tiles = [TILES[plan(kind, gelu, n, rows, cols // 128, True)[0]]
+             for kind, gelu, rows, cols in ((L.BF16, False, 3 * cfg.D, cfg.D), (L.BYTES, True, cfg.mlp, cfg.D),
+                                            (L.GATED, False, cfg.D, cfg.mlp))]
+    assert tiles == ["256x256", "192x256", "128x128"]
+    got = R.state.cpu().numpy().astype(np.float64)
+    ref, plain = (O.refine(wl, precision="model", products8=p, steps=1) for p in (True, False))
+    a, b = (float(np.sqrt(((got - x) ** 2).mean())) for x in (ref, plain))
+    print(f"[q8 large tiles] rms to the 8-bit oracle {a:.3e}, to the other one {b:.3e}", flush=True)
+    assert a <= 0.6 * b
+    # and no token alone is off: the farthest token's rms, against what 8 bits move tokens by
+    off, moved = ((x.reshape(-1) ** 2).reshape(-1, 16).mean(axis=1) ** 0.5 for x in
+                  (to_tokens(wl, got - ref), to_tokens(wl, ref - plain)))
+    print(f"[q8 large tiles] farthest token {off.max():.3e}, moved {moved.max():.3e}", flush=True)
+    assert off.max() <= moved.max()
+
+
+def to_tokens(wl, state):
+    """[token][16] from the NCHW latents of all requests."""
+    flat, out, at = np.asarray(state).reshape(-1), [], 0
+    for r in wl.requests:
+        z = flat[at:at + r.frames * 4 * r.h * r.w].reshape(r.frames, 4, r.h // 2, 2, r.w // 2, 2)
+        out.append(z.transpose(0, 2, 4, 1, 3, 5).reshape(-1, 16))
+        at += r.frames * 4 * r.h * r.w
+    return np.concatenate(out)
