@@ -116,7 +116,7 @@ __device__ __forceinline__ float finite_top(const float (&x)[N]) {
   float top = 0.0f;
 #pragma unroll
   for (int i = 0; i < N; ++i) top = fmaxf(top, fabsf(x[i]));
-  if (!(top < inf)) {
+  if (__builtin_expect(!(top < inf), 0)) {  // a branch: taken along, it costs as much as the rest
     top = 0.0f;
 #pragma unroll
     for (int i = 0; i < N; ++i) top = fabsf(x[i]) < inf ? fmaxf(top, fabsf(x[i])) : top;
