@@ -257,3 +257,20 @@ def to_tokens(wl, state):
         out.append(z.transpose(0, 2, 4, 1, 3, 5).reshape(-1, 16))
         at += r.frames * 4 * r.h * r.w
     return np.concatenate(out)
+
+
+@pytest.mark.parametrize("rows, cols, additions", [
+    # one tile: 3 of a thread's rows, 2 across a wave's, its eight waves in four pairs
+    (100, 300, 3 + 2 + 4), (128, 64, 3 + 2 + 4),
+    # beside the tiles: a thread's rows, one in 128, then 8 slices and 16 of those
+    (300, 64, 3 + 8 + 16), (2048, 333, 16 + 8 + 16),
+    # tiles whose sums are joined: four sums of a sixteenth of them, 2 for the four, 16 slices
+    (3000, 96, 9 + 2 + 2 + 16), (9677, 40, 9 + 5 + 2 + 16)])
+@pytest.mark.parametrize("name", ["f32", "bf16"])
+def test_column_sums_are_off_by_their_additions_at_most(rows, cols, additions, name):
+    x = dev(numbers(rows, cols), name)
+    sums = torch.full((cols + 3,), GUARD, device=DEV)
+    ws = torch.full((B.sphinx_q8_quantise_workspace_bytes(rows, cols),), 255, dtype=torch.uint8, device=DEV)
+    B.sphinx_q8_quantise(TYPE[name][1], x, cols, rows, cols, False, None, None, None, None, sums, ws)
+    err = (sums[:cols].double() - x.double().sum(dim=0)).abs()
+    assert bool((err <= 1.01 * additions * U * x.double().abs().sum(dim=0)).all()) and (sums[cols:] == GUARD).all()
